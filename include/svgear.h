@@ -13,6 +13,15 @@
  *                            centroid compensation of every skipped block (Eq. (1), Eq. (6))
  *   svgear_unpermute         rows of the output put back in token order
  *
+ * and around it
+ *
+ *   svgear_linear            the projections into and out of the layer: a matrix product with
+ *                            bias, activation, gate and residual in its epilogue
+ *   svgear_rotary            RMS norm of queries and keys and their rotation by the token's
+ *                            (time, height, width) position
+ *
+ * each with its backward pass.
+ *
  * Conventions that hold for every call
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library never
  *     allocates, frees or keeps device memory, and never synchronises the host.
@@ -300,6 +309,130 @@ int svgear_sparse_attn_two_stage(const void* qp, const void* kp, const void* vp,
  */
 int svgear_unpermute(const void* op, const int32_t* perm, svgear_dtype dt, int B, int H,
                      int64_t N, int d, void* o, const int64_t ostride[3], void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * linear: a matrix product with everything behind it in one pass over the result.
+ *
+ *   z[b,n,o] = sum_k x[b,n,k] w[o,k] + bias[o]
+ *   y        = residual + gate * act(z)
+ *
+ * bias, gate, residual and pre may be NULL (0, 1, 0, not wanted). Products of bf16 values are
+ * exact in fp32 and summed in fp32 (fp32 inputs: fp32 products and sums on the fp32 matrix
+ * cores); bias, activation, gate and residual are applied in fp32; y and pre are each rounded
+ * once. Results do not depend on the stream, on other calls or on what the workspace holds.
+ *   x        [B,N,d_in] dt, element strides xstride = {stride_b, stride_n}, d_in contiguous
+ *   w        [d_out,d_in] dt, rows w_stride elements apart (>= d_in)
+ *   bias     [d_out] dt
+ *   gate     [B,N,d_out] dt, gstride = {stride_b, stride_n}; stride_n = 0 is one gate for all
+ *            tokens of a batch entry (the modulation of a diffusion transformer), a stride_b of 0
+ *            one for the whole call
+ *   residual [B,N,d_out] dt, rstride
+ *   pre      [B,N,d_out] dt out, dense: z, for the backward pass (NULL: not stored)
+ *   y        [B,N,d_out] dt out, ystride. y may be the residual itself (same pointer, same
+ *            strides); no other overlap of outputs with inputs or each other is allowed.
+ * Sizes: B, N, d_in, d_out >= 1, B*N < 2^31, d_in and d_out <= 2^21; strides >= 0, those of y
+ * such that no two rows meet; any alignment that the type has. Rows of x and w that are not
+ * 16-byte aligned, or whose length is no multiple of 16 bytes, and batches of x that are not one
+ * run of evenly spaced rows are first copied into the workspace: its size depends on the same
+ * arguments (pointers are looked at for their alignment only, on the host).
+ */
+typedef enum {
+  SVGEAR_ACT_NONE = 0,
+  SVGEAR_ACT_SILU = 1,       /* z / (1 + e^-z) */
+  SVGEAR_ACT_GELU = 2,       /* z (1 + erf(z / sqrt 2)) / 2 */
+  SVGEAR_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+  SVGEAR_ACT_INT_RANGE = 0x7fffffff
+} svgear_act;
+
+size_t svgear_linear_workspace(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
+                               svgear_dtype dt, int B, int64_t N, int d_in, int d_out);
+int svgear_linear(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride, const void* bias,
+                  svgear_dtype dt, int B, int64_t N, int d_in, int d_out, svgear_act act, const void* gate,
+                  const int64_t gstride[2], const void* residual, const int64_t rstride[2], void* pre, void* y,
+                  const int64_t ystride[2], void* ws, size_t ws_bytes, void* stream);
+
+/* The gradients of svgear_linear for the output's gradient dy (the residual's gradient is dy itself):
+ *
+ *   dz = dy * gate * act'(pre)
+ *   dx = dz w,  dw = dz^T x,  dbias[o] = sum_{b,n} dz,  dgate = dy * act(pre)
+ *
+ * with dgate summed over the tokens of a batch entry where gate's stride_n is 0 (then [B,d_out],
+ * otherwise [B,N,d_out], dense; a gate whose stride_b is 0 as well still gets one row for each
+ * batch entry). Any of dx, dw, dbias, dgate may be NULL, not all.
+ * pre is what svgear_linear stored; it is read where act is not SVGEAR_ACT_NONE or dgate is wanted and may
+ * be NULL otherwise. x is read for dw only and may be NULL without it, w for dx only.
+ * bf16: dz is rounded to bf16 for the two products, whose sums are fp32; the sums of dbias and
+ * dgate take it before that rounding. All sums are made in one fixed order.
+ *   dy    [B,N,d_out] dt, dystride;  pre [B,N,d_out] dt dense;  x, w, gate as above
+ *   dx    [B,N,d_in] dt out, dxstride;  dw [d_out,d_in] dt out dense;  dbias [d_out] dt out
+ * No output may overlap an input or another output.
+ */
+size_t svgear_linear_backward_workspace(const void* dy, const int64_t dystride[2], const void* x,
+                                        const int64_t xstride[2], const void* w, int64_t w_stride, svgear_dtype dt,
+                                        int B, int64_t N, int d_in, int d_out);
+int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void* x, const int64_t xstride[2],
+                           const void* w, int64_t w_stride, const void* pre, svgear_dtype dt, int B, int64_t N,
+                           int d_in, int d_out, svgear_act act, const void* gate, const int64_t gstride[2], void* dx,
+                           const int64_t dxstride[2], void* dw, void* dbias, void* dgate, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * rotary: RMS norm and rotation by positions on up to three axes, of one or two tensors (queries
+ * and keys) at the same positions.
+ *
+ *   u = x * rsqrt(mean(x^2) + eps) * weight
+ *       the mean over the d elements of a head (SVGEAR_ROTARY_NORM_HEAD, weight [d]), over the
+ *       H*d elements of a token (SVGEAR_ROTARY_NORM_TOKEN, weight [H*d], head h at h*d), or
+ *       u = x with neither flag; a NULL weight is all ones
+ *   pair p < P = sections[0]+sections[1]+sections[2] of a token's head is turned by the angle
+ *   position[axis(p)] * inv_freq[p]:
+ *       (y_i, y_j) = (u_i cos - u_j sin, u_i sin + u_j cos)
+ *       (i,j) = (2p, 2p+1), or (p, p+P) with SVGEAR_ROTARY_HALVES
+ *   axis(p) is 0 for the first sections[0] pairs, 1 for the next sections[1], then 2. Elements from
+ *   2P on are u, and so is all of the last n_tail (text) tokens.
+ * Positions: a token list, positions [N-n_tail,3] int32 (positions_stride_b = 0: shared by the
+ * batch) or [B,N-n_tail,3] (its element stride); or, with positions NULL, token n is element
+ * first + n of a grid of grid[0] x grid[1] x grid[2] (time, height, width; the last index
+ * fastest), for a share of a sequence or a single token of it: first + N - n_tail <= the
+ * grid's size < 2^31. Angles are computed in fp64 and reduced to one turn before cos and sin, so
+ * far positions lose nothing; all else is fp32, rounded once at the end. Squares are summed in
+ * fp32: |x| up to 1e17.
+ *   src[k], dst[k]  [B,H,N,d] dt, element strides sstride[k], dstride[k]; 16-byte aligned, strides
+ *                   multiples of 16 bytes, d = 64 or 128. dst[k] may be src[k] itself (same
+ *                   strides), and no other overlap is allowed. Rows of a cache, or of a fused
+ *                   projection's output [B,N,3,H,d], are strides.
+ *   weight[k]       dt, 16-byte aligned
+ *   inv_freq        [P] fp64 (device)
+ * src, dst, sstride, dstride, weight (may be NULL) and sections, grid are HOST arrays. n_tensors
+ * is 1 or 2; H <= 128; B*N < 2^31. No workspace.
+ */
+#define SVGEAR_ROTARY_NORM_HEAD 1u
+#define SVGEAR_ROTARY_NORM_TOKEN 2u
+#define SVGEAR_ROTARY_HALVES 4u
+int svgear_rotary(int n_tensors, const void* const* src, const int64_t (*sstride)[3], void* const* dst,
+                  const int64_t (*dstride)[3], const void* const* weight, svgear_dtype dt, int B, int H, int64_t N,
+                  int64_t n_tail, int d, const double* inv_freq, const int sections[3], const int64_t grid[3],
+                  int64_t first, const int32_t* positions, int64_t positions_stride_b, unsigned flags, float eps,
+                  void* stream);
+
+/* The gradients of svgear_rotary for the outputs' gradients dy[k]:
+ *
+ *   du = the rotation by the opposite angles of dy;  g = du * weight;  f = rsqrt(mean(x^2) + eps)
+ *   dx = f (g - x f^2 mean(g x));  dweight = sum of du x f over batch and tokens (and heads, for
+ *   SVGEAR_ROTARY_NORM_HEAD);  without a norm dx = du and there is no dweight
+ *   dy[k]  [B,H,N,d] dt, dystride;  src[k] the forward call's input (may be NULL without a norm)
+ *   dx[k]  [B,H,N,d] dt out, dxstride; may be dy[k] itself (same strides), no other overlap
+ *   dweight[k] [d] or [H*d] dt out, as weight (the array, or an entry, NULL: not wanted)
+ * Sums of dweight are fp32 and made in one fixed order. Alignment and limits as above.
+ */
+size_t svgear_rotary_backward_workspace(int n_tensors, int B, int H, int64_t N, int d);
+int svgear_rotary_backward(int n_tensors, const void* const* dy, const int64_t (*dystride)[3],
+                           const void* const* src, const int64_t (*sstride)[3], void* const* dx,
+                           const int64_t (*dxstride)[3], const void* const* weight, void* const* dweight,
+                           svgear_dtype dt, int B, int H, int64_t N, int64_t n_tail, int d, const double* inv_freq,
+                           const int sections[3], const int64_t grid[3], int64_t first, const int32_t* positions,
+                           int64_t positions_stride_b, unsigned flags, float eps, void* ws, size_t ws_bytes,
+                           void* stream);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,12 @@ from .binding import (  # noqa: F401
     sparse_attn_comp,
     unpermute,
     attention_layer,
+    attention_block,
+    linear,
+    linear_backward,
+    rotary,
+    rotary_backward,
+    rotary_frequencies,
     run_pair,
     EXPORTED_SYMBOLS,
     PROBE_PLAIN,

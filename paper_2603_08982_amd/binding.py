@@ -28,11 +28,17 @@ EXPORTED_SYMBOLS = [
     "svgear_sparse_attn_comp_workspace", "svgear_sparse_attn_comp", "svgear_sparse_attn_comp_token_order",
     "svgear_sparse_attn_two_stage_workspace", "svgear_sparse_attn_two_stage",
     "svgear_unpermute",
+    "svgear_linear_workspace", "svgear_linear", "svgear_linear_backward_workspace", "svgear_linear_backward",
+    "svgear_rotary", "svgear_rotary_backward_workspace", "svgear_rotary_backward",
 ]
+
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
+ROTARY_NORMS = {None: 0, "head": 1, "token": 2}
+ROTARY_HALVES = 4
 
 _c = ctypes
 _vp, _i, _i64, _sz, _f, _u = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_size_t, _c.c_float, _c.c_uint
-_I64x3 = _c.c_int64 * 3
+_I64x2, _I64x3, _Ix3 = _c.c_int64 * 2, _c.c_int64 * 3, _c.c_int * 3
 
 
 class SvgearError(RuntimeError):
@@ -98,6 +104,26 @@ def load_library():
     lib.svgear_sparse_attn_two_stage.argtypes = lib.svgear_sparse_attn_comp.argtypes
     lib.svgear_unpermute.restype = _i
     lib.svgear_unpermute.argtypes = [_vp, _vp, _i, _i, _i, _i64, _i, _vp, _c.POINTER(_c.c_int64), _vp]
+    p2, p3 = _c.POINTER(_c.c_int64), _c.POINTER(_I64x3)
+    lib.svgear_linear_workspace.restype = _sz
+    lib.svgear_linear_workspace.argtypes = [_vp, p2, _vp, _i64, _i, _i, _i64, _i, _i]
+    lib.svgear_linear.restype = _i
+    lib.svgear_linear.argtypes = [_vp, p2, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, p2, _vp, p2, _vp, _vp, p2, _vp,
+                                  _sz, _vp]
+    lib.svgear_linear_backward_workspace.restype = _sz
+    lib.svgear_linear_backward_workspace.argtypes = [_vp, p2, _vp, p2, _vp, _i64, _i, _i, _i64, _i, _i]
+    lib.svgear_linear_backward.restype = _i
+    lib.svgear_linear_backward.argtypes = [_vp, p2, _vp, p2, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, p2, _vp, p2,
+                                           _vp, _vp, _vp, _vp, _sz, _vp]
+    pp = _c.POINTER(_vp)
+    places = [_vp, _c.POINTER(_c.c_int), p2, _i64, _vp, _i64, _u, _f]
+    lib.svgear_rotary.restype = _i
+    lib.svgear_rotary.argtypes = [_i, pp, p3, pp, p3, pp, _i, _i, _i, _i64, _i64, _i, *places, _vp]
+    lib.svgear_rotary_backward_workspace.restype = _sz
+    lib.svgear_rotary_backward_workspace.argtypes = [_i, _i, _i, _i64, _i]
+    lib.svgear_rotary_backward.restype = _i
+    lib.svgear_rotary_backward.argtypes = [_i, pp, p3, pp, p3, pp, p3, pp, pp, _i, _i, _i, _i64, _i64, _i, *places, _vp, _sz,
+                                           _vp]
     _LIB = lib
     return lib
 
@@ -332,6 +358,212 @@ def unpermute(op: torch.Tensor, perm: torch.Tensor, out: Optional[torch.Tensor] 
     return out
 
 
+def _require(ok, what: str):
+    if not ok:
+        raise SvgearError(what)
+
+
+def _same_place(first: torch.Tensor, dtype, *ts):
+    """Every tensor given lies on the first one's GPU and has its type."""
+    _need_gpu(first, *ts)
+    for t in ts:
+        _require(t is None or (t.device == first.device and t.dtype == dtype), "tensors of one call share a device and a type")
+
+
+def _as_bnd(t: torch.Tensor, what: str):
+    """[B,N,c] or [N,c] (one batch entry) as (B, N, c, strides)."""
+    _require(t.dim() in (2, 3) and (t.shape[-1] == 1 or t.stride(-1) == 1), f"{what}: expected [B,N,c] or [N,c] with contiguous c")
+    if t.dim() == 2:
+        return 1, t.shape[0], t.shape[1], _I64x2(t.shape[0] * t.stride(0), t.stride(0))
+    return t.shape[0], t.shape[1], t.shape[2], _I64x2(t.stride(0), t.stride(1))
+
+
+def _gate_strides(gate, lead, d_out: int):
+    """Strides of a gate of tokens (lead + (d_out,)) or of batch entries (without the tokens' axis), and whether it is the first."""
+    if gate is None:
+        return _I64x2(0, 0), False
+    per_token = gate.dim() == len(lead) + 1
+    _require(tuple(gate.shape) == (*lead, d_out) or tuple(gate.shape) == (*lead[:-1], d_out), "gate: expected [B,N,d_out] or [B,d_out] ([N,d_out] or [d_out] for one batch entry)")
+    _require(d_out == 1 or gate.stride(-1) == 1, "gate: expected contiguous d_out")
+    if per_token:
+        return _I64x2(gate.stride(0) if len(lead) == 2 else 0, gate.stride(-2)), True
+    return _I64x2(gate.stride(0) if len(lead) == 2 else 0, 0), False
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
+           gate: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, want_pre: bool = False,
+           out: Optional[torch.Tensor] = None):
+    """svgear_linear: residual + gate * act(x w^T + bias). x [B,N,d_in] (or [N,d_in], one batch entry), w [d_out,d_in], bias
+    [d_out]; act "none", "silu", "gelu" (erf) or "gelu_tanh"; gate [B,d_out] (one for all tokens of a batch entry) or
+    [B,N,d_out]; residual [B,N,d_out], which `out` may be. want_pre: also z = x w^T + bias, which linear_backward needs
+    where there is an activation or a gate. Returns (y, z or None)."""
+    _same_place(x, x.dtype, w, bias, gate, residual, out)
+    lib = load_library()
+    B, N, d_in, xst = _as_bnd(x, "x")
+    lead = tuple(x.shape[:-1])
+    _require(w.dim() == 2 and w.shape[1] == d_in and (d_in == 1 or w.stride(1) == 1), "w: expected [d_out,d_in] with contiguous d_in")
+    d_out = w.shape[0]
+    _require(bias is None or (bias.shape == (d_out,) and bias.is_contiguous()), "bias: expected [d_out]")
+    _require(act in ACTIVATIONS, f"act: one of {sorted(ACTIVATIONS)}")
+    gst, _ = _gate_strides(gate, lead, d_out)
+    _require(residual is None or tuple(residual.shape) == (*lead, d_out), "residual: expected the output's shape")
+    _require(out is None or tuple(out.shape) == (*lead, d_out), "out: expected the output's shape")
+    rst = _as_bnd(residual, "residual")[3] if residual is not None else _I64x2(0, 0)
+    with torch.cuda.device(x.device):
+        y = torch.empty(*lead, d_out, dtype=x.dtype, device=x.device) if out is None else out
+        pre = torch.empty(*lead, d_out, dtype=x.dtype, device=x.device) if want_pre else None
+        yst = _as_bnd(y, "out")[3]
+        ldw = w.stride(0) if d_out > 1 else max(w.stride(0), d_in)
+        head = (_ptr(x), xst, _ptr(w), ldw)
+        ws = _ws(lib.svgear_linear_workspace(*head, _dt(x), B, N, d_in, d_out), x.device)
+        rc = lib.svgear_linear(*head, _ptr(bias), _dt(x), B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
+                               _ptr(residual), rst, _ptr(pre), _ptr(y), yst, _ptr(ws), ws.numel(), _stream())
+    _check(rc, "svgear_linear")
+    return y, pre
+
+
+def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], pre: Optional[torch.Tensor] = None,
+                    act: str = "none", gate: Optional[torch.Tensor] = None, want: Sequence[str] = ("dx", "dw")):
+    """svgear_linear_backward: the gradients named in `want` ("dx", "dw", "dbias", "dgate") of linear() for the output's
+    gradient dy; the residual's is dy itself. x is needed for dw, w for dx, pre (linear's second result) for an activation or
+    dgate. dgate has the gate's shape. Returns a dict."""
+    _same_place(dy, dy.dtype, x, w, pre, gate)
+    lib = load_library()
+    B, N, d_out, dyst = _as_bnd(dy, "dy")
+    lead = tuple(dy.shape[:-1])
+    _require(len(want) > 0 and set(want) <= {"dx", "dw", "dbias", "dgate"}, "want: dx, dw, dbias, dgate")
+    _require(act in ACTIVATIONS, f"act: one of {sorted(ACTIVATIONS)}")
+    x, w = (x if "dw" in want else None), (w if "dx" in want else None)
+    _require("dw" not in want or x is not None, "dw needs x")
+    _require("dx" not in want or w is not None, "dx needs w")
+    _require("dgate" not in want or gate is not None, "dgate needs the gate")
+    d_in = w.shape[1] if w is not None else x.shape[-1] if x is not None else 1
+    _require(x is None or tuple(x.shape) == (*lead, d_in), "x: expected dy's leading sizes and d_in")
+    _require(w is None or (tuple(w.shape) == (d_out, d_in) and (d_in == 1 or w.stride(1) == 1)), "w: expected [d_out,d_in] with contiguous d_in")
+    _require(pre is None or (tuple(pre.shape) == tuple(dy.shape) and pre.is_contiguous()), "pre: expected dy's shape, dense")
+    _require(pre is not None or (act == "none" and "dgate" not in want), "an activation or dgate needs pre")
+    gst, per_token = _gate_strides(gate, lead, d_out)
+    xst = _as_bnd(x, "x")[3] if x is not None else _I64x2(0, 0)
+    _require(not per_token or gst[1] != 0 or N == 1 or "dgate" not in want, "gate: one gate for all tokens is given as [B,d_out]")
+    with torch.cuda.device(dy.device):
+        new = lambda *shape: torch.empty(*shape, dtype=dy.dtype, device=dy.device)
+        r = {}
+        for name in want:
+            r[name] = new(*lead, d_in) if name == "dx" else new(d_out, d_in) if name == "dw" else new(d_out) if name == "dbias" else new(*gate.shape)
+        dx = r.get("dx")
+        dxst = _as_bnd(dx, "dx")[3] if dx is not None else _I64x2(0, 0)
+        ldw = 0 if w is None else w.stride(0) if d_out > 1 else max(w.stride(0), d_in)
+        head = (_ptr(dy), dyst, _ptr(x), xst, _ptr(w), ldw)
+        ws = _ws(lib.svgear_linear_backward_workspace(*head, _dt(dy), B, N, d_in, d_out), dy.device)
+        rc = lib.svgear_linear_backward(*head, _ptr(pre), _dt(dy), B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
+                                        _ptr(dx), dxst, _ptr(r.get("dw")), _ptr(r.get("dbias")), _ptr(r.get("dgate")),
+                                        _ptr(ws), ws.numel(), _stream())
+    _check(rc, "svgear_linear_backward")
+    return r
+
+
+def rotary_frequencies(sections: Sequence[int], theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The frequencies of video transformers, for rotary(): theta^(-i / pairs) for pair i of each axis, fp64."""
+    f = [theta ** (-torch.arange(n, dtype=torch.float64) / max(n, 1)) for n in sections]
+    return torch.cat(f).to(device)
+
+
+def _pointers(ts):
+    return (_vp * len(ts))(*[_ptr(t) for t in ts])
+
+
+def _strides_of(ts):
+    for t in ts:
+        _require(t.dim() == 4 and t.stride(3) == 1, "expected [B,H,N,d] with contiguous d")
+    return (_I64x3 * len(ts))(*[(t.stride(0), t.stride(1), t.stride(2)) for t in ts])
+
+
+def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves):
+    """The checked arguments that rotary and its backward pass share: (weights, arguments from inv_freq to flags)."""
+    t0 = tensors[0]
+    B, H, N, d = t0.shape
+    _require(len(tensors) in (1, 2) and all(t.shape == t0.shape for t in tensors), "one or two tensors of one shape [B,H,N,d]")
+    _require(len(sections) == 3, "sections: pairs of the three axes")
+    _require(norm in ROTARY_NORMS, 'norm: None, "head" or "token"')
+    pairs = sum(sections)
+    _require(inv_freq.is_cuda and inv_freq.device == t0.device and inv_freq.dtype == torch.float64 and inv_freq.shape == (pairs,)
+             and inv_freq.is_contiguous(), "inv_freq: expected fp64 [sum(sections)]")
+    _require((positions is None) != (grid is None), "positions or grid, one of them")
+    pos_b = 0
+    if positions is not None:
+        _require(positions.is_cuda and positions.device == t0.device and positions.dtype == torch.int32
+                 and positions.is_contiguous() and tuple(positions.shape) in ((N - n_tail, 3), (B, N - n_tail, 3)),
+                 "positions: expected int32 [N-n_tail,3] or [B,N-n_tail,3]")
+        pos_b = positions.stride(0) if positions.dim() == 3 else 0
+    else:
+        _require(len(grid) == 3, "grid: (time, height, width)")
+    size = {None: None, "head": d, "token": H * d}[norm]
+    if weights is not None:
+        _require(size is not None and len(weights) == len(tensors), "weights: one for each tensor, with a norm")
+        for w in weights:
+            _require(w is None or (tuple(w.shape) == (size,) and w.is_contiguous()), "weights: expected [d] or [H*d]")
+    flags = ROTARY_NORMS[norm] | (ROTARY_HALVES if halves else 0)
+    return list(weights) if weights is not None else [None] * len(tensors), (
+        _ptr(inv_freq), _Ix3(*sections), _I64x3(*grid) if grid is not None else None, int(first), _ptr(positions), pos_b, flags)
+
+
+def rotary(tensors: Sequence[torch.Tensor], inv_freq: torch.Tensor, sections: Sequence[int], grid=None, first: int = 0,
+           positions: Optional[torch.Tensor] = None, n_tail: int = 0, norm: Optional[str] = None, weights=None,
+           eps: float = 1e-6, halves: bool = False, out=None):
+    """svgear_rotary: RMS norm (norm "head" or "token", with `weights`) and rotation of queries and keys [B,H,N,d] (any
+    strides) by positions on three axes with `sections` pairs each: token n is element first + n of `grid` = (time, height,
+    width), or has positions[n] (int32 [N-n_tail,3] or [B,N-n_tail,3]); the last n_tail tokens are not rotated. `out` may be
+    `tensors`. Returns the list of results, dense unless given."""
+    _require(len(tensors) in (1, 2), "one or two tensors")
+    t0 = tensors[0]
+    outs = [None] * len(tensors) if out is None else list(out)
+    _same_place(t0, t0.dtype, *tensors, *(weights or ()), *outs)
+    lib = load_library()
+    ws, places = _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves)
+    B, H, N, d = t0.shape
+    with torch.cuda.device(t0.device):
+        if out is None:
+            outs = [torch.empty(B, H, N, d, dtype=t0.dtype, device=t0.device) for _ in tensors]
+        _require(len(outs) == len(tensors) and all(o.shape == t0.shape for o in outs), "out: one for each tensor, of its shape")
+        rc = lib.svgear_rotary(len(tensors), _pointers(tensors), _strides_of(tensors), _pointers(outs), _strides_of(outs),
+                               _pointers(ws), _dt(t0), B, H, N, n_tail, d, *places, float(eps), _stream())
+    _check(rc, "svgear_rotary")
+    return outs
+
+
+def rotary_backward(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[torch.Tensor]], inv_freq: torch.Tensor,
+                    sections: Sequence[int], grid=None, first: int = 0, positions: Optional[torch.Tensor] = None,
+                    n_tail: int = 0, norm: Optional[str] = None, weights=None, eps: float = 1e-6, halves: bool = False,
+                    want_dweight: bool = True, out=None):
+    """svgear_rotary_backward: for the gradients of rotary()'s results, (list of its inputs' gradients, list of its weights'
+    gradients or None). `tensors`, rotary's inputs, are needed with a norm. `out` (the inputs' gradients) may be `grads`."""
+    _require(len(grads) in (1, 2), "one or two tensors")
+    g0 = grads[0]
+    outs = [None] * len(grads) if out is None else list(out)
+    _require(norm is None or (tensors is not None and len(tensors) == len(grads) and all(t.shape == g0.shape for t in tensors)),
+             "a norm needs rotary's inputs")
+    tensors = list(tensors) if norm is not None else []
+    _same_place(g0, g0.dtype, *grads, *tensors, *(weights or ()), *outs)
+    lib = load_library()
+    ws, places = _rotary_places(grads, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves)
+    B, H, N, d = g0.shape
+    n = len(grads)
+    with torch.cuda.device(g0.device):
+        if out is None:
+            outs = [torch.empty(B, H, N, d, dtype=g0.dtype, device=g0.device) for _ in grads]
+        _require(len(outs) == n and all(o.shape == g0.shape for o in outs), "out: one for each tensor, of its shape")
+        dweight = None
+        if norm is not None and want_dweight:
+            dweight = [torch.empty(d if norm == "head" else H * d, dtype=g0.dtype, device=g0.device) for _ in grads]
+        scratch = _ws(lib.svgear_rotary_backward_workspace(n, B, H, N, d) if dweight else 0, g0.device)
+        rc = lib.svgear_rotary_backward(n, _pointers(grads), _strides_of(grads), _pointers(tensors) if tensors else None,
+                                        _strides_of(tensors) if tensors else None, _pointers(outs), _strides_of(outs),
+                                        _pointers(ws), _pointers(dweight) if dweight else None, _dt(g0), B, H, N, n_tail, d,
+                                        *places, float(eps), _ptr(scratch), scratch.numel(), _stream())
+    _check(rc, "svgear_rotary_backward")
+    return outs, dweight
+
+
 _SIDE_STREAMS = {}
 
 
@@ -366,7 +598,7 @@ def run_pair(fn_side, fn_main):
 
 def attention_layer(Q, K, V, init_q, init_k, iters: int, budget_cost: int, n_tail: int = 0, flags: int = 0,
                     scale: Optional[float] = None, overlap: bool = True, top_p: Optional[float] = None, mark=None,
-                    token_order: bool = True):
+                    token_order: bool = True, out: Optional[torch.Tensor] = None):
     """One pass of the whole hot path over a batch of heads: k-means, permutation, probe + route,
     fused attention, un-permutation.
 
@@ -386,7 +618,7 @@ def attention_layer(Q, K, V, init_q, init_k, iters: int, budget_cost: int, n_tai
     so a caller can carry them to the next denoising step). With top_p the routing budget is
     the adaptive per-query-cluster one and budget_cost is ignored. mark(name), if given, is
     called on the current stream after each stage ("kmeans", "permute", "probe_route",
-    "attention", "unpermute"). Returns (O, intermediates)."""
+    "attention", "unpermute"). O is written into `out` if given. Returns (O, intermediates)."""
     B, H, N, d = Q.shape
     if scale is None:
         scale = float(d) ** -0.5
@@ -419,16 +651,44 @@ def attention_layer(Q, K, V, init_q, init_k, iters: int, budget_cost: int, n_tai
     mark("probe_route")
     if token_order:
         O, _ = sparse_attn_comp(Q, Kp, Vp, init_k, vbar, qoff, koff, r["mask_bits"], r["row_ptr"], r["col_idx"], scale,
-                                q_perm=perm_q)
+                                q_perm=perm_q, out=out)
         mark("attention")
     else:
         (Qp,) = q_rows
         Op, _ = sparse_attn_comp(Qp, Kp, Vp, init_k, vbar, qoff, koff, r["mask_bits"], r["row_ptr"], r["col_idx"],
                                  scale)
         mark("attention")
-        O = unpermute(Op, perm_q)
+        O = unpermute(Op, perm_q, out)
         r.update(Qp=Qp, Op=Op)
     mark("unpermute")
     r.update(lab_q=lab_q, lab_k=lab_k, qcnt=qcnt, kcnt=kcnt, qbar=init_q, kbar=init_k, vbar=vbar, perm_q=perm_q,
              perm_k=perm_k, qoff=qoff, koff=koff, Kp=Kp, Vp=Vp, O=O)
     return O, r
+
+
+def attention_block(x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor, init_q: torch.Tensor, init_k: torch.Tensor,
+                    iters: int, budget_cost: int, inv_freq: torch.Tensor, sections: Sequence[int], grid=None, first: int = 0,
+                    positions: Optional[torch.Tensor] = None, b_qkv: Optional[torch.Tensor] = None,
+                    b_out: Optional[torch.Tensor] = None, norm: Optional[str] = None, norm_weights=None, eps: float = 1e-6,
+                    halves: bool = False, gate: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                    n_tail: int = 0, **layer):
+    """An attention block of a video transformer from its input to its output: linear() into queries, keys and values, rotary()
+    on queries and keys where they lie, attention_layer() on the three as strided views, and linear() back with gate and
+    residual.
+
+    x [B,N,c]; w_qkv [3*H*d,c] (rows: queries of all heads, keys, values), b_qkv [3*H*d]; w_out [c_out,H*d], b_out [c_out];
+    gate [B,c_out] or [B,N,c_out] and residual [B,N,c_out] as in linear(); norm, norm_weights (of queries and keys), inv_freq,
+    sections, and grid and first, or positions, as in rotary(); init_q, init_k [B,H,C,d] (H and d are theirs), iters,
+    budget_cost, n_tail and what `layer` holds as in attention_layer(). Returns (y [B,N,c_out], intermediates of the layer)."""
+    B, N, _ = x.shape
+    H, d = init_q.shape[1], init_q.shape[3]
+    _require(w_qkv.shape[0] == 3 * H * d and w_out.shape[1] == H * d, "w_qkv: expected [3*H*d,c], w_out: [c_out,H*d]")
+    _require("out" not in layer, "the layer's output is the block's own")
+    qkv, _ = linear(x, w_qkv, b_qkv)
+    q, k, v = qkv.view(B, N, 3, H, d).permute(2, 0, 3, 1, 4)
+    rotary([q, k], inv_freq, sections, grid=grid, first=first, positions=positions, n_tail=n_tail, norm=norm,
+           weights=norm_weights, eps=eps, halves=halves, out=[q, k])
+    o = torch.empty(B, N, H, d, dtype=x.dtype, device=x.device)
+    _, r = attention_layer(q, k, v, init_q, init_k, iters, budget_cost, n_tail, out=o.transpose(1, 2), **layer)
+    y, _ = linear(o.view(B, N, H * d), w_out, b_out, gate=gate, residual=residual)
+    return y, r

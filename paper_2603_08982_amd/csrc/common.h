@@ -108,6 +108,10 @@ int sort_labels(const int32_t* labels, int BH, int64_t N, int64_t n_tail, int C,
                 int tile_len = 64);
 
 
+// out[g][c] = sum over i of part[g][i][c], rows added in one fixed order, in fp32, rounded once to dt
+// (linear.hip).
+int sum_rows(const float* part, int rows, int cols, int groups, void* out, svgear_dtype dt, hipStream_t s);
+
 // Per-head length of the probe's per-key statistic arrays (padded so that 16-byte reads
 // starting at any key stay inside the array).
 static inline int64_t probe_stat_stride(int64_t Nk) { return (int64_t)align_up((size_t)Nk + 64, 64); }

@@ -1,0 +1,157 @@
+// Shared declarations of the matrix products of svgear_linear and its backward pass (internal).
+#pragma once
+#include "common.h"
+
+namespace svgear {
+
+// One operand of a product: rows of `pitch` elements, 16-byte aligned, whole 16-byte chunks.
+struct Operand {
+  const void* p;
+  int64_t pitch;
+};
+
+// Strides of a [B,N,columns] tensor.
+struct Rows {
+  int64_t b, n;
+};
+
+// out[r][c] = sum_k Q[r][k] P[c][k], r < R rows, c < C columns, k < K. Where an operand has k contiguous, the last
+// 16-byte chunk of its rows holds zeros behind the values; where it has k over rows, its last chunk is readable.
+struct LinearArgs {
+  Operand P, Q;
+  int64_t K;
+  int R, C;
+  int splits;    // K in so many parts, each into its own slice of `partial`
+  float* partial;  // [splits][R][C] or null
+  // epilogue: row r is token r - b*n of batch entry b = r / n
+  int n;
+  const void* bias;
+  const void* gate;
+  const void* residual;
+  void* pre;
+  void* y;
+  Rows gst, rst, yst;
+  int act;
+  bool wide;  // every row of y, gate, residual and pre, and bias, 16-byte aligned, C a multiple of 16 bytes
+};
+
+// How the contraction index lies in the operands: contiguous in both (forward), in Q alone (dx), in neither (dw).
+enum { kContractBoth = 0, kContractQ = 1, kContractNone = 2 };
+
+int launch_linear_bf16(const LinearArgs& a, int form, hipStream_t s);
+int launch_linear_f32(const LinearArgs& a, int form, hipStream_t s);
+// y from the partial products of `splits` parts.
+int launch_linear_merge(const LinearArgs& a, svgear_dtype dt, hipStream_t s);
+
+// ---- activations, fp32
+// z / (1 + e^-v): silu for v = z; for v = 2u the tanh form of gelu, since (1 + tanh u) / 2 = 1 / (1 + e^-2u)
+__device__ __forceinline__ float gelu_tanh_arg(float z) {
+  const float z2 = fminf(z * z, 1e30f);  // (large z: the limit is the same, and nothing is infinity times zero)
+  return 1.5957691216057308f * (z + 0.044715f * z * z2);
+}
+__device__ __forceinline__ float act_value(int act, float z) {
+  if (act == SVGEAR_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == SVGEAR_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+  if (act == SVGEAR_ACT_GELU_TANH) return z / (1.f + expf(-gelu_tanh_arg(z)));
+  return z;
+}
+// slope, and the value in `a`
+__device__ __forceinline__ float act_slope(int act, float z, float& a) {
+  if (act == SVGEAR_ACT_NONE) {
+    a = z;
+    return 1.f;
+  }
+  if (act == SVGEAR_ACT_GELU) {
+    const float cdf = 0.5f * erfcf(-0.70710678118654752f * z);
+    a = z * cdf;
+    return cdf + z * (0.39894228040143268f * expf(-0.5f * z * z));
+  }
+  // z s(v): slope s + z s (1 - s) v', with s (1 - s) = e^-|v| / (1 + e^-|v|)^2, which loses nothing on either side
+  float v = z, dv = 1.f;
+  if (act == SVGEAR_ACT_GELU_TANH) {
+    v = gelu_tanh_arg(z);
+    dv = 1.5957691216057308f * (1.f + 0.134145f * fminf(z * z, 1e30f));
+  }
+  const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
+  const float s = v >= 0.f ? r : e * r;
+  a = z * s;
+  return s + z * (e * r * r) * dv;
+}
+
+template <typename T>
+__device__ __forceinline__ float load_as_f32(const T* p);
+template <>
+__device__ __forceinline__ float load_as_f32<float>(const float* p) { return *p; }
+template <>
+__device__ __forceinline__ float load_as_f32<bf16_t>(const bf16_t* p) { return bf16_to_f32(*p); }
+
+// Four consecutive elements, wide: one load or store.
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <>
+__device__ __forceinline__ float4 load4<bf16_t>(const bf16_t* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float lin_f32x2;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 lin_bf16x2;
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  lin_f32x2 f = {lo, hi};
+  union { lin_bf16x2 b; uint32_t u; } c;
+  c.b = __builtin_convertvector(f, lin_bf16x2);
+  return c.u;
+}
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f32_to_bf16(v); }
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, float4 v) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+}
+
+// The epilogue of four consecutive columns c.. of row r (those < C).
+template <typename T>
+__device__ __forceinline__ void finish4(const LinearArgs& a, int r, int c, float4 v) {
+  const int b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
+  T* y = static_cast<T*>(a.y) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c;
+  const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c : nullptr;
+  const T* res = a.residual ? static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c : nullptr;
+  T* pre = a.pre ? static_cast<T*>(a.pre) + (int64_t)r * a.C + c : nullptr;
+  const T* bias = a.bias ? static_cast<const T*>(a.bias) + c : nullptr;
+  if (a.wide) {
+    if (bias) {
+      const float4 w = load4(bias);
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    if (pre) store4(pre, v);
+    if (a.act != SVGEAR_ACT_NONE) {
+      v.x = act_value(a.act, v.x), v.y = act_value(a.act, v.y);
+      v.z = act_value(a.act, v.z), v.w = act_value(a.act, v.w);
+    }
+    if (gate) {
+      const float4 g = load4(gate);
+      v.x *= g.x, v.y *= g.y, v.z *= g.z, v.w *= g.w;
+    }
+    if (res) {
+      const float4 q = load4(res);
+      v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+    }
+    store4(y, v);
+    return;
+  }
+  float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (c + i >= a.C) break;
+    if (bias) e[i] += load_as_f32(bias + i);
+    if (pre) store1(pre + i, e[i]);
+    if (a.act != SVGEAR_ACT_NONE) e[i] = act_value(a.act, e[i]);
+    if (gate) e[i] *= load_as_f32(gate + i);
+    if (res) e[i] += load_as_f32(res + i);
+    store1(y + i, e[i]);
+  }
+}
+
+}  // namespace svgear

@@ -1,0 +1,406 @@
+// svgear_linear and svgear_linear_backward: argument checks, the copies of operands that the tile kernel
+// cannot read in place, and what is done element by element.
+#include "linear.h"
+
+namespace svgear {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxWidth = 1 << 21;
+constexpr int64_t kMaxPitch = 1 << 21;  // a tile's rows are addressed by 32-bit byte offsets: 256 rows of 8 MB
+
+// ---- rows copied to an even, 16-byte aligned pitch, zeros behind the values
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+pack_rows_kernel(const T* src, Rows st, int n, int rows, int width, T* dst, int64_t pitch) {
+  const int col = (blockIdx.y * kThreads + threadIdx.x);
+  if (col >= pitch) return;
+  for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+    const int b = n >= rows ? 0 : r / n;
+    const T* s = src + (int64_t)b * st.b + (int64_t)(r - b * n) * st.n;
+    dst[(int64_t)r * pitch + col] = col < width ? s[col] : T(0);
+  }
+}
+
+// ---- out[g][c] = sum over i of part[g][i][c]: eight runs of rows, then those
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+sum_rows_kernel(const float* part, int rows, int cols, int groups, T* out) {
+  __shared__ float s[8][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+  for (int g = blockIdx.y; g < groups; g += gridDim.y) {
+    const float* p = part + (int64_t)g * rows * cols;
+    float v = 0.f;
+    if (c < cols)
+      for (int i = y; i < rows; i += 8) v += p[(int64_t)i * cols + c];
+    s[y][x] = v;
+    __syncthreads();
+    if (y == 0 && c < cols) {
+      for (int k = 1; k < 8; ++k) v += s[k][x];
+      store1(out + (int64_t)g * cols + c, v);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- the epilogue on partial products
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+linear_merge_kernel(LinearArgs a, int quads) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int r = (int)(i / quads), c = (int)(i % quads) * 4;
+  if (r >= a.R) return;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < a.splits; ++p) {
+    const float* o = a.partial + ((int64_t)p * a.R + r) * a.C + c;
+    if (a.C % 4 == 0) {
+      const float4 w = *reinterpret_cast<const float4*>(o);
+      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    } else {
+      v.x += o[0];
+      if (c + 1 < a.C) v.y += o[1];
+      if (c + 2 < a.C) v.z += o[2];
+      if (c + 3 < a.C) v.w += o[3];
+    }
+  }
+  finish4<T>(a, r, c, v);
+}
+
+// ---- dz, the partial sums of dbias, and dgate
+struct GradientArgs {
+  const void* dy;
+  const void* pre;   // or null
+  const void* gate;  // or null
+  void* dz;          // [R][pitch], or null
+  void* dgate;       // [R][C] where the gate is of tokens, or null
+  float* sum_dz;     // [blocks][C] or null
+  float* sum_da;     // [blocks][C] or null: a batch entry's blocks together
+  Rows yst, gst;
+  int64_t pitch;
+  int C, n, act;
+  int blocks_b, rows_block;  // blocks of a batch entry, rows of a block
+};
+
+// A workgroup takes 64 columns of a run of rows of one batch entry: its 4 waves every fourth row.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+linear_gradient_kernel(GradientArgs a) {
+  __shared__ float s[2][4][64];
+  const int x = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int c = blockIdx.y * 64 + x, b = blockIdx.x / a.blocks_b, first = (blockIdx.x % a.blocks_b) * a.rows_block;
+  const int last = min(first + a.rows_block, a.n);
+  float sz = 0.f, sa = 0.f;
+  if (c < a.C) {
+    for (int t = first + w; t < last; t += 4) {
+      const int64_t r = (int64_t)b * a.n + t;
+      const float dy = load_as_f32(static_cast<const T*>(a.dy) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c);
+      float act = 0.f, dz = dy;
+      if (a.pre) dz = dy * act_slope(a.act, load_as_f32(static_cast<const T*>(a.pre) + r * a.C + c), act);
+      if (a.gate) dz *= load_as_f32(static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c);
+      if (a.dz) store1(static_cast<T*>(a.dz) + r * a.pitch + c, dz);
+      if (a.dgate) store1(static_cast<T*>(a.dgate) + r * a.C + c, dy * act);
+      sz += dz;
+      sa += dy * act;
+    }
+  } else if (a.dz && c < a.pitch) {
+    for (int t = first + w; t < last; t += 4) store1(static_cast<T*>(a.dz) + ((int64_t)b * a.n + t) * a.pitch + c, 0.f);
+  }
+  if (!a.sum_dz && !a.sum_da) return;
+  s[0][w][x] = sz;
+  s[1][w][x] = sa;
+  __syncthreads();
+  if (w == 0 && c < a.C) {
+    if (a.sum_dz) a.sum_dz[(int64_t)blockIdx.x * a.C + c] = s[0][0][x] + s[0][1][x] + s[0][2][x] + s[0][3][x];
+    if (a.sum_da) a.sum_da[(int64_t)blockIdx.x * a.C + c] = s[1][0][x] + s[1][1][x] + s[1][2][x] + s[1][3][x];
+  }
+}
+
+// ---- host side
+int64_t chunk(svgear_dtype dt) { return dt == SVGEAR_F32 ? 4 : 8; }
+int64_t even_pitch(int64_t width, svgear_dtype dt) { return ceil_div(width, chunk(dt)) * chunk(dt); }
+
+// Whether the tile kernel can read these rows where they are.
+bool in_place(const void* p, int64_t pitch, int64_t width, svgear_dtype dt) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch % chunk(dt) == 0 && width % chunk(dt) == 0 && pitch <= kMaxPitch;
+}
+// [B,N,width] as one run of rows: their distance, or -1.
+int64_t run_pitch(const int64_t st[2], int B, int64_t N) {
+  if (B == 1) return st[1];
+  if (N == 1) return st[0];
+  return st[0] == N * st[1] ? st[1] : -1;
+}
+bool rows_in_place(const void* p, const int64_t st[2], int B, int64_t N, int64_t width, svgear_dtype dt) {
+  const int64_t pitch = run_pitch(st, B, N);
+  return pitch >= 0 && in_place(p, pitch, width, dt);
+}
+size_t packed_bytes(int64_t rows, int64_t width, svgear_dtype dt) {
+  return align_up((size_t)rows * even_pitch(width, dt) * esize(dt), 256);
+}
+
+template <typename T>
+int pack_rows(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, void* dst, int64_t pitch, hipStream_t s) {
+  const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), (unsigned)ceil_div(pitch, kThreads));
+  pack_rows_kernel<T><<<grid, kThreads, 0, s>>>(static_cast<const T*>(src), st, (int)n, (int)rows, (int)width, static_cast<T*>(dst), pitch);
+  SVGEAR_LAUNCH_CHECK();
+  return SVGEAR_OK;
+}
+int pack(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, svgear_dtype dt, Workspace& w, Operand& out,
+         hipStream_t s) {
+  out.pitch = even_pitch(width, dt);
+  if (dt == SVGEAR_F32) {
+    float* p = w.take<float>((size_t)rows * out.pitch);
+    out.p = p;
+    return pack_rows<uint32_t>(src, st, n, rows, width, p, out.pitch, s);
+  }
+  bf16_t* p = w.take<bf16_t>((size_t)rows * out.pitch);
+  out.p = p;
+  return pack_rows<bf16_t>(src, st, n, rows, width, p, out.pitch, s);
+}
+
+bool sizes_ok(svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
+  return (dt == SVGEAR_F32 || dt == SVGEAR_BF16) && B > 0 && N > 0 && N <= INT32_MAX && (int64_t)B * N <= INT32_MAX &&
+         d_in > 0 && d_out > 0 && d_in <= kMaxWidth && d_out <= kMaxWidth;
+}
+bool input_ok(const void* p, const int64_t st[2], svgear_dtype dt) {
+  return p && st && st[0] >= 0 && st[1] >= 0 && reinterpret_cast<uintptr_t>(p) % esize(dt) == 0;
+}
+bool output_ok(const void* p, const int64_t st[2], svgear_dtype dt, int64_t B, int64_t N, int64_t width) {
+  if (!input_ok(p, st, dt)) return false;
+  const bool b_inner = st[0] < st[1];
+  const int64_t inner = b_inner ? st[0] : st[1], n_inner = b_inner ? B : N, outer = b_inner ? st[1] : st[0],
+                n_outer = b_inner ? N : B;
+  if (n_inner > 1 && inner < width) return false;
+  return n_outer == 1 || outer >= (n_inner > 1 ? (n_inner - 1) * inner : 0) + width;
+}
+bool wide_rows(const void* p, const int64_t st[2], svgear_dtype dt) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && st[0] % chunk(dt) == 0 && st[1] % chunk(dt) == 0;
+}
+
+int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
+  const int rc = dt == SVGEAR_F32 ? launch_linear_f32(a, form, s) : launch_linear_bf16(a, form, s);
+  if (rc != SVGEAR_OK || !a.partial) return rc;
+  return launch_linear_merge(a, dt, s);
+}
+
+// Parts that K is cut into where the output has too few tiles for the GPU, and the bytes of their products.
+int parts(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
+  (void)R, (void)C, (void)K, (void)dt;
+  return 1;
+}
+size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
+  const int p = parts(R, C, K, dt);
+  return p > 1 ? align_up((size_t)p * R * C * sizeof(float), 256) : 0;
+}
+void set_product(LinearArgs& a, const Operand& P, const Operand& Q, int64_t R, int64_t C, int64_t K, svgear_dtype dt,
+                 Workspace& w) {
+  a.P = P;
+  a.Q = Q;
+  a.R = (int)R;
+  a.C = (int)C;
+  a.K = K;
+  a.splits = parts(R, C, K, dt);
+  a.partial = a.splits > 1 ? w.take<float>((size_t)a.splits * R * C) : nullptr;
+}
+
+// Rows of a workgroup of linear_gradient_kernel; its workgroups of a batch entry.
+int gradient_rows(int64_t N) { return N >= 4096 ? 128 : 32; }
+int gradient_blocks(int64_t N) { return (int)ceil_div(N, gradient_rows(N)); }
+
+}  // namespace
+
+int sum_rows(const float* part, int rows, int cols, int groups, void* out, svgear_dtype dt, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(cols, 32), (unsigned)(groups < 65535 ? groups : 65535));
+  if (dt == SVGEAR_F32)
+    sum_rows_kernel<float><<<grid, kThreads, 0, s>>>(part, rows, cols, groups, static_cast<float*>(out));
+  else
+    sum_rows_kernel<bf16_t><<<grid, kThreads, 0, s>>>(part, rows, cols, groups, static_cast<bf16_t*>(out));
+  SVGEAR_LAUNCH_CHECK();
+  return SVGEAR_OK;
+}
+
+int launch_linear_merge(const LinearArgs& a, svgear_dtype dt, hipStream_t s) {
+  const int quads = (int)ceil_div(a.C, 4);
+  const unsigned blocks = (unsigned)ceil_div((int64_t)a.R * quads, kThreads);
+  if (dt == SVGEAR_F32)
+    linear_merge_kernel<float><<<blocks, kThreads, 0, s>>>(a, quads);
+  else
+    linear_merge_kernel<bf16_t><<<blocks, kThreads, 0, s>>>(a, quads);
+  SVGEAR_LAUNCH_CHECK();
+  return SVGEAR_OK;
+}
+
+}  // namespace svgear
+
+using namespace svgear;
+
+extern "C" size_t svgear_linear_workspace(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
+                                          svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
+  if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(x, xstride, dt) || !w || w_stride < d_in) return 0;
+  size_t bytes = 256;  // never empty
+  if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes((int64_t)B * N, d_in, dt);
+  if (!in_place(w, w_stride, d_in, dt)) bytes += packed_bytes(d_out, d_in, dt);
+  return bytes + parts_bytes((int64_t)B * N, d_out, d_in, dt);
+}
+
+extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
+                             const void* bias, svgear_dtype dt, int B, int64_t N, int d_in, int d_out, svgear_act act,
+                             const void* gate, const int64_t gstride[2], const void* residual,
+                             const int64_t rstride[2], void* pre, void* y, const int64_t ystride[2], void* ws,
+                             size_t ws_bytes, void* stream) {
+  if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(x, xstride, dt) || !w || reinterpret_cast<uintptr_t>(w) % esize(dt) ||
+      w_stride < d_in || !output_ok(y, ystride, dt, B, N, d_out) || (int)act < 0 || (int)act > (int)SVGEAR_ACT_GELU_TANH ||
+      (gate && !input_ok(gate, gstride, dt)) || (residual && !input_ok(residual, rstride, dt)) ||
+      reinterpret_cast<uintptr_t>(bias) % esize(dt) || reinterpret_cast<uintptr_t>(pre) % esize(dt))
+    return SVGEAR_ERR_INVALID;
+  if (residual == y && residual && (rstride[0] != ystride[0] || rstride[1] != ystride[1]) && (B > 1 || N > 1))
+    return SVGEAR_ERR_INVALID;
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 ||
+      ws_bytes < svgear_linear_workspace(x, xstride, w, w_stride, dt, B, N, d_in, d_out))
+    return SVGEAR_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Workspace space(ws, ws_bytes);
+  const int64_t M = (int64_t)B * N;
+  Operand X{x, run_pitch(xstride, B, N)}, W{w, w_stride};
+  if (!rows_in_place(x, xstride, B, N, d_in, dt)) {
+    const int rc = pack(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X, s);
+    if (rc != SVGEAR_OK) return rc;
+  }
+  if (!in_place(w, w_stride, d_in, dt)) {
+    const int rc = pack(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W, s);
+    if (rc != SVGEAR_OK) return rc;
+  }
+  LinearArgs a{};
+  set_product(a, W, X, M, d_out, d_in, dt, space);
+  a.n = (int)N;
+  a.bias = bias;
+  a.gate = gate;
+  a.residual = residual;
+  a.pre = pre;
+  a.y = y;
+  a.yst = Rows{ystride[0], ystride[1]};
+  if (gate) a.gst = Rows{gstride[0], gstride[1]};
+  if (residual) a.rst = Rows{rstride[0], rstride[1]};
+  a.act = act;
+  a.wide = d_out % chunk(dt) == 0 && wide_rows(y, ystride, dt) && (!gate || wide_rows(gate, gstride, dt)) &&
+           (!residual || wide_rows(residual, rstride, dt)) && reinterpret_cast<uintptr_t>(bias) % 16 == 0 &&
+           reinterpret_cast<uintptr_t>(pre) % 16 == 0;
+  return launch(a, dt, kContractBoth, s);
+}
+
+extern "C" size_t svgear_linear_backward_workspace(const void* dy, const int64_t dystride[2], const void* x,
+                                                   const int64_t xstride[2], const void* w, int64_t w_stride,
+                                                   svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
+  if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(dy, dystride, dt) || (x && !input_ok(x, xstride, dt)) ||
+      (w && w_stride < d_in))
+    return 0;
+  const int64_t M = (int64_t)B * N;
+  size_t bytes = 256 + packed_bytes(M, d_out, dt);  // dz
+  bytes += 2 * align_up((size_t)B * gradient_blocks(N) * d_out * sizeof(float), 256);
+  if (x) {
+    if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes(M, d_in, dt);
+    bytes += parts_bytes(d_out, d_in, M, dt);
+  }
+  if (w) {
+    if (!in_place(w, w_stride, d_in, dt)) bytes += packed_bytes(d_out, d_in, dt);
+    bytes += parts_bytes(M, d_in, d_out, dt);
+  }
+  return bytes;
+}
+
+extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void* x,
+                                      const int64_t xstride[2], const void* w, int64_t w_stride, const void* pre,
+                                      svgear_dtype dt, int B, int64_t N, int d_in, int d_out, svgear_act act,
+                                      const void* gate, const int64_t gstride[2], void* dx, const int64_t dxstride[2],
+                                      void* dw, void* dbias, void* dgate, void* ws, size_t ws_bytes, void* stream) {
+  const uintptr_t es = esize(dt);
+  if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(dy, dystride, dt) || (!dx && !dw && !dbias && !dgate) ||
+      (dw && !x) || (x && !input_ok(x, xstride, dt)) || (dx && !w) ||
+      (w && (w_stride < d_in || reinterpret_cast<uintptr_t>(w) % es)) || (int)act < 0 ||
+      (int)act > (int)SVGEAR_ACT_GELU_TANH || (gate && !input_ok(gate, gstride, dt)) || (dgate && !gate) ||
+      ((act != SVGEAR_ACT_NONE || dgate) && !pre) || (dx && !output_ok(dx, dxstride, dt, B, N, d_in)) ||
+      reinterpret_cast<uintptr_t>(pre) % es || reinterpret_cast<uintptr_t>(dw) % es ||
+      reinterpret_cast<uintptr_t>(dbias) % es || reinterpret_cast<uintptr_t>(dgate) % es)
+    return SVGEAR_ERR_INVALID;
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 ||
+      ws_bytes < svgear_linear_backward_workspace(dy, dystride, x, xstride, w, w_stride, dt, B, N, d_in, d_out))
+    return SVGEAR_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Workspace space(ws, ws_bytes);
+  const int64_t M = (int64_t)B * N;
+
+  // dz, unless it is dy itself and dy can be read where it is
+  Operand dz{dy, run_pitch(dystride, B, N)};
+  const bool same = act == SVGEAR_ACT_NONE && !gate;
+  const bool make = (dx || dw) && !(same && rows_in_place(dy, dystride, B, N, d_out, dt));
+  const bool token_gate = gate && gstride[1] != 0;
+  if (make || dbias || dgate) {
+    GradientArgs g{};
+    g.dy = dy;
+    g.pre = act != SVGEAR_ACT_NONE || dgate ? pre : nullptr;
+    g.gate = gate;
+    if (make) {
+      dz.pitch = even_pitch(d_out, dt);
+      g.dz = space.take<unsigned char>((size_t)M * dz.pitch * es);
+      dz.p = g.dz;
+    }
+    g.pitch = even_pitch(d_out, dt);
+    g.yst = Rows{dystride[0], dystride[1]};
+    if (gate) g.gst = Rows{gstride[0], gstride[1]};
+    g.C = d_out;
+    g.n = (int)N;
+    g.act = act;
+    g.rows_block = gradient_rows(N);
+    g.blocks_b = gradient_blocks(N);
+    const size_t sums = (size_t)B * g.blocks_b * d_out;
+    if (dbias) g.sum_dz = space.take<float>(sums);
+    if (dgate && !token_gate) g.sum_da = space.take<float>(sums);
+    if (dgate && token_gate) g.dgate = dgate;
+    const dim3 grid((unsigned)(B * g.blocks_b), (unsigned)ceil_div(g.pitch, 64));
+    if (dt == SVGEAR_F32)
+      linear_gradient_kernel<float><<<grid, kThreads, 0, s>>>(g);
+    else
+      linear_gradient_kernel<bf16_t><<<grid, kThreads, 0, s>>>(g);
+    SVGEAR_LAUNCH_CHECK();
+    if (dbias) {
+      const int rc = sum_rows(g.sum_dz, B * g.blocks_b, d_out, 1, dbias, dt, s);
+      if (rc != SVGEAR_OK) return rc;
+    }
+    if (g.sum_da) {
+      const int rc = sum_rows(g.sum_da, g.blocks_b, d_out, B, dgate, dt, s);
+      if (rc != SVGEAR_OK) return rc;
+    }
+  }
+
+  if (dx) {
+    Operand W{w, w_stride};
+    if (!in_place(w, w_stride, d_in, dt)) {
+      const int rc = pack(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W, s);
+      if (rc != SVGEAR_OK) return rc;
+    }
+    LinearArgs a{};
+    set_product(a, W, dz, M, d_in, d_out, dt, space);
+    a.n = (int)N;
+    a.y = dx;
+    a.yst = Rows{dxstride[0], dxstride[1]};
+    a.wide = d_in % chunk(dt) == 0 && wide_rows(dx, dxstride, dt);
+    const int rc = launch(a, dt, kContractQ, s);
+    if (rc != SVGEAR_OK) return rc;
+  }
+  if (dw) {
+    Operand X{x, run_pitch(xstride, B, N)};
+    if (!rows_in_place(x, xstride, B, N, d_in, dt)) {
+      const int rc = pack(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X, s);
+      if (rc != SVGEAR_OK) return rc;
+    }
+    LinearArgs a{};
+    set_product(a, X, dz, d_out, d_in, M, dt, space);
+    a.n = d_out;
+    a.y = dw;
+    a.yst = Rows{0, d_in};
+    const int64_t st[2] = {0, d_in};
+    a.wide = d_in % chunk(dt) == 0 && wide_rows(dw, st, dt);
+    const int rc = launch(a, dt, kContractNone, s);
+    if (rc != SVGEAR_OK) return rc;
+  }
+  return SVGEAR_OK;
+}
