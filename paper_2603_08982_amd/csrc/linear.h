@@ -21,6 +21,7 @@ struct LinearArgs {
   Operand P, Q;
   int64_t K;
   int R, C;
+  int tile;      // tile of the tile kernel: 64, 128, or (bf16) 256 rows and columns
   int splits;    // K in so many parts, each into its own slice of `partial`
   float* partial;  // [splits][R][C] or null
   // epilogue: row r is token r - b*n of batch entry b = r / n
@@ -32,7 +33,7 @@ struct LinearArgs {
   void* y;
   Rows gst, rst, yst;
   int act;
-  bool wide;  // every row of y, gate, residual and pre, and bias, 16-byte aligned, C a multiple of 16 bytes
+  bool wide;  // every row of y, gate, residual and pre, and bias, 16-byte aligned, C a multiple of 8
 };
 
 // How the contraction index lies in the operands: contiguous in both (forward), in Q alone (dx), in neither (dw).
@@ -85,16 +86,17 @@ __device__ __forceinline__ float load_as_f32<float>(const float* p) { return *p;
 template <>
 __device__ __forceinline__ float load_as_f32<bf16_t>(const bf16_t* p) { return bf16_to_f32(*p); }
 
-// Four consecutive elements, wide: one load or store.
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <>
-__device__ __forceinline__ float4 load4<bf16_t>(const bf16_t* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
+// Eight consecutive elements, 16-byte aligned.
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
+  v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
+  v[4] = __uint_as_float(u.z << 16), v[5] = __uint_as_float(u.z & 0xffff0000u);
+  v[6] = __uint_as_float(u.w << 16), v[7] = __uint_as_float(u.w & 0xffff0000u);
 }
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float lin_f32x2;
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 lin_bf16x2;
@@ -106,51 +108,58 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f32_to_bf16(v); }
-__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(bf16_t* p, float4 v) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
 
-// The epilogue of four consecutive columns c.. of row r (those < C).
+// The epilogue of eight consecutive columns c.. of row r (those < C; wide: all of them are, c is a multiple of 8).
 template <typename T>
-__device__ __forceinline__ void finish4(const LinearArgs& a, int r, int c, float4 v) {
+__device__ __forceinline__ void finish8(const LinearArgs& a, int r, int c, float (&v)[8]) {
   const int b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
   T* y = static_cast<T*>(a.y) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c;
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c : nullptr;
   const T* res = a.residual ? static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c : nullptr;
   T* pre = a.pre ? static_cast<T*>(a.pre) + (int64_t)r * a.C + c : nullptr;
   const T* bias = a.bias ? static_cast<const T*>(a.bias) + c : nullptr;
+  float w[8];
   if (a.wide) {
     if (bias) {
-      const float4 w = load4(bias);
-      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      load8(bias, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += w[i];
     }
-    if (pre) store4(pre, v);
+    if (pre) store8(pre, v);
     if (a.act != SVGEAR_ACT_NONE) {
-      v.x = act_value(a.act, v.x), v.y = act_value(a.act, v.y);
-      v.z = act_value(a.act, v.z), v.w = act_value(a.act, v.w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = act_value(a.act, v[i]);
     }
     if (gate) {
-      const float4 g = load4(gate);
-      v.x *= g.x, v.y *= g.y, v.z *= g.z, v.w *= g.w;
+      load8(gate, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= w[i];
     }
     if (res) {
-      const float4 q = load4(res);
-      v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+      load8(res, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += w[i];
     }
-    store4(y, v);
+    store8(y, v);
     return;
   }
-  float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (c + i >= a.C) break;
-    if (bias) e[i] += load_as_f32(bias + i);
-    if (pre) store1(pre + i, e[i]);
-    if (a.act != SVGEAR_ACT_NONE) e[i] = act_value(a.act, e[i]);
-    if (gate) e[i] *= load_as_f32(gate + i);
-    if (res) e[i] += load_as_f32(res + i);
-    store1(y + i, e[i]);
+  for (int i = 0; i < 8; ++i) {
+    if (c + i >= a.C) continue;
+    float e = v[i];
+    if (bias) e += load_as_f32(bias + i);
+    if (pre) store1(pre + i, e);
+    if (a.act != SVGEAR_ACT_NONE) e = act_value(a.act, e);
+    if (gate) e *= load_as_f32(gate + i);
+    if (res) e += load_as_f32(res + i);
+    store1(y + i, e);
   }
 }
 

@@ -46,24 +46,25 @@ sum_rows_kernel(const float* part, int rows, int cols, int groups, T* out) {
 // ---- the epilogue on partial products
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-linear_merge_kernel(LinearArgs a, int quads) {
+linear_merge_kernel(LinearArgs a, int runs) {
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int r = (int)(i / quads), c = (int)(i % quads) * 4;
+  const int r = (int)(i / runs), c = (int)(i % runs) * 8;
   if (r >= a.R) return;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int p = 0; p < a.splits; ++p) {
     const float* o = a.partial + ((int64_t)p * a.R + r) * a.C + c;
-    if (a.C % 4 == 0) {
-      const float4 w = *reinterpret_cast<const float4*>(o);
-      v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    if (a.C % 8 == 0) {
+      float w[8];
+      load8(o, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += w[k];
     } else {
-      v.x += o[0];
-      if (c + 1 < a.C) v.y += o[1];
-      if (c + 2 < a.C) v.z += o[2];
-      if (c + 3 < a.C) v.w += o[3];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < a.C) v[k] += o[k];
     }
   }
-  finish4<T>(a, r, c, v);
+  finish8<T>(a, r, c, v);
 }
 
 // ---- dz, the partial sums of dbias, and dgate
@@ -182,13 +183,41 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
   return launch_linear_merge(a, dt, s);
 }
 
-// Parts that K is cut into where the output has too few tiles for the GPU, and the bytes of their products.
-int parts(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
-  (void)R, (void)C, (void)K, (void)dt;
-  return 1;
+// Tile and number of parts of K of a product: the least of an estimate in microseconds,
+//   tiles of the CU that has most of them * (its steps * step + tile) + what joining the parts takes.
+// step and tile (prologue and epilogue) are measured. Both sides of the choices, us, MI355X, bf16: 1024 x 2048 of
+// 2048 in tiles of 64 / 128 / 256: 21 / 25 / 44; 9450 x 5120 of 5120: 796 / 493 / 406; 37800 x 15360 of 5120: 8795 / 5245 /
+// 4381. fp32: 1554 x 1000 of 640 in 64 / 128: 29 / 48; 8192 x 2048 of 2048: 563 / 483 (256: 544, never the least).
+struct Plan {
+  int tile, splits;
+};
+Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
+  struct Kind {
+    int tile;
+    double step, once;
+  };
+  static const Kind bf16[] = {{64, 0.19, 1.0}, {128, 0.49, 3.0}, {256, 1.45, 11.0}};
+  static const Kind f32[] = {{64, 0.53, 1.0}, {128, 2.0, 3.0}};
+  const Kind* kinds = dt == SVGEAR_F32 ? f32 : bf16;
+  const int64_t steps = ceil_div(K, dt == SVGEAR_F32 ? 32 : 64);
+  Plan best{64, 1};
+  double least = 1e300;
+  for (int i = 0; i < (dt == SVGEAR_F32 ? 2 : 3); ++i) {
+    const Kind& k = kinds[i];
+    const int64_t tiles = ceil_div(R, k.tile) * ceil_div(C, k.tile);
+    for (int p = 1; p <= 16 && (p == 1 || (steps >= 4 * p && tiles < 1024)); ++p) {
+      double us = (double)ceil_div(tiles * p, 256) * ((double)ceil_div(steps, p) * k.step + k.once);
+      if (p > 1) us += 6.0 + (double)p * (double)R * (double)C * 8.0 / 4e6;
+      if (us < least) {
+        least = us;
+        best = Plan{k.tile, p};
+      }
+    }
+  }
+  return best;
 }
 size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
-  const int p = parts(R, C, K, dt);
+  const int p = plan_product(R, C, K, dt).splits;
   return p > 1 ? align_up((size_t)p * R * C * sizeof(float), 256) : 0;
 }
 void set_product(LinearArgs& a, const Operand& P, const Operand& Q, int64_t R, int64_t C, int64_t K, svgear_dtype dt,
@@ -198,7 +227,9 @@ void set_product(LinearArgs& a, const Operand& P, const Operand& Q, int64_t R, i
   a.R = (int)R;
   a.C = (int)C;
   a.K = K;
-  a.splits = parts(R, C, K, dt);
+  const Plan plan = plan_product(R, C, K, dt);
+  a.tile = plan.tile;
+  a.splits = plan.splits;
   a.partial = a.splits > 1 ? w.take<float>((size_t)a.splits * R * C) : nullptr;
 }
 
@@ -219,12 +250,12 @@ int sum_rows(const float* part, int rows, int cols, int groups, void* out, svgea
 }
 
 int launch_linear_merge(const LinearArgs& a, svgear_dtype dt, hipStream_t s) {
-  const int quads = (int)ceil_div(a.C, 4);
-  const unsigned blocks = (unsigned)ceil_div((int64_t)a.R * quads, kThreads);
+  const int runs = (int)ceil_div(a.C, 8);
+  const unsigned blocks = (unsigned)ceil_div((int64_t)a.R * runs, kThreads);
   if (dt == SVGEAR_F32)
-    linear_merge_kernel<float><<<blocks, kThreads, 0, s>>>(a, quads);
+    linear_merge_kernel<float><<<blocks, kThreads, 0, s>>>(a, runs);
   else
-    linear_merge_kernel<bf16_t><<<blocks, kThreads, 0, s>>>(a, quads);
+    linear_merge_kernel<bf16_t><<<blocks, kThreads, 0, s>>>(a, runs);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }
@@ -281,7 +312,7 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
   if (gate) a.gst = Rows{gstride[0], gstride[1]};
   if (residual) a.rst = Rows{rstride[0], rstride[1]};
   a.act = act;
-  a.wide = d_out % chunk(dt) == 0 && wide_rows(y, ystride, dt) && (!gate || wide_rows(gate, gstride, dt)) &&
+  a.wide = d_out % 8 == 0 && wide_rows(y, ystride, dt) && (!gate || wide_rows(gate, gstride, dt)) &&
            (!residual || wide_rows(residual, rstride, dt)) && reinterpret_cast<uintptr_t>(bias) % 16 == 0 &&
            reinterpret_cast<uintptr_t>(pre) % 16 == 0;
   return launch(a, dt, kContractBoth, s);
@@ -382,7 +413,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     a.n = (int)N;
     a.y = dx;
     a.yst = Rows{dxstride[0], dxstride[1]};
-    a.wide = d_in % chunk(dt) == 0 && wide_rows(dx, dxstride, dt);
+    a.wide = d_in % 8 == 0 && wide_rows(dx, dxstride, dt);
     const int rc = launch(a, dt, kContractQ, s);
     if (rc != SVGEAR_OK) return rc;
   }
@@ -398,7 +429,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     a.y = dw;
     a.yst = Rows{0, d_in};
     const int64_t st[2] = {0, d_in};
-    a.wide = d_in % chunk(dt) == 0 && wide_rows(dw, st, dt);
+    a.wide = d_in % 8 == 0 && wide_rows(dw, st, dt);
     const int rc = launch(a, dt, kContractNone, s);
     if (rc != SVGEAR_OK) return rc;
   }

@@ -2,8 +2,8 @@
 //
 // out[r][c] = sum_k Q[r][k] P[c][k]. A workgroup makes a tile of BC columns by BR rows; its waves hold
 // their shares as 32 x 32 MFMA blocks whose row index is c, so that a lane ends with four consecutive
-// columns of one row. K is walked in steps of 128 bytes per row (64 bf16, 32 fp32), two steps' tiles in
-// LDS: the copies of the next step, straight from global memory, run under the products of this one.
+// columns of one row. K is walked in steps of 128 bytes per row (64 bf16, 32 fp32); the copies of later steps' tiles,
+// straight from global memory into LDS, run under the products of this one.
 //
 // An operand whose contraction index is contiguous lies in LDS as rows of 128 bytes; a lane's fragment is one
 // 16-byte chunk. One whose contraction index runs over rows (dx: w; dw: both) lies there as it does in
@@ -82,20 +82,14 @@ struct Tile {
     base = static_cast<const unsigned char*>(o.p) + first * ES;
     step = (OVER_ROWS ? BK * o.pitch : (int64_t)BK) * ES;
   }
-  // Copies the step whose first element is `base` into lds and goes on; `left`: k that remain.
-  __device__ __forceinline__ void copy(uint32_t lds, int64_t left, int wave) {
-    if (left >= BK) {
-#pragma unroll
-      for (int i = 0; i < COPIES; ++i)
-        async_copy_16B(base, off[i], __builtin_amdgcn_readfirstlane(lds + (wave + i * WAVES) * 1024));
-    } else {
-#pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const void* src = kk[i] < left ? static_cast<const void*>(base + off[i]) : static_cast<const void*>(g_zero_chunk);
-        async_copy_16B(src, __builtin_amdgcn_readfirstlane(lds + (wave + i * WAVES) * 1024));
-      }
-    }
-    base += step;
+  // Copy i of the step whose first element is `base` into lds; LAST: the last step, `left` k of which exist.
+  template <bool LAST>
+  __device__ __forceinline__ void copy(int i, uint32_t lds, int left, int wave) const {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (wave + i * WAVES) * 1024);
+    if constexpr (!LAST)
+      async_copy_16B(base, off[i], to);
+    else
+      async_copy_16B(kk[i] < left ? static_cast<const void*>(base + off[i]) : static_cast<const void*>(g_zero_chunk), to);
   }
 };
 
@@ -143,6 +137,11 @@ struct Reader {
   }
 };
 
+// All waves' LDS reads are done and may be overwritten; copies in flight stay so (a plain barrier waits for them).
+__device__ __forceinline__ void workgroup_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 template <typename T>
 __device__ __forceinline__ void multiply(const Frag& p, const Frag& q, f32x16& acc) {
   if constexpr (sizeof(T) == 2) {
@@ -161,22 +160,30 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
   constexpr bool P_ROWS = FORM != kContractBoth, Q_ROWS = FORM == kContractNone;
   typedef Tile<T, BC, P_ROWS, WAVES> PT;
   typedef Tile<T, BR, Q_ROWS, WAVES> QT;
-  constexpr int BK = PT::BK, STAGE = PT::BYTES + QT::BYTES;
+  constexpr int BK = PT::BK, LDS = 3 * PT::BYTES + 2 * QT::BYTES;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wc = wave % WC, wr = wave / WC;
 
-  // Tile of this workgroup. Workgroups go to the 8 XCDs in turn: each XCD gets a run of tiles of its own, in
-  // order of 8 tile rows a column at a time, so that what runs on it together shares both operands in its L2.
-  const int tiles = tiles_c * tiles_r, bid = blockIdx.x;
-  const int xcd = bid & 7, per = tiles >> 3, more = tiles & 7;
-  const int t = xcd * per + min(xcd, more) + (bid >> 3);
-  const int band = t / (8 * tiles_c), band_r = min(8, tiles_r - 8 * band), in_band = t - band * 8 * tiles_c;
-  const int r0 = (8 * band + in_band % band_r) * BR, c0 = in_band / band_r * BC;
+  // Tile of this workgroup. Tiles are numbered column by column in bands of 16 tile rows, and 256 at a time run
+  // together: 16 x 16 tiles, which read 32 panels of the operands out of the 256 MB cache behind the L2s.
+  // Workgroups go to the 8 XCDs in turn; each gets 8 x 4 tiles of those, so that its L2 serves 32 tiles with 12
+  // panels. What is left of 256 goes to them in runs.
+  const int tiles = tiles_c * tiles_r, bid = blockIdx.x, xcd = bid & 7, whole = tiles & ~255;
+  int t;
+  if (bid < whole) {
+    const int i = (bid & 255) >> 3;
+    t = (bid & ~255) + (4 * (xcd >> 1) + (i >> 3)) * 16 + 8 * (xcd & 1) + (i & 7);
+  } else {
+    const int per = (tiles - whole) >> 3, more = (tiles - whole) & 7;
+    t = whole + xcd * per + min(xcd, more) + ((bid - whole) >> 3);
+  }
+  const int band = t / (16 * tiles_c), band_r = min(16, tiles_r - 16 * band), in_band = t - band * 16 * tiles_c;
+  const int r0 = (16 * band + in_band % band_r) * BR, c0 = in_band / band_r * BC;
 
   const int64_t steps = (a.K + BK - 1) / BK, part = blockIdx.y;
   const int64_t s0 = steps * part / a.splits, s1 = steps * (part + 1) / a.splits;
-  int64_t left = a.K - s0 * BK;  // k from the next copy's first on
+  const int left = (int)min((int64_t)BK, a.K - (s1 - 1) * BK);  // k of the last step
   const int n = (int)(s1 - s0);
 
   PT pt;
@@ -187,75 +194,152 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
   Reader<T, BR, Q_ROWS, TR> qr;
   pr.init(wc * 32 * TC, lane);
   qr.init(wr * 32 * TR, lane);
-  const uint32_t lds0 = lds_address(smem);
-  auto copy = [&](int buf) __attribute__((always_inline)) {
-    pt.copy(lds0 + buf * STAGE, left, wave);
-    qt.copy(lds0 + buf * STAGE + PT::BYTES, left, wave);
-    left -= BK;
-  };
-
   f32x16 acc[TC][TR];
 #pragma unroll
   for (int i = 0; i < TC; ++i)
 #pragma unroll
     for (int j = 0; j < TR; ++j) acc[i][j] = f32x16{};
 
-  copy(0);
-  SVGEAR_WAIT_VMCNT(0);
-  __syncthreads();
-  for (int k = 0; k < n; ++k) {
-    if (k + 1 < n) copy((k + 1) & 1);
-    const unsigned char* ps = smem + (k & 1) * STAGE;
-    const unsigned char* qs = ps + PT::BYTES;
+  // The main loop's step k is four contraction steps. Under the products of each, the fragments of the next one
+  // are read, across steps too: the workgroup's barrier lies before the last products of a step, when all its
+  // fragments are in registers. Copies: P has three buffers and Q two, so P's of step k+2 go out under the first
+  // products of step k and Q's behind its barrier, and none is waited for sooner than three contraction steps later.
+  Frag pf[2][TC], qf[2][TR];
+  const uint32_t lds0 = lds_address(smem);
+  enum { kNo, kFull, kLast };
+  constexpr std::integral_constant<int, kNo> no{};
+  constexpr std::integral_constant<int, kFull> full{};
+  constexpr std::integral_constant<int, kLast> last{};
+  constexpr std::true_type yes{};
+  constexpr std::false_type none{};
+  auto copy_p = [&](int i, int slot, auto mode) __attribute__((always_inline)) {
+    pt.template copy<mode.value == kLast>(i, lds0 + slot * PT::BYTES, left, wave);
+    if (i == PT::COPIES - 1) pt.base += pt.step;
+  };
+  auto copy_q = [&](int i, int slot, auto mode) __attribute__((always_inline)) {
+    qt.template copy<mode.value == kLast>(i, lds0 + 3 * PT::BYTES + slot * QT::BYTES, left, wave);
+    if (i == QT::COPIES - 1) qt.base += qt.step;
+  };
+  auto read = [&](int i, int p_slot, int q_slot, int s, int set) __attribute__((always_inline)) {
+    if (i < TC) pf[set][i] = pr.get(smem + p_slot * PT::BYTES, i, s);
+    else if (i < TC + TR) qf[set][i - TC] = qr.get(smem + 3 * PT::BYTES + q_slot * QT::BYTES, i - TC, s);
+  };
+  // products of `set`; between them the reads of the other set's fragments, and what `more` does at each
+  constexpr int BLOCKS = TC * TR;
+  auto step = [&](int set, auto reads, int p_slot, int q_slot, int s, auto more) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      Frag pf[TC], qf[TR];
+    for (int m = 0; m < BLOCKS; ++m) {
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (reads.value) {
+        constexpr int PER = (TC + TR + BLOCKS - 1) / BLOCKS;
 #pragma unroll
-      for (int i = 0; i < TC; ++i) pf[i] = pr.get(ps, i, s);
-#pragma unroll
-      for (int j = 0; j < TR; ++j) qf[j] = qr.get(qs, j, s);
-#pragma unroll
-      for (int i = 0; i < TC; ++i)
-#pragma unroll
-        for (int j = 0; j < TR; ++j) multiply<T>(pf[i], qf[j], acc[i][j]);
+        for (int i = 0; i < PER; ++i) read(m * PER + i, p_slot, q_slot, s, set ^ 1);
+      }
+      more(m);
+      multiply<T>(pf[set][m / TR], qf[set][m % TR], acc[m / TR][m % TR]);
     }
+  };
+  auto nothing = [](int) {};
+  // `share` copies spread evenly over a contraction step's products
+  auto spread = [&](int m, int share, auto go) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < share; ++i)
+      if (i * BLOCKS / share == m) go(i);
+  };
+  int slot = 0;  // k % 3
+  auto iterate = [&](int k, auto mode, auto next) __attribute__((always_inline)) {
+    constexpr int H = PT::COPIES / 2;
+    const int before = slot == 0 ? 2 : slot - 1, after = slot == 2 ? 0 : slot + 1;
+    step(0, yes, slot, k & 1, 1, [&](int m) __attribute__((always_inline)) {
+      if constexpr (mode.value != kNo) spread(m, H, [&](int i) { copy_p(i, before, mode); });
+    });
+    step(1, yes, slot, k & 1, 2, [&](int m) __attribute__((always_inline)) {
+      if constexpr (mode.value != kNo) spread(m, PT::COPIES - H, [&](int i) { copy_p(H + i, before, mode); });
+    });
+    step(0, yes, slot, k & 1, 3, nothing);
+    if constexpr (next.value) {
+      if constexpr (mode.value != kNo)
+        SVGEAR_WAIT_VMCNT(PT::COPIES);
+      else
+        SVGEAR_WAIT_VMCNT(0);
+      workgroup_barrier();
+      step(1, yes, after, (k + 1) & 1, 0, [&](int m) __attribute__((always_inline)) {
+        if constexpr (mode.value != kNo) spread(m, QT::COPIES, [&](int i) { copy_q(i, k & 1, mode); });
+      });
+    } else {
+      step(1, none, 0, 0, 0, nothing);
+    }
+    slot = after;
+  };
+  auto copies = [&](int to, auto mode) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PT::COPIES; ++i) copy_p(i, to, mode);
+#pragma unroll
+    for (int i = 0; i < QT::COPIES; ++i) copy_q(i, to, mode);
+  };
+  if (n == 1) {
+    copies(0, last);
     SVGEAR_WAIT_VMCNT(0);
-    __syncthreads();
+  } else {
+    copies(0, full);
+    if (n == 2) copies(1, last);
+    else copies(1, full);
+    SVGEAR_WAIT_VMCNT(PT::COPIES + QT::COPIES);
   }
+  workgroup_barrier();
+#pragma unroll
+  for (int i = 0; i < TC + TR; ++i) read(i, 0, 0, 0, 0);
+  int k = 0;
+  for (; k + 3 < n; ++k) iterate(k, full, yes);
+  if (k + 2 < n) iterate(k++, last, yes);
+  if (k + 1 < n) iterate(k++, no, yes);
+  iterate(k, no, none);
+  __syncthreads();
 
-  // a lane's block holds columns 8g + 4lh + 0..3 of row li
+  // A wave's 32 rows at a time go through its own part of LDS, so that what is read and written of a row is one
+  // run of 16-byte pieces: block i, group g of a lane are columns 32i + 8g + 4lh + 0..3 of row li.
+  constexpr int COLS = 32 * TC, CHUNKS = COLS / 4, LANES = COLS / 8;  // LANES share a row
+  static_assert(32 * COLS * 4 * WAVES <= LDS, "the waves' parts must fit");
+  unsigned char* own = smem + wave * (32 * COLS * 4);
   const int li = lane & 31, lh = lane >> 5;
+  const int c = c0 + wc * COLS + (lane % LANES) * 8;
 #pragma unroll
   for (int j = 0; j < TR; ++j) {
-    const int r = r0 + (wr * TR + j) * 32 + li;
-    if (r >= a.R) continue;
 #pragma unroll
     for (int i = 0; i < TC; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = c0 + (wc * TC + i) * 32 + 8 * g + 4 * lh;
-        if (c >= a.C) continue;
-        const float4 v = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
-        if (a.partial) {
-          float* o = a.partial + (part * a.R + r) * a.C + c;
-          if (a.C % 4 == 0) {
-            *reinterpret_cast<float4*>(o) = v;
-          } else {
-            o[0] = v.x;
-            if (c + 1 < a.C) o[1] = v.y;
-            if (c + 2 < a.C) o[2] = v.z;
-            if (c + 3 < a.C) o[3] = v.w;
-          }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(own + li * (COLS * 4) + (((8 * i + 2 * g + lh) ^ (li & (CHUNKS - 1))) << 4)) =
+            make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+    for (int q = 0; q < 32; q += 64 / LANES) {
+      const int row = q + lane / LANES, r = r0 + (wr * TR + j) * 32 + row;
+      const int x = row & (CHUNKS - 1), at = 2 * (lane % LANES);
+      const float4 lo = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + ((at ^ x) << 4));
+      const float4 hi = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + (((at + 1) ^ x) << 4));
+      if (r >= a.R || c >= a.C) continue;
+      float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      if (a.partial) {
+        float* o = a.partial + (part * a.R + r) * a.C + c;
+        if (a.C % 8 == 0) {
+          store8(o, v);
         } else {
-          finish4<T>(a, r, c, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c + i < a.C) o[i] = v[i];
         }
+      } else {
+        finish8<T>(a, r, c, v);
       }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
 template <typename T, int FORM, int TC, int TR, int WC, int WR>
 int launch_tiles(const LinearArgs& a, hipStream_t s) {
-  constexpr int BC = 32 * TC * WC, BR = 32 * TR * WR, lds = 2 * (BC + BR) * 128;
+  constexpr int BC = 32 * TC * WC, BR = 32 * TR * WR, lds = (3 * BC + 2 * BR) * 128;
   const int tc = (int)ceil_div(a.C, BC), tr = (int)ceil_div(a.R, BR);
   if ((int64_t)tc * tr > INT32_MAX) return SVGEAR_ERR_UNSUPPORTED;
   auto kern = linear_tile_kernel<T, FORM, TC, TR, WC, WR>;
@@ -266,12 +350,23 @@ int launch_tiles(const LinearArgs& a, hipStream_t s) {
   return SVGEAR_OK;
 }
 
+template <typename T, int FORM>
+int launch_form(const LinearArgs& a, hipStream_t s) {
+  switch (a.tile) {
+    case 64: return launch_tiles<T, FORM, 1, 1, 2, 2>(a, s);
+    case 128: return launch_tiles<T, FORM, 2, 2, 2, 2>(a, s);
+    case 256:
+      if constexpr (sizeof(T) == 2) return launch_tiles<T, FORM, 2, 4, 4, 2>(a, s);
+  }
+  return SVGEAR_ERR_UNSUPPORTED;
+}
+
 template <typename T>
 int launch_linear(const LinearArgs& a, int form, hipStream_t s) {
   switch (form) {
-    case kContractBoth: return launch_tiles<T, kContractBoth, 2, 2, 2, 2>(a, s);
-    case kContractQ: return launch_tiles<T, kContractQ, 2, 2, 2, 2>(a, s);
-    default: return launch_tiles<T, kContractNone, 2, 2, 2, 2>(a, s);
+    case kContractBoth: return launch_form<T, kContractBoth>(a, s);
+    case kContractQ: return launch_form<T, kContractQ>(a, s);
+    default: return launch_form<T, kContractNone>(a, s);
   }
 }
 

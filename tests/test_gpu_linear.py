@@ -60,6 +60,26 @@ def test_every_epilogue(rows, act, dtype):
                 close(y, Y, by, f"bias={bias} gate={gate} residual={residual}")
 
 
+# an output of 17 x 17 tiles of 256 in each of the three products, with edges in every direction, and contractions of one to
+# several steps, with an odd end
+WIDE = [(1, 4099, 72, 4104), (1, 4099, 200, 4104), (1, 4099, 4104, 136), (2, 75, 4104, 4104), (3, 1367, 331, 4104), (1, 4099, 64, 4099)]
+
+
+@pytest.mark.parametrize("size", WIDE, ids=str)
+def test_large_outputs(size):
+    i = WIDE.index(size)
+    x, w, b, g, r = inputs(torch.bfloat16, *size, bias=True, gate=["batch", "token"][i % 2], residual=True, seed=200 + i)
+    y, pre = sv.linear(x, w, b, act="silu", gate=g, residual=r, want_pre=True)
+    Y, Z, by, bz = linear64(x, w, b, "silu", g, r)
+    close(pre, Z, bz, "pre")
+    close(y, Y, by, "y")
+    dy = rand(*pre.shape, seed=300 + i, dtype=torch.bfloat16).cuda()
+    got = sv.linear_backward(dy, x, w, pre=pre, act="silu", gate=g, want=["dx", "dw", "dbias", "dgate"])
+    ref = linear_backward64(dy, x, w, pre, "silu", g, UNIT[torch.bfloat16])
+    for name in got:
+        close(got[name], *ref[name], name)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 @pytest.mark.parametrize("size", SIZES, ids=str)
 def test_backward_of_every_size(size, dtype):
