@@ -363,6 +363,35 @@ def _require(ok, what: str):
         raise SvgearError(what)
 
 
+class _OnDevice:
+    """The given tensor's GPU as the current one, for calls whose tensors lie on another."""
+
+    def __init__(self, t: torch.Tensor):
+        self.index = t.device.index
+        self.guard = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.index:
+            self.guard = torch.cuda.device(self.index)
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    return torch.cuda.current_stream(t.device.index).cuda_stream
+
+
+def _scratch(nbytes: int, device):
+    """Workspace of an entry point that may need none: (tensor or None, its address, its size)."""
+    if nbytes == 0:
+        return None, None, 0
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return t, t.data_ptr(), nbytes
+
+
 def _same_place(first: torch.Tensor, dtype, *ts):
     """Every tensor given lies on the first one's GPU and has its type."""
     _need_gpu(first, *ts)
@@ -409,15 +438,16 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     _require(residual is None or tuple(residual.shape) == (*lead, d_out), "residual: expected the output's shape")
     _require(out is None or tuple(out.shape) == (*lead, d_out), "out: expected the output's shape")
     rst = _as_bnd(residual, "residual")[3] if residual is not None else _I64x2(0, 0)
-    with torch.cuda.device(x.device):
+    with _OnDevice(x):
         y = torch.empty(*lead, d_out, dtype=x.dtype, device=x.device) if out is None else out
         pre = torch.empty(*lead, d_out, dtype=x.dtype, device=x.device) if want_pre else None
         yst = _as_bnd(y, "out")[3]
         ldw = w.stride(0) if d_out > 1 else max(w.stride(0), d_in)
         head = (_ptr(x), xst, _ptr(w), ldw)
-        ws = _ws(lib.svgear_linear_workspace(*head, _dt(x), B, N, d_in, d_out), x.device)
-        rc = lib.svgear_linear(*head, _ptr(bias), _dt(x), B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
-                               _ptr(residual), rst, _ptr(pre), _ptr(y), yst, _ptr(ws), ws.numel(), _stream())
+        dt = _dt(x)
+        ws, *space = _scratch(lib.svgear_linear_workspace(*head, dt, B, N, d_in, d_out), x.device)
+        rc = lib.svgear_linear(*head, _ptr(bias), dt, B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
+                               _ptr(residual), rst, _ptr(pre), _ptr(y), yst, *space, _stream_of(x))
     _check(rc, "svgear_linear")
     return y, pre
 
@@ -445,7 +475,7 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[tor
     gst, per_token = _gate_strides(gate, lead, d_out)
     xst = _as_bnd(x, "x")[3] if x is not None else _I64x2(0, 0)
     _require(not per_token or gst[1] != 0 or N == 1 or "dgate" not in want, "gate: one gate for all tokens is given as [B,d_out]")
-    with torch.cuda.device(dy.device):
+    with _OnDevice(dy):
         new = lambda *shape: torch.empty(*shape, dtype=dy.dtype, device=dy.device)
         r = {}
         for name in want:
@@ -454,10 +484,10 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[tor
         dxst = _as_bnd(dx, "dx")[3] if dx is not None else _I64x2(0, 0)
         ldw = 0 if w is None else w.stride(0) if d_out > 1 else max(w.stride(0), d_in)
         head = (_ptr(dy), dyst, _ptr(x), xst, _ptr(w), ldw)
-        ws = _ws(lib.svgear_linear_backward_workspace(*head, _dt(dy), B, N, d_in, d_out), dy.device)
+        ws, *space = _scratch(lib.svgear_linear_backward_workspace(*head, _dt(dy), B, N, d_in, d_out), dy.device)
         rc = lib.svgear_linear_backward(*head, _ptr(pre), _dt(dy), B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
                                         _ptr(dx), dxst, _ptr(r.get("dw")), _ptr(r.get("dbias")), _ptr(r.get("dgate")),
-                                        _ptr(ws), ws.numel(), _stream())
+                                        *space, _stream_of(dy))
     _check(rc, "svgear_linear_backward")
     return r
 
@@ -468,14 +498,19 @@ def rotary_frequencies(sections: Sequence[int], theta: float = 10000.0, device="
     return torch.cat(f).to(device)
 
 
+_PTRS = (None, _vp * 1, _vp * 2)
+_ROWS = (None, _I64x3 * 1, _I64x3 * 2)
+
+
 def _pointers(ts):
-    return (_vp * len(ts))(*[_ptr(t) for t in ts])
+    return _PTRS[len(ts)](*[None if t is None else t.data_ptr() for t in ts])
 
 
 def _strides_of(ts):
-    for t in ts:
-        _require(t.dim() == 4 and t.stride(3) == 1, "expected [B,H,N,d] with contiguous d")
-    return (_I64x3 * len(ts))(*[(t.stride(0), t.stride(1), t.stride(2)) for t in ts])
+    strides = [t.stride() for t in ts]
+    for st in strides:
+        _require(len(st) == 4 and st[3] == 1, "expected [B,H,N,d] with contiguous d")
+    return _ROWS[len(ts)](*[st[:3] for st in strides])
 
 
 def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves):
@@ -521,12 +556,12 @@ def rotary(tensors: Sequence[torch.Tensor], inv_freq: torch.Tensor, sections: Se
     lib = load_library()
     ws, places = _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves)
     B, H, N, d = t0.shape
-    with torch.cuda.device(t0.device):
+    with _OnDevice(t0):
         if out is None:
             outs = [torch.empty(B, H, N, d, dtype=t0.dtype, device=t0.device) for _ in tensors]
         _require(len(outs) == len(tensors) and all(o.shape == t0.shape for o in outs), "out: one for each tensor, of its shape")
         rc = lib.svgear_rotary(len(tensors), _pointers(tensors), _strides_of(tensors), _pointers(outs), _strides_of(outs),
-                               _pointers(ws), _dt(t0), B, H, N, n_tail, d, *places, float(eps), _stream())
+                               _pointers(ws), _dt(t0), B, H, N, n_tail, d, *places, float(eps), _stream_of(t0))
     _check(rc, "svgear_rotary")
     return outs
 
@@ -548,18 +583,18 @@ def rotary_backward(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[to
     ws, places = _rotary_places(grads, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves)
     B, H, N, d = g0.shape
     n = len(grads)
-    with torch.cuda.device(g0.device):
+    with _OnDevice(g0):
         if out is None:
             outs = [torch.empty(B, H, N, d, dtype=g0.dtype, device=g0.device) for _ in grads]
         _require(len(outs) == n and all(o.shape == g0.shape for o in outs), "out: one for each tensor, of its shape")
         dweight = None
         if norm is not None and want_dweight:
             dweight = [torch.empty(d if norm == "head" else H * d, dtype=g0.dtype, device=g0.device) for _ in grads]
-        scratch = _ws(lib.svgear_rotary_backward_workspace(n, B, H, N, d) if dweight else 0, g0.device)
+        scratch, *space = _scratch(lib.svgear_rotary_backward_workspace(n, B, H, N, d) if dweight else 0, g0.device)
         rc = lib.svgear_rotary_backward(n, _pointers(grads), _strides_of(grads), _pointers(tensors) if tensors else None,
                                         _strides_of(tensors) if tensors else None, _pointers(outs), _strides_of(outs),
                                         _pointers(ws), _pointers(dweight) if dweight else None, _dt(g0), B, H, N, n_tail, d,
-                                        *places, float(eps), _ptr(scratch), scratch.numel(), _stream())
+                                        *places, float(eps), *space, _stream_of(g0))
     _check(rc, "svgear_rotary_backward")
     return outs, dweight
 

@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libsvgear.so")
 SOURCES = ["api.hip", "permute.hip", "kmeans.hip", "kmeans_small.hip", "probe.hip", "route.hip", "attention.hip", "attention_bf16.hip",
-           "attention_f32.hip", "rotary.hip", "linear.hip", "linear_bf16.hip", "linear_f32.hip"]
+           "attention_f32.hip", "rotary.hip", "linear.hip", "linear_bf16.hip", "linear_f32.hip", "linear_rows.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

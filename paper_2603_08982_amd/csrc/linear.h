@@ -21,7 +21,8 @@ struct LinearArgs {
   Operand P, Q;
   int64_t K;
   int R, C;
-  int tile;      // tile of the tile kernel: 64, 128, or (bf16) 256 rows and columns
+  int tile;      // tile of the tile kernel: 64, 128, or (bf16) 256 rows and columns; 0: the kernel of few rows
+  bool even;     // for it: rows of the operands are as the tile kernel needs them
   int splits;    // K in so many parts, each into its own slice of `partial`
   float* partial;  // [splits][R][C] or null
   // epilogue: row r is token r - b*n of batch entry b = r / n
@@ -41,6 +42,10 @@ enum { kContractBoth = 0, kContractQ = 1, kContractNone = 2 };
 
 int launch_linear_bf16(const LinearArgs& a, int form, hipStream_t s);
 int launch_linear_f32(const LinearArgs& a, int form, hipStream_t s);
+// The same for few rows (kContractBoth), operands at any alignment. Up to 4 in bf16: 4 / 8 rows of 5120 by 5120 18.5 / 33 us,
+// by tiles of 64 22 / 22; up to 8 in fp32, which needs no unpacking: 27 / 35 us and 42 / 42.
+static inline int few_rows(svgear_dtype dt) { return dt == SVGEAR_F32 ? 8 : 4; }
+int launch_linear_rows(const LinearArgs& a, svgear_dtype dt, hipStream_t s);
 // y from the partial products of `splits` parts.
 int launch_linear_merge(const LinearArgs& a, svgear_dtype dt, hipStream_t s);
 
@@ -116,6 +121,17 @@ __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
 
+// The epilogue of one element.
+template <typename T>
+__device__ __forceinline__ void finish1(const LinearArgs& a, const T* bias, const T* gate, const T* res, T* pre, T* y, float v) {
+  if (bias) v += load_as_f32(bias);
+  if (pre) store1(pre, v);
+  if (a.act != SVGEAR_ACT_NONE) v = act_value(a.act, v);
+  if (gate) v *= load_as_f32(gate);
+  if (res) v += load_as_f32(res);
+  store1(y, v);
+}
+
 // The epilogue of eight consecutive columns c.. of row r (those < C; wide: all of them are, c is a multiple of 8).
 template <typename T>
 __device__ __forceinline__ void finish8(const LinearArgs& a, int r, int c, float (&v)[8]) {
@@ -151,15 +167,29 @@ __device__ __forceinline__ void finish8(const LinearArgs& a, int r, int c, float
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (c + i >= a.C) continue;
-    float e = v[i];
-    if (bias) e += load_as_f32(bias + i);
-    if (pre) store1(pre + i, e);
-    if (a.act != SVGEAR_ACT_NONE) e = act_value(a.act, e);
-    if (gate) e *= load_as_f32(gate + i);
-    if (res) e += load_as_f32(res + i);
-    store1(y + i, e);
+  for (int i = 0; i < 8; ++i)
+    if (c + i < a.C) finish1<T>(a, bias ? bias + i : nullptr, gate ? gate + i : nullptr, res ? res + i : nullptr, pre ? pre + i : nullptr, y + i, v[i]);
+}
+
+template <typename T>
+__device__ __forceinline__ void finish1(const LinearArgs& a, int r, int c, float v) {
+  const int b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
+  finish1<T>(a, a.bias ? static_cast<const T*>(a.bias) + c : nullptr,
+             a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c : nullptr,
+             a.residual ? static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c : nullptr,
+             a.pre ? static_cast<T*>(a.pre) + (int64_t)r * a.C + c : nullptr,
+             static_cast<T*>(a.y) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c, v);
+}
+
+// Eight consecutive columns of a part's product.
+__device__ __forceinline__ void store_partial8(const LinearArgs& a, int64_t part, int r, int c, const float (&v)[8]) {
+  float* o = a.partial + (part * a.R + r) * a.C + c;
+  if (a.C % 8 == 0) {
+    store8(o, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < a.C) o[i] = v[i];
   }
 }
 

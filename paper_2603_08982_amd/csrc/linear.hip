@@ -158,6 +158,16 @@ int pack(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, svgea
   return pack_rows<bf16_t>(src, st, n, rows, width, p, out.pitch, s);
 }
 
+// What of svgear_linear's operands goes through the workspace. Few rows: x only, where its batches are not one run of rows.
+struct Copies {
+  bool x, w;
+};
+Copies operand_copies(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride, svgear_dtype dt, int B,
+                      int64_t N, int64_t d_in) {
+  if (B * N <= few_rows(dt)) return Copies{run_pitch(xstride, B, N) < 0, false};
+  return Copies{!rows_in_place(x, xstride, B, N, d_in, dt), !in_place(w, w_stride, d_in, dt)};
+}
+
 bool sizes_ok(svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
   return (dt == SVGEAR_F32 || dt == SVGEAR_BF16) && B > 0 && N > 0 && N <= INT32_MAX && (int64_t)B * N <= INT32_MAX &&
          d_in > 0 && d_out > 0 && d_in <= kMaxWidth && d_out <= kMaxWidth;
@@ -178,7 +188,7 @@ bool wide_rows(const void* p, const int64_t st[2], svgear_dtype dt) {
 }
 
 int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
-  const int rc = dt == SVGEAR_F32 ? launch_linear_f32(a, form, s) : launch_linear_bf16(a, form, s);
+  const int rc = a.tile == 0 ? launch_linear_rows(a, dt, s) : dt == SVGEAR_F32 ? launch_linear_f32(a, form, s) : launch_linear_bf16(a, form, s);
   if (rc != SVGEAR_OK || !a.partial) return rc;
   return launch_linear_merge(a, dt, s);
 }
@@ -188,10 +198,12 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
 // step and tile (prologue and epilogue) are measured. Both sides of the choices, us, MI355X, bf16: 1024 x 2048 of
 // 2048 in tiles of 64 / 128 / 256: 21 / 25 / 44; 9450 x 5120 of 5120: 796 / 493 / 406; 37800 x 15360 of 5120: 8795 / 5245 /
 // 4381. fp32: 1554 x 1000 of 640 in 64 / 128: 29 / 48; 8192 x 2048 of 2048: 563 / 483 (256: 544, never the least).
+// Few rows (forward only) go to the kernel that reads the weights straight into registers.
 struct Plan {
   int tile, splits;
 };
-Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
+Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
+  if (form == kContractBoth && R <= few_rows(dt)) return Plan{0, 1};
   struct Kind {
     int tile;
     double step, once;
@@ -216,18 +228,18 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
   }
   return best;
 }
-size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt) {
-  const int p = plan_product(R, C, K, dt).splits;
+size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
+  const int p = plan_product(R, C, K, dt, form).splits;
   return p > 1 ? align_up((size_t)p * R * C * sizeof(float), 256) : 0;
 }
 void set_product(LinearArgs& a, const Operand& P, const Operand& Q, int64_t R, int64_t C, int64_t K, svgear_dtype dt,
-                 Workspace& w) {
+                 int form, Workspace& w) {
   a.P = P;
   a.Q = Q;
   a.R = (int)R;
   a.C = (int)C;
   a.K = K;
-  const Plan plan = plan_product(R, C, K, dt);
+  const Plan plan = plan_product(R, C, K, dt, form);
   a.tile = plan.tile;
   a.splits = plan.splits;
   a.partial = a.splits > 1 ? w.take<float>((size_t)a.splits * R * C) : nullptr;
@@ -267,10 +279,11 @@ using namespace svgear;
 extern "C" size_t svgear_linear_workspace(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
                                           svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
   if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(x, xstride, dt) || !w || w_stride < d_in) return 0;
-  size_t bytes = 256;  // never empty
-  if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes((int64_t)B * N, d_in, dt);
-  if (!in_place(w, w_stride, d_in, dt)) bytes += packed_bytes(d_out, d_in, dt);
-  return bytes + parts_bytes((int64_t)B * N, d_out, d_in, dt);
+  const Copies copies = operand_copies(x, xstride, w, w_stride, dt, B, N, d_in);
+  size_t bytes = 0;
+  if (copies.x) bytes += packed_bytes((int64_t)B * N, d_in, dt);
+  if (copies.w) bytes += packed_bytes(d_out, d_in, dt);
+  return bytes + parts_bytes((int64_t)B * N, d_out, d_in, dt, kContractBoth);
 }
 
 extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
@@ -285,23 +298,24 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
     return SVGEAR_ERR_INVALID;
   if (residual == y && residual && (rstride[0] != ystride[0] || rstride[1] != ystride[1]) && (B > 1 || N > 1))
     return SVGEAR_ERR_INVALID;
-  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 ||
-      ws_bytes < svgear_linear_workspace(x, xstride, w, w_stride, dt, B, N, d_in, d_out))
-    return SVGEAR_ERR_WORKSPACE;
+  const size_t need = svgear_linear_workspace(x, xstride, w, w_stride, dt, B, N, d_in, d_out);
+  if (need && (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < need)) return SVGEAR_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Workspace space(ws, ws_bytes);
   const int64_t M = (int64_t)B * N;
   Operand X{x, run_pitch(xstride, B, N)}, W{w, w_stride};
-  if (!rows_in_place(x, xstride, B, N, d_in, dt)) {
+  const Copies copies = operand_copies(x, xstride, w, w_stride, dt, B, N, d_in);
+  if (copies.x) {
     const int rc = pack(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X, s);
     if (rc != SVGEAR_OK) return rc;
   }
-  if (!in_place(w, w_stride, d_in, dt)) {
+  if (copies.w) {
     const int rc = pack(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W, s);
     if (rc != SVGEAR_OK) return rc;
   }
   LinearArgs a{};
-  set_product(a, W, X, M, d_out, d_in, dt, space);
+  set_product(a, W, X, M, d_out, d_in, dt, kContractBoth, space);
+  a.even = in_place(X.p, X.pitch, d_in, dt) && in_place(W.p, W.pitch, d_in, dt);
   a.n = (int)N;
   a.bias = bias;
   a.gate = gate;
@@ -329,11 +343,11 @@ extern "C" size_t svgear_linear_backward_workspace(const void* dy, const int64_t
   bytes += 2 * align_up((size_t)B * gradient_blocks(N) * d_out * sizeof(float), 256);
   if (x) {
     if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes(M, d_in, dt);
-    bytes += parts_bytes(d_out, d_in, M, dt);
+    bytes += parts_bytes(d_out, d_in, M, dt, kContractNone);
   }
   if (w) {
     if (!in_place(w, w_stride, d_in, dt)) bytes += packed_bytes(d_out, d_in, dt);
-    bytes += parts_bytes(M, d_in, d_out, dt);
+    bytes += parts_bytes(M, d_in, d_out, dt, kContractQ);
   }
   return bytes;
 }
@@ -409,7 +423,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
       if (rc != SVGEAR_OK) return rc;
     }
     LinearArgs a{};
-    set_product(a, W, dz, M, d_in, d_out, dt, space);
+    set_product(a, W, dz, M, d_in, d_out, dt, kContractQ, space);
     a.n = (int)N;
     a.y = dx;
     a.yst = Rows{dxstride[0], dxstride[1]};
@@ -424,7 +438,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
       if (rc != SVGEAR_OK) return rc;
     }
     LinearArgs a{};
-    set_product(a, X, dz, d_out, d_in, M, dt, space);
+    set_product(a, X, dz, d_out, d_in, M, dt, kContractNone, space);
     a.n = d_out;
     a.y = dw;
     a.yst = Rows{0, d_in};

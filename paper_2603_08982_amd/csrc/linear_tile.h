@@ -321,14 +321,7 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
       if (r >= a.R || c >= a.C) continue;
       float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
       if (a.partial) {
-        float* o = a.partial + (part * a.R + r) * a.C + c;
-        if (a.C % 8 == 0) {
-          store8(o, v);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (c + i < a.C) o[i] = v[i];
-        }
+        store_partial8(a, part, r, c, v);
       } else {
         finish8<T>(a, r, c, v);
       }
