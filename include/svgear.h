@@ -342,7 +342,8 @@ typedef enum {
   SVGEAR_ACT_SILU = 1,       /* z / (1 + e^-z) */
   SVGEAR_ACT_GELU = 2,       /* z (1 + erf(z / sqrt 2)) / 2 */
   SVGEAR_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
-  SVGEAR_ACT_INT_RANGE = 0x7fffffff
+  SVGEAR_ACT_INT_LOW = -0x7fffffff - 1, /* the range of int, as for svgear_dtype */
+  SVGEAR_ACT_INT_HIGH = 0x7fffffff
 } svgear_act;
 
 size_t svgear_linear_workspace(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,

@@ -1,0 +1,117 @@
+"""What the Python entry points of linear and rotary refuse before anything is launched."""
+import pytest
+import torch
+
+import paper_2603_08982_amd as sv
+
+pytestmark = pytest.mark.gpu
+
+
+def z(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+
+X, W = (2, 3, 16), (8, 16)
+BAD_LINEAR = {
+    "another type": lambda: sv.linear(z(*X), z(*W, dtype=torch.float32)),
+    "an unknown type": lambda: sv.linear(z(*X, dtype=torch.float16), z(*W, dtype=torch.float16)),
+    "w of another width": lambda: sv.linear(z(*X), z(8, 15)),
+    "w transposed": lambda: sv.linear(z(*X), z(16, 8).t()),
+    "x transposed": lambda: sv.linear(z(2, 16, 3).transpose(1, 2), z(*W)),
+    "x of four dimensions": lambda: sv.linear(z(1, 2, 3, 16), z(*W)),
+    "bias of another length": lambda: sv.linear(z(*X), z(*W), z(9)),
+    "bias strided": lambda: sv.linear(z(*X), z(*W), z(16)[::2]),
+    "an unknown activation": lambda: sv.linear(z(*X), z(*W), act="relu"),
+    "gate of another shape": lambda: sv.linear(z(*X), z(*W), gate=z(3, 8)),
+    "gate strided": lambda: sv.linear(z(*X), z(*W), gate=z(2, 16)[:, ::2]),
+    "residual of another shape": lambda: sv.linear(z(*X), z(*W), residual=z(2, 3, 7)),
+    "out of another shape": lambda: sv.linear(z(*X), z(*W), out=z(2, 3, 9)),
+    "out whose rows meet": lambda: sv.linear(z(*X), z(*W), out=z(2, 1, 8).expand(2, 3, 8)),
+    "no tokens": lambda: sv.linear(z(2, 0, 16), z(*W)),
+    "nothing wanted": lambda: sv.linear_backward(z(2, 3, 8), z(*X), z(*W), want=[]),
+    "an unknown gradient": lambda: sv.linear_backward(z(2, 3, 8), z(*X), z(*W), want=["db"]),
+    "dw without x": lambda: sv.linear_backward(z(2, 3, 8), None, z(*W), want=["dw"]),
+    "dx without w": lambda: sv.linear_backward(z(2, 3, 8), z(*X), None, want=["dx"]),
+    "dgate without a gate": lambda: sv.linear_backward(z(2, 3, 8), z(*X), z(*W), pre=z(2, 3, 8), want=["dgate"]),
+    "an activation without pre": lambda: sv.linear_backward(z(2, 3, 8), z(*X), z(*W), act="silu"),
+    "pre of another shape": lambda: sv.linear_backward(z(2, 3, 8), z(*X), z(*W), pre=z(2, 3, 9), act="silu"),
+    "x of other tokens": lambda: sv.linear_backward(z(2, 3, 8), z(2, 4, 16), z(*W)),
+    "dgate of a token gate that is one row": lambda: sv.linear_backward(z(2, 3, 8), z(*X), z(*W), pre=z(2, 3, 8), gate=z(2, 1, 8).expand(2, 3, 8), want=["dgate"]),
+}
+
+
+@pytest.mark.parametrize("what", BAD_LINEAR)
+def test_linear_refuses(what):
+    with pytest.raises(sv.SvgearError):
+        BAD_LINEAR[what]()
+
+
+Q = (1, 2, 24, 64)
+S = (10, 11, 11)
+
+
+def rot(q=None, back=False, f=None, s=S, **kw):
+    q = z(*Q) if q is None else q
+    f = sv.rotary_frequencies(s) if f is None else f
+    kw.setdefault("grid", None if "positions" in kw else (2, 3, 4))
+    return sv.rotary_backward([q], [q], f, s, **kw) if back else sv.rotary([q], f, s, **kw)
+
+
+i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device="cuda")
+BAD_ROTARY = {
+    "an unknown type": dict(q=lambda: z(*Q, dtype=torch.float16)),
+    "heads of 32": dict(q=lambda: z(1, 2, 24, 32)),
+    "a tensor of three dimensions": dict(q=lambda: z(2, 24, 64)),
+    "d not contiguous": dict(q=lambda: z(1, 2, 64, 24).transpose(2, 3)),
+    "rows of no 16 bytes": dict(q=lambda: z(1, 2, 24, 68)[..., :64]),
+    "frequencies in 32 bits": dict(f=lambda: sv.rotary_frequencies(S).float()),
+    "frequencies of another length": dict(f=lambda: sv.rotary_frequencies((10, 11, 10))),
+    "frequencies on the host": dict(f=lambda: sv.rotary_frequencies(S, device="cpu")),
+    "two axes": dict(s=(10, 11)),
+    "too many pairs": dict(s=(11, 11, 11)),
+    "tokens past the grid": dict(first=1),
+    "a grid of two axes": dict(grid=(6, 4)),
+    "no positions at all": dict(grid=None),
+    "grid and positions": dict(grid=(2, 3, 4), positions=lambda: i32(24, 3)),
+    "positions in 64 bits": dict(positions=lambda: i32(24, 3).long()),
+    "positions of the text tokens too": dict(positions=lambda: i32(24, 3), n_tail=2),
+    "positions strided": dict(positions=lambda: i32(24, 6)[:, ::2]),
+    "an unknown norm": dict(norm="layer"),
+    "weights without a norm": dict(weights=lambda: [z(64)]),
+    "weights of another length": dict(norm="token", weights=lambda: [z(64)]),
+    "weights for two tensors": dict(norm="head", weights=lambda: [z(64), z(64)]),
+    "weights of another type": dict(norm="head", weights=lambda: [z(64, dtype=torch.float32)]),
+    "only text tokens": dict(n_tail=24),
+    "out of another shape": dict(out=lambda: [z(1, 2, 25, 64)]),
+    "out whose rows meet": dict(out=lambda: [z(1, 2, 1, 64).expand(1, 2, 24, 64)]),
+}
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("what", BAD_ROTARY)
+def test_rotary_refuses(what, back):
+    kw = {k: v() if callable(v) else v for k, v in BAD_ROTARY[what].items()}
+    with pytest.raises(sv.SvgearError):
+        rot(back=back, **kw)
+
+
+def test_rotary_refuses_three_tensors_and_a_norm_without_inputs():
+    q = z(*Q)
+    f = sv.rotary_frequencies(S)
+    with pytest.raises(sv.SvgearError):
+        sv.rotary([q, q, q], f, S, grid=(2, 3, 4))
+    with pytest.raises(sv.SvgearError):
+        sv.rotary([], f, S, grid=(2, 3, 4))
+    with pytest.raises(sv.SvgearError):
+        sv.rotary([q, z(1, 2, 23, 64)], f, S, grid=(2, 3, 4))
+    with pytest.raises(sv.SvgearError):
+        sv.rotary_backward([q], None, f, S, grid=(2, 3, 4), norm="head")
+
+
+def test_block_refuses_weights_of_other_sizes():
+    x, c = z(1, 24, 32), torch.zeros(1, 2, 3, 64, device="cuda")
+    f = sv.rotary_frequencies(S)
+    with pytest.raises(sv.SvgearError):
+        sv.attention_block(x, z(3 * 128 + 1, 32), z(32, 128), c, c.clone(), 1, 100, f, S, grid=(2, 3, 4))
+    with pytest.raises(sv.SvgearError):
+        sv.attention_block(x, z(3 * 128, 32), z(32, 127), c, c.clone(), 1, 100, f, S, grid=(2, 3, 4))
