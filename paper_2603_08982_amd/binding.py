@@ -516,6 +516,7 @@ def _strides_of(ts):
 def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves):
     """The checked arguments that rotary and its backward pass share: (weights, arguments from inv_freq to flags)."""
     t0 = tensors[0]
+    _require(t0.dim() == 4, "expected [B,H,N,d] with contiguous d")
     B, H, N, d = t0.shape
     _require(len(tensors) in (1, 2) and all(t.shape == t0.shape for t in tensors), "one or two tensors of one shape [B,H,N,d]")
     _require(len(sections) == 3, "sections: pairs of the three axes")
