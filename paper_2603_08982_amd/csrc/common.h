@@ -57,6 +57,16 @@ __device__ __forceinline__ bf16_t f32_to_bf16(float f) {
   return (bf16_t)(u >> 16);
 }
 
+// two at once, by the hardware's conversion
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32_pair;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16_pair;
+__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
+  f32_pair f = {lo, hi};
+  union { bf16_pair b; uint32_t u; } c;
+  c.b = __builtin_convertvector(f, bf16_pair);
+  return c.u;
+}
+
 // Batch*head decomposition for strided [B,H,N,d] tensors.
 struct Strides {
   int64_t b, h, n;
@@ -108,9 +118,10 @@ int sort_labels(const int32_t* labels, int BH, int64_t N, int64_t n_tail, int C,
                 int tile_len = 64);
 
 
-// out[g][c] = sum over i of part[g][i][c], rows added in one fixed order, in fp32, rounded once to dt
-// (linear.hip).
-int sum_rows(const float* part, int rows, int cols, int groups, void* out, svgear_dtype dt, hipStream_t s);
+// out[g][c] = sum over i of part[g][i][c], rows added in one fixed order, in fp32, rounded once to dt; part2
+// and out2, if not null, likewise (linear.hip).
+int sum_rows(const float* part, void* out, const float* part2, void* out2, int rows, int cols, int groups, svgear_dtype dt,
+             hipStream_t s);
 
 // Per-head length of the probe's per-key statistic arrays (padded so that 16-byte reads
 // starting at any key stay inside the array).

@@ -103,14 +103,6 @@ __device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
   v[4] = __uint_as_float(u.z << 16), v[5] = __uint_as_float(u.z & 0xffff0000u);
   v[6] = __uint_as_float(u.w << 16), v[7] = __uint_as_float(u.w & 0xffff0000u);
 }
-typedef __attribute__((__vector_size__(2 * sizeof(float)))) float lin_f32x2;
-typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 lin_bf16x2;
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  lin_f32x2 f = {lo, hi};
-  union { lin_bf16x2 b; uint32_t u; } c;
-  c.b = __builtin_convertvector(f, lin_bf16x2);
-  return c.u;
-}
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f32_to_bf16(v); }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
@@ -118,7 +110,7 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
 }
 
 // The epilogue of one element.

@@ -22,21 +22,25 @@ pack_rows_kernel(const T* src, Rows st, int n, int rows, int width, T* dst, int6
   }
 }
 
-// ---- out[g][c] = sum over i of part[g][i][c]: eight runs of rows, then those
+// ---- out[g][c] = sum over i of part[g][i][c]: 32 runs of rows, each every 32nd, then those in order
+constexpr int kSumThreads = 1024;
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
-sum_rows_kernel(const float* part, int rows, int cols, int groups, T* out) {
-  __shared__ float s[8][33];
+__global__ void __launch_bounds__(kSumThreads)
+sum_rows_kernel(const float* part, T* out, const float* part2, T* out2, int rows, int cols, int groups) {
+  __shared__ float s[32][33];
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+  if (blockIdx.z) part = part2, out = out2;
   for (int g = blockIdx.y; g < groups; g += gridDim.y) {
     const float* p = part + (int64_t)g * rows * cols;
     float v = 0.f;
     if (c < cols)
-      for (int i = y; i < rows; i += 8) v += p[(int64_t)i * cols + c];
+#pragma unroll 8
+      for (int i = y; i < rows; i += 32) v += p[(int64_t)i * cols + c];
     s[y][x] = v;
     __syncthreads();
     if (y == 0 && c < cols) {
-      for (int k = 1; k < 8; ++k) v += s[k][x];
+#pragma unroll
+      for (int k = 1; k < 32; ++k) v += s[k][x];
       store1(out + (int64_t)g * cols + c, v);
     }
     __syncthreads();
@@ -251,12 +255,13 @@ int gradient_blocks(int64_t N) { return (int)ceil_div(N, gradient_rows(N)); }
 
 }  // namespace
 
-int sum_rows(const float* part, int rows, int cols, int groups, void* out, svgear_dtype dt, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div(cols, 32), (unsigned)(groups < 65535 ? groups : 65535));
+int sum_rows(const float* part, void* out, const float* part2, void* out2, int rows, int cols, int groups, svgear_dtype dt,
+             hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(cols, 32), (unsigned)(groups < 65535 ? groups : 65535), part2 ? 2 : 1);
   if (dt == SVGEAR_F32)
-    sum_rows_kernel<float><<<grid, kThreads, 0, s>>>(part, rows, cols, groups, static_cast<float*>(out));
+    sum_rows_kernel<float><<<grid, kSumThreads, 0, s>>>(part, static_cast<float*>(out), part2, static_cast<float*>(out2), rows, cols, groups);
   else
-    sum_rows_kernel<bf16_t><<<grid, kThreads, 0, s>>>(part, rows, cols, groups, static_cast<bf16_t*>(out));
+    sum_rows_kernel<bf16_t><<<grid, kSumThreads, 0, s>>>(part, static_cast<bf16_t*>(out), part2, static_cast<bf16_t*>(out2), rows, cols, groups);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }
@@ -407,11 +412,11 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
       linear_gradient_kernel<bf16_t><<<grid, kThreads, 0, s>>>(g);
     SVGEAR_LAUNCH_CHECK();
     if (dbias) {
-      const int rc = sum_rows(g.sum_dz, B * g.blocks_b, d_out, 1, dbias, dt, s);
+      const int rc = sum_rows(g.sum_dz, dbias, nullptr, nullptr, B * g.blocks_b, d_out, 1, dt, s);
       if (rc != SVGEAR_OK) return rc;
     }
     if (g.sum_da) {
-      const int rc = sum_rows(g.sum_da, g.blocks_b, d_out, B, dgate, dt, s);
+      const int rc = sum_rows(g.sum_da, dgate, nullptr, nullptr, g.blocks_b, d_out, B, dt, s);
       if (rc != SVGEAR_OK) return rc;
     }
   }

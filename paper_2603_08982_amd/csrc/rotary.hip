@@ -15,7 +15,10 @@ namespace {
 
 constexpr int kMaxHeads = 128;
 constexpr int kRotWaves = 8;          // waves of a workgroup, at most
-constexpr int kBackwardGroups = 512;  // workgroups of the backward pass, at most: each leaves a partial dweight
+// Workgroups of the backward pass for a tensor, at most; each leaves a partial dweight. Two tensors' 512 are all on the
+// GPU at once, with five waves each for 40 heads of 128: 75,600 tokens take 1,052 us, with 384 / 512 / 768 groups a tensor
+// 1,312 / 1,396 / 1,271.
+constexpr int kBackwardGroups = 256;
 
 struct RotaryArgs {
   const void* src[2];     // x (forward), x of the norm (backward)
@@ -31,6 +34,7 @@ struct RotaryArgs {
   int sec0, sec01, pairs;
   int first, plane, width;  // grid: tokens of a time step, of a row
   int waves_per_token, its;
+  int rows;  // backward: workgroups, rows of `partial`
   float eps, sign;
 };
 
@@ -45,12 +49,7 @@ struct Chunk<bf16_t, 8> {
     return __uint_as_float((i & 1) ? (u & 0xffff0000u) : (u << 16));
   }
   static __device__ __forceinline__ Chunk of(const float* v) {
-    Chunk c;
-    c.r.x = f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16);
-    c.r.y = f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16);
-    c.r.z = f32_to_bf16(v[4]) | ((uint32_t)f32_to_bf16(v[5]) << 16);
-    c.r.w = f32_to_bf16(v[6]) | ((uint32_t)f32_to_bf16(v[7]) << 16);
-    return c;
+    return Chunk{make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]))};
   }
 };
 template <>
@@ -75,6 +74,10 @@ struct Chunk<float, 1> {
 // Heads a wave holds: `its` times 64 / (d / 2V); enough for 40 heads of 128 in 16-byte chunks.
 template <typename T, int V>
 constexpr int kMaxIts = V == 1 ? 16 : V == 4 ? 10 : 5;
+// Backward: it holds two tensors, turned gradients and the sums of dweight, so a wave takes fewer heads and a token more
+// waves: few of them up to 64 heads of 128, twice as many beyond.
+template <typename T, int V>
+constexpr int kFewIts = V == 1 ? 8 : V == 4 ? 2 : 1;
 
 enum { kNormNone = 0, kNormHead = 1, kNormToken = 2 };
 
@@ -125,7 +128,7 @@ __device__ __forceinline__ void turn(float (&xa)[V], float (&xb)[V], const float
     if (rotated <= 0) return;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float u = xa[i] * cs[i].x - xb[i] * cs[i].y, v = xa[i] * cs[i].y + xb[i] * cs[i].x;
+      const float u = __builtin_fmaf(xa[i], cs[i].x, -xb[i] * cs[i].y), v = __builtin_fmaf(xa[i], cs[i].y, xb[i] * cs[i].x);
       xa[i] = u;
       xb[i] = v;
     }
@@ -133,7 +136,7 @@ __device__ __forceinline__ void turn(float (&xa)[V], float (&xb)[V], const float
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float* x = i < V / 2 ? xa + 2 * i : xb + 2 * (i - V / 2);
-      const float u = x[0] * cs[i].x - x[1] * cs[i].y, v = x[0] * cs[i].y + x[1] * cs[i].x;
+      const float u = __builtin_fmaf(x[0], cs[i].x, -x[1] * cs[i].y), v = __builtin_fmaf(x[0], cs[i].y, x[1] * cs[i].x);
       if (i < rotated) x[0] = u, x[1] = v;
     }
   }
@@ -200,7 +203,10 @@ rotary_kernel(RotaryArgs a) {
       sum[it] = 0.f;
       if (it < a.its && h0 + it * at.per_wave < H) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[it] += xa[it].get(i) * xa[it].get(i) + xb[it].get(i) * xb[it].get(i);
+        for (int i = 0; i < V; ++i) {
+          sum[it] = __builtin_fmaf(xa[it].get(i), xa[it].get(i), sum[it]);
+          sum[it] = __builtin_fmaf(xb[it].get(i), xb[it].get(i), sum[it]);
+        }
       }
       if (NORM == kNormToken) all += sum[it];
     }
@@ -241,118 +247,163 @@ rotary_kernel(RotaryArgs a) {
 }
 
 // Backward with a norm. Every workgroup takes tokens at a distance and keeps its sums of du x f in registers
-// until the end, then leaves them, its waves' tokens added in order, as one row of `partial`.
-template <typename T, int V, int NORM, bool HALVES>
+// until the end, then leaves them, its waves' tokens added in order, as one row of `partial`. A lane has some 16
+// vector instructions an element, with the turned gradients kept for the second use; the first version, which
+// turned them twice and packed by hand, had some 40 and was bound by them.
+template <typename T, int V, int NORM, bool HALVES, int IT>
 __global__ void __launch_bounds__(64 * kRotWaves)
 rotary_backward_kernel(RotaryArgs a) {
-  constexpr int IT = kMaxIts<T, V>;
   constexpr int AT = NORM == kNormToken ? IT : 1;  // a head's weight is shared by all heads
-  __shared__ float2 rows[kRotWaves][64];
-  __shared__ float slots[kRotWaves], slots2[kRotWaves];
-  __shared__ float acc_s[kRotWaves][64][2 * V];
+  __shared__ float2 rows[2][kRotWaves][64];
+  __shared__ float2 slots[2][kRotWaves];
+  constexpr int Q = V == 1 ? 2 : 4;  // sums of a lane that go through LDS at a time
+  __shared__ float acc_s[kRotWaves][64][Q];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wpt = a.waves_per_token, per_group = (blockDim.x >> 6) / wpt;
+  const int wpt = a.waves_per_token, per_group = (blockDim.x >> 6) / wpt, first = wave - wave % wpt;
   const int k = blockIdx.y, units = a.d / (2 * V);
   const Lane<V, HALVES> at(lane, a.d, a.pairs);
   const T* weight = static_cast<const T*>(a.weight[k]);
   const int h0 = (wave % wpt) * a.its * at.per_wave + at.sub;
   float acc[AT][2 * V];
+  Chunk<T, V> wa[AT], wb[AT];
 #pragma unroll
-  for (int it = 0; it < AT; ++it)
+  for (int it = 0; it < AT; ++it) {
 #pragma unroll
     for (int i = 0; i < 2 * V; ++i) acc[it][i] = 0.f;
+    const int h = h0 + it * at.per_wave;
+    float one[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) one[i] = 1.f;
+    wa[it] = wb[it] = Chunk<T, V>::of(one);
+    if (weight && it < a.its && (NORM == kNormHead || h < a.H)) {
+      const T* w = weight + (NORM == kNormToken ? h * a.d : 0);
+      wa[it] = *reinterpret_cast<const Chunk<T, V>*>(w + at.ea);
+      wb[it] = *reinterpret_cast<const Chunk<T, V>*>(w + at.eb);
+    }
+  }
 
-  for (int t0 = blockIdx.x * per_group; t0 < a.tokens; t0 += gridDim.x * per_group) {
+  // A token's rows are on their way and its angles found while the one before it is finished. LDS rows and slots of every
+  // second token are others, so that the one barrier of a token orders both.
+  struct Token {
+    const T *x, *dy;
+    T* dx;
+    int b, n, H;
+  };
+  auto place = [&](int t0) __attribute__((always_inline)) {
     const int token = t0 + wave / wpt;
+    Token t;
     const bool on = token < a.tokens;
-    const int b = on ? token / a.N : 0, n = on ? token - b * a.N : 0;
-    const int H = on ? a.H : 0;
-    const T* src = static_cast<const T*>(a.src[k]) + (int64_t)b * a.sst[k].b + (int64_t)n * a.sst[k].n;
-    const T* dy = static_cast<const T*>(a.dy[k]) + (int64_t)b * a.yst[k].b + (int64_t)n * a.yst[k].n;
-    T* dst = static_cast<T*>(a.dst[k]) + (int64_t)b * a.dst_st[k].b + (int64_t)n * a.dst_st[k].n;
-    Chunk<T, V> xa[IT], xb[IT], ya[IT], yb[IT];
+    t.b = on ? token / a.N : 0;
+    t.n = on ? token - t.b * a.N : 0;
+    t.H = on ? a.H : 0;
+    t.x = static_cast<const T*>(a.src[k]) + (int64_t)t.b * a.sst[k].b + (int64_t)t.n * a.sst[k].n;
+    t.dy = static_cast<const T*>(a.dy[k]) + (int64_t)t.b * a.yst[k].b + (int64_t)t.n * a.yst[k].n;
+    t.dx = static_cast<T*>(a.dst[k]) + (int64_t)t.b * a.dst_st[k].b + (int64_t)t.n * a.dst_st[k].n;
+    return t;
+  };
+  Chunk<T, V> xa[IT], xb[IT], ya[IT], yb[IT], na[IT], nb[IT];  // x and dy of the token, x of the next
+  auto load_dy = [&](const Token& t) __attribute__((always_inline)) {
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int h = h0 + it * at.per_wave;
-      if (it < a.its && h < H) {
-        const T* p = src + (int64_t)h * a.sst[k].h;
-        xa[it] = *reinterpret_cast<const Chunk<T, V>*>(p + at.ea);
-        xb[it] = *reinterpret_cast<const Chunk<T, V>*>(p + at.eb);
-        const T* q = dy + (int64_t)h * a.yst[k].h;
+      if (it < a.its && h < t.H) {
+        const T* q = t.dy + (int64_t)h * a.yst[k].h;
         ya[it] = *reinterpret_cast<const Chunk<T, V>*>(q + at.ea);
         yb[it] = *reinterpret_cast<const Chunk<T, V>*>(q + at.eb);
       }
     }
-    __syncthreads();  // the last token's angles have been read
-    if (on) find_angles(a, b, n, lane, rows[wave]);
-    __syncthreads();
+  };
+  auto load_x = [&](const Token& t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+      const int h = h0 + it * at.per_wave;
+      if (it < a.its && h < t.H) {
+        const T* p = t.x + (int64_t)h * a.sst[k].h;
+        na[it] = *reinterpret_cast<const Chunk<T, V>*>(p + at.ea);
+        nb[it] = *reinterpret_cast<const Chunk<T, V>*>(p + at.eb);
+      }
+    }
+  };
+  const int stride = gridDim.x * per_group;
+  int turn_of = 0;
+  Token now = place(blockIdx.x * per_group);
+  load_x(now);
+  load_dy(now);
+  if (now.H && wave == first) find_angles(a, now.b, now.n, lane, rows[0][first]);
+  __syncthreads();
+  for (int t0 = blockIdx.x * per_group; t0 < a.tokens; t0 += stride, turn_of ^= 1) {
+    const int n = now.n, H = now.H;
     float2 cs[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) cs[i] = rows[wave][at.p0 + i];
+    for (int i = 0; i < V; ++i) cs[i] = rows[turn_of][first][at.p0 + i];
+#pragma unroll
+    for (int it = 0; it < IT; ++it) xa[it] = na[it], xb[it] = nb[it];
     const int rotated = (n < a.n_rot ? a.pairs : 0) - at.p0;
 
-    // du, g = du weight and the sums of x^2 and g x of iteration `it`
-    auto gradient = [&](int it, int h, float (&ua)[V], float (&ub)[V], float (&ga)[V], float (&gb)[V], float& xx,
-                        float& gx) __attribute__((always_inline)) {
+    float ua[IT][V], ub[IT][V];  // du
+    float xx[IT], gx[IT];        // sums of x^2 and g x, by head or all in [0]
 #pragma unroll
-      for (int i = 0; i < V; ++i) ua[i] = ya[it].get(i), ub[i] = yb[it].get(i);
-      turn<V, HALVES>(ua, ub, cs, rotated);
+    for (int it = 0; it < IT; ++it) {
+      xx[it] = gx[it] = 0.f;
+      if (it < a.its && h0 + it * at.per_wave < H) {
+        const int iw = NORM == kNormToken ? it : 0;
 #pragma unroll
-      for (int i = 0; i < V; ++i) ga[i] = ua[i], gb[i] = ub[i];
-      if (weight) {
-        const T* w = weight + (NORM == kNormToken ? h * a.d : 0);
-        const Chunk<T, V> wa = *reinterpret_cast<const Chunk<T, V>*>(w + at.ea);
-        const Chunk<T, V> wb = *reinterpret_cast<const Chunk<T, V>*>(w + at.eb);
+        for (int i = 0; i < V; ++i) ua[it][i] = ya[it].get(i), ub[it][i] = yb[it].get(i);
+        turn<V, HALVES>(ua[it], ub[it], cs, rotated);
 #pragma unroll
-        for (int i = 0; i < V; ++i) ga[i] *= wa.get(i), gb[i] *= wb.get(i);
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float x0 = xa[it].get(i), x1 = xb[it].get(i);
-        xx += x0 * x0 + x1 * x1;
-        gx += ga[i] * x0 + gb[i] * x1;
-      }
-    };
-
-    float f = 0.f, c = 0.f;  // f and f^2 mean(g x)
-    if (NORM == kNormToken) {
-      float xx = 0.f, gx = 0.f;
-#pragma unroll
-      for (int it = 0; it < IT; ++it) {
-        const int h = h0 + it * at.per_wave;
-        if (it < a.its && h < H) {
-          float ua[V], ub[V], ga[V], gb[V];
-          gradient(it, h, ua, ub, ga, gb, xx, gx);
+        for (int i = 0; i < V; ++i) {
+          const float x0 = xa[it].get(i), x1 = xb[it].get(i);
+          xx[it] = __builtin_fmaf(x0, x0, xx[it]);
+          xx[it] = __builtin_fmaf(x1, x1, xx[it]);
+          gx[it] = __builtin_fmaf(ua[it][i] * x0, wa[iw].get(i), gx[it]);
+          gx[it] = __builtin_fmaf(ub[it][i] * x1, wb[iw].get(i), gx[it]);
         }
       }
-      xx = sum_over<NORM>(xx, 64, wpt, wave, lane, slots);
-      gx = sum_over<NORM>(gx, 64, wpt, wave, lane, slots2);
+      if (NORM == kNormToken && it > 0) xx[0] += xx[it], gx[0] += gx[it];
+    }
+    T* const dst = now.dx;
+    if (t0 + stride < a.tokens) {
+      now = place(t0 + stride);
+      load_x(now);
+      load_dy(now);
+      if (now.H && wave == first) find_angles(a, now.b, now.n, lane, rows[turn_of ^ 1][first]);
+    }
+    float f = 0.f, c = 0.f;  // f and f^3 mean(g x)
+    if (NORM == kNormToken) {
+      for (int o = 1; o < 64; o <<= 1) xx[0] += __shfl_xor(xx[0], o), gx[0] += __shfl_xor(gx[0], o);
+      if (wpt > 1 && lane == 0) slots[turn_of][wave] = make_float2(xx[0], gx[0]);
+    }
+    __syncthreads();
+    if (NORM == kNormToken) {
+      if (wpt > 1) {
+        xx[0] = gx[0] = 0.f;
+        for (int w = 0; w < wpt; ++w) xx[0] += slots[turn_of][first + w].x, gx[0] += slots[turn_of][first + w].y;
+      }
       const float inv = 1.f / (float)(a.H * a.d);
-      f = 1.f / sqrtf(xx * inv + a.eps);
-      c = f * f * (gx * inv);
+      f = 1.f / sqrtf(xx[0] * inv + a.eps);
+      c = f * f * f * (gx[0] * inv);
     }
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int h = h0 + it * at.per_wave;
       if (it >= a.its) break;
-      float ua[V], ub[V], ga[V], gb[V], xx = 0.f, gx = 0.f;
-      if (h < H) gradient(it, h, ua, ub, ga, gb, xx, gx);
       if (NORM == kNormHead) {
-        xx = sum_over<NORM>(xx, units, 1, wave, lane, nullptr);
-        gx = sum_over<NORM>(gx, units, 1, wave, lane, nullptr);
+        for (int o = 1; o < units; o <<= 1) xx[it] += __shfl_xor(xx[it], o), gx[it] += __shfl_xor(gx[it], o);
         const float inv = 1.f / (float)a.d;
-        f = 1.f / sqrtf(xx * inv + a.eps);
-        c = f * f * (gx * inv);
+        f = 1.f / sqrtf(xx[it] * inv + a.eps);
+        c = f * f * f * (gx[it] * inv);
       }
       if (h >= H) continue;
       const int ia = NORM == kNormToken ? it : 0;
+      float ga[V], gb[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float x0 = xa[it].get(i), x1 = xb[it].get(i);
-        acc[ia][i] += ua[i] * (x0 * f);
-        acc[ia][V + i] += ub[i] * (x1 * f);
-        ga[i] = f * (ga[i] - x0 * c);
-        gb[i] = f * (gb[i] - x1 * c);
+        const float fa = f * ua[it][i], fb = f * ub[it][i];
+        acc[ia][i] = __builtin_fmaf(fa, x0, acc[ia][i]);
+        acc[ia][V + i] = __builtin_fmaf(fb, x1, acc[ia][V + i]);
+        ga[i] = __builtin_fmaf(-c, x0, fa * wa[ia].get(i));
+        gb[i] = __builtin_fmaf(-c, x1, fb * wb[ia].get(i));
       }
       T* o = dst + (int64_t)h * a.dst_st[k].h;
       *reinterpret_cast<Chunk<T, V>*>(o + at.ea) = Chunk<T, V>::of(ga);
@@ -370,28 +421,20 @@ rotary_backward_kernel(RotaryArgs a) {
 #pragma unroll
   for (int it = 0; it < AT; ++it) {
     if (it >= a.its) break;
-    __syncthreads();
+    const int h = h0 + it * at.per_wave;
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) acc_s[wave][lane][i] = acc[it][i];
-    __syncthreads();
-    if (NORM == kNormToken) {
-      const int h = h0 + it * at.per_wave;
-      if (wave < wpt && h < a.H) {
+    for (int q = 0; q < 2 * V; q += Q) {
+      __syncthreads();
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float sa = 0.f, sb = 0.f;
-          for (int g = 0; g < per_group; ++g) sa += acc_s[wave + g * wpt][lane][i], sb += acc_s[wave + g * wpt][lane][V + i];
-          out[h * a.d + at.ea + i] = sa;
-          out[h * a.d + at.eb + i] = sb;
-        }
-      }
-    } else if (wave == 0 && lane < units) {
+      for (int i = 0; i < Q; ++i) acc_s[wave][lane][i] = acc[it][q + i];
+      __syncthreads();
+      const bool mine = NORM == kNormToken ? wave < wpt && h < a.H : wave == 0 && lane < units;
+      if (!mine) continue;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float sa = 0.f, sb = 0.f;
-        for (int g = 0; g < (int)(blockDim.x >> 6); ++g) sa += acc_s[g][lane][i], sb += acc_s[g][lane][V + i];
-        out[at.ea + i] = sa;
-        out[at.eb + i] = sb;
+      for (int i = 0; i < Q; ++i) {
+        float v = 0.f;
+        for (int w = NORM == kNormToken ? wave : 0; w < (int)(blockDim.x >> 6); w += NORM == kNormToken ? wpt : 1) v += acc_s[w][lane][i];
+        out[(NORM == kNormToken ? h * a.d : 0) + (q + i < V ? at.ea + q + i : at.eb + q + i - V)] = v;
       }
     }
   }
@@ -474,49 +517,51 @@ bool wide_pairs(svgear_dtype dt, int pairs, unsigned flags) {
   return !(flags & SVGEAR_ROTARY_HALVES) || pairs % (dt == SVGEAR_F32 ? 4 : 8) == 0;
 }
 
-// How a token's heads lie in waves; the workgroup's threads.
-int plan_waves(RotaryArgs& a, int V, int max_its) {
+// How a token's heads lie in waves; the threads of a workgroup, of `waves` waves if that is not fewer than a token's.
+int plan_waves(RotaryArgs& a, int V, int max_its, int waves) {
   const int per_wave = 64 / (a.d / (2 * V));
   a.waves_per_token = (int)ceil_div(a.H, per_wave * max_its);
   a.its = (int)ceil_div(a.H, per_wave * a.waves_per_token);
-  const int group = a.waves_per_token >= 4 ? 1 : 4 / a.waves_per_token;
-  return 64 * a.waves_per_token * group;
+  return 64 * a.waves_per_token * (a.waves_per_token >= waves ? 1 : waves / a.waves_per_token);
 }
 
-template <typename T, int V, int NORM>
-int launch_mode(RotaryArgs& a, int n_tensors, unsigned flags, bool backward, hipStream_t s) {
-  const int threads = plan_waves(a, V, kMaxIts<T, V>), per_group = threads / 64 / a.waves_per_token;
-  const unsigned groups = (unsigned)ceil_div(a.tokens, per_group);
-  if constexpr (V == 1) {
-    if (!(flags & SVGEAR_ROTARY_HALVES)) return SVGEAR_ERR_INVALID;
-    if (backward && NORM != kNormNone) {
-      if constexpr (NORM != kNormNone)
-        rotary_backward_kernel<T, V, NORM, true><<<dim3(groups < kBackwardGroups ? groups : kBackwardGroups, n_tensors), threads, 0, s>>>(a);
-    } else {
-      rotary_kernel<T, V, NORM, true><<<dim3(groups, n_tensors), threads, 0, s>>>(a);
-    }
-  } else {
-    const bool halves = flags & SVGEAR_ROTARY_HALVES;
-    if (backward && NORM != kNormNone) {
-      if constexpr (NORM != kNormNone) {
-        const dim3 g(groups < kBackwardGroups ? groups : kBackwardGroups, n_tensors);
-        if (halves) rotary_backward_kernel<T, V, NORM, true><<<g, threads, 0, s>>>(a);
-        else rotary_backward_kernel<T, V, NORM, false><<<g, threads, 0, s>>>(a);
-      }
-    } else {
-      if (halves) rotary_kernel<T, V, NORM, true><<<dim3(groups, n_tensors), threads, 0, s>>>(a);
-      else rotary_kernel<T, V, NORM, false><<<dim3(groups, n_tensors), threads, 0, s>>>(a);
+template <typename T, int V, int NORM, bool HALVES>
+int launch_mode(RotaryArgs& a, int n_tensors, bool backward, hipStream_t s) {
+  if constexpr (NORM != kNormNone) {
+    if (backward) {
+      const int few = kFewIts<T, V>;
+      const bool wide = a.H > kRotWaves * few * (64 / (a.d / (2 * V)));
+      const int threads = plan_waves(a, V, wide ? 2 * few : few, kRotWaves);
+      a.rows = (int)ceil_div(a.tokens, threads / 64 / a.waves_per_token);
+      if (a.rows > kBackwardGroups) a.rows = kBackwardGroups;
+      const dim3 grid((unsigned)a.rows, (unsigned)n_tensors);
+      if (wide)
+        rotary_backward_kernel<T, V, NORM, HALVES, 2 * kFewIts<T, V>><<<grid, threads, 0, s>>>(a);
+      else
+        rotary_backward_kernel<T, V, NORM, HALVES, kFewIts<T, V>><<<grid, threads, 0, s>>>(a);
+      SVGEAR_LAUNCH_CHECK();
+      return SVGEAR_OK;
     }
   }
+  const int threads = plan_waves(a, V, kMaxIts<T, V>, 4);
+  const unsigned groups = (unsigned)ceil_div(a.tokens, threads / 64 / a.waves_per_token);
+  rotary_kernel<T, V, NORM, HALVES><<<dim3(groups, (unsigned)n_tensors), threads, 0, s>>>(a);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }
 
+template <typename T, int V, int NORM>
+int launch_pairs(RotaryArgs& a, int n_tensors, unsigned flags, bool backward, hipStream_t s) {
+  if (flags & SVGEAR_ROTARY_HALVES) return launch_mode<T, V, NORM, true>(a, n_tensors, backward, s);
+  if constexpr (V == 1) return SVGEAR_ERR_INVALID;  // interleaved pairs always lie in whole chunks
+  else return launch_mode<T, V, NORM, false>(a, n_tensors, backward, s);
+}
+
 template <typename T, int V>
 int launch_width(RotaryArgs& a, int n_tensors, unsigned flags, bool backward, hipStream_t s) {
-  if (flags & SVGEAR_ROTARY_NORM_HEAD) return launch_mode<T, V, kNormHead>(a, n_tensors, flags, backward, s);
-  if (flags & SVGEAR_ROTARY_NORM_TOKEN) return launch_mode<T, V, kNormToken>(a, n_tensors, flags, backward, s);
-  return launch_mode<T, V, kNormNone>(a, n_tensors, flags, backward, s);
+  if (flags & SVGEAR_ROTARY_NORM_HEAD) return launch_pairs<T, V, kNormHead>(a, n_tensors, flags, backward, s);
+  if (flags & SVGEAR_ROTARY_NORM_TOKEN) return launch_pairs<T, V, kNormToken>(a, n_tensors, flags, backward, s);
+  return launch_pairs<T, V, kNormNone>(a, n_tensors, flags, backward, s);
 }
 
 int launch_rotary(RotaryArgs& a, svgear_dtype dt, int n_tensors, unsigned flags, bool backward, hipStream_t s) {
@@ -617,13 +662,8 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
   const int done = launch_rotary(a, dt, n_tensors, flags, true, s);
   if (done != SVGEAR_OK || !any) return done;
   const int cols = (flags & SVGEAR_ROTARY_NORM_TOKEN) ? H * d : d;
-  const int threads = 64 * a.waves_per_token * (a.waves_per_token >= 4 ? 1 : 4 / a.waves_per_token);
-  const int64_t groups = ceil_div(a.tokens, threads / 64 / a.waves_per_token);
-  const int rows = (int)(groups < kBackwardGroups ? groups : kBackwardGroups);
-  for (int k = 0; k < n_tensors; ++k)
-    if (a.partial[k]) {
-      const int r = sum_rows(a.partial[k], rows, cols, 1, dweight[k], dt, s);
-      if (r != SVGEAR_OK) return r;
-    }
-  return SVGEAR_OK;
+  if (n_tensors == 2 && a.partial[0] && a.partial[1])
+    return sum_rows(a.partial[0], dweight[0], a.partial[1], dweight[1], a.rows, cols, 1, dt, s);
+  const int k = a.partial[0] ? 0 : 1;
+  return sum_rows(a.partial[k], dweight[k], nullptr, nullptr, a.rows, cols, 1, dt, s);
 }
