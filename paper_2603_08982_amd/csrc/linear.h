@@ -55,13 +55,27 @@ __device__ __forceinline__ float gelu_tanh_arg(float z) {
   const float z2 = fminf(z * z, 1e30f);  // (large z: the limit is the same, and nothing is infinity times zero)
   return 1.5957691216057308f * (z + 0.044715f * z * z2);
 }
+// e^x and 1/x. For bf16 results the hardware's exponential of x log2(e) and its reciprocal: off by 2^-17 where x is near 88,
+// by 2^-22 around 0, beside the 2^-9 of the result's rounding; a third of the instructions.
+template <typename T>
+__device__ __forceinline__ float act_exp(float x) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(x * 1.44269504f);
+  return expf(x);
+}
+template <typename T>
+__device__ __forceinline__ float act_inverse(float x) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(x);
+  return 1.f / x;
+}
+template <typename T>
 __device__ __forceinline__ float act_value(int act, float z) {
-  if (act == SVGEAR_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == SVGEAR_ACT_SILU) return z * act_inverse<T>(1.f + act_exp<T>(-z));
   if (act == SVGEAR_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-  if (act == SVGEAR_ACT_GELU_TANH) return z / (1.f + expf(-gelu_tanh_arg(z)));
+  if (act == SVGEAR_ACT_GELU_TANH) return z * act_inverse<T>(1.f + act_exp<T>(-gelu_tanh_arg(z)));
   return z;
 }
 // slope, and the value in `a`
+template <typename T>
 __device__ __forceinline__ float act_slope(int act, float z, float& a) {
   if (act == SVGEAR_ACT_NONE) {
     a = z;
@@ -70,18 +84,18 @@ __device__ __forceinline__ float act_slope(int act, float z, float& a) {
   if (act == SVGEAR_ACT_GELU) {
     const float cdf = 0.5f * erfcf(-0.70710678118654752f * z);
     a = z * cdf;
-    return cdf + z * (0.39894228040143268f * expf(-0.5f * z * z));
+    return __builtin_fmaf(z, 0.39894228040143268f * act_exp<T>(-0.5f * z * z), cdf);
   }
   // z s(v): slope s + z s (1 - s) v', with s (1 - s) = e^-|v| / (1 + e^-|v|)^2, which loses nothing on either side
   float v = z, dv = 1.f;
   if (act == SVGEAR_ACT_GELU_TANH) {
     v = gelu_tanh_arg(z);
-    dv = 1.5957691216057308f * (1.f + 0.134145f * fminf(z * z, 1e30f));
+    dv = 1.5957691216057308f * __builtin_fmaf(0.134145f, fminf(z * z, 1e30f), 1.f);
   }
-  const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
+  const float e = act_exp<T>(-fabsf(v)), r = act_inverse<T>(1.f + e);
   const float s = v >= 0.f ? r : e * r;
   a = z * s;
-  return s + z * (e * r * r) * dv;
+  return __builtin_fmaf(z * (e * r * r), dv, s);
 }
 
 template <typename T>
@@ -113,64 +127,72 @@ __device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
 }
 
+// Eight consecutive elements as they lie in memory.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<bf16_t> {
+  uint4 u;
+  __device__ __forceinline__ void load(const bf16_t* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t w = i < 2 ? u.x : i < 4 ? u.y : i < 6 ? u.z : u.w;
+    return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
+  }
+};
+template <>
+struct Eight<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* p) { load8(p, v); }
+  __device__ __forceinline__ float get(int i) const { return v[i]; }
+};
+
+// Element offsets of row r: token t of batch entry b.
+struct Place {
+  int64_t y, gate, res;
+  Place() = default;
+  __device__ __forceinline__ Place(const LinearArgs& a, int r) {
+    const int b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
+    y = (int64_t)b * a.yst.b + (int64_t)t * a.yst.n;
+    gate = (int64_t)b * a.gst.b + (int64_t)t * a.gst.n;
+    res = (int64_t)b * a.rst.b + (int64_t)t * a.rst.n;
+  }
+};
+
 // The epilogue of one element.
 template <typename T>
-__device__ __forceinline__ void finish1(const LinearArgs& a, const T* bias, const T* gate, const T* res, T* pre, T* y, float v) {
-  if (bias) v += load_as_f32(bias);
-  if (pre) store1(pre, v);
-  if (a.act != SVGEAR_ACT_NONE) v = act_value(a.act, v);
-  if (gate) v *= load_as_f32(gate);
-  if (res) v += load_as_f32(res);
-  store1(y, v);
-}
-
-// The epilogue of eight consecutive columns c.. of row r (those < C; wide: all of them are, c is a multiple of 8).
-template <typename T>
-__device__ __forceinline__ void finish8(const LinearArgs& a, int r, int c, float (&v)[8]) {
-  const int b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
-  T* y = static_cast<T*>(a.y) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c;
-  const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c : nullptr;
-  const T* res = a.residual ? static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c : nullptr;
-  T* pre = a.pre ? static_cast<T*>(a.pre) + (int64_t)r * a.C + c : nullptr;
-  const T* bias = a.bias ? static_cast<const T*>(a.bias) + c : nullptr;
-  float w[8];
-  if (a.wide) {
-    if (bias) {
-      load8(bias, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += w[i];
-    }
-    if (pre) store8(pre, v);
-    if (a.act != SVGEAR_ACT_NONE) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = act_value(a.act, v[i]);
-    }
-    if (gate) {
-      load8(gate, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= w[i];
-    }
-    if (res) {
-      load8(res, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += w[i];
-    }
-    store8(y, v);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < a.C) finish1<T>(a, bias ? bias + i : nullptr, gate ? gate + i : nullptr, res ? res + i : nullptr, pre ? pre + i : nullptr, y + i, v[i]);
-}
-
-template <typename T>
 __device__ __forceinline__ void finish1(const LinearArgs& a, int r, int c, float v) {
-  const int b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
-  finish1<T>(a, a.bias ? static_cast<const T*>(a.bias) + c : nullptr,
-             a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c : nullptr,
-             a.residual ? static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c : nullptr,
-             a.pre ? static_cast<T*>(a.pre) + (int64_t)r * a.C + c : nullptr,
-             static_cast<T*>(a.y) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c, v);
+  const Place p(a, r);
+  if (a.bias) v += load_as_f32(static_cast<const T*>(a.bias) + c);
+  if (a.pre) store1(static_cast<T*>(a.pre) + (int64_t)r * a.C + c, v);
+  if (a.act != SVGEAR_ACT_NONE) v = act_value<T>(a.act, v);
+  if (a.gate) v *= load_as_f32(static_cast<const T*>(a.gate) + p.gate + c);
+  if (a.residual) v += load_as_f32(static_cast<const T*>(a.residual) + p.res + c);
+  store1(static_cast<T*>(a.y) + p.y + c, v);
+}
+
+// The epilogue of eight consecutive columns c.. of row r, wide (all of them < C, c a multiple of 8).
+template <typename T>
+__device__ __forceinline__ void finish8(const LinearArgs& a, int r, int c, float (&v)[8], const float (&bias)[8]) {
+  const Place p(a, r);
+  Eight<T> gate, res;
+  if (a.gate) gate.load(static_cast<const T*>(a.gate) + p.gate + c);
+  if (a.residual) res.load(static_cast<const T*>(a.residual) + p.res + c);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] += bias[i];
+  if (a.pre) store8(static_cast<T*>(a.pre) + (int64_t)r * a.C + c, v);
+  if (a.act != SVGEAR_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = act_value<T>(a.act, v[i]);
+  }
+  if (a.gate) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= gate.get(i);
+  }
+  if (a.residual) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += res.get(i);
+  }
+  store8(static_cast<T*>(a.y) + p.y + c, v);
 }
 
 // Eight consecutive columns of a part's product.

@@ -68,10 +68,27 @@ linear_merge_kernel(LinearArgs a, int runs) {
         if (c + k < a.C) v[k] += o[k];
     }
   }
-  finish8<T>(a, r, c, v);
+  if (a.wide) {
+    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.bias) load8(static_cast<const T*>(a.bias) + c, bias);
+    finish8<T>(a, r, c, v, bias);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c + k < a.C) finish1<T>(a, r, c + k, v[k]);
+  }
 }
 
 // ---- dz, the partial sums of dbias, and dgate
+template <typename T>
+__device__ __forceinline__ void load_values(const T* p, float (&v)[8]) { load8(p, v); }
+template <typename T>
+__device__ __forceinline__ void load_values(const T* p, float (&v)[1]) { v[0] = load_as_f32(p); }
+template <typename T>
+__device__ __forceinline__ void store_values(T* p, const float (&v)[8]) { store8(p, v); }
+template <typename T>
+__device__ __forceinline__ void store_values(T* p, const float (&v)[1]) { store1(p, v[0]); }
+
 struct GradientArgs {
   const void* dy;
   const void* pre;   // or null
@@ -86,38 +103,70 @@ struct GradientArgs {
   int blocks_b, rows_block;  // blocks of a batch entry, rows of a block
 };
 
-// A workgroup takes 64 columns of a run of rows of one batch entry: its 4 waves every fourth row.
-template <typename T>
+// A workgroup takes 256 columns of a run of rows of one batch entry, 8 a thread, its 8 half waves every eighth row.
+// Where rows are not 16-byte aligned, 64 columns, one a lane, and its 4 waves every fourth row.
+template <typename T, int V>
 __global__ void __launch_bounds__(kThreads)
 linear_gradient_kernel(GradientArgs a) {
-  __shared__ float s[2][4][64];
-  const int x = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int c = blockIdx.y * 64 + x, b = blockIdx.x / a.blocks_b, first = (blockIdx.x % a.blocks_b) * a.rows_block;
+  constexpr int LANES = V == 8 ? 32 : 64, WAYS = kThreads / LANES;
+  __shared__ float s[2][WAYS][LANES * V + 4];
+  const int x = threadIdx.x % LANES, way = threadIdx.x / LANES;
+  const int c0 = blockIdx.y * LANES * V, c = c0 + x * V;
+  const int b = blockIdx.x / a.blocks_b, first = (blockIdx.x % a.blocks_b) * a.rows_block;
   const int last = min(first + a.rows_block, a.n);
-  float sz = 0.f, sa = 0.f;
+  const T* dy = static_cast<const T*>(a.dy) + (int64_t)b * a.yst.b + c;
+  const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + c : nullptr;
+  const int64_t r0 = (int64_t)b * a.n;
+  float sz[V], sa[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sz[i] = sa[i] = 0.f;
   if (c < a.C) {
-    for (int t = first + w; t < last; t += 4) {
-      const int64_t r = (int64_t)b * a.n + t;
-      const float dy = load_as_f32(static_cast<const T*>(a.dy) + (int64_t)b * a.yst.b + (int64_t)t * a.yst.n + c);
-      float act = 0.f, dz = dy;
-      if (a.pre) dz = dy * act_slope(a.act, load_as_f32(static_cast<const T*>(a.pre) + r * a.C + c), act);
-      if (a.gate) dz *= load_as_f32(static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c);
-      if (a.dz) store1(static_cast<T*>(a.dz) + r * a.pitch + c, dz);
-      if (a.dgate) store1(static_cast<T*>(a.dgate) + r * a.C + c, dy * act);
-      sz += dz;
-      sa += dy * act;
+    float g[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = 1.f;
+    const bool one_gate = gate && a.gst.n == 0;
+    if (one_gate) load_values(gate, g);
+    for (int t = first + way; t < last; t += WAYS) {
+      float d[V], z[V], act[V];
+      load_values(dy + (int64_t)t * a.yst.n, d);
+      if (a.pre) load_values(static_cast<const T*>(a.pre) + (r0 + t) * a.C + c, z);
+      if (gate && !one_gate) load_values(gate + (int64_t)t * a.gst.n, g);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float y = d[i];
+        act[i] = 0.f;
+        if (a.pre) d[i] = y * act_slope<T>(a.act, z[i], act[i]);
+        act[i] *= y;
+        if (gate) d[i] *= g[i];
+        sz[i] += d[i];
+        sa[i] += act[i];
+      }
+      if (a.dz) store_values(static_cast<T*>(a.dz) + (r0 + t) * a.pitch + c, d);
+      if (a.dgate) store_values(static_cast<T*>(a.dgate) + (r0 + t) * a.C + c, act);
     }
-  } else if (a.dz && c < a.pitch) {
-    for (int t = first + w; t < last; t += 4) store1(static_cast<T*>(a.dz) + ((int64_t)b * a.n + t) * a.pitch + c, 0.f);
+  } else if (V == 1 && a.dz && c < a.pitch) {
+    for (int t = first + way; t < last; t += WAYS) store1(static_cast<T*>(a.dz) + (r0 + t) * a.pitch + c, 0.f);
   }
   if (!a.sum_dz && !a.sum_da) return;
-  s[0][w][x] = sz;
-  s[1][w][x] = sa;
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[0][way][x * V + i] = sz[i], s[1][way][x * V + i] = sa[i];
   __syncthreads();
-  if (w == 0 && c < a.C) {
-    if (a.sum_dz) a.sum_dz[(int64_t)blockIdx.x * a.C + c] = s[0][0][x] + s[0][1][x] + s[0][2][x] + s[0][3][x];
-    if (a.sum_da) a.sum_da[(int64_t)blockIdx.x * a.C + c] = s[1][0][x] + s[1][1][x] + s[1][2][x] + s[1][3][x];
+  for (int i = threadIdx.x; i < LANES * V; i += kThreads) {
+    if (c0 + i >= a.C) break;
+    float z = 0.f, v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAYS; ++w) z += s[0][w][i], v += s[1][w][i];
+    if (a.sum_dz) a.sum_dz[(int64_t)blockIdx.x * a.C + c0 + i] = z;
+    if (a.sum_da) a.sum_da[(int64_t)blockIdx.x * a.C + c0 + i] = v;
   }
+}
+
+template <typename T>
+void launch_gradient(const GradientArgs& g, unsigned blocks, bool wide, hipStream_t s) {
+  if (wide)
+    linear_gradient_kernel<T, 8><<<dim3(blocks, (unsigned)ceil_div(g.C, 256)), kThreads, 0, s>>>(g);
+  else
+    linear_gradient_kernel<T, 1><<<dim3(blocks, (unsigned)ceil_div(g.pitch, 64)), kThreads, 0, s>>>(g);
 }
 
 // ---- host side
@@ -405,11 +454,12 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     if (dbias) g.sum_dz = space.take<float>(sums);
     if (dgate && !token_gate) g.sum_da = space.take<float>(sums);
     if (dgate && token_gate) g.dgate = dgate;
-    const dim3 grid((unsigned)(B * g.blocks_b), (unsigned)ceil_div(g.pitch, 64));
+    const bool wide = d_out % 8 == 0 && wide_rows(dy, dystride, dt) && (!gate || wide_rows(gate, gstride, dt)) &&
+                      reinterpret_cast<uintptr_t>(g.pre) % 16 == 0 && reinterpret_cast<uintptr_t>(g.dgate) % 16 == 0;
     if (dt == SVGEAR_F32)
-      linear_gradient_kernel<float><<<grid, kThreads, 0, s>>>(g);
+      launch_gradient<float>(g, (unsigned)(B * g.blocks_b), wide, s);
     else
-      linear_gradient_kernel<bf16_t><<<grid, kThreads, 0, s>>>(g);
+      launch_gradient<bf16_t>(g, (unsigned)(B * g.blocks_b), wide, s);
     SVGEAR_LAUNCH_CHECK();
     if (dbias) {
       const int rc = sum_rows(g.sum_dz, dbias, nullptr, nullptr, B * g.blocks_b, d_out, 1, dt, s);

@@ -298,13 +298,11 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
 
   // A wave's 32 rows at a time go through its own part of LDS, so that what is read and written of a row is one
   // run of 16-byte pieces: block i, group g of a lane are columns 32i + 8g + 4lh + 0..3 of row li.
-  constexpr int COLS = 32 * TC, CHUNKS = COLS / 4, LANES = COLS / 8;  // LANES share a row
+  constexpr int COLS = 32 * TC, CHUNKS = COLS / 4;
   static_assert(32 * COLS * 4 * WAVES <= LDS, "the waves' parts must fit");
   unsigned char* own = smem + wave * (32 * COLS * 4);
   const int li = lane & 31, lh = lane >> 5;
-  const int c = c0 + wc * COLS + (lane % LANES) * 8;
-#pragma unroll
-  for (int j = 0; j < TR; ++j) {
+  auto stage = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < TC; ++i)
 #pragma unroll
@@ -312,21 +310,105 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
         *reinterpret_cast<float4*>(own + li * (COLS * 4) + (((8 * i + 2 * g + lh) ^ (li & (CHUNKS - 1))) << 4)) =
             make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 1
-    for (int q = 0; q < 32; q += 64 / LANES) {
-      const int row = q + lane / LANES, r = r0 + (wr * TR + j) * 32 + row;
-      const int x = row & (CHUNKS - 1), at = 2 * (lane % LANES);
+  };
+  const int rw = r0 + wr * TR * 32;  // the wave's first row
+  if (a.wide || a.partial) {
+    constexpr int LANES = COLS / 8, ROWS = 64 / LANES, PASSES = 32 / ROWS;  // LANES share a row, eight columns each
+    const int sub = lane / LANES, at = 2 * (lane % LANES), c = c0 + wc * COLS + (lane % LANES) * 8;
+    auto staged = [&](int q, float (&v)[8]) __attribute__((always_inline)) {
+      const int row = q * ROWS + sub, x = row & (CHUNKS - 1);
       const float4 lo = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + ((at ^ x) << 4));
       const float4 hi = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + (((at + 1) ^ x) << 4));
-      if (r >= a.R || c >= a.C) continue;
-      float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-      if (a.partial) {
-        store_partial8(a, part, r, c, v);
+      v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+    };
+    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.bias && !a.partial && c < a.C) load8(static_cast<const T*>(a.bias) + c, bias);
+    const bool plain = a.act == SVGEAR_ACT_NONE && !a.pre && !a.partial;
+#pragma unroll
+    for (int j = 0; j < TR; ++j) {
+      if (plain) {
+        // no activation: gate and residual of all 32 rows are on their way together (a pass at a time, 256 tiles of 256 x 256
+        // wait some 30 us for them)
+        Eight<T> gate[PASSES], res[PASSES];
+        int64_t to[PASSES];
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+          const int r = min(rw + j * 32 + q * ROWS + sub, a.R - 1), b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
+          to[q] = (int64_t)b * a.yst.b + (int64_t)t * a.yst.n;
+          if (c < a.C) {
+            if (a.gate) gate[q].load(static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c);
+            if (a.residual) res[q].load(static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c);
+          }
+        }
+        stage(j);
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+          float v[8];
+          staged(q, v);
+          if (rw + j * 32 + q * ROWS + sub >= a.R || c >= a.C) continue;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += bias[i];
+          if (a.gate) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= gate[q].get(i);
+          }
+          if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += res[q].get(i);
+          }
+          store8(static_cast<T*>(a.y) + to[q] + c, v);
+        }
       } else {
-        finish8<T>(a, r, c, v);
+        stage(j);
+#pragma unroll 1
+        for (int q = 0; q < PASSES; ++q) {
+          float v[8];
+          staged(q, v);
+          const int r = rw + j * 32 + q * ROWS + sub;
+          if (r >= a.R || c >= a.C) continue;
+          if (a.partial)
+            store_partial8(a, part, r, c, v);
+          else
+            finish8<T>(a, r, c, v, bias);
+        }
       }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  } else {  // rows at any alignment: neighbouring lanes take neighbouring elements, four rows' inputs on their way together
+    constexpr int ACROSS = COLS < 64 ? COLS : 64, ROWS = 64 / ACROSS, N4 = 4;
+    const int sub = lane / ACROSS;
+#pragma unroll
+    for (int j = 0; j < TR; ++j) {
+      stage(j);
+#pragma unroll
+      for (int half = 0; half < COLS; half += ACROSS) {
+        const int col = half + lane % ACROSS, e = c0 + wc * COLS + col;
+        const float bias = a.bias && e < a.C ? load_as_f32(static_cast<const T*>(a.bias) + e) : 0.f;
+#pragma unroll 1
+        for (int q = 0; q < 32; q += N4 * ROWS) {
+          Place p[N4];
+          float gate[N4], res[N4];
+#pragma unroll
+          for (int i = 0; i < N4; ++i) {
+            const int r = rw + j * 32 + q + i * ROWS + sub;
+            p[i] = Place(a, min(r, a.R - 1));
+            gate[i] = a.gate && e < a.C ? load_as_f32(static_cast<const T*>(a.gate) + p[i].gate + e) : 1.f;
+            res[i] = a.residual && e < a.C ? load_as_f32(static_cast<const T*>(a.residual) + p[i].res + e) : 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < N4; ++i) {
+            const int row = q + i * ROWS + sub, r = rw + j * 32 + row;
+            float v = *reinterpret_cast<const float*>(own + row * (COLS * 4) + (((col >> 2) ^ (row & (CHUNKS - 1))) << 4) + (col & 3) * 4);
+            if (r >= a.R || e >= a.C) continue;
+            v += bias;
+            if (a.pre) store1(static_cast<T*>(a.pre) + (int64_t)r * a.C + e, v);
+            if (a.act != SVGEAR_ACT_NONE) v = act_value<T>(a.act, v);
+            store1(static_cast<T*>(a.y) + p[i].y + e, __builtin_fmaf(v, gate[i], res[i]));
+          }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
   }
 }
 
