@@ -246,11 +246,13 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
   return launch_linear_merge(a, dt, s);
 }
 
-// Tile and number of parts of K of a product: the least of an estimate in microseconds,
-//   tiles of the CU that has most of them * (its steps * step + tile) + what joining the parts takes.
-// step and tile (prologue and epilogue) are measured. Both sides of the choices, us, MI355X, bf16: 1024 x 2048 of
-// 2048 in tiles of 64 / 128 / 256: 21 / 25 / 44; 9450 x 5120 of 5120: 796 / 493 / 406; 37800 x 15360 of 5120: 8795 / 5245 /
-// 4381. fp32: 1554 x 1000 of 640 in 64 / 128: 29 / 48; 8192 x 2048 of 2048: 563 / 483 (256: 544, never the least).
+// Tile and number of parts of K of a product: the least of an estimate in microseconds. m tiles on the CU that has most
+// of them take their steps in turn, max(alone, m * step) each (a single workgroup waits for its own copies and barriers;
+// 256 x 256: one at a time), and `once` for their prologues and epilogues; joining parts costs a launch and their products'
+// way to memory and back. The constants are measured. Both sides of the choices, us, MI355X, bf16, C x R of K: 5120 x 256 of 4096
+// in tiles of 64 / 128 / 128 in 3 parts: 30 / 34 / 25; 2048 x 512 of 2048 in 64 / 128: 12 / 17; 5120 x 2000 of 5120 in 128 / 256:
+// 118 / 100; 2048 x 4000 of 6000: 106 / 114. fp32, 1000 x 1554 of 640 in 64 / 128: 27 / 45, 1536 x 2103 of 1024 70 / 69; 1000 x 700 of 3000
+// in 64, one part / 4: 56 / 46.
 // Few rows (forward only) go to the kernel that reads the weights straight into registers.
 struct Plan {
   int tile, splits;
@@ -259,10 +261,10 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
   if (form == kContractBoth && R <= few_rows(dt)) return Plan{0, 1};
   struct Kind {
     int tile;
-    double step, once;
+    double alone, step, once;
   };
-  static const Kind bf16[] = {{64, 0.19, 1.0}, {128, 0.49, 3.0}, {256, 1.45, 11.0}};
-  static const Kind f32[] = {{64, 0.53, 1.0}, {128, 2.0, 3.0}};
+  static const Kind bf16[] = {{64, 0.40, 0.19, 1.0}, {128, 0.50, 0.475, 1.5}, {256, 1.3, 1.3, 9.0}};
+  static const Kind f32[] = {{64, 0.56, 0.53, 1.0}, {128, 1.9, 1.85, 2.0}};
   const Kind* kinds = dt == SVGEAR_F32 ? f32 : bf16;
   const int64_t steps = ceil_div(K, dt == SVGEAR_F32 ? 32 : 64);
   Plan best{64, 1};
@@ -271,8 +273,9 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
     const Kind& k = kinds[i];
     const int64_t tiles = ceil_div(R, k.tile) * ceil_div(C, k.tile);
     for (int p = 1; p <= 16 && (p == 1 || (steps >= 4 * p && tiles < 1024)); ++p) {
-      double us = (double)ceil_div(tiles * p, 256) * ((double)ceil_div(steps, p) * k.step + k.once);
-      if (p > 1) us += 6.0 + (double)p * (double)R * (double)C * 8.0 / 4e6;
+      const double m = (double)ceil_div(tiles * p, 256), each = m * k.step;
+      double us = (double)ceil_div(steps, p) * (each > k.alone ? each : k.alone) + m * k.once;
+      if (p > 1) us += 4.0 + (double)p * (double)R * (double)C * 8.0 / 5e6;
       if (us < least) {
         least = us;
         best = Plan{k.tile, p};
