@@ -9,16 +9,22 @@ constexpr int kThreads = 256;
 constexpr int kMaxWidth = 1 << 21;
 constexpr int64_t kMaxPitch = 1 << 21;  // a tile's rows are addressed by 32-bit byte offsets: 256 rows of 8 MB
 
-// ---- rows copied to an even, 16-byte aligned pitch, zeros behind the values
+// ---- rows copied to an even, 16-byte aligned pitch, zeros behind the values; a 16-byte piece a thread
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 pack_rows_kernel(const T* src, Rows st, int n, int rows, int width, T* dst, int64_t pitch) {
-  const int col = (blockIdx.y * kThreads + threadIdx.x);
+  constexpr int CH = 16 / sizeof(T);
+  const int col = (blockIdx.y * kThreads + threadIdx.x) * CH;
   if (col >= pitch) return;
   for (int r = blockIdx.x; r < rows; r += gridDim.x) {
     const int b = n >= rows ? 0 : r / n;
-    const T* s = src + (int64_t)b * st.b + (int64_t)(r - b * n) * st.n;
-    dst[(int64_t)r * pitch + col] = col < width ? s[col] : T(0);
+    const T* s = src + (int64_t)b * st.b + (int64_t)(r - b * n) * st.n + col;
+    T e[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) e[i] = col + i < width ? s[i] : T(0);
+    uint4 u;
+    __builtin_memcpy(&u, e, 16);
+    *reinterpret_cast<uint4*>(dst + (int64_t)r * pitch + col) = u;
   }
 }
 
@@ -193,7 +199,7 @@ size_t packed_bytes(int64_t rows, int64_t width, svgear_dtype dt) {
 
 template <typename T>
 int pack_rows(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, void* dst, int64_t pitch, hipStream_t s) {
-  const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), (unsigned)ceil_div(pitch, kThreads));
+  const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), (unsigned)ceil_div(pitch, (int64_t)(kThreads * 16 / sizeof(T))));
   pack_rows_kernel<T><<<grid, kThreads, 0, s>>>(static_cast<const T*>(src), st, (int)n, (int)rows, (int)width, static_cast<T*>(dst), pitch);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
@@ -248,10 +254,10 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
 
 // Tile and number of parts of K of a product: the least of an estimate in microseconds. m tiles on the CU that has most
 // of them take their steps in turn, max(alone, m * step) each (a single workgroup waits for its own copies and barriers;
-// 256 x 256: one at a time), and `once` for their prologues and epilogues; joining parts costs a launch and their products'
+// 256 x 256: one at a time), `once` for their prologues and epilogues, `first` for those that nothing hides; joining parts costs a launch and their products'
 // way to memory and back. The constants are measured. Both sides of the choices, us, MI355X, bf16, C x R of K: 5120 x 256 of 4096
 // in tiles of 64 / 128 / 128 in 3 parts: 30 / 34 / 25; 2048 x 512 of 2048 in 64 / 128: 12 / 17; 5120 x 2000 of 5120 in 128 / 256:
-// 118 / 100; 2048 x 4000 of 6000: 106 / 114. fp32, 1000 x 1554 of 640 in 64 / 128: 27 / 45, 1536 x 2103 of 1024 70 / 69; 1000 x 700 of 3000
+// 118 / 100; 2048 x 4000 of 6000: 106 / 114. fp32, 1000 x 1554 of 640 in 64 / 128: 27 / 45, 1536 x 2103 of 1024 70 / 69, 1541 x 2103 of 1003 with a full epilogue 100 / 114; 1000 x 700 of 3000
 // in 64, one part / 4: 56 / 46.
 // Few rows (forward only) go to the kernel that reads the weights straight into registers.
 struct Plan {
@@ -261,10 +267,10 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
   if (form == kContractBoth && R <= few_rows(dt)) return Plan{0, 1};
   struct Kind {
     int tile;
-    double alone, step, once;
+    double alone, step, once, first;
   };
-  static const Kind bf16[] = {{64, 0.40, 0.19, 1.0}, {128, 0.50, 0.475, 1.5}, {256, 1.3, 1.3, 9.0}};
-  static const Kind f32[] = {{64, 0.56, 0.53, 1.0}, {128, 1.9, 1.85, 2.0}};
+  static const Kind bf16[] = {{64, 0.40, 0.19, 1.0, 0.0}, {128, 0.50, 0.475, 1.5, 0.0}, {256, 1.3, 1.3, 9.0, 0.0}};
+  static const Kind f32[] = {{64, 0.56, 0.53, 1.0, 0.0}, {128, 1.9, 1.85, 2.0, 10.0}};
   const Kind* kinds = dt == SVGEAR_F32 ? f32 : bf16;
   const int64_t steps = ceil_div(K, dt == SVGEAR_F32 ? 32 : 64);
   Plan best{64, 1};
@@ -274,7 +280,7 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
     const int64_t tiles = ceil_div(R, k.tile) * ceil_div(C, k.tile);
     for (int p = 1; p <= 16 && (p == 1 || (steps >= 4 * p && tiles < 1024)); ++p) {
       const double m = (double)ceil_div(tiles * p, 256), each = m * k.step;
-      double us = (double)ceil_div(steps, p) * (each > k.alone ? each : k.alone) + m * k.once;
+      double us = (double)ceil_div(steps, p) * (each > k.alone ? each : k.alone) + m * k.once + k.first;
       if (p > 1) us += 4.0 + (double)p * (double)R * (double)C * 8.0 / 5e6;
       if (us < least) {
         least = us;
