@@ -6,6 +6,7 @@ stream. No arithmetic of the method happens here.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -363,25 +364,16 @@ def _require(ok, what: str):
         raise SvgearError(what)
 
 
-class _OnDevice:
-    """The given tensor's GPU as the current one, for calls whose tensors lie on another."""
-
-    def __init__(self, t: torch.Tensor):
-        self.index = t.device.index
-        self.guard = None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.index:
-            self.guard = torch.cuda.device(self.index)
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_HERE_ALREADY = contextlib.nullcontext()
 
 
-def _stream_of(t: torch.Tensor) -> int:
-    return torch.cuda.current_stream(t.device.index).cuda_stream
+def _on_device(device: torch.device):
+    """The device as the current one, for calls whose tensors lie on another."""
+    return _HERE_ALREADY if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _stream_of(device: torch.device) -> int:
+    return torch.cuda.current_stream(device.index).cuda_stream
 
 
 def _scratch(nbytes: int, device):
@@ -392,25 +384,40 @@ def _scratch(nbytes: int, device):
     return t, t.data_ptr(), nbytes
 
 
-def _same_place(first: torch.Tensor, dtype, *ts):
-    """Every tensor given lies on the first one's GPU and has its type."""
-    _need_gpu(first, *ts)
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _same_place(first: torch.Tensor, *ts) -> int:
+    """Every tensor given lies on the first one's GPU and has its type, which is returned as the library's."""
+    if not first.is_cuda:
+        _need_gpu(first)
+    device, dtype = first.device, first.dtype
     for t in ts:
-        _require(t is None or (t.device == first.device and t.dtype == dtype), "tensors of one call share a device and a type")
+        if t is not None and (t.device != device or t.dtype != dtype):
+            _need_gpu(t)
+            raise SvgearError("tensors of one call share a device and a type")
+    dt = _DTYPES.get(dtype)
+    return _dt(first) if dt is None else dt
+
+
+_NO_ROWS = _I64x2(0, 0)
 
 
 def _as_bnd(t: torch.Tensor, what: str):
     """[B,N,c] or [N,c] (one batch entry) as (B, N, c, strides)."""
-    _require(t.dim() in (2, 3) and (t.shape[-1] == 1 or t.stride(-1) == 1), f"{what}: expected [B,N,c] or [N,c] with contiguous c")
-    if t.dim() == 2:
-        return 1, t.shape[0], t.shape[1], _I64x2(t.shape[0] * t.stride(0), t.stride(0))
-    return t.shape[0], t.shape[1], t.shape[2], _I64x2(t.stride(0), t.stride(1))
+    shape, st = t.shape, t.stride()
+    n = len(st)
+    if not ((n == 3 or n == 2) and (st[-1] == 1 or shape[-1] == 1)):
+        raise SvgearError(f"{what}: expected [B,N,c] or [N,c] with contiguous c")
+    if n == 2:
+        return 1, shape[0], shape[1], _I64x2(shape[0] * st[0], st[0])
+    return shape[0], shape[1], shape[2], _I64x2(st[0], st[1])
 
 
 def _gate_strides(gate, lead, d_out: int):
     """Strides of a gate of tokens (lead + (d_out,)) or of batch entries (without the tokens' axis), and whether it is the first."""
     if gate is None:
-        return _I64x2(0, 0), False
+        return _NO_ROWS, False
     per_token = gate.dim() == len(lead) + 1
     _require(tuple(gate.shape) == (*lead, d_out) or tuple(gate.shape) == (*lead[:-1], d_out), "gate: expected [B,N,d_out] or [B,d_out] ([N,d_out] or [d_out] for one batch entry)")
     _require(d_out == 1 or gate.stride(-1) == 1, "gate: expected contiguous d_out")
@@ -426,28 +433,35 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     [d_out]; act "none", "silu", "gelu" (erf) or "gelu_tanh"; gate [B,d_out] (one for all tokens of a batch entry) or
     [B,N,d_out]; residual [B,N,d_out], which `out` may be. want_pre: also z = x w^T + bias, which linear_backward needs
     where there is an activation or a gate. Returns (y, z or None)."""
-    _same_place(x, x.dtype, w, bias, gate, residual, out)
+    dt = _same_place(x, w, bias, gate, residual, out)
     lib = load_library()
     B, N, d_in, xst = _as_bnd(x, "x")
-    lead = tuple(x.shape[:-1])
-    _require(w.dim() == 2 and w.shape[1] == d_in and (d_in == 1 or w.stride(1) == 1), "w: expected [d_out,d_in] with contiguous d_in")
+    lead = x.shape[:-1]
+    wst = w.stride()
+    if len(wst) != 2 or w.shape[1] != d_in or (wst[1] != 1 and d_in != 1):
+        raise SvgearError("w: expected [d_out,d_in] with contiguous d_in")
     d_out = w.shape[0]
-    _require(bias is None or (bias.shape == (d_out,) and bias.is_contiguous()), "bias: expected [d_out]")
-    _require(act in ACTIVATIONS, f"act: one of {sorted(ACTIVATIONS)}")
-    gst, _ = _gate_strides(gate, lead, d_out)
-    _require(residual is None or tuple(residual.shape) == (*lead, d_out), "residual: expected the output's shape")
-    _require(out is None or tuple(out.shape) == (*lead, d_out), "out: expected the output's shape")
-    rst = _as_bnd(residual, "residual")[3] if residual is not None else _I64x2(0, 0)
-    with _OnDevice(x):
-        y = torch.empty(*lead, d_out, dtype=x.dtype, device=x.device) if out is None else out
-        pre = torch.empty(*lead, d_out, dtype=x.dtype, device=x.device) if want_pre else None
+    shape = (*lead, d_out)
+    if bias is not None and (bias.shape != (d_out,) or not bias.is_contiguous()):
+        raise SvgearError("bias: expected [d_out]")
+    act_code = ACTIVATIONS.get(act)
+    if act_code is None:
+        raise SvgearError(f"act: one of {sorted(ACTIVATIONS)}")
+    gst = _gate_strides(gate, lead, d_out)[0]
+    if residual is not None and residual.shape != shape:
+        raise SvgearError("residual: expected the output's shape")
+    if out is not None and out.shape != shape:
+        raise SvgearError("out: expected the output's shape")
+    rst = _as_bnd(residual, "residual")[3] if residual is not None else _NO_ROWS
+    device = x.device
+    with _on_device(device):
+        y = torch.empty(shape, dtype=x.dtype, device=device) if out is None else out
+        pre = torch.empty(shape, dtype=x.dtype, device=device) if want_pre else None
         yst = _as_bnd(y, "out")[3]
-        ldw = w.stride(0) if d_out > 1 else max(w.stride(0), d_in)
-        head = (_ptr(x), xst, _ptr(w), ldw)
-        dt = _dt(x)
-        ws, *space = _scratch(lib.svgear_linear_workspace(*head, dt, B, N, d_in, d_out), x.device)
-        rc = lib.svgear_linear(*head, _ptr(bias), dt, B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
-                               _ptr(residual), rst, _ptr(pre), _ptr(y), yst, *space, _stream_of(x))
+        head = (x.data_ptr(), xst, w.data_ptr(), wst[0] if d_out > 1 else max(wst[0], d_in))
+        ws, *space = _scratch(lib.svgear_linear_workspace(*head, dt, B, N, d_in, d_out), device)
+        rc = lib.svgear_linear(*head, _ptr(bias), dt, B, N, d_in, d_out, act_code, _ptr(gate), gst, _ptr(residual), rst,
+                               _ptr(pre), y.data_ptr(), yst, *space, _stream_of(device))
     _check(rc, "svgear_linear")
     return y, pre
 
@@ -457,12 +471,13 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[tor
     """svgear_linear_backward: the gradients named in `want` ("dx", "dw", "dbias", "dgate") of linear() for the output's
     gradient dy; the residual's is dy itself. x is needed for dw, w for dx, pre (linear's second result) for an activation or
     dgate. dgate has the gate's shape. Returns a dict."""
-    _same_place(dy, dy.dtype, x, w, pre, gate)
+    dt = _same_place(dy, x, w, pre, gate)
     lib = load_library()
     B, N, d_out, dyst = _as_bnd(dy, "dy")
     lead = tuple(dy.shape[:-1])
     _require(len(want) > 0 and set(want) <= {"dx", "dw", "dbias", "dgate"}, "want: dx, dw, dbias, dgate")
-    _require(act in ACTIVATIONS, f"act: one of {sorted(ACTIVATIONS)}")
+    if act not in ACTIVATIONS:
+        raise SvgearError(f"act: one of {sorted(ACTIVATIONS)}")
     x, w = (x if "dw" in want else None), (w if "dx" in want else None)
     _require("dw" not in want or x is not None, "dw needs x")
     _require("dx" not in want or w is not None, "dx needs w")
@@ -473,21 +488,21 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[tor
     _require(pre is None or (tuple(pre.shape) == tuple(dy.shape) and pre.is_contiguous()), "pre: expected dy's shape, dense")
     _require(pre is not None or (act == "none" and "dgate" not in want), "an activation or dgate needs pre")
     gst, per_token = _gate_strides(gate, lead, d_out)
-    xst = _as_bnd(x, "x")[3] if x is not None else _I64x2(0, 0)
+    xst = _as_bnd(x, "x")[3] if x is not None else _NO_ROWS
     _require(not per_token or gst[1] != 0 or N == 1 or "dgate" not in want, "gate: one gate for all tokens is given as [B,d_out]")
-    with _OnDevice(dy):
+    with _on_device(dy.device):
         new = lambda *shape: torch.empty(*shape, dtype=dy.dtype, device=dy.device)
         r = {}
         for name in want:
             r[name] = new(*lead, d_in) if name == "dx" else new(d_out, d_in) if name == "dw" else new(d_out) if name == "dbias" else new(*gate.shape)
         dx = r.get("dx")
-        dxst = _as_bnd(dx, "dx")[3] if dx is not None else _I64x2(0, 0)
+        dxst = _as_bnd(dx, "dx")[3] if dx is not None else _NO_ROWS
         ldw = 0 if w is None else w.stride(0) if d_out > 1 else max(w.stride(0), d_in)
         head = (_ptr(dy), dyst, _ptr(x), xst, _ptr(w), ldw)
-        ws, *space = _scratch(lib.svgear_linear_backward_workspace(*head, _dt(dy), B, N, d_in, d_out), dy.device)
-        rc = lib.svgear_linear_backward(*head, _ptr(pre), _dt(dy), B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
+        ws, *space = _scratch(lib.svgear_linear_backward_workspace(*head, dt, B, N, d_in, d_out), dy.device)
+        rc = lib.svgear_linear_backward(*head, _ptr(pre), dt, B, N, d_in, d_out, ACTIVATIONS[act], _ptr(gate), gst,
                                         _ptr(dx), dxst, _ptr(r.get("dw")), _ptr(r.get("dbias")), _ptr(r.get("dgate")),
-                                        *space, _stream_of(dy))
+                                        *space, _stream_of(dy.device))
     _check(rc, "svgear_linear_backward")
     return r
 
@@ -516,31 +531,41 @@ def _strides_of(ts):
 def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves):
     """The checked arguments that rotary and its backward pass share: (weights, arguments from inv_freq to flags)."""
     t0 = tensors[0]
-    _require(t0.dim() == 4, "expected [B,H,N,d] with contiguous d")
+    if t0.dim() != 4 or len(tensors) > 2 or (len(tensors) == 2 and tensors[1].shape != t0.shape):
+        raise SvgearError("one or two tensors of one shape [B,H,N,d]")
     B, H, N, d = t0.shape
-    _require(len(tensors) in (1, 2) and all(t.shape == t0.shape for t in tensors), "one or two tensors of one shape [B,H,N,d]")
-    _require(len(sections) == 3, "sections: pairs of the three axes")
-    _require(norm in ROTARY_NORMS, 'norm: None, "head" or "token"')
-    pairs = sum(sections)
-    _require(inv_freq.is_cuda and inv_freq.device == t0.device and inv_freq.dtype == torch.float64 and inv_freq.shape == (pairs,)
-             and inv_freq.is_contiguous(), "inv_freq: expected fp64 [sum(sections)]")
-    _require((positions is None) != (grid is None), "positions or grid, one of them")
-    pos_b = 0
+    if len(sections) != 3:
+        raise SvgearError("sections: pairs of the three axes")
+    if norm not in ROTARY_NORMS:
+        raise SvgearError('norm: None, "head" or "token"')
+    if (inv_freq.device != t0.device or inv_freq.dtype != torch.float64 or inv_freq.shape != (sum(sections),)
+            or not inv_freq.is_contiguous()):
+        raise SvgearError("inv_freq: expected fp64 [sum(sections)] on the tensors' device")
+    if (positions is None) == (grid is None):
+        raise SvgearError("positions or grid, one of them")
+    pos_b, size3 = 0, None
     if positions is not None:
-        _require(positions.is_cuda and positions.device == t0.device and positions.dtype == torch.int32
-                 and positions.is_contiguous() and tuple(positions.shape) in ((N - n_tail, 3), (B, N - n_tail, 3)),
-                 "positions: expected int32 [N-n_tail,3] or [B,N-n_tail,3]")
-        pos_b = positions.stride(0) if positions.dim() == 3 else 0
+        shape = positions.shape
+        if (positions.device != t0.device or positions.dtype != torch.int32 or not positions.is_contiguous()
+                or (shape != (N - n_tail, 3) and shape != (B, N - n_tail, 3))):
+            raise SvgearError("positions: expected int32 [N-n_tail,3] or [B,N-n_tail,3] on the tensors' device")
+        if len(shape) == 3:
+            pos_b = 3 * shape[1]
     else:
-        _require(len(grid) == 3, "grid: (time, height, width)")
-    size = {None: None, "head": d, "token": H * d}[norm]
-    if weights is not None:
-        _require(size is not None and len(weights) == len(tensors), "weights: one for each tensor, with a norm")
+        if len(grid) != 3:
+            raise SvgearError("grid: (time, height, width)")
+        size3 = _I64x3(*grid)
+    if weights is None:
+        weights = (None,) * len(tensors)
+    else:
+        size = d if norm == "head" else H * d
+        if norm is None or len(weights) != len(tensors):
+            raise SvgearError("weights: one for each tensor, with a norm")
         for w in weights:
-            _require(w is None or (tuple(w.shape) == (size,) and w.is_contiguous()), "weights: expected [d] or [H*d]")
-    flags = ROTARY_NORMS[norm] | (ROTARY_HALVES if halves else 0)
-    return list(weights) if weights is not None else [None] * len(tensors), (
-        _ptr(inv_freq), _Ix3(*sections), _I64x3(*grid) if grid is not None else None, int(first), _ptr(positions), pos_b, flags)
+            if w is not None and (w.shape != (size,) or not w.is_contiguous()):
+                raise SvgearError("weights: expected [d] or [H*d]")
+    return weights, (inv_freq.data_ptr(), _Ix3(*sections), size3, first, _ptr(positions), pos_b,
+                     ROTARY_NORMS[norm] | (ROTARY_HALVES if halves else 0))
 
 
 def rotary(tensors: Sequence[torch.Tensor], inv_freq: torch.Tensor, sections: Sequence[int], grid=None, first: int = 0,
@@ -553,16 +578,16 @@ def rotary(tensors: Sequence[torch.Tensor], inv_freq: torch.Tensor, sections: Se
     _require(len(tensors) in (1, 2), "one or two tensors")
     t0 = tensors[0]
     outs = [None] * len(tensors) if out is None else list(out)
-    _same_place(t0, t0.dtype, *tensors, *(weights or ()), *outs)
+    dt = _same_place(t0, *tensors, *(weights or ()), *outs)
     lib = load_library()
     ws, places = _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves)
     B, H, N, d = t0.shape
-    with _OnDevice(t0):
+    with _on_device(t0.device):
         if out is None:
             outs = [torch.empty(B, H, N, d, dtype=t0.dtype, device=t0.device) for _ in tensors]
         _require(len(outs) == len(tensors) and all(o.shape == t0.shape for o in outs), "out: one for each tensor, of its shape")
         rc = lib.svgear_rotary(len(tensors), _pointers(tensors), _strides_of(tensors), _pointers(outs), _strides_of(outs),
-                               _pointers(ws), _dt(t0), B, H, N, n_tail, d, *places, float(eps), _stream_of(t0))
+                               _pointers(ws), dt, B, H, N, n_tail, d, *places, float(eps), _stream_of(t0.device))
     _check(rc, "svgear_rotary")
     return outs
 
@@ -579,12 +604,12 @@ def rotary_backward(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[to
     _require(norm is None or (tensors is not None and len(tensors) == len(grads) and all(t.shape == g0.shape for t in tensors)),
              "a norm needs rotary's inputs")
     tensors = list(tensors) if norm is not None else []
-    _same_place(g0, g0.dtype, *grads, *tensors, *(weights or ()), *outs)
+    dt = _same_place(g0, *grads, *tensors, *(weights or ()), *outs)
     lib = load_library()
     ws, places = _rotary_places(grads, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves)
     B, H, N, d = g0.shape
     n = len(grads)
-    with _OnDevice(g0):
+    with _on_device(g0.device):
         if out is None:
             outs = [torch.empty(B, H, N, d, dtype=g0.dtype, device=g0.device) for _ in grads]
         _require(len(outs) == n and all(o.shape == g0.shape for o in outs), "out: one for each tensor, of its shape")
@@ -594,8 +619,8 @@ def rotary_backward(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[to
         scratch, *space = _scratch(lib.svgear_rotary_backward_workspace(n, B, H, N, d) if dweight else 0, g0.device)
         rc = lib.svgear_rotary_backward(n, _pointers(grads), _strides_of(grads), _pointers(tensors) if tensors else None,
                                         _strides_of(tensors) if tensors else None, _pointers(outs), _strides_of(outs),
-                                        _pointers(ws), _pointers(dweight) if dweight else None, _dt(g0), B, H, N, n_tail, d,
-                                        *places, float(eps), *space, _stream_of(g0))
+                                        _pointers(ws), _pointers(dweight) if dweight else None, dt, B, H, N, n_tail, d,
+                                        *places, float(eps), *space, _stream_of(g0.device))
     _check(rc, "svgear_rotary_backward")
     return outs, dweight
 
