@@ -307,9 +307,14 @@ void set_product(LinearArgs& a, const Operand& P, const Operand& Q, int64_t R, i
   a.partial = a.splits > 1 ? w.take<float>((size_t)a.splits * R * C) : nullptr;
 }
 
-// Rows of a workgroup of linear_gradient_kernel; its workgroups of a batch entry.
-int gradient_rows(int64_t N) { return N >= 4096 ? 128 : 32; }
-int gradient_blocks(int64_t N) { return (int)ceil_div(N, gradient_rows(N)); }
+// Rows of a workgroup of linear_gradient_kernel, its workgroups of a batch entry: 128 rows where that makes 1,024 workgroups
+// or more, down to 8 where it does not (fp32, 1,554 x 1,000 values: 12.4 us with 32 rows, 9.7 with 8).
+int gradient_rows(int B, int64_t N, int d_out) {
+  int rows = 128;
+  while (rows > 8 && (int64_t)B * ceil_div(N, rows) * ceil_div(d_out, 256) < 1024) rows /= 2;
+  return rows;
+}
+int gradient_blocks(int B, int64_t N, int d_out) { return (int)ceil_div(N, gradient_rows(B, N, d_out)); }
 
 }  // namespace
 
@@ -403,7 +408,7 @@ extern "C" size_t svgear_linear_backward_workspace(const void* dy, const int64_t
     return 0;
   const int64_t M = (int64_t)B * N;
   size_t bytes = 256 + packed_bytes(M, d_out, dt);  // dz
-  bytes += 2 * align_up((size_t)B * gradient_blocks(N) * d_out * sizeof(float), 256);
+  bytes += 2 * align_up((size_t)B * gradient_blocks(B, N, d_out) * d_out * sizeof(float), 256);
   if (x) {
     if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes(M, d_in, dt);
     bytes += parts_bytes(d_out, d_in, M, dt, kContractNone);
@@ -457,8 +462,8 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     g.C = d_out;
     g.n = (int)N;
     g.act = act;
-    g.rows_block = gradient_rows(N);
-    g.blocks_b = gradient_blocks(N);
+    g.rows_block = gradient_rows(B, N, d_out);
+    g.blocks_b = gradient_blocks(B, N, d_out);
     const size_t sums = (size_t)B * g.blocks_b * d_out;
     if (dbias) g.sum_dz = space.take<float>(sums);
     if (dgate && !token_gate) g.sum_da = space.take<float>(sums);
@@ -470,11 +475,12 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     else
       launch_gradient<bf16_t>(g, (unsigned)(B * g.blocks_b), wide, s);
     SVGEAR_LAUNCH_CHECK();
+    const bool together = dbias && g.sum_da && B == 1;
     if (dbias) {
-      const int rc = sum_rows(g.sum_dz, dbias, nullptr, nullptr, B * g.blocks_b, d_out, 1, dt, s);
+      const int rc = sum_rows(g.sum_dz, dbias, together ? g.sum_da : nullptr, together ? dgate : nullptr, B * g.blocks_b, d_out, 1, dt, s);
       if (rc != SVGEAR_OK) return rc;
     }
-    if (g.sum_da) {
+    if (g.sum_da && !together) {
       const int rc = sum_rows(g.sum_da, dgate, nullptr, nullptr, g.blocks_b, d_out, B, dt, s);
       if (rc != SVGEAR_OK) return rc;
     }
