@@ -329,8 +329,9 @@ int svgear_unpermute(const void* op, const int32_t* perm, svgear_dtype dt, int B
  *   residual [B,N,d_out] dt, rstride
  *   pre      [B,N,d_out] dt out, dense: z, for the backward pass (NULL: not stored)
  *   y        [B,N,d_out] dt out, ystride. y may be the residual itself (same pointer, same
- *            strides); no other overlap of outputs with inputs or each other is allowed.
- * Sizes: B, N, d_in, d_out >= 1, B*N < 2^31, d_in and d_out <= 2^21; strides >= 0, those of y
+ *            strides); no other overlap of outputs with inputs or each other is allowed (one at the same
+ *            address is refused).
+ * Sizes: B, N, d_in, d_out >= 1, B*N <= 2^30, d_in and d_out <= 2^21; strides >= 0, those of y
  * such that no two rows meet; any alignment that the type has. Rows of x and w that are not
  * 16-byte aligned, or whose length is no multiple of 16 bytes, and batches of x that are not one
  * run of evenly spaced rows are first copied into the workspace, which also holds partial products where
@@ -367,7 +368,7 @@ int svgear_linear(const void* x, const int64_t xstride[2], const void* w, int64_
  * dgate take it before that rounding. All sums are made in one fixed order.
  *   dy    [B,N,d_out] dt, dystride;  pre [B,N,d_out] dt dense;  x, w, gate as above
  *   dx    [B,N,d_in] dt out, dxstride;  dw [d_out,d_in] dt out dense;  dbias [d_out] dt out
- * No output may overlap an input or another output.
+ * No output may overlap an input or another output (one at the same address is refused).
  */
 size_t svgear_linear_backward_workspace(const void* dy, const int64_t dystride[2], const void* x,
                                         const int64_t xstride[2], const void* w, int64_t w_stride, svgear_dtype dt,
@@ -398,15 +399,15 @@ int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void
  * fastest), for a share of a sequence or a single token of it: first + N - n_tail <= the
  * grid's size < 2^31. Angles are computed in fp64 and reduced to one turn before cos and sin, so
  * far positions lose nothing; all else is fp32, rounded once at the end. Squares are summed in
- * fp32: |x| up to 1e17.
+ * fp32: |x| up to 1e17. With eps = 0 a row of zeros gives NaN.
  *   src[k], dst[k]  [B,H,N,d] dt, element strides sstride[k], dstride[k]; 16-byte aligned, strides
  *                   multiples of 16 bytes, d = 64 or 128. dst[k] may be src[k] itself (same
- *                   strides), and no other overlap is allowed. Rows of a cache, or of a fused
+ *                   strides), and no other overlap is allowed (one at the same address is refused). Rows of a cache, or of a fused
  *                   projection's output [B,N,3,H,d], are strides.
  *   weight[k]       dt, 16-byte aligned
  *   inv_freq        [P] fp64 (device)
  * src, dst, sstride, dstride, weight (may be NULL) and sections, grid are HOST arrays. n_tensors
- * is 1 or 2; H <= 128; B*N < 2^31. No workspace.
+ * is 1 or 2; H <= 128; B*N <= 2^30. No workspace.
  */
 #define SVGEAR_ROTARY_NORM_HEAD 1u
 #define SVGEAR_ROTARY_NORM_TOKEN 2u
@@ -423,7 +424,8 @@ int svgear_rotary(int n_tensors, const void* const* src, const int64_t (*sstride
  *   dx = f (g - x f^2 mean(g x));  dweight = sum of du x f over batch and tokens (and heads, for
  *   SVGEAR_ROTARY_NORM_HEAD);  without a norm dx = du and there is no dweight
  *   dy[k]  [B,H,N,d] dt, dystride;  src[k] the forward call's input (may be NULL without a norm)
- *   dx[k]  [B,H,N,d] dt out, dxstride; may be dy[k] itself (same strides), no other overlap
+ *   dx[k]  [B,H,N,d] dt out, dxstride; may be dy[k] itself (same strides), no other overlap (one at
+ *          the same address is refused)
  *   dweight[k] [d] or [H*d] dt out, as weight (the array, or an entry, NULL: not wanted)
  * Sums of dweight are fp32 and made in one fixed order. Alignment and limits as above.
  */

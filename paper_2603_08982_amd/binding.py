@@ -741,6 +741,7 @@ def attention_block(x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor, i
     gate [B,c_out] or [B,N,c_out] and residual [B,N,c_out] as in linear(); norm, norm_weights (of queries and keys), inv_freq,
     sections, and grid and first, or positions, as in rotary(); init_q, init_k [B,H,C,d] (H and d are theirs), iters,
     budget_cost, n_tail and what `layer` holds as in attention_layer(). Returns (y [B,N,c_out], intermediates of the layer)."""
+    _require(x.dim() == 3 and init_q.dim() == 4, "x: expected [B,N,c], init_q: [B,H,C,d]")
     B, N, _ = x.shape
     H, d = init_q.shape[1], init_q.shape[3]
     _require(w_qkv.shape[0] == 3 * H * d and w_out.shape[1] == H * d, "w_qkv: expected [3*H*d,c], w_out: [c_out,H*d]")

@@ -7,6 +7,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxWidth = 1 << 21;
+constexpr int64_t kMaxRows = 1 << 30;
 constexpr int64_t kMaxPitch = 1 << 21;  // a tile's rows are addressed by 32-bit byte offsets: 256 rows of 8 MB
 
 // ---- rows copied to an even, 16-byte aligned pitch, zeros behind the values; a 16-byte piece a thread
@@ -228,7 +229,7 @@ Copies operand_copies(const void* x, const int64_t xstride[2], const void* w, in
 }
 
 bool sizes_ok(svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
-  return (dt == SVGEAR_F32 || dt == SVGEAR_BF16) && B > 0 && N > 0 && N <= INT32_MAX && (int64_t)B * N <= INT32_MAX &&
+  return (dt == SVGEAR_F32 || dt == SVGEAR_BF16) && B > 0 && N > 0 && N <= kMaxRows && (int64_t)B * N <= kMaxRows &&
          d_in > 0 && d_out > 0 && d_in <= kMaxWidth && d_out <= kMaxWidth;
 }
 bool input_ok(const void* p, const int64_t st[2], svgear_dtype dt) {
@@ -364,6 +365,8 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
       (gate && !input_ok(gate, gstride, dt)) || (residual && !input_ok(residual, rstride, dt)) ||
       reinterpret_cast<uintptr_t>(bias) % esize(dt) || reinterpret_cast<uintptr_t>(pre) % esize(dt))
     return SVGEAR_ERR_INVALID;
+  if (y == x || y == w || y == gate || y == bias || (pre && (pre == y || pre == x || pre == w || pre == gate || pre == residual || pre == bias)))
+    return SVGEAR_ERR_INVALID;
   if (residual == y && residual && (rstride[0] != ystride[0] || rstride[1] != ystride[1]) && (B > 1 || N > 1))
     return SVGEAR_ERR_INVALID;
   const size_t need = svgear_linear_workspace(x, xstride, w, w_stride, dt, B, N, d_in, d_out);
@@ -434,6 +437,14 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
       reinterpret_cast<uintptr_t>(pre) % es || reinterpret_cast<uintptr_t>(dw) % es ||
       reinterpret_cast<uintptr_t>(dbias) % es || reinterpret_cast<uintptr_t>(dgate) % es)
     return SVGEAR_ERR_INVALID;
+  const void* ins[] = {dy, x, w, pre, gate};
+  void* outs[] = {dx, dw, dbias, dgate};
+  for (int i = 0; i < 4; ++i) {
+    for (const void* in : ins)
+      if (outs[i] && outs[i] == in) return SVGEAR_ERR_INVALID;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return SVGEAR_ERR_INVALID;
+  }
   if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 ||
       ws_bytes < svgear_linear_backward_workspace(dy, dystride, x, xstride, w, w_stride, dt, B, N, d_in, d_out))
     return SVGEAR_ERR_WORKSPACE;

@@ -14,6 +14,7 @@ namespace svgear {
 namespace {
 
 constexpr int kMaxHeads = 128;
+constexpr int64_t kMaxTokens = 1 << 30;
 constexpr int kRotWaves = 8;          // waves of a workgroup, at most
 // Workgroups of the backward pass for a tensor, at most; each leaves a partial dweight. Two tensors' 512 are all on the
 // GPU at once, with five waves each for 40 heads of 128: 75,600 tokens take 1,052 us, with 384 / 512 / 768 groups a tensor
@@ -440,7 +441,7 @@ rotary_backward_kernel(RotaryArgs a) {
   }
 }
 
-bool finite_aligned_strides(const int64_t st[3], size_t es, const void* p) {
+bool aligned_strides(const int64_t st[3], size_t es, const void* p) {
   if (reinterpret_cast<uintptr_t>(p) % 16) return false;
   for (int i = 0; i < 3; ++i)
     if (st[i] < 0 || (st[i] * (int64_t)es) % 16) return false;
@@ -465,6 +466,16 @@ bool rows_apart(const int64_t st[3], int64_t B, int64_t H, int64_t N, int64_t d)
   return true;
 }
 
+// Whether output k lies where an input or the other output does, other than the input it may replace (at its own strides).
+bool meets(void* const* out, const int64_t (*ost)[3], const void* const* own, const int64_t (*own_st)[3], const void* const* other,
+           int n, int k) {
+  for (int j = 0; j < n; ++j) {
+    if (j != k && (out[k] == out[j] || out[k] == own[j])) return true;
+    if (other && out[k] == other[j]) return true;
+  }
+  return out[k] == own[k] && (ost[k][0] != own_st[k][0] || ost[k][1] != own_st[k][1] || ost[k][2] != own_st[k][2]);
+}
+
 struct Shape {
   int B, H;
   int64_t N, n_tail;
@@ -475,7 +486,7 @@ int fill_args(RotaryArgs& a, int n_tensors, svgear_dtype dt, const Shape& z, con
               const int sections[3], const int64_t grid[3], int64_t first, const int32_t* positions,
               int64_t positions_stride_b, unsigned flags, float eps) {
   if (n_tensors < 1 || n_tensors > 2 || (dt != SVGEAR_F32 && dt != SVGEAR_BF16) || z.B <= 0 || z.H <= 0 ||
-      z.H > kMaxHeads || z.N <= 0 || z.n_tail < 0 || z.n_tail >= z.N || z.N > INT32_MAX || (int64_t)z.B * z.N > INT32_MAX ||
+      z.H > kMaxHeads || z.N <= 0 || z.n_tail < 0 || z.n_tail >= z.N || z.N > kMaxTokens || (int64_t)z.B * z.N > kMaxTokens ||
       (z.d != 64 && z.d != 128) || !sections || (flags & ~7u) || ((flags & 3u) == 3u) || !(eps >= 0.f))
     return SVGEAR_ERR_INVALID;
   for (int i = 0; i < 3; ++i)
@@ -593,13 +604,14 @@ extern "C" int svgear_rotary(int n_tensors, const void* const* src, const int64_
   if (rc != SVGEAR_OK) return rc;
   if (!src || !sstride || !dst || !dstride) return SVGEAR_ERR_INVALID;
   for (int k = 0; k < n_tensors; ++k) {
-    if (!src[k] || !dst[k] || !finite_aligned_strides(sstride[k], esize(dt), src[k]) ||
-        !finite_aligned_strides(dstride[k], esize(dt), dst[k]) || !rows_apart(dstride[k], B, H, N, d))
+    if (!src[k] || !dst[k] || !aligned_strides(sstride[k], esize(dt), src[k]) ||
+        !aligned_strides(dstride[k], esize(dt), dst[k]) || !rows_apart(dstride[k], B, H, N, d))
       return SVGEAR_ERR_INVALID;
     a.src[k] = src[k];
     a.dst[k] = dst[k];
     a.weight[k] = weight ? weight[k] : nullptr;
     if (a.weight[k] && (!(flags & 3u) || reinterpret_cast<uintptr_t>(a.weight[k]) % 16)) return SVGEAR_ERR_INVALID;
+    if (meets(dst, dstride, src, sstride, nullptr, n_tensors, k)) return SVGEAR_ERR_INVALID;
     a.sst[k] = Strides{sstride[k][0], sstride[k][1], sstride[k][2]};
     a.dst_st[k] = Strides{dstride[k][0], dstride[k][1], dstride[k][2]};
   }
@@ -608,8 +620,8 @@ extern "C" int svgear_rotary(int n_tensors, const void* const* src, const int64_
 }
 
 extern "C" size_t svgear_rotary_backward_workspace(int n_tensors, int B, int H, int64_t N, int d) {
-  if (n_tensors < 1 || n_tensors > 2 || B <= 0 || H <= 0 || H > kMaxHeads || N <= 0 || N > INT32_MAX ||
-      (int64_t)B * N > INT32_MAX || (d != 64 && d != 128))
+  if (n_tensors < 1 || n_tensors > 2 || B <= 0 || H <= 0 || H > kMaxHeads || N <= 0 || N > kMaxTokens ||
+      (int64_t)B * N > kMaxTokens || (d != 64 && d != 128))
     return 0;
   return (size_t)n_tensors * align_up((size_t)partial_rows(B, N) * H * d * sizeof(float), 256);
 }
@@ -629,8 +641,8 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
   if (!dy || !dystride || !dx || !dxstride || (norm && (!src || !sstride))) return SVGEAR_ERR_INVALID;
   bool any = false;
   for (int k = 0; k < n_tensors; ++k) {
-    if (!dy[k] || !dx[k] || !finite_aligned_strides(dystride[k], esize(dt), dy[k]) ||
-        !finite_aligned_strides(dxstride[k], esize(dt), dx[k]) || !rows_apart(dxstride[k], B, H, N, d))
+    if (!dy[k] || !dx[k] || !aligned_strides(dystride[k], esize(dt), dy[k]) ||
+        !aligned_strides(dxstride[k], esize(dt), dx[k]) || !rows_apart(dxstride[k], B, H, N, d))
       return SVGEAR_ERR_INVALID;
     a.weight[k] = weight ? weight[k] : nullptr;
     if (a.weight[k] && (!norm || reinterpret_cast<uintptr_t>(a.weight[k]) % 16)) return SVGEAR_ERR_INVALID;
@@ -643,10 +655,12 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
     a.dst[k] = dx[k];
     a.dst_st[k] = Strides{dxstride[k][0], dxstride[k][1], dxstride[k][2]};
     if (norm) {
-      if (!src[k] || !finite_aligned_strides(sstride[k], esize(dt), src[k])) return SVGEAR_ERR_INVALID;
+      if (!src[k] || !aligned_strides(sstride[k], esize(dt), src[k])) return SVGEAR_ERR_INVALID;
+      if (meets(dx, dxstride, dy, dystride, src, n_tensors, k)) return SVGEAR_ERR_INVALID;
       a.src[k] = src[k];
       a.sst[k] = Strides{sstride[k][0], sstride[k][1], sstride[k][2]};
     } else {  // the forward kernel with the angles' signs turned
+      if (meets(dx, dxstride, dy, dystride, nullptr, n_tensors, k)) return SVGEAR_ERR_INVALID;
       a.src[k] = dy[k];
       a.sst[k] = a.yst[k];
     }

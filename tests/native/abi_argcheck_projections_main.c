@@ -15,6 +15,8 @@ static void expect(const char* what, long long got, long long want) {
 
 static void* const fake = (void*)0x10000;
 static void* const odd = (void*)0x10001;
+static void* const out = (void*)0x80000;
+static void* const out2 = (void*)0x90000;
 static const size_t big = (size_t)1 << 50;
 
 static int lin(const void* x, const int64_t* xst, const void* w, int64_t ldw, svgear_dtype dt, int B, int64_t N, int k, int o,
@@ -28,46 +30,54 @@ static void linear(void) {
   const int64_t inner_b[2] = {16, 32}, inner_meet[2] = {16, 31};
   const svgear_dtype H = SVGEAR_BF16;
   /* B = 2, N = 100, 16 to 16 */
-  expect("linear: null x", lin(NULL, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: null strides", lin(fake, NULL, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: null w", lin(fake, s, NULL, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
+  expect("linear: null x", lin(NULL, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: null strides", lin(fake, NULL, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: null w", lin(fake, s, NULL, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
   expect("linear: null y", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, NULL, s, big), -1);
-  expect("linear: null y strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, NULL, big), -1);
-  expect("linear: B = 0", lin(fake, s, fake, 16, H, 0, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: N = 0", lin(fake, s, fake, 16, H, 2, 0, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: d_in = 0", lin(fake, s, fake, 16, H, 2, 100, 0, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: d_out < 0", lin(fake, s, fake, 16, H, 2, 100, 16, -3, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: d_in too large", lin(fake, s, fake, 1 << 22, H, 2, 100, (1 << 21) + 1, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: too many rows", lin(fake, s, fake, 16, H, 4, (int64_t)1 << 30, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: N past 32 bits", lin(fake, s, fake, 16, H, 1, (int64_t)1 << 40, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: w_stride < d_in", lin(fake, s, fake, 15, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: negative stride of x", lin(fake, neg, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: rows of y meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, meet, big), -1);
-  expect("linear: batches of y meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, meet_b, big), -1);
-  expect("linear: batches within tokens meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, inner_meet, big), -1);
-  expect("linear: bad type", lin(fake, s, fake, 16, (svgear_dtype)2, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: bad activation", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 4, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: negative activation", lin(fake, s, fake, 16, H, 2, 100, 16, 16, -1, NULL, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: gate without strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, fake, NULL, NULL, NULL, fake, s, big), -1);
-  expect("linear: residual without strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, fake, NULL, fake, s, big), -1);
-  expect("linear: negative stride of residual", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, fake, neg, fake, s, big), -1);
+  expect("linear: null y strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, NULL, big), -1);
+  expect("linear: B = 0", lin(fake, s, fake, 16, H, 0, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: N = 0", lin(fake, s, fake, 16, H, 2, 0, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: d_in = 0", lin(fake, s, fake, 16, H, 2, 100, 0, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: d_out < 0", lin(fake, s, fake, 16, H, 2, 100, 16, -3, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: d_in too large", lin(fake, s, fake, 1 << 22, H, 2, 100, (1 << 21) + 1, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: too many rows", lin(fake, s, fake, 16, H, 4, (int64_t)1 << 30, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: N past 32 bits", lin(fake, s, fake, 16, H, 1, (int64_t)1 << 40, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: w_stride < d_in", lin(fake, s, fake, 15, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: negative stride of x", lin(fake, neg, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: rows of y meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, meet, big), -1);
+  expect("linear: batches of y meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, meet_b, big), -1);
+  expect("linear: batches within tokens meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, inner_meet, big), -1);
+  expect("linear: bad type", lin(fake, s, fake, 16, (svgear_dtype)2, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: bad activation", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 4, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: negative activation", lin(fake, s, fake, 16, H, 2, 100, 16, 16, -1, NULL, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: gate without strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, fake, NULL, NULL, NULL, out, s, big), -1);
+  expect("linear: residual without strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, fake, NULL, out, s, big), -1);
+  expect("linear: negative stride of residual", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, fake, neg, out, s, big), -1);
   expect("linear: y over the residual with other strides", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, fake, other, fake, s, big), -1);
-  expect("linear: x at an odd address", lin(odd, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
+  expect("linear: y over x", lin(fake, s, (void*)0x20000, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
+  expect("linear: y over w", lin((void*)0x20000, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, fake, s, big), -1);
+  expect("linear: pre over y",
+         svgear_linear((void*)0x20000, s, (void*)0x30000, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, fake, fake, s, fake, big, NULL), -1);
+  expect("linear_backward: dx over dy",
+         svgear_linear_backward(fake, s, (void*)0x20000, s, (void*)0x30000, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, s, NULL, NULL, NULL, fake, big, NULL), -1);
+  expect("linear_backward: dbias over dw",
+         svgear_linear_backward(fake, s, (void*)0x20000, s, (void*)0x30000, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, (void*)0x40000, (void*)0x40000, NULL, fake, big, NULL), -1);
+  expect("linear: x at an odd address", lin(odd, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
   expect("linear: y at an odd address", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, odd, s, big), -1);
   {
     const int64_t packed[2] = {1700, 17};
     const size_t need = svgear_linear_workspace(fake, packed, fake, 17, H, 2, 100, 17, 16);
     expect("linear_workspace: unaligned rows need some", need > 0, 1);
-    expect("linear: workspace too small", lin(fake, packed, fake, 17, H, 2, 100, 17, 16, 0, NULL, NULL, NULL, NULL, fake, s, need - 1), -2);
+    expect("linear: workspace too small", lin(fake, packed, fake, 17, H, 2, 100, 17, 16, 0, NULL, NULL, NULL, NULL, out, s, need - 1), -2);
     expect("linear: workspace null",
-           svgear_linear(fake, packed, fake, 17, NULL, H, 2, 100, 17, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, fake, s, NULL, big, NULL), -2);
+           svgear_linear(fake, packed, fake, 17, NULL, H, 2, 100, 17, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, out, s, NULL, big, NULL), -2);
     expect("linear: workspace not aligned",
-           svgear_linear(fake, packed, fake, 17, NULL, H, 2, 100, 17, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, fake, s, (void*)0x10010, big, NULL), -2);
+           svgear_linear(fake, packed, fake, 17, NULL, H, 2, 100, 17, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, out, s, (void*)0x10010, big, NULL), -2);
   }
   expect("linear: bias at an odd address",
-         svgear_linear(fake, s, fake, 16, odd, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, fake, s, fake, big, NULL), -1);
+         svgear_linear(fake, s, fake, 16, odd, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, out, s, fake, big, NULL), -1);
   expect("linear: pre at an odd address",
-         svgear_linear(fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, odd, fake, s, fake, big, NULL), -1);
+         svgear_linear(fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, odd, out, s, fake, big, NULL), -1);
   expect("linear_workspace: aligned large calls need none", (long long)svgear_linear_workspace(fake, s, fake, 5120, H, 1, 75600, 5120, 15360), 0);
   expect("linear_workspace: invalid", (long long)svgear_linear_workspace(fake, s, fake, 16, H, 0, 100, 16, 16), 0);
   expect("linear_workspace: extreme returns", svgear_linear_workspace(fake, inner_b, odd, 1 << 21, SVGEAR_F32, 1 << 15, 1 << 15, 1 << 21, 1 << 21) > 0, 1);
@@ -75,25 +85,25 @@ static void linear(void) {
   expect("linear_backward: nothing wanted",
          svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: null dy",
-         svgear_linear_backward(NULL, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, s, NULL, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(NULL, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, out, s, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: dx without w",
-         svgear_linear_backward(fake, s, fake, s, NULL, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, s, NULL, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, NULL, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, out, s, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: dx without strides",
-         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, NULL, NULL, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, out, NULL, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: dw without x",
-         svgear_linear_backward(fake, s, NULL, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, fake, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, NULL, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, out, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: activation without pre",
-         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_SILU, NULL, NULL, fake, s, NULL, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_SILU, NULL, NULL, out, s, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: dgate without gate",
-         svgear_linear_backward(fake, s, fake, s, fake, 16, fake, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, NULL, fake, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, fake, 16, fake, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, NULL, NULL, NULL, NULL, out, fake, big, NULL), -1);
   expect("linear_backward: dgate without pre",
-         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, fake, s, NULL, NULL, NULL, NULL, fake, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, fake, s, NULL, NULL, NULL, NULL, out, fake, big, NULL), -1);
   expect("linear_backward: rows of dx meet",
-         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, meet, NULL, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, out, meet, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: w_stride < d_in",
-         svgear_linear_backward(fake, s, fake, s, fake, 8, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, s, NULL, NULL, NULL, fake, big, NULL), -1);
+         svgear_linear_backward(fake, s, fake, s, fake, 8, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, out, s, NULL, NULL, NULL, fake, big, NULL), -1);
   expect("linear_backward: workspace too small",
-         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, fake, s, fake, fake, NULL, fake, 16, NULL), -2);
+         svgear_linear_backward(fake, s, fake, s, fake, 16, NULL, H, 2, 100, 16, 16, SVGEAR_ACT_NONE, NULL, NULL, out, s, out2, (void*)0xa0000, NULL, fake, 16, NULL), -2);
   expect("linear_backward_workspace: extreme returns",
          svgear_linear_backward_workspace(fake, s, fake, s, fake, 1 << 21, SVGEAR_F32, 1 << 15, 1 << 15, 1 << 21, 1 << 21) > 0, 1);
   expect("linear_backward_workspace: invalid", (long long)svgear_linear_backward_workspace(fake, s, fake, s, fake, 16, H, 2, -1, 16, 16), 0);
@@ -176,6 +186,9 @@ static void rotary(void) {
   REFUSED("negative stride", r.st[0][1] = -1920);
   REFUSED("rows of the output meet", r.dst[0][2] = 56);
   REFUSED("heads of the output meet", r.dst[0][1] = 1856);
+  REFUSED("two outputs at one address", (r.n = 2, r.out[1] = r.out[0]));
+  REFUSED("an output over the other input", (r.n = 2, r.src[1] = (void*)0x50000, r.out[1] = (void*)0x30000, r.out[0] = (void*)0x50000));
+  REFUSED("in place at other strides", (r.out[0] = (void*)r.src[0], r.dst[0][0] = 11520));
   REFUSED("batches of the output meet", r.dst[0][0] = 5696);
   {
     Rot r = ordinary();

@@ -258,3 +258,76 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for a, e in zip(out, ref):
             assert torch.equal(a, e)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_rows_that_lie_more_than_4_gib_apart(dtype):
+    """Element offsets past 32 bits in x, w, the gate, the residual and the output."""
+    far = (1 << 31) + 72
+    n, k, o = 3, 72, 40
+
+    def rows(count, width, seed):
+        buf = torch.empty(far * (count - 1) + width, dtype=dtype, device="cuda")
+        t = buf.as_strided((count, width), (far, 1))
+        t.copy_(rand(count, width, seed=seed, dtype=dtype))
+        return t
+
+    x, res, gate = rows(n, k, 1), rows(n, o, 2), rows(n, o, 3)
+    w = rand(o, k, seed=4, dtype=dtype, scale=0.1).cuda()
+    out = rows(n, o, 5)
+    sv.linear(x, w, act="silu", gate=gate, residual=res, out=out)
+    Y, _, by, _ = linear64(x, w, None, "silu", gate, res)
+    close(out, Y, by)
+    del res, out
+    many = rand(70, k, seed=6, dtype=dtype).cuda()  # the tile kernel: the weights' rows far apart
+    wf = rows(2, k, 7)
+    y, _ = sv.linear(many, wf)
+    Y, _, by, _ = linear64(many, wf)
+    close(y, Y, by)
+    got = sv.linear_backward(rand(n, o, seed=8, dtype=dtype).cuda(), x, w, want=["dx", "dw"])
+    ref = linear_backward64(rand(n, o, seed=8, dtype=dtype), x, w, None, unit=0.0)
+    for name in got:
+        close(got[name], *ref[name], name)
+
+
+def test_calls_on_two_streams_at_once():
+    """Forward and backward passes of two sizes on two streams side by side give what they give alone."""
+    a = inputs(torch.bfloat16, 2, 700, 1000, 520, True, "batch", True, seed=400)
+    b = inputs(torch.bfloat16, 1, 900, 333, 1111, True, "token", True, seed=410)
+
+    def step(x, w, bias, g, r):
+        y, pre = sv.linear(x, w, bias, act="gelu_tanh", gate=g, residual=r, want_pre=True)
+        return [y, *sv.linear_backward(y, x, w, pre=pre, act="gelu_tanh", gate=g, want=["dx", "dw", "dbias", "dgate"]).values()]
+
+    ra, rb = step(*a), step(*b)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            got.append((step(*a), ra))
+        with torch.cuda.stream(s2):
+            got.append((step(*b), rb))
+    torch.cuda.synchronize()
+    for g, r in got:
+        assert all(torch.equal(u, v) for u, v in zip(g, r))
+
+
+def test_captured_large_tiles():
+    """The 256 x 256 tiles, whose LDS is all of a CU's, recorded and replayed."""
+    x, w, b, _, r = inputs(torch.bfloat16, 1, 4100, 136, 4104, True, "none", True, seed=420)
+    xs = x.clone()
+    sv.linear(xs, w, b, residual=r)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, _ = sv.linear(xs, w, b, residual=r)
+        dx = sv.linear_backward(y, xs, w, want=["dx"])["dx"]
+    for k in range(3):
+        x2 = rand(*x.shape, seed=430 + k, dtype=x.dtype).cuda()
+        xs.copy_(x2)
+        graph.replay()
+        y2, _ = sv.linear(x2, w, b, residual=r)
+        dx2 = sv.linear_backward(y2, x2, w, want=["dx"])["dx"]
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2) and torch.equal(dx, dx2)

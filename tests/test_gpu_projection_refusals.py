@@ -108,6 +108,22 @@ def test_rotary_refuses_three_tensors_and_a_norm_without_inputs():
         sv.rotary_backward([q], None, f, S, grid=(2, 3, 4), norm="head")
 
 
+def test_outputs_over_inputs_are_refused():
+    x = z(2, 3, 16)
+    w = z(16, 16)
+    with pytest.raises(sv.SvgearError):
+        sv.linear(x, w, out=x)
+    q, k = z(*Q), z(*Q)
+    f = sv.rotary_frequencies(S)
+    for out in ([k, q], [q, q]):
+        with pytest.raises(sv.SvgearError):
+            sv.rotary([q, k], f, S, grid=(2, 3, 4), out=out)
+        with pytest.raises(sv.SvgearError):
+            sv.rotary_backward([q, k], None, f, S, grid=(2, 3, 4), out=out)
+    with pytest.raises(sv.SvgearError):
+        sv.rotary_backward([q], [k], f, S, grid=(2, 3, 4), norm="head", out=[k])
+
+
 def test_block_refuses_weights_of_other_sizes():
     x, c = z(1, 24, 32), torch.zeros(1, 2, 3, 64, device="cuda")
     f = sv.rotary_frequencies(S)

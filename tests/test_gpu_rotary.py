@@ -191,3 +191,44 @@ def test_captured_and_replayed():
         ref = step(a, b)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(out, ref))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_a_cache_of_more_than_4_gib(dtype):
+    """Heads that lie more than 2^31 elements apart, forward and backward."""
+    far, d, n = (1 << 31) + 64, 64, 5
+    x = rand(1, 2, n, d, seed=1, dtype=dtype).cuda()
+    f, sections = sv.rotary_frequencies((10, 11, 11)), (10, 11, 11)
+    kw = {"grid": (1, 1, n), "norm": "head"}
+    w = rand(d, seed=2, dtype=dtype).cuda()
+    cache = torch.empty(far + n * d, dtype=dtype, device="cuda").as_strided((1, 2, n, d), (2 * far, far, d, 1))
+    sv.rotary([x], f, sections, weights=[w], out=[cache], **kw)
+    close(cache, *rotary64(x, f, sections, weight=w, **kw))
+    g = rand(1, 2, n, d, seed=3, dtype=dtype).cuda()
+    dx, dw = sv.rotary_backward([g], [cache], f, sections, weights=[w], **kw)
+    rdx, bdx, rdw, bdw = rotary_backward64(g, cache, f, sections, weight=w, **kw)
+    close(dx[0], rdx, bdx)
+    close(dw[0], rdw, bdw)
+
+
+def test_calls_on_two_streams_at_once():
+    a = setup((2, 40, (1, 5, 30), 0, 7, 128, (22, 21, 21)), torch.bfloat16, "token", None, seed=30)
+    b = setup((1, 5, (3, 20, 10), 0, 0, 64, (8, 12, 11)), torch.float32, "head", "batch", seed=40)
+
+    def step(q, k, f, sections, weights, kw):
+        y = sv.rotary([q, k], f, sections, weights=weights, **kw)
+        dx, dw = sv.rotary_backward(y, [q, k], f, sections, weights=weights, **kw)
+        return [*y, *dx, *dw]
+
+    ra, rb = step(*a), step(*b)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            got.append((step(*a), ra))
+        with torch.cuda.stream(s2):
+            got.append((step(*b), rb))
+    torch.cuda.synchronize()
+    for g, r in got:
+        assert all(torch.equal(u, v) for u, v in zip(g, r))
