@@ -5,7 +5,8 @@
 //
 // One pass over the data: a wave holds all heads of a token (or its share of them) in registers, 16 bytes a
 // load, so the mean over a token's heads costs no second read; the angles of a token are found once, one pair
-// a lane, and shared by its heads through LDS. Bound by memory.
+// a lane, and shared by its heads through LDS. Bound by memory: two tensors of 75,600 tokens of 40 heads of 128, bf16, norm over
+// the token: 600 us, 5.2 TB/s, as a plain copy; a single token 7 us, the launch and three dependent loads.
 #include "common.h"
 
 #include <math.h>
