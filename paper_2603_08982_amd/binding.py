@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -105,7 +106,7 @@ def load_library():
     lib.svgear_sparse_attn_two_stage.argtypes = lib.svgear_sparse_attn_comp.argtypes
     lib.svgear_unpermute.restype = _i
     lib.svgear_unpermute.argtypes = [_vp, _vp, _i, _i, _i, _i64, _i, _vp, _c.POINTER(_c.c_int64), _vp]
-    p2, p3 = _c.POINTER(_c.c_int64), _c.POINTER(_I64x3)
+    p2 = _vp
     lib.svgear_linear_workspace.restype = _sz
     lib.svgear_linear_workspace.argtypes = [_vp, p2, _vp, _i64, _i, _i, _i64, _i, _i]
     lib.svgear_linear.restype = _i
@@ -116,14 +117,14 @@ def load_library():
     lib.svgear_linear_backward.restype = _i
     lib.svgear_linear_backward.argtypes = [_vp, p2, _vp, p2, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, p2, _vp, p2,
                                            _vp, _vp, _vp, _vp, _sz, _vp]
-    pp = _c.POINTER(_vp)
-    places = [_vp, _c.POINTER(_c.c_int), p2, _i64, _vp, _i64, _u, _f]
+    # host arrays of pointers, strides, sections and sizes as plain addresses: ctypes checks less of them in each call
+    places = [_vp, _vp, _vp, _i64, _vp, _i64, _u, _f]
     lib.svgear_rotary.restype = _i
-    lib.svgear_rotary.argtypes = [_i, pp, p3, pp, p3, pp, _i, _i, _i, _i64, _i64, _i, *places, _vp]
+    lib.svgear_rotary.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i64, _i64, _i, *places, _vp]
     lib.svgear_rotary_backward_workspace.restype = _sz
     lib.svgear_rotary_backward_workspace.argtypes = [_i, _i, _i, _i64, _i]
     lib.svgear_rotary_backward.restype = _i
-    lib.svgear_rotary_backward.argtypes = [_i, pp, p3, pp, p3, pp, p3, pp, pp, _i, _i, _i, _i64, _i64, _i, *places, _vp, _sz,
+    lib.svgear_rotary_backward.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i64, _i64, _i, *places, _vp, _sz,
                                            _vp]
     _LIB = lib
     return lib
@@ -373,7 +374,8 @@ def _on_device(device: torch.device):
 
 
 def _stream_of(device: torch.device) -> int:
-    return torch.cuda.current_stream(device.index).cuda_stream
+    """The current stream's handle, without the object that torch.cuda.current_stream makes of it (1 us of a small call's 12)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _scratch(nbytes: int, device):
@@ -514,7 +516,9 @@ def rotary_frequencies(sections: Sequence[int], theta: float = 10000.0, device="
 
 
 _PTRS = (None, _vp * 1, _vp * 2)
-_ROWS = (None, _I64x3 * 1, _I64x3 * 2)
+_STRIDES = (None, _c.c_int64 * 3, _c.c_int64 * 6)  # int64_t[n][3], one behind the other
+_sections = functools.lru_cache(maxsize=64)(lambda *s: _Ix3(*s))
+_grid = functools.lru_cache(maxsize=64)(lambda *g: _I64x3(*g))
 
 
 def _pointers(ts):
@@ -522,10 +526,13 @@ def _pointers(ts):
 
 
 def _strides_of(ts):
-    strides = [t.stride() for t in ts]
-    for st in strides:
-        _require(len(st) == 4 and st[3] == 1, "expected [B,H,N,d] with contiguous d")
-    return _ROWS[len(ts)](*[st[:3] for st in strides])
+    flat = []
+    for t in ts:
+        st = t.stride()
+        if len(st) != 4 or st[3] != 1:
+            raise SvgearError("expected [B,H,N,d] with contiguous d")
+        flat += st[:3]
+    return _STRIDES[len(ts)](*flat)
 
 
 def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, norm, weights, halves):
@@ -554,7 +561,7 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
     else:
         if len(grid) != 3:
             raise SvgearError("grid: (time, height, width)")
-        size3 = _I64x3(*grid)
+        size3 = _grid(*grid)
     if weights is None:
         weights = (None,) * len(tensors)
     else:
@@ -564,7 +571,7 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
         for w in weights:
             if w is not None and (w.shape != (size,) or not w.is_contiguous()):
                 raise SvgearError("weights: expected [d] or [H*d]")
-    return weights, (inv_freq.data_ptr(), _Ix3(*sections), size3, first, _ptr(positions), pos_b,
+    return weights, (inv_freq.data_ptr(), _sections(*sections), size3, first, _ptr(positions), pos_b,
                      ROTARY_NORMS[norm] | (ROTARY_HALVES if halves else 0))
 
 
