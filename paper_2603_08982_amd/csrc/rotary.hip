@@ -16,10 +16,11 @@ namespace {
 
 constexpr int kMaxHeads = 128;
 constexpr int64_t kMaxTokens = 1 << 30;
-constexpr int kRotWaves = 8;          // waves of a workgroup, at most
-// Workgroups of the backward pass for a tensor, at most; each leaves a partial dweight. Two tensors' 512 are all on the
-// GPU at once, with five waves each for 40 heads of 128: 75,600 tokens take 1,052 us, with 384 / 512 / 768 groups a tensor
-// 1,312 / 1,396 / 1,271.
+constexpr int kRotWaves = 8;  // waves of a workgroup, at most; of the backward pass in bf16 up to 64 heads of 128:
+constexpr int kRotBackWaves = 16;
+// Workgroups of the backward pass, at most; each leaves a partial dweight. One on each CU, three tokens of 40 heads of 128 at a
+// time (15 waves, all that its registers allow): two tensors of 75,600 tokens take 1,014 us; two on each of one token (five
+// waves: a third does not fit the four SIMDs) 1,052, and with 768 to 1,536 of these, a part of which waits, 1,271 to 1,396.
 constexpr int kBackwardGroups = 256;
 
 struct RotaryArgs {
@@ -80,6 +81,8 @@ constexpr int kMaxIts = V == 1 ? 16 : V == 4 ? 10 : 5;
 // waves: few of them up to 64 heads of 128, twice as many beyond.
 template <typename T, int V>
 constexpr int kFewIts = V == 1 ? 8 : V == 4 ? 2 : 1;
+template <int V, int IT>
+constexpr int kBackWaves = V == 8 && IT == 1 ? kRotBackWaves : kRotWaves;
 
 enum { kNormNone = 0, kNormHead = 1, kNormToken = 2 };
 
@@ -253,13 +256,14 @@ rotary_kernel(RotaryArgs a) {
 // vector instructions an element, with the turned gradients kept for the second use; the first version, which
 // turned them twice and packed by hand, had some 40 and was bound by them.
 template <typename T, int V, int NORM, bool HALVES, int IT>
-__global__ void __launch_bounds__(64 * kRotWaves)
+__global__ void __launch_bounds__((64 * kBackWaves<V, IT>))
 rotary_backward_kernel(RotaryArgs a) {
   constexpr int AT = NORM == kNormToken ? IT : 1;  // a head's weight is shared by all heads
-  __shared__ float2 rows[2][kRotWaves][64];
-  __shared__ float2 slots[2][kRotWaves];
+  constexpr int MW = kBackWaves<V, IT>;
+  __shared__ float2 rows[2][MW][64];
+  __shared__ float2 slots[2][MW];
   constexpr int Q = V == 1 ? 2 : 4;  // sums of a lane that go through LDS at a time
-  __shared__ float acc_s[kRotWaves][64][Q];
+  __shared__ float acc_s[MW][64][Q];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wpt = a.waves_per_token, per_group = (blockDim.x >> 6) / wpt, first = wave - wave % wpt;
   const int k = blockIdx.y, units = a.d / (2 * V);
@@ -541,16 +545,16 @@ template <typename T, int V, int NORM, bool HALVES>
 int launch_mode(RotaryArgs& a, int n_tensors, bool backward, hipStream_t s) {
   if constexpr (NORM != kNormNone) {
     if (backward) {
-      const int few = kFewIts<T, V>;
+      constexpr int few = kFewIts<T, V>;
       const bool wide = a.H > kRotWaves * few * (64 / (a.d / (2 * V)));
-      const int threads = plan_waves(a, V, wide ? 2 * few : few, kRotWaves);
+      const int threads = plan_waves(a, V, wide ? 2 * few : few, wide ? kBackWaves<V, 2 * few> : kBackWaves<V, few>);
       a.rows = (int)ceil_div(a.tokens, threads / 64 / a.waves_per_token);
-      if (a.rows > kBackwardGroups) a.rows = kBackwardGroups;
+      if (a.rows > kBackwardGroups / n_tensors) a.rows = kBackwardGroups / n_tensors;
       const dim3 grid((unsigned)a.rows, (unsigned)n_tensors);
       if (wide)
-        rotary_backward_kernel<T, V, NORM, HALVES, 2 * kFewIts<T, V>><<<grid, threads, 0, s>>>(a);
+        rotary_backward_kernel<T, V, NORM, HALVES, 2 * few><<<grid, threads, 0, s>>>(a);
       else
-        rotary_backward_kernel<T, V, NORM, HALVES, kFewIts<T, V>><<<grid, threads, 0, s>>>(a);
+        rotary_backward_kernel<T, V, NORM, HALVES, few><<<grid, threads, 0, s>>>(a);
       SVGEAR_LAUNCH_CHECK();
       return SVGEAR_OK;
     }
@@ -583,10 +587,10 @@ int launch_rotary(RotaryArgs& a, svgear_dtype dt, int n_tensors, unsigned flags,
   return wide ? launch_width<bf16_t, 8>(a, n_tensors, flags, backward, s) : launch_width<bf16_t, 1>(a, n_tensors, flags, backward, s);
 }
 
-// Rows that the backward pass leaves in `partial`: no more than there are tokens.
-int64_t partial_rows(int B, int64_t N) {
-  const int64_t tokens = (int64_t)B * N;
-  return tokens < kBackwardGroups ? tokens : kBackwardGroups;
+// Rows that the backward pass leaves in `partial` for a tensor: no more than there are tokens.
+int64_t partial_rows(int n_tensors, int B, int64_t N) {
+  const int64_t tokens = (int64_t)B * N, most = kBackwardGroups / n_tensors;
+  return tokens < most ? tokens : most;
 }
 
 }  // namespace
@@ -624,7 +628,7 @@ extern "C" size_t svgear_rotary_backward_workspace(int n_tensors, int B, int H, 
   if (n_tensors < 1 || n_tensors > 2 || B <= 0 || H <= 0 || H > kMaxHeads || N <= 0 || N > kMaxTokens ||
       (int64_t)B * N > kMaxTokens || (d != 64 && d != 128))
     return 0;
-  return (size_t)n_tensors * align_up((size_t)partial_rows(B, N) * H * d * sizeof(float), 256);
+  return (size_t)n_tensors * align_up((size_t)partial_rows(n_tensors, B, N) * H * d * sizeof(float), 256);
 }
 
 extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, const int64_t (*dystride)[3],
@@ -672,7 +676,7 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
   if (any) {
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < svgear_rotary_backward_workspace(n_tensors, B, H, N, d))
       return SVGEAR_ERR_WORKSPACE;
-    for (int k = 0; k < n_tensors; ++k) a.partial[k] = dweight[k] ? w.take<float>((size_t)partial_rows(B, N) * H * d) : nullptr;
+    for (int k = 0; k < n_tensors; ++k) a.partial[k] = dweight[k] ? w.take<float>((size_t)partial_rows(n_tensors, B, N) * H * d) : nullptr;
   }
   const int done = launch_rotary(a, dt, n_tensors, flags, true, s);
   if (done != SVGEAR_OK || !any) return done;
