@@ -42,8 +42,8 @@ enum { kContractBoth = 0, kContractQ = 1, kContractNone = 2 };
 
 int launch_linear_bf16(const LinearArgs& a, int form, hipStream_t s);
 int launch_linear_f32(const LinearArgs& a, int form, hipStream_t s);
-// The same for few rows (kContractBoth), operands at any alignment. Up to 4 in bf16: 4 / 8 rows of 5120 by 5120 18.5 / 33 us,
-// by tiles of 64 22 / 22; up to 8 in fp32, which needs no unpacking: 27 / 35 us and 42 / 42.
+// The same for few rows (kContractBoth), operands at any alignment. Up to 4 in bf16: 4 / 8 rows of 5120 by 5120 16.7 / 22.9 us,
+// by tiles of 64 18.7 / 19.0; up to 8 in fp32: 27 / 35 us and 41 / 41.
 static inline int few_rows(svgear_dtype dt) { return dt == SVGEAR_F32 ? 8 : 4; }
 int launch_linear_rows(const LinearArgs& a, svgear_dtype dt, hipStream_t s);
 // y from the partial products of `splits` parts.

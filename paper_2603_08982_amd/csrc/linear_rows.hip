@@ -2,10 +2,10 @@
 // all of them, so it is bound by memory, and by latency where the weights are few.
 //
 // out[r][c] = sum_k Q[r][k] P[c][k]. A wave reads whole rows of weights, 1 KB at a time and several rows and pieces in
-// flight, and multiplies them with the rows of Q on the vector ALU. The waves of a workgroup have the same few columns and K in turn, their
+// flight, and multiplies them with the rows of Q on the vector ALU, bf16 by pairs. The waves of a workgroup have the same few columns and K in turn, their
 // sums are added in order. Workgroups are small, so that all CUs get the same share of the weights: with the 16
 // columns that a matrix instruction wants for each, 5,120 columns are 320 shares for 256 CUs (1 row of 5120 by 5120,
-// bf16: 18.3 us that way, 13.4 this way; by 30720: 66 and 60 us, 5.2 TB/s).
+// bf16: 18.3 us that way, 12.9 this way; by 30720: 66 and 60 us, 5.2 TB/s).
 #include "linear.h"
 
 namespace svgear {
@@ -13,37 +13,39 @@ namespace {
 
 constexpr int kMaxWaves = 8;
 
+// 16 bytes of a row: elements k.. of it, those < K, others 0; EVEN: all or none of them.
+template <typename T, bool EVEN>
+__device__ __forceinline__ uint4 load_piece(const T* row, int64_t k, int64_t K) {
+  if constexpr (EVEN) {
+    return k < K ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(0, 0, 0, 0);
+  } else {
+    constexpr int CH = 16 / sizeof(T);
+    T e[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) e[i] = k + i < K ? row[k + i] : T(0);
+    uint4 u;
+    __builtin_memcpy(&u, e, 16);
+    return u;
+  }
+}
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+// acc + the products of two pieces, bf16 by pairs (exact products, fp32 sums).
 template <typename T>
-struct Piece {  // 16 bytes of a row
-  static constexpr int CH = 16 / sizeof(T);
-  float v[CH];
-  // elements k.. of a row, those < K, others 0; EVEN: all or none of them
-  template <bool EVEN>
-  static __device__ __forceinline__ uint4 load(const T* row, int64_t k, int64_t K) {
-    if constexpr (EVEN) {
-      return k < K ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(0, 0, 0, 0);
+__device__ __forceinline__ float multiply_piece(uint4 x, uint4 w, float acc) {
+  const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      acc = __builtin_fmaf(__uint_as_float(a[i]), __uint_as_float(b[i]), acc);
     } else {
-      T e[CH];
-#pragma unroll
-      for (int i = 0; i < CH; ++i) e[i] = k + i < K ? row[k + i] : T(0);
-      uint4 u;
-      __builtin_memcpy(&u, e, 16);
-      return u;
+      union { uint32_t u; bf16x2v v; } p, q;
+      p.u = a[i], q.u = b[i];
+      acc = __builtin_amdgcn_fdot2_f32_bf16(p.v, q.v, acc, false);
     }
   }
-  __device__ __forceinline__ explicit Piece(uint4 u) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        v[i] = __uint_as_float(w[i]);
-      } else {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
-  }
-};
+  return acc;
+}
 
 // NR rows or fewer, CW columns a workgroup. EVEN: rows of both operands 16-byte aligned, K a whole number of pieces.
 template <typename T, int NR, int CW, bool EVEN>
@@ -70,22 +72,16 @@ linear_rows_kernel(LinearArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int c = 0; c < CW; ++c) w[u][c] = Piece<T>::template load<EVEN>(p[c], k + u * STEP, a.K);
+      for (int c = 0; c < CW; ++c) w[u][c] = load_piece<T, EVEN>(p[c], k + u * STEP, a.K);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       uint4 x[NR];
 #pragma unroll
-      for (int r = 0; r < NR; ++r) x[r] = Piece<T>::template load<EVEN>(q[r], k + u * STEP, a.K);
+      for (int r = 0; r < NR; ++r) x[r] = load_piece<T, EVEN>(q[r], k + u * STEP, a.K);
 #pragma unroll
-      for (int c = 0; c < CW; ++c) {
-        const Piece<T> y(w[u][c]);
+      for (int c = 0; c < CW; ++c)
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          const Piece<T> z(x[r]);
-#pragma unroll
-          for (int i = 0; i < CH; ++i) acc[r][c] = __builtin_fmaf(z.v[i], y.v[i], acc[r][c]);
-        }
-      }
+        for (int r = 0; r < NR; ++r) acc[r][c] = multiply_piece<T>(x[r], w[u][c], acc[r][c]);
     }
   }
 #pragma unroll
@@ -121,11 +117,12 @@ void launch_kernel(const LinearArgs& a, hipStream_t s) {
 
 template <typename T>
 int launch_type(const LinearArgs& a, hipStream_t s) {
-  const bool many = a.C >= 4096;  // then four columns a workgroup still are 1,024 of them
+  // four columns a workgroup where they still are 1,024 of them, or where more rows than two make rereading those dear
+  const bool many = a.C >= 4096 || a.R > 2;
   if (a.R <= 1) many ? launch_kernel<T, 1, 4>(a, s) : launch_kernel<T, 1, 1>(a, s);
   else if (a.R <= 2) many ? launch_kernel<T, 2, 4>(a, s) : launch_kernel<T, 2, 1>(a, s);
-  else if (a.R <= 4) many ? launch_kernel<T, 4, 4>(a, s) : launch_kernel<T, 4, 1>(a, s);
-  else if constexpr (sizeof(T) == 4) many ? launch_kernel<T, 8, 4>(a, s) : launch_kernel<T, 8, 1>(a, s);
+  else if (a.R <= 4) launch_kernel<T, 4, 4>(a, s);
+  else if constexpr (sizeof(T) == 4) launch_kernel<T, 8, 4>(a, s);
   else return SVGEAR_ERR_UNSUPPORTED;
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
