@@ -10,22 +10,29 @@ constexpr int kMaxWidth = 1 << 21;
 constexpr int64_t kMaxRows = 1 << 30;
 constexpr int64_t kMaxPitch = 1 << 21;  // a tile's rows are addressed by 32-bit byte offsets: 256 rows of 8 MB
 
-// ---- rows copied to an even, 16-byte aligned pitch, zeros behind the values; a 16-byte piece a thread
+// ---- rows copied to an even, 16-byte aligned pitch, zeros behind the values; a 16-byte piece a thread, one or two operands
+struct PackJob {
+  const void* src;
+  void* dst;
+  Rows st;
+  int64_t pitch, pieces;  // of a row of dst; in all
+  int n, rows, width;
+};
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-pack_rows_kernel(const T* src, Rows st, int n, int rows, int width, T* dst, int64_t pitch) {
+pack_rows_kernel(PackJob a, PackJob b) {
   constexpr int CH = 16 / sizeof(T);
-  const int col = (blockIdx.y * kThreads + threadIdx.x) * CH;
-  if (col >= pitch) return;
-  for (int r = blockIdx.x; r < rows; r += gridDim.x) {
-    const int b = n >= rows ? 0 : r / n;
-    const T* s = src + (int64_t)b * st.b + (int64_t)(r - b * n) * st.n + col;
-    T e[CH];
+  const PackJob& p = blockIdx.y ? b : a;
+  const int64_t across = p.pitch / CH;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.pieces; i += (int64_t)gridDim.x * kThreads) {
+    const int r = (int)(i / across), col = (int)(i - r * across) * CH, e = p.n >= p.rows ? 0 : r / p.n;
+    const T* s = static_cast<const T*>(p.src) + (int64_t)e * p.st.b + (int64_t)(r - e * p.n) * p.st.n + col;
+    T v[CH];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) e[i] = col + i < width ? s[i] : T(0);
+    for (int k = 0; k < CH; ++k) v[k] = col + k < p.width ? s[k] : T(0);
     uint4 u;
-    __builtin_memcpy(&u, e, 16);
-    *reinterpret_cast<uint4*>(dst + (int64_t)r * pitch + col) = u;
+    __builtin_memcpy(&u, v, 16);
+    *reinterpret_cast<uint4*>(static_cast<T*>(p.dst) + (int64_t)r * p.pitch + col) = u;
   }
 }
 
@@ -198,25 +205,30 @@ size_t packed_bytes(int64_t rows, int64_t width, svgear_dtype dt) {
   return align_up((size_t)rows * even_pitch(width, dt) * esize(dt), 256);
 }
 
-template <typename T>
-int pack_rows(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, void* dst, int64_t pitch, hipStream_t s) {
-  const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), (unsigned)ceil_div(pitch, (int64_t)(kThreads * 16 / sizeof(T))));
-  pack_rows_kernel<T><<<grid, kThreads, 0, s>>>(static_cast<const T*>(src), st, (int)n, (int)rows, (int)width, static_cast<T*>(dst), pitch);
-  SVGEAR_LAUNCH_CHECK();
-  return SVGEAR_OK;
-}
-int pack(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, svgear_dtype dt, Workspace& w, Operand& out,
-         hipStream_t s) {
-  out.pitch = even_pitch(width, dt);
-  if (dt == SVGEAR_F32) {
-    float* p = w.take<float>((size_t)rows * out.pitch);
-    out.p = p;
-    return pack_rows<uint32_t>(src, st, n, rows, width, p, out.pitch, s);
+// The copies that a call needs, made by one launch.
+struct Packing {
+  PackJob job[2] = {};
+  int jobs = 0;
+  void add(const void* src, Rows st, int64_t n, int64_t rows, int64_t width, svgear_dtype dt, Workspace& w, Operand& out) {
+    out.pitch = even_pitch(width, dt);
+    void* dst = w.take<unsigned char>((size_t)rows * out.pitch * esize(dt));
+    out.p = dst;
+    job[jobs++] = PackJob{src, dst, st, out.pitch, rows * (out.pitch / chunk(dt)), (int)n, (int)rows, (int)width};
   }
-  bf16_t* p = w.take<bf16_t>((size_t)rows * out.pitch);
-  out.p = p;
-  return pack_rows<bf16_t>(src, st, n, rows, width, p, out.pitch, s);
-}
+  int launch(svgear_dtype dt, hipStream_t s) const {
+    if (jobs == 0) return SVGEAR_OK;
+    int64_t blocks = 1;
+    for (int k = 0; k < jobs; ++k)
+      if (ceil_div(job[k].pieces, kThreads) > blocks) blocks = ceil_div(job[k].pieces, kThreads);
+    const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20), (unsigned)jobs);
+    if (dt == SVGEAR_F32)
+      pack_rows_kernel<uint32_t><<<grid, kThreads, 0, s>>>(job[0], job[1]);
+    else
+      pack_rows_kernel<bf16_t><<<grid, kThreads, 0, s>>>(job[0], job[1]);
+    SVGEAR_LAUNCH_CHECK();
+    return SVGEAR_OK;
+  }
+};
 
 // What of svgear_linear's operands goes through the workspace. Few rows: x only, where its batches are not one run of rows.
 struct Copies {
@@ -376,14 +388,11 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
   const int64_t M = (int64_t)B * N;
   Operand X{x, run_pitch(xstride, B, N)}, W{w, w_stride};
   const Copies copies = operand_copies(x, xstride, w, w_stride, dt, B, N, d_in);
-  if (copies.x) {
-    const int rc = pack(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X, s);
-    if (rc != SVGEAR_OK) return rc;
-  }
-  if (copies.w) {
-    const int rc = pack(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W, s);
-    if (rc != SVGEAR_OK) return rc;
-  }
+  Packing packing;
+  if (copies.x) packing.add(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X);
+  if (copies.w) packing.add(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W);
+  const int rc = packing.launch(dt, s);
+  if (rc != SVGEAR_OK) return rc;
   LinearArgs a{};
   set_product(a, W, X, M, d_out, d_in, dt, kContractBoth, space);
   a.even = in_place(X.p, X.pitch, d_in, dt) && in_place(W.p, W.pitch, d_in, dt);
@@ -497,12 +506,14 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     }
   }
 
+  Operand W{w, w_stride}, X{x, dw ? run_pitch(xstride, B, N) : 0};
+  Packing packing;
+  if (dx && !in_place(w, w_stride, d_in, dt)) packing.add(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W);
+  if (dw && !rows_in_place(x, xstride, B, N, d_in, dt))
+    packing.add(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X);
+  const int packed = packing.launch(dt, s);
+  if (packed != SVGEAR_OK) return packed;
   if (dx) {
-    Operand W{w, w_stride};
-    if (!in_place(w, w_stride, d_in, dt)) {
-      const int rc = pack(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W, s);
-      if (rc != SVGEAR_OK) return rc;
-    }
     LinearArgs a{};
     set_product(a, W, dz, M, d_in, d_out, dt, kContractQ, space);
     a.n = (int)N;
@@ -513,11 +524,6 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     if (rc != SVGEAR_OK) return rc;
   }
   if (dw) {
-    Operand X{x, run_pitch(xstride, B, N)};
-    if (!rows_in_place(x, xstride, B, N, d_in, dt)) {
-      const int rc = pack(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X, s);
-      if (rc != SVGEAR_OK) return rc;
-    }
     LinearArgs a{};
     set_product(a, X, dz, d_out, d_in, M, dt, kContractNone, space);
     a.n = d_out;
