@@ -331,7 +331,7 @@ int svgear_unpermute(const void* op, const int32_t* perm, svgear_dtype dt, int B
  *   y        [B,N,d_out] dt out, ystride. y may be the residual itself (same pointer, same
  *            strides); no other overlap of outputs with inputs or each other is allowed (one at the same
  *            address is refused).
- * Sizes: B, N, d_in, d_out >= 1, B*N <= 2^30, d_in and d_out <= 2^21; strides >= 0, those of y
+ * Sizes: B, N, d_in, d_out >= 1, B*N <= 2^30, d_in and d_out <= 2^21; strides from 0 to 2^48, those of y
  * such that no two rows meet; any alignment that the type has. Rows of x and w that are not
  * 16-byte aligned, or whose length is no multiple of 16 bytes, and batches of x that are not one
  * run of evenly spaced rows are first copied into the workspace, which also holds partial products where
@@ -407,7 +407,7 @@ int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void
  *   weight[k]       dt, 16-byte aligned
  *   inv_freq        [P] fp64 (device)
  * src, dst, sstride, dstride, weight (may be NULL) and sections, grid are HOST arrays. n_tensors
- * is 1 or 2; H <= 128; B*N <= 2^30. No workspace.
+ * is 1 or 2; H <= 128; B*N <= 2^30; strides up to 2^48. No workspace.
  */
 #define SVGEAR_ROTARY_NORM_HEAD 1u
 #define SVGEAR_ROTARY_NORM_TOKEN 2u

@@ -42,6 +42,10 @@ struct Workspace {
   bool ok() const { return used <= size; }
 };
 
+// The longest stride, in elements, that an entry point with strides of its own takes: products of it with a size or an
+// element's bytes stay within 128 (64) bits.
+constexpr int64_t kMaxStride = (int64_t)1 << 48;
+
 static inline size_t esize(svgear_dtype dt) { return dt == SVGEAR_F32 ? 4 : 2; }
 
 // ---- device-side element access ------------------------------------------------------

@@ -195,7 +195,7 @@ bool in_place(const void* p, int64_t pitch, int64_t width, svgear_dtype dt) {
 int64_t run_pitch(const int64_t st[2], int B, int64_t N) {
   if (B == 1) return st[1];
   if (N == 1) return st[0];
-  return st[0] == N * st[1] ? st[1] : -1;
+  return st[0] == (__int128)N * st[1] ? st[1] : -1;
 }
 bool rows_in_place(const void* p, const int64_t st[2], int B, int64_t N, int64_t width, svgear_dtype dt) {
   const int64_t pitch = run_pitch(st, B, N);
@@ -245,7 +245,7 @@ bool sizes_ok(svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
          d_in > 0 && d_out > 0 && d_in <= kMaxWidth && d_out <= kMaxWidth;
 }
 bool input_ok(const void* p, const int64_t st[2], svgear_dtype dt) {
-  return p && st && st[0] >= 0 && st[1] >= 0 && reinterpret_cast<uintptr_t>(p) % esize(dt) == 0;
+  return p && st && st[0] >= 0 && st[1] >= 0 && st[0] <= kMaxStride && st[1] <= kMaxStride && reinterpret_cast<uintptr_t>(p) % esize(dt) == 0;
 }
 bool output_ok(const void* p, const int64_t st[2], svgear_dtype dt, int64_t B, int64_t N, int64_t width) {
   if (!input_ok(p, st, dt)) return false;
@@ -253,10 +253,10 @@ bool output_ok(const void* p, const int64_t st[2], svgear_dtype dt, int64_t B, i
   const int64_t inner = b_inner ? st[0] : st[1], n_inner = b_inner ? B : N, outer = b_inner ? st[1] : st[0],
                 n_outer = b_inner ? N : B;
   if (n_inner > 1 && inner < width) return false;
-  return n_outer == 1 || outer >= (n_inner > 1 ? (n_inner - 1) * inner : 0) + width;
+  return n_outer == 1 || outer >= (n_inner > 1 ? (__int128)(n_inner - 1) * inner : 0) + width;
 }
-bool wide_rows(const void* p, const int64_t st[2], svgear_dtype dt) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && st[0] % chunk(dt) == 0 && st[1] % chunk(dt) == 0;
+bool wide_rows(const void* p, const int64_t st[2], svgear_dtype dt, int64_t B, int64_t N) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (B == 1 || st[0] % chunk(dt) == 0) && (N == 1 || st[1] % chunk(dt) == 0);
 }
 
 int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
@@ -359,7 +359,9 @@ using namespace svgear;
 
 extern "C" size_t svgear_linear_workspace(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
                                           svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
-  if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(x, xstride, dt) || !w || w_stride < d_in) return 0;
+  if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(x, xstride, dt) || !w || w_stride < d_in ||
+      w_stride > kMaxStride)
+    return 0;
   const Copies copies = operand_copies(x, xstride, w, w_stride, dt, B, N, d_in);
   size_t bytes = 0;
   if (copies.x) bytes += packed_bytes((int64_t)B * N, d_in, dt);
@@ -373,7 +375,7 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
                              const int64_t rstride[2], void* pre, void* y, const int64_t ystride[2], void* ws,
                              size_t ws_bytes, void* stream) {
   if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(x, xstride, dt) || !w || reinterpret_cast<uintptr_t>(w) % esize(dt) ||
-      w_stride < d_in || !output_ok(y, ystride, dt, B, N, d_out) || (int)act < 0 || (int)act > (int)SVGEAR_ACT_GELU_TANH ||
+      w_stride < d_in || w_stride > kMaxStride || !output_ok(y, ystride, dt, B, N, d_out) || (int)act < 0 || (int)act > (int)SVGEAR_ACT_GELU_TANH ||
       (gate && !input_ok(gate, gstride, dt)) || (residual && !input_ok(residual, rstride, dt)) ||
       reinterpret_cast<uintptr_t>(bias) % esize(dt) || reinterpret_cast<uintptr_t>(pre) % esize(dt))
     return SVGEAR_ERR_INVALID;
@@ -406,8 +408,8 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
   if (gate) a.gst = Rows{gstride[0], gstride[1]};
   if (residual) a.rst = Rows{rstride[0], rstride[1]};
   a.act = act;
-  a.wide = d_out % 8 == 0 && wide_rows(y, ystride, dt) && (!gate || wide_rows(gate, gstride, dt)) &&
-           (!residual || wide_rows(residual, rstride, dt)) && reinterpret_cast<uintptr_t>(bias) % 16 == 0 &&
+  a.wide = d_out % 8 == 0 && wide_rows(y, ystride, dt, B, N) && (!gate || wide_rows(gate, gstride, dt, B, N)) &&
+           (!residual || wide_rows(residual, rstride, dt, B, N)) && reinterpret_cast<uintptr_t>(bias) % 16 == 0 &&
            reinterpret_cast<uintptr_t>(pre) % 16 == 0;
   return launch(a, dt, kContractBoth, s);
 }
@@ -416,7 +418,7 @@ extern "C" size_t svgear_linear_backward_workspace(const void* dy, const int64_t
                                                    const int64_t xstride[2], const void* w, int64_t w_stride,
                                                    svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
   if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(dy, dystride, dt) || (x && !input_ok(x, xstride, dt)) ||
-      (w && w_stride < d_in))
+      (w && (w_stride < d_in || w_stride > kMaxStride)))
     return 0;
   const int64_t M = (int64_t)B * N;
   size_t bytes = 256 + packed_bytes(M, d_out, dt);  // dz
@@ -440,7 +442,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
   const uintptr_t es = esize(dt);
   if (!sizes_ok(dt, B, N, d_in, d_out) || !input_ok(dy, dystride, dt) || (!dx && !dw && !dbias && !dgate) ||
       (dw && !x) || (x && !input_ok(x, xstride, dt)) || (dx && !w) ||
-      (w && (w_stride < d_in || reinterpret_cast<uintptr_t>(w) % es)) || (int)act < 0 ||
+      (w && (w_stride < d_in || w_stride > kMaxStride || reinterpret_cast<uintptr_t>(w) % es)) || (int)act < 0 ||
       (int)act > (int)SVGEAR_ACT_GELU_TANH || (gate && !input_ok(gate, gstride, dt)) || (dgate && !gate) ||
       ((act != SVGEAR_ACT_NONE || dgate) && !pre) || (dx && !output_ok(dx, dxstride, dt, B, N, d_in)) ||
       reinterpret_cast<uintptr_t>(pre) % es || reinterpret_cast<uintptr_t>(dw) % es ||
@@ -488,7 +490,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     if (dbias) g.sum_dz = space.take<float>(sums);
     if (dgate && !token_gate) g.sum_da = space.take<float>(sums);
     if (dgate && token_gate) g.dgate = dgate;
-    const bool wide = d_out % 8 == 0 && wide_rows(dy, dystride, dt) && (!gate || wide_rows(gate, gstride, dt)) &&
+    const bool wide = d_out % 8 == 0 && wide_rows(dy, dystride, dt, B, N) && (!gate || wide_rows(gate, gstride, dt, B, N)) &&
                       reinterpret_cast<uintptr_t>(g.pre) % 16 == 0 && reinterpret_cast<uintptr_t>(g.dgate) % 16 == 0;
     if (dt == SVGEAR_F32)
       launch_gradient<float>(g, (unsigned)(B * g.blocks_b), wide, s);
@@ -519,7 +521,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     a.n = (int)N;
     a.y = dx;
     a.yst = Rows{dxstride[0], dxstride[1]};
-    a.wide = d_in % 8 == 0 && wide_rows(dx, dxstride, dt);
+    a.wide = d_in % 8 == 0 && wide_rows(dx, dxstride, dt, B, N);
     const int rc = launch(a, dt, kContractQ, s);
     if (rc != SVGEAR_OK) return rc;
   }
@@ -530,7 +532,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     a.y = dw;
     a.yst = Rows{0, d_in};
     const int64_t st[2] = {0, d_in};
-    a.wide = d_in % 8 == 0 && wide_rows(dw, st, dt);
+    a.wide = d_in % 8 == 0 && wide_rows(dw, st, dt, 1, d_out);
     const int rc = launch(a, dt, kContractNone, s);
     if (rc != SVGEAR_OK) return rc;
   }

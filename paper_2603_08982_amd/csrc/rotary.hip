@@ -446,10 +446,12 @@ rotary_backward_kernel(RotaryArgs a) {
   }
 }
 
-bool aligned_strides(const int64_t st[3], size_t es, const void* p) {
+// (the stride of a dimension of one element does not matter)
+bool aligned_strides(const int64_t st[3], size_t es, const void* p, int64_t B, int64_t H, int64_t N) {
   if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+  const int64_t n[3] = {B, H, N};
   for (int i = 0; i < 3; ++i)
-    if (st[i] < 0 || (st[i] * (int64_t)es) % 16) return false;
+    if (n[i] > 1 && (st[i] < 0 || st[i] > kMaxStride || (st[i] * (int64_t)es) % 16)) return false;
   return true;
 }
 
@@ -462,11 +464,11 @@ bool rows_apart(const int64_t st[3], int64_t B, int64_t H, int64_t N, int64_t d)
         const int64_t t = s[i], u = n[i];
         s[i] = s[j], n[i] = n[j], s[j] = t, n[j] = u;
       }
-  int64_t span = d;
+  __int128 span = d;
   for (int i = 0; i < 3; ++i) {
     if (n[i] == 1) continue;
     if (s[i] < span) return false;
-    span += (n[i] - 1) * s[i];
+    span += (__int128)(n[i] - 1) * s[i];
   }
   return true;
 }
@@ -502,7 +504,7 @@ int fill_args(RotaryArgs& a, int n_tensors, svgear_dtype dt, const Shape& z, con
   if (a.pairs > z.d / 2 || (a.pairs > 0 && !inv_freq)) return SVGEAR_ERR_INVALID;
   const int64_t n_rot = z.N - z.n_tail;
   if (positions) {
-    if (positions_stride_b != 0 && positions_stride_b < 3 * n_rot && z.B > 1) return SVGEAR_ERR_INVALID;
+    if (z.B > 1 && positions_stride_b != 0 && (positions_stride_b < 3 * n_rot || positions_stride_b > kMaxStride)) return SVGEAR_ERR_INVALID;
     if (reinterpret_cast<uintptr_t>(positions) % 4) return SVGEAR_ERR_INVALID;
     a.plane = a.width = 1;
   } else {
@@ -609,8 +611,8 @@ extern "C" int svgear_rotary(int n_tensors, const void* const* src, const int64_
   if (rc != SVGEAR_OK) return rc;
   if (!src || !sstride || !dst || !dstride) return SVGEAR_ERR_INVALID;
   for (int k = 0; k < n_tensors; ++k) {
-    if (!src[k] || !dst[k] || !aligned_strides(sstride[k], esize(dt), src[k]) ||
-        !aligned_strides(dstride[k], esize(dt), dst[k]) || !rows_apart(dstride[k], B, H, N, d))
+    if (!src[k] || !dst[k] || !aligned_strides(sstride[k], esize(dt), src[k], B, H, N) ||
+        !aligned_strides(dstride[k], esize(dt), dst[k], B, H, N) || !rows_apart(dstride[k], B, H, N, d))
       return SVGEAR_ERR_INVALID;
     a.src[k] = src[k];
     a.dst[k] = dst[k];
@@ -646,8 +648,8 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
   if (!dy || !dystride || !dx || !dxstride || (norm && (!src || !sstride))) return SVGEAR_ERR_INVALID;
   bool any = false;
   for (int k = 0; k < n_tensors; ++k) {
-    if (!dy[k] || !dx[k] || !aligned_strides(dystride[k], esize(dt), dy[k]) ||
-        !aligned_strides(dxstride[k], esize(dt), dx[k]) || !rows_apart(dxstride[k], B, H, N, d))
+    if (!dy[k] || !dx[k] || !aligned_strides(dystride[k], esize(dt), dy[k], B, H, N) ||
+        !aligned_strides(dxstride[k], esize(dt), dx[k], B, H, N) || !rows_apart(dxstride[k], B, H, N, d))
       return SVGEAR_ERR_INVALID;
     a.weight[k] = weight ? weight[k] : nullptr;
     if (a.weight[k] && (!norm || reinterpret_cast<uintptr_t>(a.weight[k]) % 16)) return SVGEAR_ERR_INVALID;
@@ -660,7 +662,7 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
     a.dst[k] = dx[k];
     a.dst_st[k] = Strides{dxstride[k][0], dxstride[k][1], dxstride[k][2]};
     if (norm) {
-      if (!src[k] || !aligned_strides(sstride[k], esize(dt), src[k])) return SVGEAR_ERR_INVALID;
+      if (!src[k] || !aligned_strides(sstride[k], esize(dt), src[k], B, H, N)) return SVGEAR_ERR_INVALID;
       if (meets(dx, dxstride, dy, dystride, src, n_tensors, k)) return SVGEAR_ERR_INVALID;
       a.src[k] = src[k];
       a.sst[k] = Strides{sstride[k][0], sstride[k][1], sstride[k][2]};

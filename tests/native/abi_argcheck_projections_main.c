@@ -44,6 +44,13 @@ static void linear(void) {
   expect("linear: N past 32 bits", lin(fake, s, fake, 16, H, 1, (int64_t)1 << 40, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
   expect("linear: w_stride < d_in", lin(fake, s, fake, 15, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
   expect("linear: negative stride of x", lin(fake, neg, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+  {
+    const int64_t huge[2] = {INT64_MAX, INT64_MAX};
+    expect("linear: strides of x that overflow", lin(fake, huge, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+    expect("linear: strides of y that overflow", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, huge, big), -1);
+    expect("linear: w_stride that overflows", lin(fake, s, fake, INT64_MAX, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, s, big), -1);
+    expect("linear_workspace: strides that overflow", (long long)svgear_linear_workspace(fake, huge, fake, 16, H, 2, 100, 16, 16), 0);
+  }
   expect("linear: rows of y meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, meet, big), -1);
   expect("linear: batches of y meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, meet_b, big), -1);
   expect("linear: batches within tokens meet", lin(fake, s, fake, 16, H, 2, 100, 16, 16, 0, NULL, NULL, NULL, NULL, out, inner_meet, big), -1);
@@ -184,6 +191,8 @@ static void rotary(void) {
   REFUSED("weight not 16-byte aligned", r.weight[0] = (void*)0x40002);
   REFUSED("strides of no 16 bytes", r.st[0][2] = 65);
   REFUSED("negative stride", r.st[0][1] = -1920);
+  REFUSED("a stride that overflows", r.st[0][0] = INT64_MAX - 7);
+  REFUSED("an output's stride that overflows", r.dst[0][0] = INT64_MAX - 7);
   REFUSED("rows of the output meet", r.dst[0][2] = 56);
   REFUSED("heads of the output meet", r.dst[0][1] = 1856);
   REFUSED("two outputs at one address", (r.n = 2, r.out[1] = r.out[0]));

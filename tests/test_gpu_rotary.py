@@ -232,3 +232,14 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for g, r in got:
         assert all(torch.equal(u, v) for u, v in zip(g, r))
+
+
+def test_strides_of_single_elements_do_not_matter():
+    """[1,H,1,d] views whose batch and token strides are no whole chunks."""
+    x = rand(1, 5, 1, 64, seed=1).cuda()
+    odd = torch.empty(5 * 64 + 64, device="cuda").as_strided((1, 5, 1, 64), (7, 64, 3, 1))
+    odd.copy_(x)
+    f, sections = sv.rotary_frequencies((10, 11, 11)), (10, 11, 11)
+    kw = {"grid": (3, 4, 5), "first": 33, "norm": "token"}
+    ref, got = sv.rotary([x], f, sections, **kw)[0], sv.rotary([odd], f, sections, out=[odd], **kw)[0]
+    assert torch.equal(ref, got)
