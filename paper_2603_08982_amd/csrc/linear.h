@@ -21,7 +21,7 @@ struct LinearArgs {
   Operand P, Q;
   int64_t K;
   int R, C;
-  int tile;      // tile of the tile kernel: 64, 128, or (bf16) 256 rows and columns; 0: the kernel of few rows
+  int tile;      // tile of the tile kernel: 64, 128, or (bf16) 256 rows and columns, (fp32) 32 rows of 128; 0: the kernel of few rows
   bool even;     // for it: rows of the operands are as the tile kernel needs them
   int splits;    // K in so many parts, each into its own slice of `partial`
   float* partial;  // [splits][R][C] or null

@@ -272,6 +272,9 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
 // in tiles of 64 / 128 / 128 in 3 parts: 30 / 34 / 25; 2048 x 512 of 2048 in 64 / 128: 12 / 17; 5120 x 2000 of 5120 in 128 / 256:
 // 118 / 100; 2048 x 4000 of 6000: 106 / 114. fp32, 1000 x 1554 of 640 in 64 / 128: 27 / 45, 1536 x 2103 of 1024 70 / 69, 1541 x 2103 of 1003 with a full epilogue 100 / 114; 1000 x 700 of 3000
 // in 64, one part / 4: 56 / 46.
+// Up to 32 rows in fp32, whose matrix cores the idle rows of a tile of 64 would keep busy, have one of 32 x 128 (30,720 x 9 of 5,120:
+// 169 us by 64, 119; 5,120 x 32 of 5,120 39 and 28; for more rows it is no faster, nor is
+// it in bf16; the weights' gradient, whose rows are d_out, has none).
 // Few rows (forward only) go to the kernel that reads the weights straight into registers.
 struct Plan {
   int tile, splits;
@@ -279,18 +282,19 @@ struct Plan {
 Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
   if (form == kContractBoth && R <= few_rows(dt)) return Plan{0, 1};
   struct Kind {
-    int tile;
+    int tile, rows, cols;
     double alone, step, once, first;
   };
-  static const Kind bf16[] = {{64, 0.40, 0.19, 1.0, 0.0}, {128, 0.50, 0.475, 1.5, 0.0}, {256, 1.3, 1.3, 9.0, 0.0}};
-  static const Kind f32[] = {{64, 0.56, 0.53, 1.0, 0.0}, {128, 1.9, 1.85, 2.0, 10.0}};
+  static const Kind bf16[] = {{64, 64, 64, 0.40, 0.19, 1.0, 0.0}, {128, 128, 128, 0.50, 0.475, 1.5, 0.0}, {256, 256, 256, 1.3, 1.3, 9.0, 0.0}};
+  static const Kind f32[] = {{64, 64, 64, 0.56, 0.53, 1.0, 0.0}, {128, 128, 128, 1.9, 1.85, 2.0, 10.0}, {32, 32, 128, 0.6, 0.55, 1.0, 0.0}};
   const Kind* kinds = dt == SVGEAR_F32 ? f32 : bf16;
   const int64_t steps = ceil_div(K, dt == SVGEAR_F32 ? 32 : 64);
   Plan best{64, 1};
   double least = 1e300;
-  for (int i = 0; i < (dt == SVGEAR_F32 ? 2 : 3); ++i) {
+  for (int i = 0; i < 3; ++i) {
     const Kind& k = kinds[i];
-    const int64_t tiles = ceil_div(R, k.tile) * ceil_div(C, k.tile);
+    if (k.rows == 32 && (R > 32 || form == kContractNone)) continue;
+    const int64_t tiles = ceil_div(R, k.rows) * ceil_div(C, k.cols);
     for (int p = 1; p <= 16 && (p == 1 || (steps >= 4 * p && tiles < 1024)); ++p) {
       const double m = (double)ceil_div(tiles * p, 256), each = m * k.step;
       double us = (double)ceil_div(steps, p) * (each > k.alone ? each : k.alone) + m * k.once + k.first;

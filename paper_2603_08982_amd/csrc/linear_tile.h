@@ -59,6 +59,7 @@ struct Tile {
   static constexpr int BYTES = E * 128;
   static constexpr int COPIES = BYTES / 1024 / WAVES;        // wave-wide copies of 1 KB, each wave
   static_assert(BYTES % (1024 * WAVES) == 0, "copies must split evenly over the waves");
+  static_assert(!OVER_ROWS || ES == 2 || ROWB >= 256, "the chunk swizzle needs 16 chunks in a row");
 
   static __device__ __forceinline__ int swz(int row) {
     if (!OVER_ROWS) return (row >> 1) & 7;
@@ -437,12 +438,16 @@ int launch_tiles(const LinearArgs& a, hipStream_t s) {
 template <typename T, int FORM>
 int launch_form(const LinearArgs& a, hipStream_t s) {
   switch (a.tile) {
+    case 32:
+      if constexpr (sizeof(T) == 4 && FORM != kContractNone) return launch_tiles<T, FORM, 1, 1, 4, 1>(a, s);
+      break;
     case 64: return launch_tiles<T, FORM, 1, 1, 2, 2>(a, s);
     // 8 waves, not 4 of 64 x 64: twice the waves for prologue and epilogue (fp32, 5,120 x 4,096 of 256: 91 us against 111; bf16,
     // 5,120 x 5,120 of 16: 20 against 23; at large K the two are within 2 %, at 6,000 x 4,000 of 2,048 4 of 64 x 64 gain 4 %)
     case 128: return launch_tiles<T, FORM, 1, 2, 4, 2>(a, s);
     case 256:
       if constexpr (sizeof(T) == 2) return launch_tiles<T, FORM, 2, 4, 4, 2>(a, s);
+      break;
   }
   return SVGEAR_ERR_UNSUPPORTED;
 }

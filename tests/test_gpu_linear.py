@@ -80,6 +80,30 @@ def test_large_outputs(size):
         close(got[name], *ref[name], name)
 
 
+# products of up to 32 rows by so many columns that they take more than one tile of 64 x 64 on a compute unit: of the forward
+# pass, of dx, and of dw (24 outputs)
+FLAT = [(1, 9, 72, 17000), (1, 32, 200, 17003), (2, 15, 17000, 72), (1, 3, 17003, 24), (1, 33, 17000, 40), (1, 300, 17000, 24)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("size", FLAT, ids=str)
+def test_few_rows_of_many_columns(size, dtype):
+    i = FLAT.index(size)
+    x, w, b, g, r = inputs(dtype, *size, bias=True, gate=["batch", "token"][i % 2], residual=True, seed=400 + i)
+    y, pre = sv.linear(x, w, b, act="silu", gate=g, residual=r, want_pre=True)
+    Y, Z, by, bz = linear64(x, w, b, "silu", g, r)
+    close(pre, Z, bz, "pre")
+    close(y, Y, by, "y")
+    y, _ = sv.linear(x, w, b, gate=g, residual=r)
+    Y, _, by, _ = linear64(x, w, b, "none", g, r)
+    close(y, Y, by, "y without activation")
+    dy = rand(*pre.shape, seed=500 + i, dtype=dtype).cuda()
+    got = sv.linear_backward(dy, x, w, pre=pre, act="silu", gate=g, want=["dx", "dw", "dbias", "dgate"])
+    ref = linear_backward64(dy, x, w, pre, "silu", g, UNIT[dtype])
+    for name in got:
+        close(got[name], *ref[name], name)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 @pytest.mark.parametrize("size", SIZES, ids=str)
 def test_backward_of_every_size(size, dtype):
