@@ -46,6 +46,14 @@ struct Workspace {
 // element's bytes stay within 128 (64) bits.
 constexpr int64_t kMaxStride = (int64_t)1 << 48;
 
+// A launch takes fewer than 2^32 threads along x: of a grid that may be longer, workgroups from kGridX on lie along z. The last
+// layer has workgroups past the last one, which have nothing to do.
+constexpr unsigned kGridX = 1u << 21;
+static inline dim3 long_grid(int64_t groups, int64_t y) {
+  return dim3((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)y, (unsigned)((groups + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ unsigned long_grid_index() { return blockIdx.z * kGridX + blockIdx.x; }
+
 static inline size_t esize(svgear_dtype dt) { return dt == SVGEAR_F32 ? 4 : 2; }
 
 // ---- device-side element access ------------------------------------------------------

@@ -114,7 +114,7 @@ struct GradientArgs {
   Rows yst, gst;
   int64_t pitch;
   int C, n, act;
-  int blocks_b, rows_block;  // blocks of a batch entry, rows of a block
+  int blocks, blocks_b, rows_block;  // blocks, those of a batch entry, rows of a block
 };
 
 // A workgroup takes 256 columns of a run of rows of one batch entry, 8 a thread, its 8 half waves every eighth row.
@@ -126,7 +126,9 @@ linear_gradient_kernel(GradientArgs a) {
   __shared__ float s[2][WAYS][LANES * V + 4];
   const int x = threadIdx.x % LANES, way = threadIdx.x / LANES;
   const int c0 = blockIdx.y * LANES * V, c = c0 + x * V;
-  const int b = blockIdx.x / a.blocks_b, first = (blockIdx.x % a.blocks_b) * a.rows_block;
+  const int block = (int)long_grid_index();
+  if (block >= a.blocks) return;
+  const int b = block / a.blocks_b, first = block % a.blocks_b * a.rows_block;
   const int last = min(first + a.rows_block, a.n);
   const T* dy = static_cast<const T*>(a.dy) + (int64_t)b * a.yst.b + c;
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + c : nullptr;
@@ -170,17 +172,17 @@ linear_gradient_kernel(GradientArgs a) {
     float z = 0.f, v = 0.f;
 #pragma unroll
     for (int w = 0; w < WAYS; ++w) z += s[0][w][i], v += s[1][w][i];
-    if (a.sum_dz) a.sum_dz[(int64_t)blockIdx.x * a.C + c0 + i] = z;
-    if (a.sum_da) a.sum_da[(int64_t)blockIdx.x * a.C + c0 + i] = v;
+    if (a.sum_dz) a.sum_dz[(int64_t)block * a.C + c0 + i] = z;
+    if (a.sum_da) a.sum_da[(int64_t)block * a.C + c0 + i] = v;
   }
 }
 
 template <typename T>
-void launch_gradient(const GradientArgs& g, unsigned blocks, bool wide, hipStream_t s) {
+void launch_gradient(const GradientArgs& g, bool wide, hipStream_t s) {
   if (wide)
-    linear_gradient_kernel<T, 8><<<dim3(blocks, (unsigned)ceil_div(g.C, 256)), kThreads, 0, s>>>(g);
+    linear_gradient_kernel<T, 8><<<long_grid(g.blocks, ceil_div(g.C, 256)), kThreads, 0, s>>>(g);
   else
-    linear_gradient_kernel<T, 1><<<dim3(blocks, (unsigned)ceil_div(g.pitch, 64)), kThreads, 0, s>>>(g);
+    linear_gradient_kernel<T, 1><<<long_grid(g.blocks, ceil_div(g.pitch, 64)), kThreads, 0, s>>>(g);
 }
 
 // ---- host side
@@ -331,6 +333,8 @@ int gradient_rows(int B, int64_t N, int d_out) {
   while (rows > 8 && (int64_t)B * ceil_div(N, rows) * ceil_div(d_out, 256) < 1024) rows /= 2;
   return rows;
 }
+// Batch entries of one token each count as tokens of one entry, dgate included: its row is their own.
+bool one_token_each(int B, int64_t N) { return N == 1 && B > 1; }
 int gradient_blocks(int B, int64_t N, int d_out) { return (int)ceil_div(N, gradient_rows(B, N, d_out)); }
 
 }  // namespace
@@ -426,7 +430,9 @@ extern "C" size_t svgear_linear_backward_workspace(const void* dy, const int64_t
     return 0;
   const int64_t M = (int64_t)B * N;
   size_t bytes = 256 + packed_bytes(M, d_out, dt);  // dz
-  bytes += 2 * align_up((size_t)B * gradient_blocks(B, N, d_out) * d_out * sizeof(float), 256);
+  const bool fold = one_token_each(B, N);
+  const int gb = fold ? 1 : B;
+  bytes += 2 * align_up((size_t)gb * gradient_blocks(gb, fold ? B : N, d_out) * d_out * sizeof(float), 256);
   if (x) {
     if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes(M, d_in, dt);
     bytes += parts_bytes(d_out, d_in, M, dt, kContractNone);
@@ -471,7 +477,8 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
   Operand dz{dy, run_pitch(dystride, B, N)};
   const bool same = act == SVGEAR_ACT_NONE && !gate;
   const bool make = (dx || dw) && !(same && rows_in_place(dy, dystride, B, N, d_out, dt));
-  const bool token_gate = gate && gstride[1] != 0;
+  const bool fold = one_token_each(B, N), token_gate = gate && (gstride[1] != 0 || fold);
+  const int gb = fold ? 1 : B, gn = fold ? B : (int)N;
   if (make || dbias || dgate) {
     GradientArgs g{};
     g.dy = dy;
@@ -483,31 +490,32 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
       dz.p = g.dz;
     }
     g.pitch = even_pitch(d_out, dt);
-    g.yst = Rows{dystride[0], dystride[1]};
-    if (gate) g.gst = Rows{gstride[0], gstride[1]};
+    g.yst = fold ? Rows{0, dystride[0]} : Rows{dystride[0], dystride[1]};
+    if (gate) g.gst = fold ? Rows{0, gstride[0]} : Rows{gstride[0], gstride[1]};
     g.C = d_out;
-    g.n = (int)N;
+    g.n = gn;
     g.act = act;
-    g.rows_block = gradient_rows(B, N, d_out);
-    g.blocks_b = gradient_blocks(B, N, d_out);
-    const size_t sums = (size_t)B * g.blocks_b * d_out;
+    g.rows_block = gradient_rows(gb, gn, d_out);
+    g.blocks_b = gradient_blocks(gb, gn, d_out);
+    g.blocks = gb * g.blocks_b;
+    const size_t sums = (size_t)g.blocks * d_out;
     if (dbias) g.sum_dz = space.take<float>(sums);
     if (dgate && !token_gate) g.sum_da = space.take<float>(sums);
     if (dgate && token_gate) g.dgate = dgate;
     const bool wide = d_out % 8 == 0 && wide_rows(dy, dystride, dt, B, N) && (!gate || wide_rows(gate, gstride, dt, B, N)) &&
                       reinterpret_cast<uintptr_t>(g.pre) % 16 == 0 && reinterpret_cast<uintptr_t>(g.dgate) % 16 == 0;
     if (dt == SVGEAR_F32)
-      launch_gradient<float>(g, (unsigned)(B * g.blocks_b), wide, s);
+      launch_gradient<float>(g, wide, s);
     else
-      launch_gradient<bf16_t>(g, (unsigned)(B * g.blocks_b), wide, s);
+      launch_gradient<bf16_t>(g, wide, s);
     SVGEAR_LAUNCH_CHECK();
-    const bool together = dbias && g.sum_da && B == 1;
+    const bool together = dbias && g.sum_da && gb == 1;
     if (dbias) {
-      const int rc = sum_rows(g.sum_dz, dbias, together ? g.sum_da : nullptr, together ? dgate : nullptr, B * g.blocks_b, d_out, 1, dt, s);
+      const int rc = sum_rows(g.sum_dz, dbias, together ? g.sum_da : nullptr, together ? dgate : nullptr, g.blocks, d_out, 1, dt, s);
       if (rc != SVGEAR_OK) return rc;
     }
     if (g.sum_da && !together) {
-      const int rc = sum_rows(g.sum_da, dgate, nullptr, nullptr, g.blocks_b, d_out, B, dt, s);
+      const int rc = sum_rows(g.sum_da, dgate, nullptr, nullptr, g.blocks_b, d_out, gb, dt, s);
       if (rc != SVGEAR_OK) return rc;
     }
   }

@@ -179,7 +179,8 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
   // Workgroups go to the 8 XCDs in turn; each gets 8 x 4 tiles of those, so that its L2 serves 32 tiles with 12
   // panels. What is left of 256 goes to them in runs. (Each XCD with a run of tiles of its own from the start: 68 panels
   // at a time, 37,800 x 15,360 of 5,120 4.9 instead of 4.6 ms.)
-  const int tiles = tiles_c * tiles_r, bid = blockIdx.x, xcd = bid & 7, whole = tiles & ~255;
+  const int tiles = tiles_c * tiles_r, bid = (int)long_grid_index(), xcd = bid & 7, whole = tiles & ~255;
+  if (bid >= tiles) return;
   int t;
   if (bid < whole) {
     const int i = (bid & 255) >> 3;
@@ -426,11 +427,11 @@ template <typename T, int FORM, int TC, int TR, int WC, int WR>
 int launch_tiles(const LinearArgs& a, hipStream_t s) {
   constexpr int BC = 32 * TC * WC, BR = 32 * TR * WR, lds = (3 * BC + 2 * BR) * 128;
   const int tc = (int)ceil_div(a.C, BC), tr = (int)ceil_div(a.R, BR);
-  if ((int64_t)tc * tr > INT32_MAX) return SVGEAR_ERR_UNSUPPORTED;
+  if ((int64_t)tc * tr > 1 << 30) return SVGEAR_ERR_UNSUPPORTED;
   auto kern = linear_tile_kernel<T, FORM, TC, TR, WC, WR>;
   if (lds > 65536)
     SVGEAR_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-  kern<<<dim3((unsigned)(tc * tr), (unsigned)a.splits), 64 * WC * WR, lds, s>>>(a, tc, tr);
+  kern<<<long_grid(tc * tr, a.splits), 64 * WC * WR, lds, s>>>(a, tc, tr);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }

@@ -172,7 +172,7 @@ rotary_kernel(RotaryArgs a) {
   __shared__ float slots[kRotWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wpt = a.waves_per_token, per_group = (blockDim.x >> 6) / wpt;
-  const int token = blockIdx.x * per_group + wave / wpt;
+  const int token = (int)long_grid_index() * per_group + wave / wpt;
   const bool on = token < a.tokens;
   const int k = blockIdx.y;
   const int b = on ? token / a.N : 0, n = on ? token - b * a.N : 0;
@@ -562,8 +562,8 @@ int launch_mode(RotaryArgs& a, int n_tensors, bool backward, hipStream_t s) {
     }
   }
   const int threads = plan_waves(a, V, kMaxIts<T, V>, 4);
-  const unsigned groups = (unsigned)ceil_div(a.tokens, threads / 64 / a.waves_per_token);
-  rotary_kernel<T, V, NORM, HALVES><<<dim3(groups, (unsigned)n_tensors), threads, 0, s>>>(a);
+  const int64_t groups = ceil_div(a.tokens, threads / 64 / a.waves_per_token);
+  rotary_kernel<T, V, NORM, HALVES><<<long_grid(groups, n_tensors), threads, 0, s>>>(a);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }

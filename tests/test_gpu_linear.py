@@ -355,3 +355,51 @@ def test_captured_large_tiles():
         dx2 = sv.linear_backward(y2, x2, w, want=["dx"])["dx"]
         torch.cuda.synchronize()
         assert torch.equal(y, y2) and torch.equal(dx, dx2)
+
+
+# batches of one token each: their rows count as one entry's
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("gate", ["none", "batch", "token", "shared"])
+@pytest.mark.parametrize("size", [(1, 1, 40, 24), (2, 1, 40, 24), (70, 1, 33, 67), (1300, 1, 64, 264)], ids=str)
+def test_batches_of_one_token(size, gate, dtype):
+    B, N, k, o = size
+    x, w, b, g, _ = inputs(dtype, *size, bias=True, gate=gate if gate != "shared" else "none", residual=False, seed=7)
+    if gate == "shared":
+        g = rand(o, seed=8, dtype=dtype).cuda().expand(B, o)
+    _, pre = sv.linear(x, w, b, act="gelu", gate=g, want_pre=True)
+    big = rand(B, 3, o + 5, seed=9, dtype=dtype).cuda()
+    dy = big[:, 1:2, 2:2 + o]
+    want = ["dx", "dw", "dbias"] + (["dgate"] if g is not None else [])
+    got = sv.linear_backward(dy, x, w, pre=pre, act="gelu", gate=g, want=want)
+    ref = linear_backward64(dy, x, w, pre, "gelu", g, UNIT[dtype])
+    for name in want:
+        close(got[name], ref[name][0], ref[name][1], name)
+
+
+def test_batches_past_the_longest_launch():
+    """2^24 batch entries are as many workgroups of the gradient's kernel, 2^32 threads."""
+    B = (1 << 24) + 5
+    for N in (1, 2):
+        g = torch.Generator(device="cuda").manual_seed(N)
+        dy = torch.randn(B, N, 8, device="cuda", generator=g).bfloat16()
+        pre = torch.randn(B, N, 8, device="cuda", generator=g).bfloat16()
+        gate = torch.randn(B, 8, device="cuda", generator=g).bfloat16()
+        got = sv.linear_backward(dy, None, None, pre=pre, act="silu", gate=gate, want=["dgate"])["dgate"]
+        for at in (0, B // 2, B - 300):
+            part = slice(at, at + 300)
+            ref = linear_backward64(dy[part], None, None, pre[part], "silu", gate[part], UNIT[torch.bfloat16])["dgate"]
+            close(got[part], *ref, f"{N} {at}")
+
+
+def test_the_most_rows():
+    """2^30 rows, in more tiles than one launch may hold threads for along one axis. d_in = 1: the products are exact in fp32 and
+    rounded once, as torch's are."""
+    rows = 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(1 << 20, 1, device="cuda", generator=g).bfloat16().repeat(rows >> 20, 1)
+    w = rand(1, 1, seed=4, dtype=torch.bfloat16).cuda()
+    x[-5:] = 3.0
+    y, _ = sv.linear(x, w)
+    for at in range(0, rows, 1 << 27):
+        part = slice(at, at + (1 << 27))
+        assert torch.equal(y[part], x[part] * w)

@@ -243,3 +243,22 @@ def test_strides_of_single_elements_do_not_matter():
     kw = {"grid": (3, 4, 5), "first": 33, "norm": "token"}
     ref, got = sv.rotary([x], f, sections, **kw)[0], sv.rotary([odd], f, sections, out=[odd], **kw)[0]
     assert torch.equal(ref, got)
+
+
+@pytest.mark.parametrize("norm", [None, "head", "token"])
+def test_more_tokens_than_a_launch_has_threads_for(norm):
+    """2^26 tokens are 2^32 threads. Shares of them, anywhere, come to what a call of their own gives."""
+    n, d, sections = (1 << 26) + 9, 64, (10, 11, 11)
+    x = rand(1, 1, 1 << 14, d, seed=1, dtype=torch.bfloat16).cuda().repeat(1, 1, (n >> 14) + 1, 1)[:, :, :n]
+    x[:, :, -9:] = 2.0
+    f, grid = sv.rotary_frequencies(sections), (n, 1, 1)
+    weights = [rand(64, seed=2, dtype=torch.bfloat16).cuda()] if norm else None
+    y, = sv.rotary([x], f, sections, grid=grid, norm=norm, weights=weights)
+    dx, _ = sv.rotary_backward([x], [x] if norm else None, f, sections, grid=grid, norm=norm, weights=weights, want_dweight=False)
+    for at in (0, n // 2 + 1, (1 << 26) - 50, n - 100):
+        part = x[:, :, at:at + 100]
+        want, = sv.rotary([part], f, sections, grid=grid, first=at, norm=norm, weights=weights)
+        assert torch.equal(y[:, :, at:at + 100], want), at
+        want, _ = sv.rotary_backward([part], [part] if norm else None, f, sections, grid=grid, first=at, norm=norm, weights=weights,
+                                     want_dweight=False)
+        assert torch.equal(dx[0][:, :, at:at + 100], want[0]), at
