@@ -27,11 +27,15 @@ pack_rows_kernel(PackJob a, PackJob b) {
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.pieces; i += (int64_t)gridDim.x * kThreads) {
     const int r = (int)(i / across), col = (int)(i - r * across) * CH, e = p.n >= p.rows ? 0 : r / p.n;
     const T* s = static_cast<const T*>(p.src) + (int64_t)e * p.st.b + (int64_t)(r - e * p.n) * p.st.n + col;
-    T v[CH];
-#pragma unroll
-    for (int k = 0; k < CH; ++k) v[k] = col + k < p.width ? s[k] : T(0);
     uint4 u;
-    __builtin_memcpy(&u, v, 16);
+    if (col + CH <= p.width) {
+      u = load16(s);
+    } else {
+      T v[CH];
+#pragma unroll
+      for (int k = 0; k < CH; ++k) v[k] = col + k < p.width ? s[k] : T(0);
+      __builtin_memcpy(&u, v, 16);
+    }
     *reinterpret_cast<uint4*>(static_cast<T*>(p.dst) + (int64_t)r * p.pitch + col) = u;
   }
 }
@@ -68,10 +72,11 @@ linear_merge_kernel(LinearArgs a, int runs) {
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int r = (int)(i / runs), c = (int)(i % runs) * 8;
   if (r >= a.R) return;
+  const bool whole8 = c + 8 <= a.C;
   float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int p = 0; p < a.splits; ++p) {
     const float* o = a.partial + ((int64_t)p * a.R + r) * a.C + c;
-    if (a.C % 8 == 0) {
+    if (whole8) {
       float w[8];
       load8(o, w);
 #pragma unroll
@@ -82,7 +87,7 @@ linear_merge_kernel(LinearArgs a, int runs) {
         if (c + k < a.C) v[k] += o[k];
     }
   }
-  if (a.wide) {
+  if (whole8) {
     float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (a.bias) load8(static_cast<const T*>(a.bias) + c, bias);
     finish8<T>(a, r, c, v, bias);
@@ -94,14 +99,26 @@ linear_merge_kernel(LinearArgs a, int runs) {
 }
 
 // ---- dz, the partial sums of dbias, and dgate
+// eight elements, those of them that exist, others 0
 template <typename T>
-__device__ __forceinline__ void load_values(const T* p, float (&v)[8]) { load8(p, v); }
+__device__ __forceinline__ void load_values(const T* p, int left, float (&v)[8]) {
+  if (left >= 8) {
+    load8(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? load_as_f32(p + i) : 0.f;
+  }
+}
 template <typename T>
-__device__ __forceinline__ void load_values(const T* p, float (&v)[1]) { v[0] = load_as_f32(p); }
-template <typename T>
-__device__ __forceinline__ void store_values(T* p, const float (&v)[8]) { store8(p, v); }
-template <typename T>
-__device__ __forceinline__ void store_values(T* p, const float (&v)[1]) { store1(p, v[0]); }
+__device__ __forceinline__ void store_values(T* p, int left, const float (&v)[8]) {
+  if (left >= 8) {
+    store8(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) store1(p + i, v[i]);
+  }
+}
 
 struct GradientArgs {
   const void* dy;
@@ -117,15 +134,15 @@ struct GradientArgs {
   int blocks, blocks_b, rows_block;  // blocks, those of a batch entry, rows of a block
 };
 
-// A workgroup takes 256 columns of a run of rows of one batch entry, 8 a thread, its 8 half waves every eighth row.
-// Where rows are not 16-byte aligned, 64 columns, one a lane, and its 4 waves every fourth row.
-template <typename T, int V>
+// A workgroup takes 256 columns of a run of rows of one batch entry, 8 a thread, its 8 half waves every eighth row. WHOLE: C is a
+// multiple of 8.
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kThreads)
 linear_gradient_kernel(GradientArgs a) {
-  constexpr int LANES = V == 8 ? 32 : 64, WAYS = kThreads / LANES;
+  constexpr int V = 8, LANES = 32, WAYS = kThreads / LANES;
   __shared__ float s[2][WAYS][LANES * V + 4];
   const int x = threadIdx.x % LANES, way = threadIdx.x / LANES;
-  const int c0 = blockIdx.y * LANES * V, c = c0 + x * V;
+  const int c0 = blockIdx.y * LANES * V, c = c0 + x * V, left = WHOLE ? 8 : a.C - c;
   const int block = (int)long_grid_index();
   if (block >= a.blocks) return;
   const int b = block / a.blocks_b, first = block % a.blocks_b * a.rows_block;
@@ -141,12 +158,12 @@ linear_gradient_kernel(GradientArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) g[i] = 1.f;
     const bool one_gate = gate && a.gst.n == 0;
-    if (one_gate) load_values(gate, g);
+    if (one_gate) load_values(gate, left, g);
     for (int t = first + way; t < last; t += WAYS) {
       float d[V], z[V], act[V];
-      load_values(dy + (int64_t)t * a.yst.n, d);
-      if (a.pre) load_values(static_cast<const T*>(a.pre) + (r0 + t) * a.C + c, z);
-      if (gate && !one_gate) load_values(gate + (int64_t)t * a.gst.n, g);
+      load_values(dy + (int64_t)t * a.yst.n, left, d);
+      if (a.pre) load_values(static_cast<const T*>(a.pre) + (r0 + t) * a.C + c, left, z);
+      if (gate && !one_gate) load_values(gate + (int64_t)t * a.gst.n, left, g);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float y = d[i];
@@ -157,11 +174,10 @@ linear_gradient_kernel(GradientArgs a) {
         sz[i] += d[i];
         sa[i] += act[i];
       }
-      if (a.dz) store_values(static_cast<T*>(a.dz) + (r0 + t) * a.pitch + c, d);
-      if (a.dgate) store_values(static_cast<T*>(a.dgate) + (r0 + t) * a.C + c, act);
+      // (dz's rows are whole 16-byte pieces, zeros behind the values)
+      if (a.dz) store_values(static_cast<T*>(a.dz) + (r0 + t) * a.pitch + c, WHOLE ? V : (int)min(a.pitch - c, (int64_t)V), d);
+      if (a.dgate) store_values(static_cast<T*>(a.dgate) + (r0 + t) * a.C + c, left, act);
     }
-  } else if (V == 1 && a.dz && c < a.pitch) {
-    for (int t = first + way; t < last; t += WAYS) store1(static_cast<T*>(a.dz) + (r0 + t) * a.pitch + c, 0.f);
   }
   if (!a.sum_dz && !a.sum_da) return;
 #pragma unroll
@@ -175,14 +191,6 @@ linear_gradient_kernel(GradientArgs a) {
     if (a.sum_dz) a.sum_dz[(int64_t)block * a.C + c0 + i] = z;
     if (a.sum_da) a.sum_da[(int64_t)block * a.C + c0 + i] = v;
   }
-}
-
-template <typename T>
-void launch_gradient(const GradientArgs& g, bool wide, hipStream_t s) {
-  if (wide)
-    linear_gradient_kernel<T, 8><<<long_grid(g.blocks, ceil_div(g.C, 256)), kThreads, 0, s>>>(g);
-  else
-    linear_gradient_kernel<T, 1><<<long_grid(g.blocks, ceil_div(g.pitch, 64)), kThreads, 0, s>>>(g);
 }
 
 // ---- host side
@@ -256,9 +264,6 @@ bool output_ok(const void* p, const int64_t st[2], svgear_dtype dt, int64_t B, i
                 n_outer = b_inner ? N : B;
   if (n_inner > 1 && inner < width) return false;
   return n_outer == 1 || outer >= (n_inner > 1 ? (__int128)(n_inner - 1) * inner : 0) + width;
-}
-bool wide_rows(const void* p, const int64_t st[2], svgear_dtype dt, int64_t B, int64_t N) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (B == 1 || st[0] % chunk(dt) == 0) && (N == 1 || st[1] % chunk(dt) == 0);
 }
 
 int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
@@ -405,7 +410,6 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
   if (rc != SVGEAR_OK) return rc;
   LinearArgs a{};
   set_product(a, W, X, M, d_out, d_in, dt, kContractBoth, space);
-  a.even = in_place(X.p, X.pitch, d_in, dt) && in_place(W.p, W.pitch, d_in, dt);
   a.n = (int)N;
   a.bias = bias;
   a.gate = gate;
@@ -416,9 +420,6 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
   if (gate) a.gst = Rows{gstride[0], gstride[1]};
   if (residual) a.rst = Rows{rstride[0], rstride[1]};
   a.act = act;
-  a.wide = d_out % 8 == 0 && wide_rows(y, ystride, dt, B, N) && (!gate || wide_rows(gate, gstride, dt, B, N)) &&
-           (!residual || wide_rows(residual, rstride, dt, B, N)) && reinterpret_cast<uintptr_t>(bias) % 16 == 0 &&
-           reinterpret_cast<uintptr_t>(pre) % 16 == 0;
   return launch(a, dt, kContractBoth, s);
 }
 
@@ -502,12 +503,12 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     if (dbias) g.sum_dz = space.take<float>(sums);
     if (dgate && !token_gate) g.sum_da = space.take<float>(sums);
     if (dgate && token_gate) g.dgate = dgate;
-    const bool wide = d_out % 8 == 0 && wide_rows(dy, dystride, dt, B, N) && (!gate || wide_rows(gate, gstride, dt, B, N)) &&
-                      reinterpret_cast<uintptr_t>(g.pre) % 16 == 0 && reinterpret_cast<uintptr_t>(g.dgate) % 16 == 0;
+    const dim3 grid = long_grid(g.blocks, ceil_div(d_out, 256));
+    const bool whole = d_out % 8 == 0;
     if (dt == SVGEAR_F32)
-      launch_gradient<float>(g, wide, s);
+      whole ? linear_gradient_kernel<float, true><<<grid, kThreads, 0, s>>>(g) : linear_gradient_kernel<float, false><<<grid, kThreads, 0, s>>>(g);
     else
-      launch_gradient<bf16_t>(g, wide, s);
+      whole ? linear_gradient_kernel<bf16_t, true><<<grid, kThreads, 0, s>>>(g) : linear_gradient_kernel<bf16_t, false><<<grid, kThreads, 0, s>>>(g);
     SVGEAR_LAUNCH_CHECK();
     const bool together = dbias && g.sum_da && gb == 1;
     if (dbias) {
@@ -533,7 +534,6 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     a.n = (int)N;
     a.y = dx;
     a.yst = Rows{dxstride[0], dxstride[1]};
-    a.wide = d_in % 8 == 0 && wide_rows(dx, dxstride, dt, B, N);
     const int rc = launch(a, dt, kContractQ, s);
     if (rc != SVGEAR_OK) return rc;
   }
@@ -543,8 +543,6 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
     a.n = d_out;
     a.y = dw;
     a.yst = Rows{0, d_in};
-    const int64_t st[2] = {0, d_in};
-    a.wide = d_in % 8 == 0 && wide_rows(dw, st, dt, 1, d_out);
     const int rc = launch(a, dt, kContractNone, s);
     if (rc != SVGEAR_OK) return rc;
   }

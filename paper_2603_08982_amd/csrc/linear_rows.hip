@@ -13,13 +13,14 @@ namespace {
 
 constexpr int kMaxWaves = 8;
 
-// 16 bytes of a row: elements k.. of it, those < K, others 0; EVEN: all or none of them.
-template <typename T, bool EVEN>
+// 16 bytes of a row: elements k.. of it, those < K, others 0; WHOLE: all or none of them.
+template <typename T, bool WHOLE>
 __device__ __forceinline__ uint4 load_piece(const T* row, int64_t k, int64_t K) {
-  if constexpr (EVEN) {
-    return k < K ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(0, 0, 0, 0);
+  constexpr int CH = 16 / sizeof(T);
+  if constexpr (WHOLE) {
+    return k < K ? load16(row + k) : make_uint4(0, 0, 0, 0);
   } else {
-    constexpr int CH = 16 / sizeof(T);
+    if (k + CH <= K) return load16(row + k);
     T e[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) e[i] = k + i < K ? row[k + i] : T(0);
@@ -47,8 +48,8 @@ __device__ __forceinline__ float multiply_piece(uint4 x, uint4 w, float acc) {
   return acc;
 }
 
-// NR rows or fewer, CW columns a workgroup. EVEN: rows of both operands 16-byte aligned, K a whole number of pieces.
-template <typename T, int NR, int CW, bool EVEN>
+// NR rows or fewer, CW columns a workgroup. WHOLE: K is a whole number of pieces.
+template <typename T, int NR, int CW, bool WHOLE>
 __global__ void __launch_bounds__(64 * kMaxWaves)
 linear_rows_kernel(LinearArgs a) {
   constexpr int CH = 16 / sizeof(T), STEP = 64 * CH, U = 8 / CW;  // eight pieces of weights in flight
@@ -72,12 +73,12 @@ linear_rows_kernel(LinearArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int c = 0; c < CW; ++c) w[u][c] = load_piece<T, EVEN>(p[c], k + u * STEP, a.K);
+      for (int c = 0; c < CW; ++c) w[u][c] = load_piece<T, WHOLE>(p[c], k + u * STEP, a.K);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       uint4 x[NR];
 #pragma unroll
-      for (int r = 0; r < NR; ++r) x[r] = load_piece<T, EVEN>(q[r], k + u * STEP, a.K);
+      for (int r = 0; r < NR; ++r) x[r] = load_piece<T, WHOLE>(q[r], k + u * STEP, a.K);
 #pragma unroll
       for (int c = 0; c < CW; ++c)
 #pragma unroll
@@ -109,7 +110,7 @@ void launch_kernel(const LinearArgs& a, hipStream_t s) {
   const int64_t steps = ceil_div(a.K, (int64_t)(64 * 16 / sizeof(T)) * (8 / CW));
   int waves = grid >= 1024 ? 2 : kMaxWaves;
   while (waves > 1 && waves > steps) waves /= 2;
-  if (a.even)
+  if (a.K % (16 / sizeof(T)) == 0)
     linear_rows_kernel<T, NR, CW, true><<<grid, 64 * waves, 0, s>>>(a);
   else
     linear_rows_kernel<T, NR, CW, false><<<grid, 64 * waves, 0, s>>>(a);

@@ -161,9 +161,10 @@ __device__ __forceinline__ void multiply(const Frag& p, const Frag& q, f32x16& a
   }
 }
 
-// WC x WR waves, each TC x TR blocks of 32 x 32.
+// WC x WR waves, each TC x TR blocks of 32 x 32. Registers for as many workgroups on a CU as the LDS holds: one of 256 x 256, two
+// or more of the others.
 template <typename T, int FORM, int TC, int TR, int WC, int WR>
-__global__ void __launch_bounds__(64 * WC * WR, WC * WR / 4)
+__global__ void __launch_bounds__(64 * WC * WR, (TC * TR > 2 ? WC * WR / 4 : WC * WR / 2))
 linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
   constexpr int WAVES = WC * WR, BC = 32 * TC * WC, BR = 32 * TR * WR;
   constexpr bool P_ROWS = FORM != kContractBoth, Q_ROWS = FORM == kContractNone;
@@ -323,103 +324,77 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
   const int rw = r0 + wr * TR * 32;  // the wave's first row
-  if (a.wide || a.partial) {
-    constexpr int LANES = COLS / 8, ROWS = 64 / LANES, PASSES = 32 / ROWS;  // LANES share a row, eight columns each
-    const int sub = lane / LANES, at = 2 * (lane % LANES), c = c0 + wc * COLS + (lane % LANES) * 8;
-    auto staged = [&](int q, float (&v)[8]) __attribute__((always_inline)) {
-      const int row = q * ROWS + sub, x = row & (CHUNKS - 1);
-      const float4 lo = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + ((at ^ x) << 4));
-      const float4 hi = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + (((at + 1) ^ x) << 4));
-      v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-    };
-    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.bias && !a.partial && c < a.C) load8(static_cast<const T*>(a.bias) + c, bias);
-    const bool plain = a.act == SVGEAR_ACT_NONE && !a.pre && !a.partial;
+  constexpr int LANES = COLS / 8, ROWS = 64 / LANES, PASSES = 32 / ROWS;  // LANES share a row, eight columns each
+  const int sub = lane / LANES, at = 2 * (lane % LANES), c = c0 + wc * COLS + (lane % LANES) * 8;
+  auto staged = [&](int q, float (&v)[8]) __attribute__((always_inline)) {
+    const int row = q * ROWS + sub, x = row & (CHUNKS - 1);
+    const float4 lo = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + ((at ^ x) << 4));
+    const float4 hi = *reinterpret_cast<const float4*>(own + row * (COLS * 4) + (((at + 1) ^ x) << 4));
+    v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+  };
+  const bool whole8 = c + 8 <= a.C;
+  // columns behind the last whole eight: eight lanes a row
+  const int first_tail = a.C % 8 && !a.partial ? (a.C & ~7) - c0 - wc * COLS : -1;
+  float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (a.bias && !a.partial && whole8) load8(static_cast<const T*>(a.bias) + c, bias);
+  const bool plain = sizeof(T) == 2 && a.act == SVGEAR_ACT_NONE && !a.pre && !a.partial;
 #pragma unroll
-    for (int j = 0; j < TR; ++j) {
-      if (plain) {
-        // no activation: gate and residual of all 32 rows are on their way together (18,900 x 5,120 of 5,120 with both: 885 us
-        // a pass at a time, 776 together)
-        Eight<T> gate[PASSES], res[PASSES];
-        int64_t to[PASSES];
+  for (int j = 0; j < TR; ++j) {
+    if (plain) {
+      // bf16 (fp32 has no registers for it), no activation: gate and residual of all 32 rows are on their way together (18,900 x 5,120 of 5,120 with both: 885 us
+      // a pass at a time, 776 together)
+      Eight<T> gate[PASSES], res[PASSES];
+      int64_t to[PASSES];
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q) {
-          const int r = min(rw + j * 32 + q * ROWS + sub, a.R - 1), b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
-          to[q] = (int64_t)b * a.yst.b + (int64_t)t * a.yst.n;
-          if (c < a.C) {
-            if (a.gate) gate[q].load(static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c);
-            if (a.residual) res[q].load(static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c);
-          }
-        }
-        stage(j);
-#pragma unroll
-        for (int q = 0; q < PASSES; ++q) {
-          float v[8];
-          staged(q, v);
-          if (rw + j * 32 + q * ROWS + sub >= a.R || c >= a.C) continue;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] += bias[i];
-          if (a.gate) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= gate[q].get(i);
-          }
-          if (a.residual) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += res[q].get(i);
-          }
-          store8(static_cast<T*>(a.y) + to[q] + c, v);
-        }
-      } else {
-        stage(j);
-#pragma unroll 1
-        for (int q = 0; q < PASSES; ++q) {
-          float v[8];
-          staged(q, v);
-          const int r = rw + j * 32 + q * ROWS + sub;
-          if (r >= a.R || c >= a.C) continue;
-          if (a.partial)
-            store_partial8(a, part, r, c, v);
-          else
-            finish8<T>(a, r, c, v, bias);
+      for (int q = 0; q < PASSES; ++q) {
+        const int r = min(rw + j * 32 + q * ROWS + sub, a.R - 1), b = a.n >= a.R ? 0 : r / a.n, t = r - b * a.n;
+        to[q] = (int64_t)b * a.yst.b + (int64_t)t * a.yst.n;
+        if (whole8) {
+          if (a.gate) gate[q].load(static_cast<const T*>(a.gate) + (int64_t)b * a.gst.b + (int64_t)t * a.gst.n + c);
+          if (a.residual) res[q].load(static_cast<const T*>(a.residual) + (int64_t)b * a.rst.b + (int64_t)t * a.rst.n + c);
         }
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-  } else {  // rows at any alignment: neighbouring lanes take neighbouring elements, four rows' inputs on their way together
-    constexpr int ACROSS = COLS < 64 ? COLS : 64, ROWS = 64 / ACROSS, N4 = 4;
-    const int sub = lane / ACROSS;
-#pragma unroll
-    for (int j = 0; j < TR; ++j) {
       stage(j);
 #pragma unroll
-      for (int half = 0; half < COLS; half += ACROSS) {
-        const int col = half + lane % ACROSS, e = c0 + wc * COLS + col;
-        const float bias = a.bias && e < a.C ? load_as_f32(static_cast<const T*>(a.bias) + e) : 0.f;
-#pragma unroll 1
-        for (int q = 0; q < 32; q += N4 * ROWS) {
-          Place p[N4];
-          float gate[N4], res[N4];
+      for (int q = 0; q < PASSES; ++q) {
+        float v[8];
+        staged(q, v);
+        if (rw + j * 32 + q * ROWS + sub >= a.R || !whole8) continue;
 #pragma unroll
-          for (int i = 0; i < N4; ++i) {
-            const int r = rw + j * 32 + q + i * ROWS + sub;
-            p[i] = Place(a, min(r, a.R - 1));
-            gate[i] = a.gate && e < a.C ? load_as_f32(static_cast<const T*>(a.gate) + p[i].gate + e) : 1.f;
-            res[i] = a.residual && e < a.C ? load_as_f32(static_cast<const T*>(a.residual) + p[i].res + e) : 0.f;
-          }
+        for (int i = 0; i < 8; ++i) v[i] += bias[i];
+        if (a.gate) {
 #pragma unroll
-          for (int i = 0; i < N4; ++i) {
-            const int row = q + i * ROWS + sub, r = rw + j * 32 + row;
-            float v = *reinterpret_cast<const float*>(own + row * (COLS * 4) + (((col >> 2) ^ (row & (CHUNKS - 1))) << 4) + (col & 3) * 4);
-            if (r >= a.R || e >= a.C) continue;
-            v += bias;
-            if (a.pre) store1(static_cast<T*>(a.pre) + (int64_t)r * a.C + e, v);
-            if (a.act != SVGEAR_ACT_NONE) v = act_value<T>(a.act, v);
-            store1(static_cast<T*>(a.y) + p[i].y + e, __builtin_fmaf(v, gate[i], res[i]));
-          }
+          for (int i = 0; i < 8; ++i) v[i] *= gate[q].get(i);
         }
+        if (a.residual) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += res[q].get(i);
+        }
+        store8(static_cast<T*>(a.y) + to[q] + c, v);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    } else {
+      stage(j);
+#pragma unroll 1
+      for (int q = 0; q < PASSES; ++q) {
+        float v[8];
+        staged(q, v);
+        const int r = rw + j * 32 + q * ROWS + sub;
+        if (r >= a.R || c >= a.C) continue;
+        if (a.partial)
+          store_partial8(a, part, r, c, v);
+        else if (whole8)
+          finish8<T>(a, r, c, v, bias);
+      }
     }
+    if (first_tail >= 0 && first_tail < COLS) {
+#pragma unroll 1
+      for (int q = 0; q < 32; q += 8) {
+        const int row = q + (lane >> 3), col = first_tail + (lane & 7), r = rw + j * 32 + row, e = c0 + wc * COLS + col;
+        if (r < a.R && e < a.C)
+          finish1<T>(a, r, e, *reinterpret_cast<const float*>(own + row * (COLS * 4) + (((col >> 2) ^ (row & (CHUNKS - 1))) << 4) + (col & 3) * 4));
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
