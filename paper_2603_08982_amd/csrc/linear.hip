@@ -277,7 +277,7 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
 // 256 x 256: one at a time), `once` for their prologues and epilogues, `first` for those that nothing hides; joining parts costs a launch and their products'
 // way to memory and back. The constants are measured. Both sides of the choices, us, MI355X, bf16, C x R of K: 5120 x 256 of 4096
 // in tiles of 64 / 128 / 128 in 3 parts: 30 / 34 / 25; 2048 x 512 of 2048 in 64 / 128: 12 / 17; 5120 x 2000 of 5120 in 128 / 256:
-// 118 / 100; 2048 x 4000 of 6000: 106 / 114. fp32, 1000 x 1554 of 640 in 64 / 128: 27 / 45, 1536 x 2103 of 1024 70 / 69, 1541 x 2103 of 1003 with a full epilogue 100 / 114; 1000 x 700 of 3000
+// 118 / 100; 2048 x 4000 of 6000: 106 / 114. fp32, 1000 x 1554 of 640 in 64 / 128: 27 / 45, 1536 x 2103 of 1024 73 / 69, 1541 x 2103 of 1003 with a full epilogue 90 / 88; 1000 x 700 of 3000
 // in 64, one part / 4: 56 / 46.
 // Up to 32 rows in fp32, whose matrix cores the idle rows of a tile of 64 would keep busy, have one of 32 x 128 (30,720 x 9 of 5,120:
 // 169 us by 64, 119; 5,120 x 32 of 5,120 39 and 28; for more rows it is no faster, nor is
