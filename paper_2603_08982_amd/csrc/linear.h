@@ -22,6 +22,7 @@ struct LinearArgs {
   int64_t K;
   int R, C;
   int tile;      // tile of the tile kernel: 64, 128, or (bf16) 256 rows and columns, (fp32) 32 rows of 128; 0: the kernel of few rows
+  bool by_element;  // the tile kernel copies P by the fp32 element (rows of any alignment and length); tiles of 32 and 64 rows only
   int splits;    // K in so many parts, each into its own slice of `partial`
   float* partial;  // [splits][R][C] or null
   // epilogue: row r is token r - b*n of batch entry b = r / n

@@ -240,6 +240,14 @@ struct Packing {
   }
 };
 
+// Whether the tile kernel reads the weights where they are by the element: fp32 rows that it cannot read by 16 bytes, where the
+// product has few rows, so that a copy costs more than four times the loads (forward and dx, us with the copy and without it: 60 rows, 14,453 in,
+// 4,239 out 188 / 189 and 106 / 98; 128 rows, 3,723 in, 5,001 out 83 / 85 and 65 / 64; 256 rows 121 / 124 and 115 / 107; 384 rows 162 / 161 and
+// 160 / 167).
+bool by_element(const void* w, int64_t w_stride, int64_t d_in, svgear_dtype dt, int64_t rows) {
+  return dt == SVGEAR_F32 && rows <= 256 && w_stride <= kMaxPitch && !in_place(w, w_stride, d_in, dt);
+}
+
 // What of svgear_linear's operands goes through the workspace. Few rows: x only, where its batches are not one run of rows.
 struct Copies {
   bool x, w;
@@ -247,7 +255,7 @@ struct Copies {
 Copies operand_copies(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride, svgear_dtype dt, int B,
                       int64_t N, int64_t d_in) {
   if (B * N <= few_rows(dt)) return Copies{run_pitch(xstride, B, N) < 0, false};
-  return Copies{!rows_in_place(x, xstride, B, N, d_in, dt), !in_place(w, w_stride, d_in, dt)};
+  return Copies{!rows_in_place(x, xstride, B, N, d_in, dt), !in_place(w, w_stride, d_in, dt) && !by_element(w, w_stride, d_in, dt, B * N)};
 }
 
 bool sizes_ok(svgear_dtype dt, int B, int64_t N, int d_in, int d_out) {
@@ -286,7 +294,8 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
 struct Plan {
   int tile, splits;
 };
-Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
+// element: by_element's rows, for which there are tiles of 32 and 64 alone.
+Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form, bool element) {
   if (form == kContractBoth && R <= few_rows(dt)) return Plan{0, 1};
   struct Kind {
     int tile, rows, cols;
@@ -301,6 +310,7 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
   for (int i = 0; i < 3; ++i) {
     const Kind& k = kinds[i];
     if (k.rows == 32 && (R > 32 || form == kContractNone)) continue;
+    if (k.rows == 128 && element) continue;
     const int64_t tiles = ceil_div(R, k.rows) * ceil_div(C, k.cols);
     for (int p = 1; p <= 16 && (p == 1 || (steps >= 4 * p && tiles < 1024)); ++p) {
       const double m = (double)ceil_div(tiles * p, 256), each = m * k.step;
@@ -314,18 +324,19 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
   }
   return best;
 }
-size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form) {
-  const int p = plan_product(R, C, K, dt, form).splits;
+size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form, bool element) {
+  const int p = plan_product(R, C, K, dt, form, element).splits;
   return p > 1 ? align_up((size_t)p * R * C * sizeof(float), 256) : 0;
 }
 void set_product(LinearArgs& a, const Operand& P, const Operand& Q, int64_t R, int64_t C, int64_t K, svgear_dtype dt,
-                 int form, Workspace& w) {
+                 int form, bool element, Workspace& w) {
   a.P = P;
   a.Q = Q;
   a.R = (int)R;
   a.C = (int)C;
   a.K = K;
-  const Plan plan = plan_product(R, C, K, dt, form);
+  const Plan plan = plan_product(R, C, K, dt, form, element);
+  a.by_element = element && plan.tile != 0;
   a.tile = plan.tile;
   a.splits = plan.splits;
   a.partial = a.splits > 1 ? w.take<float>((size_t)a.splits * R * C) : nullptr;
@@ -379,7 +390,7 @@ extern "C" size_t svgear_linear_workspace(const void* x, const int64_t xstride[2
   size_t bytes = 0;
   if (copies.x) bytes += packed_bytes((int64_t)B * N, d_in, dt);
   if (copies.w) bytes += packed_bytes(d_out, d_in, dt);
-  return bytes + parts_bytes((int64_t)B * N, d_out, d_in, dt, kContractBoth);
+  return bytes + parts_bytes((int64_t)B * N, d_out, d_in, dt, kContractBoth, by_element(w, w_stride, d_in, dt, (int64_t)B * N));
 }
 
 extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void* w, int64_t w_stride,
@@ -409,7 +420,7 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
   const int rc = packing.launch(dt, s);
   if (rc != SVGEAR_OK) return rc;
   LinearArgs a{};
-  set_product(a, W, X, M, d_out, d_in, dt, kContractBoth, space);
+  set_product(a, W, X, M, d_out, d_in, dt, kContractBoth, by_element(w, w_stride, d_in, dt, M), space);
   a.n = (int)N;
   a.bias = bias;
   a.gate = gate;
@@ -436,11 +447,12 @@ extern "C" size_t svgear_linear_backward_workspace(const void* dy, const int64_t
   bytes += 2 * align_up((size_t)gb * gradient_blocks(gb, fold ? B : N, d_out) * d_out * sizeof(float), 256);
   if (x) {
     if (!rows_in_place(x, xstride, B, N, d_in, dt)) bytes += packed_bytes(M, d_in, dt);
-    bytes += parts_bytes(d_out, d_in, M, dt, kContractNone);
+    bytes += parts_bytes(d_out, d_in, M, dt, kContractNone, false);
   }
   if (w) {
-    if (!in_place(w, w_stride, d_in, dt)) bytes += packed_bytes(d_out, d_in, dt);
-    bytes += parts_bytes(M, d_in, d_out, dt, kContractQ);
+    const bool element = by_element(w, w_stride, d_in, dt, M);
+    if (!in_place(w, w_stride, d_in, dt) && !element) bytes += packed_bytes(d_out, d_in, dt);
+    bytes += parts_bytes(M, d_in, d_out, dt, kContractQ, element);
   }
   return bytes;
 }
@@ -523,14 +535,15 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
 
   Operand W{w, w_stride}, X{x, dw ? run_pitch(xstride, B, N) : 0};
   Packing packing;
-  if (dx && !in_place(w, w_stride, d_in, dt)) packing.add(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W);
+  const bool element = dx && by_element(w, w_stride, d_in, dt, M);
+  if (dx && !in_place(w, w_stride, d_in, dt) && !element) packing.add(w, Rows{0, w_stride}, d_out, d_out, d_in, dt, space, W);
   if (dw && !rows_in_place(x, xstride, B, N, d_in, dt))
     packing.add(x, Rows{xstride[0], xstride[1]}, N, M, d_in, dt, space, X);
   const int packed = packing.launch(dt, s);
   if (packed != SVGEAR_OK) return packed;
   if (dx) {
     LinearArgs a{};
-    set_product(a, W, dz, M, d_in, d_out, dt, kContractQ, space);
+    set_product(a, W, dz, M, d_in, d_out, dt, kContractQ, element, space);
     a.n = (int)N;
     a.y = dx;
     a.yst = Rows{dxstride[0], dxstride[1]};
@@ -539,7 +552,7 @@ extern "C" int svgear_linear_backward(const void* dy, const int64_t dystride[2],
   }
   if (dw) {
     LinearArgs a{};
-    set_product(a, X, dz, d_out, d_in, M, dt, kContractNone, space);
+    set_product(a, X, dz, d_out, d_in, M, dt, kContractNone, false, space);
     a.n = d_out;
     a.y = dw;
     a.yst = Rows{0, d_in};

@@ -48,8 +48,9 @@ struct Frag {
   };
 };
 
-// One operand's tile: E extent (rows of the output's r or c), contraction contiguous or over rows.
-template <typename T, int E, bool OVER_ROWS, int WAVES>
+// One operand's tile: E extent (rows of the output's r or c), contraction contiguous or over rows; copied by G bytes a lane: 16, or
+// one fp32 element, for rows at any alignment and of any length.
+template <typename T, int E, bool OVER_ROWS, int WAVES, int G>
 struct Tile {
   static constexpr int ES = sizeof(T);
   static constexpr int BK = 128 / ES;                        // k of a step
@@ -57,8 +58,9 @@ struct Tile {
   static constexpr int ROWB = OVER_ROWS ? E * ES : 128;      // bytes of an LDS row
   static constexpr int CPR = ROWB / 16;                      // its chunks
   static constexpr int BYTES = E * 128;
-  static constexpr int COPIES = BYTES / 1024 / WAVES;        // wave-wide copies of 1 KB, each wave
-  static_assert(BYTES % (1024 * WAVES) == 0, "copies must split evenly over the waves");
+  static constexpr int COPIES = BYTES / (64 * G) / WAVES;    // wave-wide copies, each wave
+  static_assert(BYTES % (64 * G * WAVES) == 0, "copies must split evenly over the waves");
+  static_assert(G == 16 || (G == 4 && ES == 4), "chunks or fp32 elements");
   static_assert(!OVER_ROWS || ES == 2 || ROWB >= 256, "the chunk swizzle needs 16 chunks in a row");
 
   static __device__ __forceinline__ int swz(int row) {
@@ -67,7 +69,7 @@ struct Tile {
     return ROWB >= 256 ? (row & 3) << 2 : (row & 2) << 1;
   }
 
-  uint32_t off[COPIES];   // byte offset of the lane's chunk from the tile's first row / step's first k
+  uint32_t off[COPIES];   // byte offset of the lane's G bytes from the tile's first row / step's first k
   int kk[COPIES];         // its k within the step
   const unsigned char* base;  // wave-uniform: the step's first element
   int64_t step;               // bytes from step to step
@@ -76,14 +78,15 @@ struct Tile {
   __device__ __forceinline__ void init(const Operand& o, int e0, int limit, int64_t k0, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
-      const int slot = (wave + i * WAVES) * 64 + lane, row = slot / CPR, chunk = (slot % CPR) ^ swz(row);
+      const int slot = ((wave + i * WAVES) * 64 + lane) * G / 16, row = slot / CPR, chunk = (slot % CPR) ^ swz(row);
+      const int part = G == 16 ? 0 : lane & 3;  // element of the chunk
       if (!OVER_ROWS) {
         // rows past the last repeat it: what they give is never stored
-        off[i] = (uint32_t)(min(row, limit - 1 - e0) * (int64_t)(o.pitch * ES) + chunk * 16);
-        kk[i] = chunk * CH;
+        off[i] = (uint32_t)(min(row, limit - 1 - e0) * (int64_t)(o.pitch * ES) + chunk * 16 + part * G);
+        kk[i] = chunk * CH + part;
       } else {
-        const int last = (limit - 1 - e0) / CH;  // chunks past the last likewise
-        off[i] = (uint32_t)(row * (int64_t)(o.pitch * ES) + min(chunk, last) * 16);
+        const int last = limit - 1 - e0;  // chunks (elements) past the last likewise
+        off[i] = (uint32_t)(row * (int64_t)(o.pitch * ES) + (G == 16 ? min(chunk, last / CH) * 16 : min(chunk * CH + part, last) * ES));
         kk[i] = row;
       }
     }
@@ -94,11 +97,14 @@ struct Tile {
   // Copy i of the step whose first element is `base` into lds; LAST: the last step, `left` k of which exist.
   template <bool LAST>
   __device__ __forceinline__ void copy(int i, uint32_t lds, int left, int wave) const {
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (wave + i * WAVES) * 1024);
-    if constexpr (!LAST)
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (wave + i * WAVES) * (64 * G));
+    const void* from = LAST && kk[i] >= left ? static_cast<const void*>(g_zero_chunk) : static_cast<const void*>(base + off[i]);
+    if constexpr (G == 4)
+      async_copy_4B(from, to);
+    else if constexpr (!LAST)
       async_copy_16B(base, off[i], to);
     else
-      async_copy_16B(kk[i] < left ? static_cast<const void*>(base + off[i]) : static_cast<const void*>(g_zero_chunk), to);
+      async_copy_16B(from, to);
   }
 };
 
@@ -162,14 +168,14 @@ __device__ __forceinline__ void multiply(const Frag& p, const Frag& q, f32x16& a
 }
 
 // WC x WR waves, each TC x TR blocks of 32 x 32. Registers for as many workgroups on a CU as the LDS holds: one of 256 x 256, two
-// or more of the others.
-template <typename T, int FORM, int TC, int TR, int WC, int WR>
+// or more of the others. PG: bytes a lane of P's copies.
+template <typename T, int FORM, int TC, int TR, int WC, int WR, int PG>
 __global__ void __launch_bounds__(64 * WC * WR, (TC * TR > 2 ? WC * WR / 4 : WC * WR / 2))
 linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
   constexpr int WAVES = WC * WR, BC = 32 * TC * WC, BR = 32 * TR * WR;
   constexpr bool P_ROWS = FORM != kContractBoth, Q_ROWS = FORM == kContractNone;
-  typedef Tile<T, BC, P_ROWS, WAVES> PT;
-  typedef Tile<T, BR, Q_ROWS, WAVES> QT;
+  typedef Tile<T, BC, P_ROWS, WAVES, PG> PT;
+  typedef Tile<T, BR, Q_ROWS, WAVES, 16> QT;
   constexpr int BK = PT::BK, LDS = 3 * PT::BYTES + 2 * QT::BYTES;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -398,12 +404,12 @@ linear_tile_kernel(LinearArgs a, int tiles_c, int tiles_r) {
   }
 }
 
-template <typename T, int FORM, int TC, int TR, int WC, int WR>
+template <typename T, int FORM, int TC, int TR, int WC, int WR, int PG = 16>
 int launch_tiles(const LinearArgs& a, hipStream_t s) {
   constexpr int BC = 32 * TC * WC, BR = 32 * TR * WR, lds = (3 * BC + 2 * BR) * 128;
   const int tc = (int)ceil_div(a.C, BC), tr = (int)ceil_div(a.R, BR);
   if ((int64_t)tc * tr > 1 << 30) return SVGEAR_ERR_UNSUPPORTED;
-  auto kern = linear_tile_kernel<T, FORM, TC, TR, WC, WR>;
+  auto kern = linear_tile_kernel<T, FORM, TC, TR, WC, WR, PG>;
   if (lds > 65536)
     SVGEAR_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
   kern<<<long_grid(tc * tr, a.splits), 64 * WC * WR, lds, s>>>(a, tc, tr);
@@ -413,6 +419,11 @@ int launch_tiles(const LinearArgs& a, hipStream_t s) {
 
 template <typename T, int FORM>
 int launch_form(const LinearArgs& a, hipStream_t s) {
+  if constexpr (sizeof(T) == 4 && FORM != kContractNone) {
+    if (a.by_element)
+      return a.tile == 32 ? launch_tiles<T, FORM, 1, 1, 4, 1, 4>(a, s) : a.tile == 64 ? launch_tiles<T, FORM, 1, 1, 2, 2, 4>(a, s) : SVGEAR_ERR_UNSUPPORTED;
+  }
+  if (a.by_element) return SVGEAR_ERR_UNSUPPORTED;
   switch (a.tile) {
     case 32:
       if constexpr (sizeof(T) == 4 && FORM != kContractNone) return launch_tiles<T, FORM, 1, 1, 4, 1>(a, s);

@@ -403,3 +403,30 @@ def test_the_most_rows():
     for at in range(0, rows, 1 << 27):
         part = slice(at, at + (1 << 27))
         assert torch.equal(y[part], x[part] * w)
+
+
+# 9 to 256 rows, and one more, with weights whose rows lie at odd addresses: odd lengths, shorter than 16 bytes, longer than
+# a step (32 fp32) by one, tiles of both kinds, a contraction in parts; as slices of a larger tensor at every offset
+ODD_FEW = [(1, 9, 1003, 17000), (1, 64, 131, 259), (1, 65, 131, 259), (2, 32, 5001, 129), (1, 12, 4239, 5), (1, 10, 1, 1), (1, 20, 3, 17000),
+           (1, 33, 33, 67), (4, 8, 65, 33), (1, 256, 131, 259), (1, 257, 131, 67), (2, 100, 1003, 17)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("lead", [0, 1, 2, 3])
+@pytest.mark.parametrize("size", ODD_FEW, ids=str)
+def test_few_rows_with_weights_at_odd_addresses(size, lead, dtype):
+    i = ODD_FEW.index(size)
+    x, w, b, g, r = inputs(dtype, *size, bias=True, gate="token", residual=True, seed=600 + i)
+    o, k = w.shape
+    big = torch.full((o, lead + k + 1 + lead), float("nan"), dtype=dtype, device="cuda")
+    big[:, lead:lead + k] = w
+    w = big[:, lead:lead + k]
+    y, pre = sv.linear(x, w, b, act="silu", gate=g, residual=r, want_pre=True)
+    Y, Z, by, bz = linear64(x, w, b, "silu", g, r)
+    close(pre, Z, bz, "pre")
+    close(y, Y, by, "y")
+    dy = rand(*pre.shape, seed=700 + i, dtype=dtype).cuda()
+    got = sv.linear_backward(dy, x, w, pre=pre, act="silu", gate=g, want=["dx", "dw", "dbias"])
+    ref = linear_backward64(dy, x, w, pre, "silu", g, UNIT[dtype])
+    for name in got:
+        close(got[name], *ref[name], name)
