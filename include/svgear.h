@@ -334,7 +334,7 @@ int svgear_unpermute(const void* op, const int32_t* perm, svgear_dtype dt, int B
  * Sizes: B, N, d_in, d_out >= 1, B*N <= 2^30, d_in and d_out <= 2^21; strides from 0 to 2^48, those of y
  * such that no two rows meet; any alignment that the type has. Rows of x and w that are not
  * 16-byte aligned, or whose length is no multiple of 16 bytes, and batches of x that are not one
- * run of evenly spaced rows are first copied into the workspace, which also holds partial products where
+ * run of evenly spaced rows are first copied into the workspace (where that pays), which also holds partial products where
  * the output is small: its size depends on the same arguments (pointers are looked at for their
  * alignment only, on the host). Where it is 0, ws may be NULL; it is 0 for invalid arguments too.
  */

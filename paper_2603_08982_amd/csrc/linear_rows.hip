@@ -5,7 +5,7 @@
 // flight, and multiplies them with the rows of Q on the vector ALU, bf16 by pairs. The waves of a workgroup have the same few columns and K in turn, their
 // sums are added in order. Workgroups are small, so that all CUs get the same share of the weights: with the 16
 // columns that a matrix instruction wants for each, 5,120 columns are 320 shares for 256 CUs (1 row of 5120 by 5120,
-// bf16: 18.3 us that way, 12.9 this way; by 30720: 66 and 60 us, 5.2 TB/s).
+// bf16: 18.3 us that way, 12.9 this way; by 30,720: 66 and 60 us, 5.2 TB/s).
 #include "linear.h"
 
 namespace svgear {
