@@ -347,14 +347,23 @@ def sparse_attn_comp(qp, kp, vp, kbar, vbar, q_offsets, k_offsets, mask_bits, ro
     return op, lse
 
 
+def _check_out(out: torch.Tensor, like: torch.Tensor):
+    """A caller's output of the layer: of the shape, type and device of the tensor that it belongs to, with contiguous d."""
+    _require(out.shape == like.shape and out.dtype == like.dtype and out.device == like.device and out.stride(-1) == 1,
+             f"out: expected {tuple(like.shape)}, {like.dtype}, {like.device}, with contiguous d")
+
+
 def unpermute(op: torch.Tensor, perm: torch.Tensor, out: Optional[torch.Tensor] = None):
-    """svgear_unpermute: out[b,h,perm[p]] = op[b,h,p]."""
+    """svgear_unpermute: out[b,h,perm[p]] = op[b,h,p]. out, if given: [B,H,N,d] as op, any strides with contiguous d."""
     _need_gpu(op, perm, out)
     lib = load_library()
     B, H, N, d = op.shape
     assert op.is_contiguous() and perm.is_contiguous()
+    _require(perm.shape == (B, H, N) and perm.dtype == torch.int32 and perm.device == op.device, "perm: expected int32 [B,H,N] on op's device")
     if out is None:
         out = torch.empty_like(op)
+    else:
+        _check_out(out, op)
     rc = lib.svgear_unpermute(_ptr(op), _ptr(perm), _dt(op), B, H, N, d, _ptr(out), _strides4(out), _stream())
     _check(rc, "svgear_unpermute")
     return out
@@ -686,8 +695,12 @@ def attention_layer(Q, K, V, init_q, init_k, iters: int, budget_cost: int, n_tai
     so a caller can carry them to the next denoising step). With top_p the routing budget is
     the adaptive per-query-cluster one and budget_cost is ignored. mark(name), if given, is
     called on the current stream after each stage ("kmeans", "permute", "probe_route",
-    "attention", "unpermute"). O is written into `out` if given. Returns (O, intermediates)."""
+    "attention", "unpermute"). O is written into `out` if given ([B,H,N,d] as Q, any strides with contiguous d, over none
+    of Q, K and V). Returns (O, intermediates)."""
     B, H, N, d = Q.shape
+    if out is not None:
+        _need_gpu(Q, out)
+        _check_out(out, Q)
     if scale is None:
         scale = float(d) ** -0.5
     Cq, Ck = init_q.shape[2], init_k.shape[2]
