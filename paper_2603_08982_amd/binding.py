@@ -106,16 +106,15 @@ def load_library():
     lib.svgear_sparse_attn_two_stage.argtypes = lib.svgear_sparse_attn_comp.argtypes
     lib.svgear_unpermute.restype = _i
     lib.svgear_unpermute.argtypes = [_vp, _vp, _i, _i, _i, _i64, _i, _vp, _c.POINTER(_c.c_int64), _vp]
-    p2 = _vp
     lib.svgear_linear_workspace.restype = _sz
-    lib.svgear_linear_workspace.argtypes = [_vp, p2, _vp, _i64, _i, _i, _i64, _i, _i]
+    lib.svgear_linear_workspace.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _i64, _i, _i]
     lib.svgear_linear.restype = _i
-    lib.svgear_linear.argtypes = [_vp, p2, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, p2, _vp, p2, _vp, _vp, p2, _vp,
+    lib.svgear_linear.argtypes = [_vp, _vp, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                   _sz, _vp]
     lib.svgear_linear_backward_workspace.restype = _sz
-    lib.svgear_linear_backward_workspace.argtypes = [_vp, p2, _vp, p2, _vp, _i64, _i, _i, _i64, _i, _i]
+    lib.svgear_linear_backward_workspace.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _i64, _i, _i]
     lib.svgear_linear_backward.restype = _i
-    lib.svgear_linear_backward.argtypes = [_vp, p2, _vp, p2, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, p2, _vp, p2,
+    lib.svgear_linear_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _vp, _i, _i, _i64, _i, _i, _i, _vp, _vp, _vp, _vp,
                                            _vp, _vp, _vp, _vp, _sz, _vp]
     # host arrays of pointers, strides, sections and sizes as plain addresses: ctypes checks less of them in each call
     places = [_vp, _vp, _vp, _i64, _vp, _i64, _u, _f]
