@@ -412,6 +412,14 @@ def _same_place(first: torch.Tensor, *ts) -> int:
 
 _NO_ROWS = _I64x2(0, 0)
 
+# The library's limits, looked at here too: ctypes keeps the low bits of what an argument does not hold.
+_MOST_ROWS, _WIDEST, _MOST_HEADS, _GRID = 1 << 30, 1 << 21, 128, 1 << 31
+
+
+def _linear_sizes(B: int, N: int, d_in: int, d_out: int):
+    if not (0 < B * N <= _MOST_ROWS and 0 < d_in <= _WIDEST and 0 < d_out <= _WIDEST):
+        raise SvgearError(f"{B} x {N} rows of {d_in} to {d_out}: expected 1 to 2^30 rows of 1 to 2^21 each")
+
 
 def _as_bnd(t: torch.Tensor, what: str):
     """[B,N,c] or [N,c] (one batch entry) as (B, N, c, strides)."""
@@ -451,6 +459,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     if len(wst) != 2 or w.shape[1] != d_in or (wst[1] != 1 and d_in != 1):
         raise SvgearError("w: expected [d_out,d_in] with contiguous d_in")
     d_out = w.shape[0]
+    _linear_sizes(B, N, d_in, d_out)
     shape = (*lead, d_out)
     if bias is not None and (bias.shape != (d_out,) or not bias.is_contiguous()):
         raise SvgearError("bias: expected [d_out]")
@@ -493,6 +502,7 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[tor
     _require("dx" not in want or w is not None, "dx needs w")
     _require("dgate" not in want or gate is not None, "dgate needs the gate")
     d_in = w.shape[1] if w is not None else x.shape[-1] if x is not None else 1
+    _linear_sizes(B, N, d_in, d_out)
     _require(x is None or tuple(x.shape) == (*lead, d_in), "x: expected dy's leading sizes and d_in")
     _require(w is None or (tuple(w.shape) == (d_out, d_in) and (d_in == 1 or w.stride(1) == 1)), "w: expected [d_out,d_in] with contiguous d_in")
     _require(pre is None or (tuple(pre.shape) == tuple(dy.shape) and pre.is_contiguous()), "pre: expected dy's shape, dense")
@@ -549,7 +559,9 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
     if t0.dim() != 4 or len(tensors) > 2 or (len(tensors) == 2 and tensors[1].shape != t0.shape):
         raise SvgearError("one or two tensors of one shape [B,H,N,d]")
     B, H, N, d = t0.shape
-    if len(sections) != 3:
+    if not (0 < B * N <= _MOST_ROWS and 0 < H <= _MOST_HEADS and (d == 64 or d == 128) and 0 <= n_tail < N):
+        raise SvgearError(f"[B,H,N,d] = {tuple(t0.shape)} with {n_tail} text tokens: expected 1 to 2^30 tokens, some of them rotated, of 1 to 128 heads of 64 or 128")
+    if len(sections) != 3 or min(sections) < 0 or max(sections) > d // 2:
         raise SvgearError("sections: pairs of the three axes")
     if norm not in ROTARY_NORMS:
         raise SvgearError('norm: None, "head" or "token"')
@@ -567,8 +579,8 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
         if len(shape) == 3:
             pos_b = 3 * shape[1]
     else:
-        if len(grid) != 3:
-            raise SvgearError("grid: (time, height, width)")
+        if len(grid) != 3 or min(grid) < 1 or max(grid) >= _GRID or not 0 <= first < _GRID:
+            raise SvgearError("grid: (time, height, width), first: a token of it")
         size3 = _grid(*grid)
     if weights is None:
         weights = (None,) * len(tensors)
@@ -579,7 +591,7 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
         for w in weights:
             if w is not None and (w.shape != (size,) or not w.is_contiguous()):
                 raise SvgearError("weights: expected [d] or [H*d]")
-    return weights, (inv_freq.data_ptr(), _sections(*sections), size3, first, _ptr(positions), pos_b,
+    return weights, (inv_freq.data_ptr(), _sections(*sections), size3, 0 if size3 is None else first, _ptr(positions), pos_b,
                      ROTARY_NORMS[norm] | (ROTARY_HALVES if halves else 0))
 
 

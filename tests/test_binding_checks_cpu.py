@@ -63,3 +63,86 @@ def test_layer_refuses_such_an_output_before_its_centroids_change(no_library, wh
         sv.attention_layer(q, q, q, c, c.clone(), 1, 100, overlap=False, token_order=token_order, out=BAD_OUT[what]())
     with pytest.raises(Reached, match="kmeans"):
         sv.attention_layer(q, q, q, c, c.clone(), 1, 100, overlap=False, token_order=token_order, out=torch.empty(*OP))
+
+
+@pytest.fixture
+def no_device(no_library, monkeypatch):
+    """The same for the entry points that take strides, whose tensors are then on no device at all (they have sizes alone)."""
+    import contextlib
+
+    monkeypatch.setattr(binding, "_on_device", lambda device: contextlib.nullcontext())
+    monkeypatch.setattr(binding, "_stream_of", lambda device: 0)
+
+
+def meta(*shape, strides=None, dtype=torch.bfloat16):
+    t = torch.empty(1, dtype=dtype, device="meta")
+    if strides is None:
+        return torch.empty(*shape, dtype=dtype, device="meta")
+    return t.expand(*shape) if strides == "one" else t.as_strided(shape, strides)
+
+
+# sizes whose low 32 bits are an ordinary call's, and the first past each limit
+PAST = 1 << 32
+TOO_LARGE = {
+    "batch entries past 32 bits": lambda: sv.linear(meta(1, 1, 8).expand(PAST + 1, 1, 8), meta(16, 8)),
+    "d_in past 32 bits": lambda: sv.linear(meta(1, 2, PAST + 8), meta(16, PAST + 8)),
+    "d_out past 32 bits": lambda: sv.linear(meta(1, 2, 8), meta(PAST + 16, 8)),
+    "rows past 2^30": lambda: sv.linear(meta(1, 1, 8).expand(1 << 15, (1 << 15) + 1, 8), meta(16, 8)),
+    "d_in past 2^21": lambda: sv.linear(meta(1, 2, (1 << 21) + 1), meta(16, (1 << 21) + 1)),
+    "backward, batch entries past 32 bits": lambda: sv.linear_backward(meta(1, 1, 16).expand(PAST + 1, 1, 16), None, meta(16, 8), want=["dx"]),
+    "backward, d_in past 32 bits": lambda: sv.linear_backward(meta(1, 2, 16), None, meta(16, PAST + 8), want=["dx"]),
+    "backward, d_out past 32 bits": lambda: sv.linear_backward(meta(1, 2, PAST + 16), meta(1, 2, 8), None, want=["dw"]),
+    "backward, dbias alone": lambda: sv.linear_backward(meta(1, 2, PAST + 16), None, None, want=["dbias"]),
+}
+
+
+@pytest.mark.parametrize("what", TOO_LARGE)
+def test_linear_refuses_sizes_that_its_arguments_do_not_hold(no_device, what):
+    with pytest.raises(sv.SvgearError):
+        TOO_LARGE[what]()
+
+
+def test_linear_of_the_largest_sizes_goes_on(no_device):
+    with pytest.raises(Reached):
+        sv.linear(meta(1, 1, 1 << 21).expand(1 << 15, 1 << 15, 1 << 21), meta(1 << 21, 1 << 21))
+    with pytest.raises(Reached):
+        sv.linear_backward(meta(1, 1, 1 << 21).expand(1 << 15, 1 << 15, 1 << 21), None, meta(1 << 21, 1 << 21), want=["dx"])
+
+
+def rotary_call(back, shape=(1, 2, 24, 64), sections=(10, 11, 11), **kw):
+    q = meta(1, 1, 1, shape[3]).expand(*shape)
+    f = torch.empty(sum(sections), dtype=torch.float64, device="meta")
+    if "positions" not in kw:
+        kw.setdefault("grid", (2, 3, 4))
+    return sv.rotary_backward([q], None, f, sections, **kw) if back else sv.rotary([q], f, sections, **kw)
+
+
+ROTARY_TOO_LARGE = {
+    "batch entries": dict(shape=(PAST + 1, 2, 24, 64)),
+    "heads": dict(shape=(1, PAST + 2, 24, 64)),
+    "tokens": dict(shape=(1, 1, (1 << 30) + 1, 64), grid=((1 << 30) + 1, 1, 1)),
+    "elements of a head": dict(shape=(1, 2, 24, PAST + 64)),
+    "text tokens": dict(n_tail=(1 << 64) + 1),
+    "text tokens below none": dict(n_tail=-(1 << 64) + 1),
+    "first": dict(first=1 << 64),
+    "first below none": dict(first=-(1 << 64)),
+    "grid": dict(grid=((1 << 64) + 2, 3, 4)),
+    "grid past 31 bits": dict(grid=(1 << 31, 1, 1)),
+    "sections": dict(sections=(PAST + 10, 11 - PAST, 11)),
+}
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("what", ROTARY_TOO_LARGE)
+def test_rotary_refuses_sizes_that_its_arguments_do_not_hold(no_device, what, back):
+    with pytest.raises(sv.SvgearError):
+        rotary_call(back, **ROTARY_TOO_LARGE[what])
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_rotary_of_the_largest_sizes_goes_on(no_device, back):
+    for kw in (dict(), dict(shape=(1, 128, 1 << 23, 128), grid=(1 << 30, 1, 1), first=(1 << 30) - (1 << 23)),
+               dict(shape=(1 << 15, 1, 1 << 15, 64), grid=(1 << 15, 1, 1)), dict(n_tail=23, grid=((1 << 31) - 1, 1, 1)),
+               dict(positions=torch.empty(24, 3, dtype=torch.int32, device="meta"), first=1 << 64)):
+        with pytest.raises(Reached):
+            rotary_call(back, **kw)
