@@ -399,7 +399,7 @@ int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void
  * fastest), for a share of a sequence or a single token of it: first + N - n_tail <= the
  * grid's size < 2^31. Angles are computed in fp64 and reduced to one turn before cos and sin, so
  * far positions lose nothing; all else is fp32, rounded once at the end. Squares are summed in
- * fp32: |x| up to 1e17. With eps = 0 a row of zeros gives NaN.
+ * fp32: |x| up to 1e17, and with eps = 0 a root mean square from 1e-17 on. With eps = 0 a row of zeros gives NaN.
  *   src[k], dst[k]  [B,H,N,d] dt, element strides sstride[k], dstride[k]; 16-byte aligned, strides
  *                   multiples of 16 bytes, d = 64 or 128. dst[k] may be src[k] itself (same
  *                   strides), and no other overlap is allowed (one at the same address is refused). Rows of a cache, or of a fused
@@ -427,7 +427,8 @@ int svgear_rotary(int n_tensors, const void* const* src, const int64_t (*sstride
  *   dx[k]  [B,H,N,d] dt out, dxstride; may be dy[k] itself (same strides), no other overlap (one at
  *          the same address is refused)
  *   dweight[k] [d] or [H*d] dt out, as weight (the array, or an entry, NULL: not wanted)
- * Sums of dweight are fp32 and made in one fixed order. Alignment and limits as above.
+ * Sums of dweight are fp32 and made in one fixed order. Alignment and limits as above; so is |dy weight|, whose products with x are
+ * summed in fp32, up to 1e17.
  */
 size_t svgear_rotary_backward_workspace(int n_tensors, int B, int H, int64_t N, int d);
 int svgear_rotary_backward(int n_tensors, const void* const* dy, const int64_t (*dystride)[3],

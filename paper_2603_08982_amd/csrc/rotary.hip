@@ -252,7 +252,7 @@ rotary_kernel(RotaryArgs a) {
 }
 
 // Backward with a norm. Every workgroup takes tokens at a distance and keeps its sums of du x f in registers
-// until the end, then leaves them, its waves' tokens added in order, as one row of `partial`. A lane has some 16
+// until the end, then leaves them, its waves' tokens added in order, as one row of `partial`. A lane has some 17
 // vector instructions an element, with the turned gradients kept for the second use; the first version, which
 // turned them twice and packed by hand, had some 40 and was bound by them.
 template <typename T, int V, int NORM, bool HALVES, int IT>
@@ -374,7 +374,9 @@ rotary_backward_kernel(RotaryArgs a) {
       load_dy(now);
       if (now.H && wave == first) find_angles(a, now.b, now.n, lane, rows[turn_of ^ 1][first]);
     }
-    float f = 0.f, c = 0.f;  // f and f^3 mean(g x)
+    // f and mean(g x f): dx = f (g - x f mean(g x f)). Neither f^3 nor f^2, which leave fp32 from |x| of 1e13 on, nor their
+    // products with a mean, which do for gradients that are small too.
+    float f = 0.f, c = 0.f;
     if (NORM == kNormToken) {
       for (int o = 1; o < 64; o <<= 1) xx[0] += __shfl_xor(xx[0], o), gx[0] += __shfl_xor(gx[0], o);
       if (wpt > 1 && lane == 0) slots[turn_of][wave] = make_float2(xx[0], gx[0]);
@@ -387,7 +389,7 @@ rotary_backward_kernel(RotaryArgs a) {
       }
       const float inv = 1.f / (float)(a.H * a.d);
       f = 1.f / sqrtf(xx[0] * inv + a.eps);
-      c = f * f * f * (gx[0] * inv);
+      c = f * (gx[0] * inv);
     }
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
@@ -397,19 +399,18 @@ rotary_backward_kernel(RotaryArgs a) {
         for (int o = 1; o < units; o <<= 1) xx[it] += __shfl_xor(xx[it], o), gx[it] += __shfl_xor(gx[it], o);
         const float inv = 1.f / (float)a.d;
         f = 1.f / sqrtf(xx[it] * inv + a.eps);
-        c = f * f * f * (gx[it] * inv);
+        c = f * (gx[it] * inv);
       }
       if (h >= H) continue;
       const int ia = NORM == kNormToken ? it : 0;
       float ga[V], gb[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float x0 = xa[it].get(i), x1 = xb[it].get(i);
-        const float fa = f * ua[it][i], fb = f * ub[it][i];
-        acc[ia][i] = __builtin_fmaf(fa, x0, acc[ia][i]);
-        acc[ia][V + i] = __builtin_fmaf(fb, x1, acc[ia][V + i]);
-        ga[i] = __builtin_fmaf(-c, x0, fa * wa[ia].get(i));
-        gb[i] = __builtin_fmaf(-c, x1, fb * wb[ia].get(i));
+        const float x0 = f * xa[it].get(i), x1 = f * xb[it].get(i);
+        acc[ia][i] = __builtin_fmaf(ua[it][i], x0, acc[ia][i]);
+        acc[ia][V + i] = __builtin_fmaf(ub[it][i], x1, acc[ia][V + i]);
+        ga[i] = f * __builtin_fmaf(-c, x0, ua[it][i] * wa[ia].get(i));
+        gb[i] = f * __builtin_fmaf(-c, x1, ub[it][i] * wb[ia].get(i));
       }
       T* o = dst + (int64_t)h * a.dst_st[k].h;
       *reinterpret_cast<Chunk<T, V>*>(o + at.ea) = Chunk<T, V>::of(ga);
