@@ -329,8 +329,8 @@ int svgear_unpermute(const void* op, const int32_t* perm, svgear_dtype dt, int B
  *   residual [B,N,d_out] dt, rstride
  *   pre      [B,N,d_out] dt out, dense: z, for the backward pass (NULL: not stored)
  *   y        [B,N,d_out] dt out, ystride. y may be the residual itself (same pointer, same
- *            strides); no other overlap of outputs with inputs or each other is allowed (one at the same
- *            address is refused).
+ *            strides, but for that of a dimension of one element); no other overlap of outputs with
+ *            inputs or each other is allowed (one at the same address is refused).
  * Sizes: B, N, d_in, d_out >= 1, B*N <= 2^30, d_in and d_out <= 2^21; strides from 0 to 2^48, those of y
  * such that no two rows meet; any alignment that the type has. Rows of x and w that are not
  * 16-byte aligned, or whose length is no multiple of 16 bytes, and batches of x that are not one

@@ -405,7 +405,7 @@ extern "C" int svgear_linear(const void* x, const int64_t xstride[2], const void
     return SVGEAR_ERR_INVALID;
   if (y == x || y == w || y == gate || y == bias || (pre && (pre == y || pre == x || pre == w || pre == gate || pre == residual || pre == bias)))
     return SVGEAR_ERR_INVALID;
-  if (residual == y && residual && (rstride[0] != ystride[0] || rstride[1] != ystride[1]) && (B > 1 || N > 1))
+  if (residual == y && ((B > 1 && rstride[0] != ystride[0]) || (N > 1 && rstride[1] != ystride[1])))
     return SVGEAR_ERR_INVALID;
   const size_t need = svgear_linear_workspace(x, xstride, w, w_stride, dt, B, N, d_in, d_out);
   if (need && (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < need)) return SVGEAR_ERR_WORKSPACE;
