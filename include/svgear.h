@@ -402,8 +402,9 @@ int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void
  * fp32: |x| up to 1e17, and with eps = 0 a root mean square from 1e-17 on. With eps = 0 a row of zeros gives NaN.
  *   src[k], dst[k]  [B,H,N,d] dt, element strides sstride[k], dstride[k]; 16-byte aligned, strides
  *                   multiples of 16 bytes, d = 64 or 128. dst[k] may be src[k] itself (same
- *                   strides), and no other overlap is allowed (one at the same address is refused). Rows of a cache, or of a fused
- *                   projection's output [B,N,3,H,d], are strides.
+ *                   strides), and no other overlap is allowed (one at the same address is refused). Rows of a
+ *                   cache, or of a fused projection's output [B,N,3,H,d], are strides. The stride of a
+ *                   dimension of one element does not matter.
  *   weight[k]       dt, 16-byte aligned
  *   inv_freq        [P] fp64 (device)
  * src, dst, sstride, dstride, weight (may be NULL) and sections, grid are HOST arrays. n_tensors

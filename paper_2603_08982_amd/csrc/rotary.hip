@@ -474,21 +474,23 @@ bool rows_apart(const int64_t st[3], int64_t B, int64_t H, int64_t N, int64_t d)
   return true;
 }
 
-// Whether output k lies where an input or the other output does, other than the input it may replace (at its own strides).
-bool meets(void* const* out, const int64_t (*ost)[3], const void* const* own, const int64_t (*own_st)[3], const void* const* other,
-           int n, int k) {
-  for (int j = 0; j < n; ++j) {
-    if (j != k && (out[k] == out[j] || out[k] == own[j])) return true;
-    if (other && out[k] == other[j]) return true;
-  }
-  return out[k] == own[k] && (ost[k][0] != own_st[k][0] || ost[k][1] != own_st[k][1] || ost[k][2] != own_st[k][2]);
-}
-
 struct Shape {
   int B, H;
   int64_t N, n_tail;
   int d;
 };
+
+// Whether output k lies where an input or the other output does, other than the input it may replace (at its own strides; that
+// of a dimension of one element does not matter).
+bool meets(void* const* out, const int64_t (*ost)[3], const void* const* own, const int64_t (*own_st)[3], const void* const* other,
+           int n, int k, const Shape& z) {
+  for (int j = 0; j < n; ++j) {
+    if (j != k && (out[k] == out[j] || out[k] == own[j])) return true;
+    if (other && out[k] == other[j]) return true;
+  }
+  return out[k] == own[k] && ((z.B > 1 && ost[k][0] != own_st[k][0]) || (z.H > 1 && ost[k][1] != own_st[k][1]) ||
+                              (z.N > 1 && ost[k][2] != own_st[k][2]));
+}
 
 int fill_args(RotaryArgs& a, int n_tensors, svgear_dtype dt, const Shape& z, const double* inv_freq,
               const int sections[3], const int64_t grid[3], int64_t first, const int32_t* positions,
@@ -607,7 +609,8 @@ extern "C" int svgear_rotary(int n_tensors, const void* const* src, const int64_
                              const int64_t grid[3], int64_t first, const int32_t* positions,
                              int64_t positions_stride_b, unsigned flags, float eps, void* stream) {
   RotaryArgs a{};
-  const int rc = fill_args(a, n_tensors, dt, Shape{B, H, N, n_tail, d}, inv_freq, sections, grid, first, positions,
+  const Shape z{B, H, N, n_tail, d};
+  const int rc = fill_args(a, n_tensors, dt, z, inv_freq, sections, grid, first, positions,
                            positions_stride_b, flags, eps);
   if (rc != SVGEAR_OK) return rc;
   if (!src || !sstride || !dst || !dstride) return SVGEAR_ERR_INVALID;
@@ -619,7 +622,7 @@ extern "C" int svgear_rotary(int n_tensors, const void* const* src, const int64_
     a.dst[k] = dst[k];
     a.weight[k] = weight ? weight[k] : nullptr;
     if (a.weight[k] && (!(flags & 3u) || reinterpret_cast<uintptr_t>(a.weight[k]) % 16)) return SVGEAR_ERR_INVALID;
-    if (meets(dst, dstride, src, sstride, nullptr, n_tensors, k)) return SVGEAR_ERR_INVALID;
+    if (meets(dst, dstride, src, sstride, nullptr, n_tensors, k, z)) return SVGEAR_ERR_INVALID;
     a.sst[k] = Strides{sstride[k][0], sstride[k][1], sstride[k][2]};
     a.dst_st[k] = Strides{dstride[k][0], dstride[k][1], dstride[k][2]};
   }
@@ -642,7 +645,8 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
                                       int64_t first, const int32_t* positions, int64_t positions_stride_b,
                                       unsigned flags, float eps, void* ws, size_t ws_bytes, void* stream) {
   RotaryArgs a{};
-  const int rc = fill_args(a, n_tensors, dt, Shape{B, H, N, n_tail, d}, inv_freq, sections, grid, first, positions,
+  const Shape z{B, H, N, n_tail, d};
+  const int rc = fill_args(a, n_tensors, dt, z, inv_freq, sections, grid, first, positions,
                            positions_stride_b, flags, eps);
   if (rc != SVGEAR_OK) return rc;
   const bool norm = flags & 3u;
@@ -664,11 +668,11 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
     a.dst_st[k] = Strides{dxstride[k][0], dxstride[k][1], dxstride[k][2]};
     if (norm) {
       if (!src[k] || !aligned_strides(sstride[k], esize(dt), src[k], B, H, N)) return SVGEAR_ERR_INVALID;
-      if (meets(dx, dxstride, dy, dystride, src, n_tensors, k)) return SVGEAR_ERR_INVALID;
+      if (meets(dx, dxstride, dy, dystride, src, n_tensors, k, z)) return SVGEAR_ERR_INVALID;
       a.src[k] = src[k];
       a.sst[k] = Strides{sstride[k][0], sstride[k][1], sstride[k][2]};
     } else {  // the forward kernel with the angles' signs turned
-      if (meets(dx, dxstride, dy, dystride, nullptr, n_tensors, k)) return SVGEAR_ERR_INVALID;
+      if (meets(dx, dxstride, dy, dystride, nullptr, n_tensors, k, z)) return SVGEAR_ERR_INVALID;
       a.src[k] = dy[k];
       a.sst[k] = a.yst[k];
     }

@@ -27,3 +27,27 @@ def test_a_residual_in_place_may_differ_where_a_stride_does_not_matter():
     assert linear(B=7, N=1, residual=0x200000, rst=(1700, 5)) == WORKSPACE  # one token of each
     assert linear(B=7, N=1, residual=0x200000, rst=(1701, 17)) == INVALID
     assert linear(B=2, residual=0x200000, rst=(1701, 17)) == INVALID
+
+
+def rotary(B=1, H=3, N=30, dst=0x100000, dst_st=(5760, 1920, 64), src_st=(5760, 1920, 64), back=False):
+    """In place, 64 elements a head, with a norm over the token; the backward pass wants dweight and has too little room for it. The
+    forward pass has no workspace: only what it refuses can be asked."""
+    lib = sv.load_library()
+    ptr = lambda p: (ctypes.c_void_p * 1)(p)
+    st = lambda s: (ctypes.c_int64 * 3)(*s)
+    places = (0x10000, (ctypes.c_int * 3)(10, 11, 11), (ctypes.c_int64 * 3)(2, 3, 5), 0, None, 0, 2, 1e-6)
+    if not back:
+        return lib.svgear_rotary(1, ptr(0x100000), st(src_st), ptr(dst), st(dst_st), None, BF16, B, H, N, 0, 64, *places, None)
+    return lib.svgear_rotary_backward(1, ptr(0x100000), st(src_st), ptr(0x400000), st(src_st), ptr(dst), st(dst_st), None, ptr(0x500000), BF16, B, H,
+                                      N, 0, 64, *places, 0x300000, 1, None)
+
+
+def test_rotary_in_place_at_other_strides():
+    for back in (False, True):
+        assert rotary(dst_st=(5760, 1920, 72), back=back) == INVALID
+        assert rotary(dst_st=(5760, 1928, 64), back=back) == INVALID
+        assert rotary(B=2, N=10, dst_st=(5768, 1920, 64), back=back) == INVALID
+    assert rotary(back=True) == WORKSPACE
+    assert rotary(dst_st=(7, 1920, 64), back=True) == WORKSPACE                                     # one batch entry
+    assert rotary(H=1, src_st=(5760, 5, 64), dst_st=(9, 1920, 64), back=True) == WORKSPACE            # and one head
+    assert rotary(N=1, src_st=(64, 1920, 3), dst_st=(64, 1920, 72), back=True) == WORKSPACE           # one token
