@@ -51,3 +51,20 @@ def test_rotary_in_place_at_other_strides():
     assert rotary(dst_st=(7, 1920, 64), back=True) == WORKSPACE                                     # one batch entry
     assert rotary(H=1, src_st=(5760, 5, 64), dst_st=(9, 1920, 64), back=True) == WORKSPACE            # and one head
     assert rotary(N=1, src_st=(64, 1920, 3), dst_st=(64, 1920, 72), back=True) == WORKSPACE           # one token
+
+
+def test_rotary_refuses_gradients_of_weights_over_other_tensors():
+    lib = sv.load_library()
+    pair = lambda *p: (ctypes.c_void_p * 2)(*p)
+    st = (ctypes.c_int64 * 6)(*(2 * [5760, 1920, 64]))
+    places = (0x10000, (ctypes.c_int * 3)(10, 11, 11), (ctypes.c_int64 * 3)(2, 3, 5), 0, None, 0, 2, 1e-6)
+    dy, src, dx, weight = (0x100000, 0x200000), (0x300000, 0x400000), (0x500000, 0x600000), (0x700000, 0x800000)
+
+    def call(*dweight):
+        return lib.svgear_rotary_backward(2, pair(*dy), st, pair(*src), st, pair(*dx), st, pair(*weight), pair(*dweight), BF16, 1, 3, 30, 0, 64,
+                                          *places, 0x900000, 1, None)
+
+    assert call(0xa00000, 0xb00000) == call(0xa00000, None) == call(None, 0xb00000) == WORKSPACE
+    assert call(0xa00000, 0xa00000) == INVALID
+    for other in dy + src + dx + weight:
+        assert call(other, 0xb00000) == INVALID and call(0xa00000, other) == INVALID, hex(other)
