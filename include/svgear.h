@@ -428,7 +428,7 @@ int svgear_rotary(int n_tensors, const void* const* src, const int64_t (*sstride
  *   dx[k]  [B,H,N,d] dt out, dxstride; may be dy[k] itself (same strides), no other overlap (one at
  *          the same address is refused)
  *   dweight[k] [d] or [H*d] dt out, as weight (the array, or an entry, NULL: not wanted); no overlap
- *          with any other tensor (one at the same address is refused)
+ *          with any other tensor (another output at the same address is refused)
  * Sums of dweight are fp32 and made in one fixed order. Alignment and limits as above; so is |dy weight|, whose products with x are
  * summed in fp32, up to 1e17.
  */

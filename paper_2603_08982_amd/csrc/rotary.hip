@@ -677,12 +677,9 @@ extern "C" int svgear_rotary_backward(int n_tensors, const void* const* dy, cons
       a.sst[k] = a.yst[k];
     }
   }
-  for (int k = 0; any && k < n_tensors; ++k) {  // (there is a norm, and src)
-    if (!dweight[k]) continue;
+  for (int k = 0; any && k < n_tensors; ++k)
     for (int j = 0; j < n_tensors; ++j)
-      if (dweight[k] == dy[j] || dweight[k] == src[j] || dweight[k] == dx[j] || dweight[k] == a.weight[j] || (j != k && dweight[k] == dweight[j]))
-        return SVGEAR_ERR_INVALID;
-  }
+      if (dweight[k] && (dweight[k] == dx[j] || (j != k && dweight[k] == dweight[j]))) return SVGEAR_ERR_INVALID;
   a.sign = -1.f;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Workspace w(ws, ws_bytes);
