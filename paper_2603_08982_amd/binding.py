@@ -777,11 +777,14 @@ def attention_block(x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor, i
     H, d = init_q.shape[1], init_q.shape[3]
     _require(w_qkv.shape[0] == 3 * H * d and w_out.shape[1] == H * d, "w_qkv: expected [3*H*d,c], w_out: [c_out,H*d]")
     _require("out" not in layer, "the layer's output is the block's own")
-    qkv, _ = linear(x, w_qkv, b_qkv)
-    q, k, v = qkv.view(B, N, 3, H, d).permute(2, 0, 3, 1, 4)
-    rotary([q, k], inv_freq, sections, grid=grid, first=first, positions=positions, n_tail=n_tail, norm=norm,
-           weights=norm_weights, eps=eps, halves=halves, out=[q, k])
-    o = torch.empty(B, N, H, d, dtype=x.dtype, device=x.device)
-    _, r = attention_layer(q, k, v, init_q, init_k, iters, budget_cost, n_tail, out=o.transpose(1, 2), **layer)
-    y, _ = linear(o.view(B, N, H * d), w_out, b_out, gate=gate, residual=residual)
-    return y, r
+    _need_gpu(x)
+    _require(init_q.device == init_k.device == x.device, "init_q, init_k: expected on x's device")
+    with _on_device(x.device):
+        qkv, _ = linear(x, w_qkv, b_qkv)
+        q, k, v = qkv.view(B, N, 3, H, d).permute(2, 0, 3, 1, 4)
+        rotary([q, k], inv_freq, sections, grid=grid, first=first, positions=positions, n_tail=n_tail, norm=norm,
+               weights=norm_weights, eps=eps, halves=halves, out=[q, k])
+        o = torch.empty(B, N, H, d, dtype=x.dtype, device=x.device)
+        _, r = attention_layer(q, k, v, init_q, init_k, iters, budget_cost, n_tail, out=o.transpose(1, 2), **layer)
+        y, _ = linear(o.view(B, N, H * d), w_out, b_out, gate=gate, residual=residual)
+        return y, r

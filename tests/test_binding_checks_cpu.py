@@ -146,3 +146,42 @@ def test_rotary_of_the_largest_sizes_goes_on(no_device, back):
                dict(positions=torch.empty(24, 3, dtype=torch.int32, device="meta"), first=1 << 64)):
         with pytest.raises(Reached):
             rotary_call(back, **kw)
+
+
+def test_block_runs_on_its_tensors_device(monkeypatch):
+    """Every call of the block, the layer's too, is made with x's device as the current one."""
+    import contextlib
+
+    seen, current = [], []
+
+    @contextlib.contextmanager
+    def on(device):
+        current.append(device)
+        yield
+        current.pop()
+
+    def linear(x, w, *a, **kw):
+        seen.append(("linear", tuple(current)))
+        return x.new_empty(*x.shape[:-1], w.shape[0]), None
+
+    def layer(q, k, v, *a, **kw):
+        seen.append(("attention_layer", tuple(current)))
+        return None, {}
+
+    monkeypatch.setattr(binding, "_need_gpu", lambda *ts: None)
+    monkeypatch.setattr(binding, "_on_device", on)
+    monkeypatch.setattr(binding, "linear", linear)
+    monkeypatch.setattr(binding, "rotary", lambda *a, **kw: seen.append(("rotary", tuple(current))))
+    monkeypatch.setattr(binding, "attention_layer", layer)
+    x, c = meta(1, 24, 32), meta(1, 2, 3, 64, dtype=torch.float32)
+    y, _ = sv.attention_block(x, meta(3 * 128, 32), meta(40, 128), c, c, 1, 100, meta(32, dtype=torch.float64), (10, 11, 11), grid=(2, 3, 4))
+    assert y.shape == (1, 24, 40)
+    assert seen == [(name, (x.device,)) for name in ("linear", "rotary", "attention_layer", "linear")]
+    assert not current
+
+
+def test_block_refuses_centroids_of_another_device(no_device):
+    x, c = meta(1, 24, 32), meta(1, 2, 3, 64, dtype=torch.float32)
+    for q, k in ((torch.zeros(1, 2, 3, 64), c), (c, torch.zeros(1, 2, 3, 64))):
+        with pytest.raises(sv.SvgearError):
+            sv.attention_block(x, meta(3 * 128, 32), meta(40, 128), q, k, 1, 100, meta(32, dtype=torch.float64), (10, 11, 11), grid=(2, 3, 4))
