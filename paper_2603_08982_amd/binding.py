@@ -178,6 +178,13 @@ def kmeans_list_threshold(min_centroids: int = 0) -> int:
     return int(lib.svgear_kmeans_list_threshold(int(min_centroids)))
 
 
+def _check_centroids(c: torch.Tensor, B: int, H: int, d: int, device: torch.device):
+    """Starting centroids, which are written: those of every head of what is clustered."""
+    if not (c.dim() == 4 and c.shape[:2] == (B, H) and c.shape[3] == d and c.dtype == torch.float32 and c.is_contiguous()
+            and c.device == device):
+        raise SvgearError(f"centroids: expected dense fp32 [{B},{H},C,{d}] on {device}")
+
+
 def kmeans(x: torch.Tensor, centroids: torch.Tensor, iters: int, n_tail: int = 0,
            x2: Optional[torch.Tensor] = None, one_launch: bool = True):
     """svgear_kmeans (one_launch=False: svgear_kmeans_stepwise, the same results with launches of its own for
@@ -186,8 +193,8 @@ def kmeans(x: torch.Tensor, centroids: torch.Tensor, iters: int, n_tail: int = 0
     _need_gpu(x, centroids, x2)
     lib = load_library()
     B, H, N, d = x.shape
+    _check_centroids(centroids, B, H, d, x.device)
     C = centroids.shape[2]
-    assert centroids.dtype == torch.float32 and centroids.is_contiguous()
     if x2 is not None:
         assert x2.shape == x.shape and x2.stride() == x.stride() and x2.dtype == x.dtype
     labels = torch.empty(B, H, N - n_tail, dtype=torch.int32, device=x.device)
@@ -709,8 +716,10 @@ def attention_layer(Q, K, V, init_q, init_k, iters: int, budget_cost: int, n_tai
     "attention", "unpermute"). O is written into `out` if given ([B,H,N,d] as Q, any strides with contiguous d, over none
     of Q, K and V). Returns (O, intermediates)."""
     B, H, N, d = Q.shape
+    _need_gpu(Q, K, init_q, init_k, out)
+    _check_centroids(init_q, B, H, d, Q.device)
+    _check_centroids(init_k, B, H, d, Q.device)  # and K's, which kmeans holds it to
     if out is not None:
-        _need_gpu(Q, out)
         _check_out(out, Q)
     if scale is None:
         scale = float(d) ** -0.5
@@ -778,7 +787,8 @@ def attention_block(x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor, i
     _require(w_qkv.shape[0] == 3 * H * d and w_out.shape[1] == H * d, "w_qkv: expected [3*H*d,c], w_out: [c_out,H*d]")
     _require("out" not in layer, "the layer's output is the block's own")
     _need_gpu(x)
-    _require(init_q.device == init_k.device == x.device, "init_q, init_k: expected on x's device")
+    for c in (init_q, init_k):
+        _check_centroids(c, B, H, d, x.device)
     with _on_device(x.device):
         qkv, _ = linear(x, w_qkv, b_qkv)
         q, k, v = qkv.view(B, N, 3, H, d).permute(2, 0, 3, 1, 4)

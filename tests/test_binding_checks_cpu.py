@@ -185,3 +185,29 @@ def test_block_refuses_centroids_of_another_device(no_device):
     for q, k in ((torch.zeros(1, 2, 3, 64), c), (c, torch.zeros(1, 2, 3, 64))):
         with pytest.raises(sv.SvgearError):
             sv.attention_block(x, meta(3 * 128, 32), meta(40, 128), q, k, 1, 100, meta(32, dtype=torch.float64), (10, 11, 11), grid=(2, 3, 4))
+
+
+BAD_CENTROIDS = [(2, 2, 3, 64), (1, 1, 3, 64), (1, 2, 3, 128), (2, 3, 64)]
+
+
+@pytest.mark.parametrize("shape", BAD_CENTROIDS, ids=str)
+def test_kmeans_refuses_centroids_of_other_heads(no_library, shape):
+    """They are written, [B,H,C,d] of them."""
+    x = torch.zeros(*OP)
+    with pytest.raises(sv.SvgearError):
+        sv.kmeans(x, torch.zeros(*shape), 1)
+    with pytest.raises(Reached):
+        sv.kmeans(x, torch.zeros(1, 2, 3, 64), 1)
+
+
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("shape", BAD_CENTROIDS, ids=str)
+def test_layer_and_block_refuse_centroids_of_other_heads(no_device, shape, which):
+    """Before anything is launched: the queries' k-means would have changed its centroids."""
+    q, good, bad = torch.zeros(*OP), torch.zeros(1, 2, 3, 64), torch.zeros(*shape)
+    init = (bad, good) if which == 0 else (good, bad)
+    with pytest.raises(sv.SvgearError):
+        sv.attention_layer(q, q, q, *init, 1, 100, overlap=False)
+    x, w, o, f = torch.zeros(1, 24, 32), torch.zeros(3 * 128, 32), torch.zeros(40, 128), torch.zeros(32, dtype=torch.float64)
+    with pytest.raises(sv.SvgearError):
+        sv.attention_block(x, w, o, *init, 1, 100, f, (10, 11, 11), grid=(2, 3, 4))
