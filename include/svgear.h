@@ -319,7 +319,8 @@ int svgear_unpermute(const void* op, const int32_t* perm, svgear_dtype dt, int B
  * bias, gate, residual and pre may be NULL (0, 1, 0, not wanted). Products of bf16 values are
  * exact in fp32 and summed in fp32 (fp32 inputs: fp32 products and sums on the fp32 matrix
  * cores); bias, activation, gate and residual are applied in fp32; y and pre are each rounded
- * once. Results do not depend on the stream, on other calls or on what the workspace holds.
+ * once. Results do not depend on the stream, on other calls, on where the operands lie (address,
+ * strides) or on what the workspace holds.
  *   x        [B,N,d_in] dt, element strides xstride = {stride_b, stride_n}, d_in contiguous
  *   w        [d_out,d_in] dt, rows w_stride elements apart (>= d_in)
  *   bias     [d_out] dt

@@ -294,7 +294,10 @@ int launch(const LinearArgs& a, svgear_dtype dt, int form, hipStream_t s) {
 struct Plan {
   int tile, splits;
 };
-// element: by_element's rows, for which there are tiles of 32 and 64 alone.
+// element: by_element's rows, for which there are tiles of 32 and 64 alone. K is cut for them as for aligned rows, so that results
+// do not depend on where the weights lie (every tile adds a part's products in one order). That costs something where aligned
+// rows have tiles of 128, some 2 % of the sizes of 9 to 256 rows (200 rows, 8,192 in, 5,120 out at an odd address, in 4 parts and
+// in 3: 212 and 222 us; 100 rows, 20,480 in, 8,192 out, 2 and 8: 391 and 420).
 Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form, bool element) {
   if (form == kContractBoth && R <= few_rows(dt)) return Plan{0, 1};
   struct Kind {
@@ -310,7 +313,6 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form, bo
   for (int i = 0; i < 3; ++i) {
     const Kind& k = kinds[i];
     if (k.rows == 32 && (R > 32 || form == kContractNone)) continue;
-    if (k.rows == 128 && element) continue;
     const int64_t tiles = ceil_div(R, k.rows) * ceil_div(C, k.cols);
     for (int p = 1; p <= 16 && (p == 1 || (steps >= 4 * p && tiles < 1024)); ++p) {
       const double m = (double)ceil_div(tiles * p, 256), each = m * k.step;
@@ -322,6 +324,7 @@ Plan plan_product(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form, bo
       }
     }
   }
+  if (element && best.tile == 128) best.tile = 64;
   return best;
 }
 size_t parts_bytes(int64_t R, int64_t C, int64_t K, svgear_dtype dt, int form, bool element) {
