@@ -41,3 +41,32 @@ def test_bits_do_not_depend_on_alignment(size, dtype):
             assert torch.equal(aligned[name], got[name]), (name, lead)
     only_w = sv.linear(x, moved(w, 1), b, act="silu", gate=g, residual=r)[0]
     assert torch.equal(aligned["y"], only_w)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("size", [(2, 2, 64, 40), (3, 1, 72, 136), (2, 100, 136, 72), (2, 300, 131, 67)], ids=str)
+def test_bits_do_not_depend_on_strides(size, dtype):
+    """Batches within tokens, tokens and batches far apart, and one row (stride 0) for a whole batch entry or call."""
+    B, N, k, o = size
+    x, w, b, g, r = inputs(dtype, B, N, k, o, True, "token", True, seed=B * N)
+    dy = rand(B, N, o, seed=9, dtype=dtype).cuda()
+
+    def far(t):
+        big = torch.full((t.shape[0], t.shape[1], (1 << 21) + 8), float("nan"), dtype=t.dtype, device="cuda")
+        big[..., :t.shape[2]] = t
+        return big[..., :t.shape[2]]
+
+    def calls(x, g, r, dy):
+        y, pre = sv.linear(x, w, b, act="silu", gate=g, residual=r, want_pre=True)
+        grads = sv.linear_backward(dy, x, w, pre=pre, act="silu", gate=g, want=["dx", "dw", "dbias"] + (["dgate"] if g.stride(1) else []))
+        plain = sv.linear_backward(dy, x, w, want=["dx", "dw"])
+        return {"y": y, "pre": pre, **grads, **{"plain " + n: t for n, t in plain.items()}}
+
+    inner = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)
+    one_of_each = lambda t: t[:, :1].expand(-1, N, -1)
+    one = lambda t: t[:1, :1].expand(B, N, -1)
+    for place in (inner, far, one_of_each, one):
+        args = [place(t) for t in (x, g, r, dy)]
+        want, got = calls(*[t.contiguous() for t in args]), calls(*args)
+        for name in got:
+            assert torch.equal(want[name], got[name]), name
