@@ -367,6 +367,8 @@ int svgear_linear(const void* x, const int64_t xstride[2], const void* w, int64_
  * be NULL otherwise. x is read for dw only and may be NULL without it, w for dx only.
  * bf16: dz is rounded to bf16 for the two products, whose sums are fp32; the sums of dbias and
  * dgate take it before that rounding. All sums are made in one fixed order.
+ * The workspace has room for dz and for the partial sums of dbias and dgate, and for x's and w's copies where x and w are
+ * given, whichever gradients are wanted.
  *   dy    [B,N,d_out] dt, dystride;  pre [B,N,d_out] dt dense;  x, w, gate as above
  *   dx    [B,N,d_in] dt out, dxstride;  dw [d_out,d_in] dt out dense;  dbias [d_out] dt out
  * No output may overlap an input or another output (one at the same address is refused).
@@ -398,8 +400,8 @@ int svgear_linear_backward(const void* dy, const int64_t dystride[2], const void
  * batch) or [B,N-n_tail,3] (its element stride); or, with positions NULL, token n is element
  * first + n of a grid of grid[0] x grid[1] x grid[2] (time, height, width; the last index
  * fastest), for a share of a sequence or a single token of it: first + N - n_tail <= the
- * grid's size < 2^31. Angles are computed in fp64 and reduced to one turn before cos and sin, so
- * far positions lose nothing; all else is fp32, rounded once at the end. Squares are summed in
+ * grid's size < 2^31. One token at least is rotated: 0 <= n_tail < N. Angles are computed in fp64
+ * and reduced to one turn before cos and sin, so far positions lose nothing; all else is fp32, rounded once at the end. Squares are summed in
  * fp32: |x| up to 1e17, and with eps = 0 a root mean square from 1e-17 on. With eps = 0 a row of zeros gives NaN.
  *   src[k], dst[k]  [B,H,N,d] dt, element strides sstride[k], dstride[k]; 16-byte aligned, strides
  *                   multiples of 16 bytes, d = 64 or 128. dst[k] may be src[k] itself (same

