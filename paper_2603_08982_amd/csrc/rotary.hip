@@ -19,8 +19,9 @@ constexpr int64_t kMaxTokens = 1 << 30;
 constexpr int kRotWaves = 8;  // waves of a workgroup, at most; of the backward pass in bf16 up to 64 heads of 128:
 constexpr int kRotBackWaves = 16;
 // Workgroups of the backward pass, at most; each leaves a partial dweight. One on each CU, three tokens of 40 heads of 128 at a
-// time (15 waves, all that its registers allow): two tensors of 75,600 tokens take 1,014 us; two on each of one token (five
-// waves: a third does not fit the four SIMDs) 1,052, and with 768 to 1,536 of these, a part of which waits, 1,271 to 1,396.
+// time (15 waves, all that its registers allow): two tensors of 75,600 tokens take 1,019 us (1,014 with a multiplication an element
+// less, as the rest of these); two on each of one token (five waves: a third does not fit the four SIMDs) 1,052, and with 768 to
+// 1,536 of these, a part of which waits, 1,271 to 1,396.
 constexpr int kBackwardGroups = 256;
 
 struct RotaryArgs {
