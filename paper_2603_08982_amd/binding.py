@@ -544,8 +544,21 @@ def rotary_frequencies(sections: Sequence[int], theta: float = 10000.0, device="
 
 _PTRS = (None, _vp * 1, _vp * 2)
 _STRIDES = (None, _c.c_int64 * 3, _c.c_int64 * 6)  # int64_t[n][3], one behind the other
-_sections = functools.lru_cache(maxsize=64)(lambda *s: _Ix3(*s))
-_grid = functools.lru_cache(maxsize=64)(lambda *g: _I64x3(*g))
+
+
+# (looked at once: what is kept is in range)
+@functools.lru_cache(maxsize=64)
+def _sections(*s):
+    if len(s) != 3 or min(s) < 0 or max(s) > 64:
+        raise SvgearError("sections: pairs of the three axes")
+    return _Ix3(*s)
+
+
+@functools.lru_cache(maxsize=64)
+def _grid(*g):
+    if len(g) != 3 or min(g) < 1 or max(g) >= _GRID:
+        raise SvgearError("grid: (time, height, width)")
+    return _I64x3(*g)
 
 
 def _pointers(ts):
@@ -571,8 +584,7 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
     if not (0 < B * N <= _MOST_ROWS and 0 < H <= _MOST_HEADS and (d == 64 or d == 128) and 0 <= n_tail < N):
         raise SvgearError(f"[B,H,N,d] = {tuple(t0.shape)}, {n_tail} text tokens: expected 1 to 2^30 tokens, some of them rotated, of 1 to "
                           "128 heads of 64 or 128")
-    if len(sections) != 3 or min(sections) < 0 or max(sections) > d // 2:
-        raise SvgearError("sections: pairs of the three axes")
+    sections3 = _sections(*sections)
     if norm not in ROTARY_NORMS:
         raise SvgearError('norm: None, "head" or "token"')
     if (inv_freq.device != t0.device or inv_freq.dtype != torch.float64 or inv_freq.shape != (sum(sections),)
@@ -589,9 +601,9 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
         if len(shape) == 3:
             pos_b = 3 * shape[1]
     else:
-        if len(grid) != 3 or min(grid) < 1 or max(grid) >= _GRID or not 0 <= first < _GRID:
-            raise SvgearError("grid: (time, height, width), first: a token of it")
         size3 = _grid(*grid)
+        if not 0 <= first < _GRID:
+            raise SvgearError("first: a token of the grid")
     if weights is None:
         weights = (None,) * len(tensors)
     else:
@@ -601,7 +613,7 @@ def _rotary_places(tensors, inv_freq, sections, grid, first, positions, n_tail, 
         for w in weights:
             if w is not None and (w.shape != (size,) or not w.is_contiguous()):
                 raise SvgearError("weights: expected [d] or [H*d]")
-    return weights, (inv_freq.data_ptr(), _sections(*sections), size3, 0 if size3 is None else first, _ptr(positions), pos_b,
+    return weights, (inv_freq.data_ptr(), sections3, size3, 0 if size3 is None else first, _ptr(positions), pos_b,
                      ROTARY_NORMS[norm] | (ROTARY_HALVES if halves else 0))
 
 
