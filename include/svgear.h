@@ -19,6 +19,8 @@
  *                            bias, activation, gate and residual in its epilogue
  *   svgear_rotary            RMS norm of queries and keys and their rotation by the token's
  *                            (time, height, width) position
+ *   svgear_layer_norm        the layer norm in front, modulated by a scale and a shift
+ *   svgear_attention         dense attention with masks: to text tokens, of packed clips, in order
  *
  * each with its backward pass.
  *
@@ -443,6 +445,107 @@ int svgear_rotary_backward(int n_tensors, const void* const* dy, const int64_t (
                            const int sections[3], const int64_t grid[3], int64_t first, const int32_t* positions,
                            int64_t positions_stride_b, unsigned flags, float eps, void* ws, size_t ws_bytes,
                            void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * layer norm with modulation:
+ *
+ *   h = (x - mean(x)) / sqrt(mean((x - mean)^2) + eps) over the c elements of a token
+ *   y = (h * weight + bias) * (1 + scale) + shift
+ *
+ * weight and bias [c], scale and shift may each be NULL (1, 0, 0, 0). Everything is fp32 from the loads on, the squares summed
+ * around the mean, and y rounded once.
+ *   x     [B,N,c] dt, element strides xstride = {stride_b, stride_n}, c contiguous
+ *   scale, shift  [B,N,c] dt, sstride, hstride; a stride_n of 0 is one row for all tokens of a batch entry (the
+ *         modulation of a diffusion transformer), a stride_b of 0 one for the whole call
+ *   y     [B,N,c] dt out, ystride; may be x itself (same pointer, same strides), no other overlap of an output with an input or
+ *         another output is allowed (one at the same address is refused)
+ * B, N >= 1, B*N <= 2^30, 1 <= c <= 2^15; strides from 0 to 2^48, those of y such that no two rows meet (the stride of a dimension
+ * of one element does not matter); any alignment that the type has. |x| up to 1e17; with eps = 0 a row of equal values gives NaN.
+ * No workspace.
+ */
+int svgear_layer_norm(const void* x, const int64_t xstride[2], const void* weight, const void* bias, const void* scale,
+                      const int64_t sstride[2], const void* shift, const int64_t hstride[2], svgear_dtype dt, int B,
+                      int64_t N, int c, float eps, void* y, const int64_t ystride[2], void* stream);
+
+/* The gradients of svgear_layer_norm for the output's gradient dy:
+ *
+ *   du = dy (1 + scale), g = du weight, dx = (g - mean(g) - h mean(g h)) / sqrt(var + eps)
+ *   dweight = sum of du h, dbias = sum of du over all tokens
+ *   dscale = dy (h weight + bias), dshift = dy; with SVGEAR_NORM_BATCH summed over the tokens of a batch entry
+ *
+ * Any of dx, dweight, dbias, dscale, dshift may be NULL, not all. `modulation` says whose scale and shift were: of nobody
+ * (scale, dscale and dshift NULL), of batch entries (scale's stride_n 0; dscale, dshift [B,c] dense, one row for each entry also
+ * where scale's stride_b is 0), of tokens (dscale, dshift [B,N,c] dense). bias is read for dscale alone. Sums are fp32 and made
+ * in one fixed order; every output is rounded once. The workspace is used where dweight, dbias or the sums of SVGEAR_NORM_BATCH are
+ * wanted.
+ *   dy [B,N,c] dt, dystride;  dx [B,N,c] dt out, dxstride; dx may be dy itself (same strides), no other overlap (one at the
+ *   same address is refused)
+ */
+#define SVGEAR_NORM_PLAIN 0
+#define SVGEAR_NORM_BATCH 1
+#define SVGEAR_NORM_TOKEN 2
+size_t svgear_layer_norm_backward_workspace(svgear_dtype dt, int B, int64_t N, int c, int modulation);
+int svgear_layer_norm_backward(const void* dy, const int64_t dystride[2], const void* x, const int64_t xstride[2],
+                               const void* weight, const void* bias, const void* scale, const int64_t sstride[2],
+                               int modulation, svgear_dtype dt, int B, int64_t N, int c, float eps, void* dx,
+                               const int64_t dxstride[2], void* dweight, void* dbias, void* dscale, void* dshift, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * dense attention with masks: every query over all keys that it sees. For the text tokens of a prompt, clips packed
+ * one behind the other, generation in order; the layer above is the sparse one.
+ *
+ *   s_ij = scale q_i.k_j;  with cap > 0 s_ij = cap tanh(s_ij / cap);  with slopes s_ij -= slopes[h] |p_i - j|
+ *   o_i = sum_j e^(s_ij) v_j / sum_j e^(s_ij) over the keys j that i sees,  lse_i = ln of that denominator
+ *
+ * Query head h reads key head h / (H / Hk). Document t of a batch entry is its queries [q_offsets[t], q_offsets[t+1]) and keys
+ * [k_offsets[t], k_offsets[t+1]); a query sees keys of its own document alone. With n queries and m keys in it, query i (from 0)
+ * stands at key position p_i = i + m - n: the last query at the last key, new tokens behind a past. With
+ * SVGEAR_ATTENTION_CAUSAL it sees the keys j <= p_i and those before the document's prefix; otherwise all. A query that sees no
+ * key (of no document, of one without keys, before the first key) has o = 0 and lse = -inf. K and V rows of no document,
+ * and keys behind the last that a tile of 128 queries sees, are not read.
+ *   q [B,H,Nq,d], k, v [B,Hk,Nk,d] dt, element strides qstride.. = {stride_b, stride_h, stride_n}, d contiguous
+ *   slopes    [H] fp32 or NULL
+ *   q_offsets, k_offsets  [B,n_docs+1] int32, ascending from 0 on within the rows (what is not is taken as the nearest
+ *             row; nothing out of range is read); NULL: one document of all rows. n_docs is 0 where both are, 1 where
+ *             one is (padded texts: k_offsets alone, {0, length})
+ *   prefix    [B,max(n_docs,1)] int32 or NULL, with SVGEAR_ATTENTION_CAUSAL only
+ *             (SVGEAR_ATTENTION_SHARED_DOCUMENTS: one row of offsets and prefixes for all batch entries)
+ *   o [B,H,Nq,d] dt out, ostride;  lse [B,H,Nq] fp32 out dense, or NULL
+ * bf16: products and sums in fp32, the weights e^(s - running maximum) rounded to bf16 for the product with v, o rounded once.
+ * fp32: everything in fp32. Results do not depend on the stream, on other calls or on where tensors lie.
+ * d = 64 or 128; Hk divides H; tensors 16-byte aligned, strides multiples of 16 bytes from 0 to 2^48 (that of a dimension of one
+ * element does not matter), those of o such that no two rows meet; no output at the address of another tensor of the call.
+ * Nq H / Hk, Nk, B H <= 2^30; n_docs <= 2^20. Where B Hk ceil(Nq H / Hk / 128) tiles of queries are fewer than 256, the keys are
+ * cut into parts, up to 64, whose results lie in the workspace: parts * B*H*Nq * (4 d + 8) bytes. Where it is 0, ws may be NULL.
+ */
+#define SVGEAR_ATTENTION_CAUSAL 1u
+#define SVGEAR_ATTENTION_SHARED_DOCUMENTS 2u
+size_t svgear_attention_workspace(svgear_dtype dt, int B, int H, int Hk, int64_t Nq, int64_t Nk, int d, int n_docs);
+int svgear_attention(const void* q, const int64_t qstride[3], const void* k, const int64_t kstride[3], const void* v,
+                     const int64_t vstride[3], svgear_dtype dt, int B, int H, int Hk, int64_t Nq, int64_t Nk, int d,
+                     float scale, float cap, const float* slopes, unsigned flags, int n_docs, const int32_t* q_offsets,
+                     const int32_t* k_offsets, const int32_t* prefix, void* o, const int64_t ostride[3], float* lse, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* The gradients of svgear_attention for the output's gradient dy, from what it returned (o, lse):
+ *
+ *   p_ij = e^(s_ij - lse_i),  ds_ij = p_ij (dy_i.v_j - dy_i.o_i), with a cap times 1 - tanh^2
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dy_i
+ *
+ * summed over the query heads that share a key head. dq may be NULL, or dk and dv both. Rows that see nothing, or are seen by
+ * nothing, get zeros. No gradient of the slopes. bf16: p and ds are rounded to bf16 for the products, whose sums are fp32. All
+ * sums are made in one fixed order, without atomics. Arguments as above; dy, o [B,H,Nq,d], strided; dq, dk, dv as q, k, v, strided.
+ * The workspace holds dy_i.o_i and partial sums.
+ */
+size_t svgear_attention_backward_workspace(svgear_dtype dt, int B, int H, int Hk, int64_t Nq, int64_t Nk, int d, int n_docs);
+int svgear_attention_backward(const void* dy, const int64_t dystride[3], const void* q, const int64_t qstride[3], const void* k,
+                              const int64_t kstride[3], const void* v, const int64_t vstride[3], const void* o,
+                              const int64_t ostride[3], const float* lse, svgear_dtype dt, int B, int H, int Hk, int64_t Nq,
+                              int64_t Nk, int d, float scale, float cap, const float* slopes, unsigned flags, int n_docs,
+                              const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* prefix, void* dq,
+                              const int64_t dqstride[3], void* dk, const int64_t dkstride[3], void* dv,
+                              const int64_t dvstride[3], void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,10 @@ from .binding import (  # noqa: F401
     rotary,
     rotary_backward,
     rotary_frequencies,
+    layer_norm,
+    layer_norm_backward,
+    attention,
+    attention_backward,
     run_pair,
     EXPORTED_SYMBOLS,
     PROBE_PLAIN,

@@ -32,11 +32,14 @@ EXPORTED_SYMBOLS = [
     "svgear_unpermute",
     "svgear_linear_workspace", "svgear_linear", "svgear_linear_backward_workspace", "svgear_linear_backward",
     "svgear_rotary", "svgear_rotary_backward_workspace", "svgear_rotary_backward",
+    "svgear_layer_norm", "svgear_layer_norm_backward_workspace", "svgear_layer_norm_backward",
+    "svgear_attention_workspace", "svgear_attention", "svgear_attention_backward_workspace", "svgear_attention_backward",
 ]
 
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
 ROTARY_NORMS = {None: 0, "head": 1, "token": 2}
 ROTARY_HALVES = 4
+ATTENTION_CAUSAL, ATTENTION_SHARED_DOCUMENTS = 1, 2
 
 _c = ctypes
 _vp, _i, _i64, _sz, _f, _u = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_size_t, _c.c_float, _c.c_uint
@@ -125,6 +128,22 @@ def load_library():
     lib.svgear_rotary_backward.restype = _i
     lib.svgear_rotary_backward.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i64, _i64, _i, *places, _vp, _sz,
                                            _vp]
+    lib.svgear_layer_norm.restype = _i
+    lib.svgear_layer_norm.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i64, _i, _f, _vp, _vp, _vp]
+    lib.svgear_layer_norm_backward_workspace.restype = _sz
+    lib.svgear_layer_norm_backward_workspace.argtypes = [_i, _i, _i64, _i, _i]
+    lib.svgear_layer_norm_backward.restype = _i
+    lib.svgear_layer_norm_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i64, _i, _f, _vp, _vp, _vp, _vp, _vp,
+                                               _vp, _vp, _sz, _vp]
+    sizes, mask = [_i, _i, _i, _i, _i64, _i64, _i], [_f, _f, _vp, _u, _i, _vp, _vp, _vp]
+    lib.svgear_attention_workspace.restype = _sz
+    lib.svgear_attention_workspace.argtypes = [*sizes, _i]
+    lib.svgear_attention.restype = _i
+    lib.svgear_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, *sizes, *mask, _vp, _vp, _vp, _vp, _sz, _vp]
+    lib.svgear_attention_backward_workspace.restype = _sz
+    lib.svgear_attention_backward_workspace.argtypes = [*sizes, _i]
+    lib.svgear_attention_backward.restype = _i
+    lib.svgear_attention_backward.argtypes = [_vp] * 11 + [*sizes, *mask] + [_vp] * 7 + [_sz, _vp]
     _LIB = lib
     return lib
 
@@ -440,13 +459,14 @@ def _as_bnd(t: torch.Tensor, what: str):
     return shape[0], shape[1], shape[2], _I64x2(st[0], st[1])
 
 
-def _gate_strides(gate, lead, d_out: int):
-    """Strides of a gate of tokens (lead + (d_out,)) or of batch entries (without the tokens' axis), and whether it is the first."""
+def _gate_strides(gate, lead, d_out: int, what: str = "gate", width: str = "d_out"):
+    """Strides of a gate (or another vector for each token) of tokens (lead + (d_out,)) or of batch entries (without the tokens' axis), and whether it is the first."""
     if gate is None:
         return _NO_ROWS, False
     per_token = gate.dim() == len(lead) + 1
-    _require(tuple(gate.shape) == (*lead, d_out) or tuple(gate.shape) == (*lead[:-1], d_out), "gate: expected [B,N,d_out] or [B,d_out] ([N,d_out] or [d_out] for one batch entry)")
-    _require(d_out == 1 or gate.stride(-1) == 1, "gate: expected contiguous d_out")
+    _require(tuple(gate.shape) == (*lead, d_out) or tuple(gate.shape) == (*lead[:-1], d_out),
+             f"{what}: expected [B,N,{width}] or [B,{width}] ([N,{width}] or [{width}] for one batch entry)")
+    _require(d_out == 1 or gate.stride(-1) == 1, f"{what}: expected contiguous {width}")
     if per_token:
         return _I64x2(gate.stride(0) if len(lead) == 2 else 0, gate.stride(-2)), True
     return _I64x2(gate.stride(0) if len(lead) == 2 else 0, 0), False
@@ -674,6 +694,160 @@ def rotary_backward(grads: Sequence[torch.Tensor], tensors: Optional[Sequence[to
                                         *places, float(eps), *space, _stream_of(g0.device))
     _check(rc, "svgear_rotary_backward")
     return outs, dweight
+
+
+def _norm_arguments(x, weight, bias, scale, shift, eps: float):
+    """The checked arguments that layer_norm and its backward pass share: (B, N, c, x's strides, strides of scale, of shift, whether
+    either is one of tokens)."""
+    B, N, c, xst = _as_bnd(x, "x")
+    _require(0 < B * N <= _MOST_ROWS and 0 < c <= 1 << 15, f"{B} x {N} tokens of {c}: expected 1 to 2^30 tokens of 1 to 2^15 each")
+    for w in (weight, bias):
+        if w is not None and (w.shape != (c,) or not w.is_contiguous()):
+            raise SvgearError("weight, bias: expected [c]")
+    _require(0.0 <= eps < float("inf"), "eps: expected a number from 0 on")
+    places, of_tokens = [], []
+    for m, what in ((scale, "scale"), (shift, "shift")):
+        st, per_token = _gate_strides(m, x.shape[:-1], c, what, "c")
+        places.append(st)
+        of_tokens.append(per_token and m is not None)
+    _require(scale is None or shift is None or of_tokens[0] == of_tokens[1], "scale and shift: both of batch entries or both of tokens")
+    return B, N, c, xst, places[0], places[1], any(of_tokens)
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               scale: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               out: Optional[torch.Tensor] = None):
+    """svgear_layer_norm: (h * weight + bias) * (1 + scale) + shift for h = (x - mean) / sqrt(var + eps) over the last dimension.
+    x [B,N,c] (or [N,c], one batch entry); weight, bias [c]; scale, shift [B,c] (one for all tokens of a batch entry) or
+    [B,N,c]. `out` may be x. Not a part of torch's graph of gradients: layer_norm_backward is called for them."""
+    dt = _same_place(x, weight, bias, scale, shift, out)
+    lib = load_library()
+    B, N, c, xst, sst, hst, _ = _norm_arguments(x, weight, bias, scale, shift, eps)
+    if out is not None and out.shape != x.shape:
+        raise SvgearError("out: expected x's shape")
+    with _on_device(x.device):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        rc = lib.svgear_layer_norm(x.data_ptr(), xst, _ptr(weight), _ptr(bias), _ptr(scale), sst, _ptr(shift), hst, dt, B, N, c,
+                                   float(eps), y.data_ptr(), _as_bnd(y, "out")[3], _stream_of(x.device))
+    _check(rc, "svgear_layer_norm")
+    return y
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                        scale: Optional[torch.Tensor] = None, eps: float = 1e-6, want: Sequence[str] = ("dx",)):
+    """svgear_layer_norm_backward: the gradients named in `want` ("dx", "dweight", "dbias", "dscale", "dshift") of layer_norm() for
+    the output's gradient dy. bias is needed for dscale; dscale and dshift have scale's shape and need it. Returns a dict."""
+    dt = _same_place(dy, x, weight, bias, scale)
+    lib = load_library()
+    _require(dy.shape == x.shape, "dy: expected x's shape")
+    B, N, c, xst, sst, _, per_token = _norm_arguments(x, weight, bias, scale, None, eps)
+    yst = _as_bnd(dy, "dy")[3]
+    _require(len(want) > 0 and set(want) <= {"dx", "dweight", "dbias", "dscale", "dshift"}, "want: dx, dweight, dbias, dscale, dshift")
+    _require(scale is not None or not {"dscale", "dshift"} & set(want), "dscale and dshift need the scale")
+    modulation = 0 if scale is None else 2 if per_token else 1
+    with _on_device(x.device):
+        new = lambda *shape: torch.empty(*shape, dtype=x.dtype, device=x.device)
+        r = {n: new(*x.shape) if n == "dx" else new(c) if n in ("dweight", "dbias") else new(*scale.shape) for n in want}
+        dx = r.get("dx")
+        sums = {"dweight", "dbias"} & set(want) or (modulation == 1 and {"dscale", "dshift"} & set(want))
+        ws, *space = _scratch(lib.svgear_layer_norm_backward_workspace(dt, B, N, c, modulation) if sums else 0, x.device)
+        rc = lib.svgear_layer_norm_backward(dy.data_ptr(), yst, x.data_ptr(), xst, _ptr(weight), _ptr(bias), _ptr(scale), sst, modulation,
+                                            dt, B, N, c, float(eps), _ptr(dx), _as_bnd(dx, "dx")[3] if dx is not None else _NO_ROWS,
+                                            _ptr(r.get("dweight")), _ptr(r.get("dbias")), _ptr(r.get("dscale")), _ptr(r.get("dshift")),
+                                            *space, _stream_of(x.device))
+    _check(rc, "svgear_layer_norm_backward")
+    return r
+
+
+def _strides_bhn(t: torch.Tensor, what: str):
+    st = t.stride()
+    if len(st) != 4 or st[3] != 1:
+        raise SvgearError(f"{what}: expected [B,heads,N,d] with contiguous d")
+    return _I64x3(*st[:3])
+
+
+def _attention_arguments(q, k, v, scale, cap, slopes, causal, prefix, q_offsets, k_offsets):
+    """The checked arguments that attention and its backward pass share: (sizes, arguments from scale to prefix)."""
+    _require(q.dim() == 4 and k.dim() == 4 and k.shape == v.shape, "expected q [B,H,Nq,d], k and v [B,Hk,Nk,d]")
+    B, H, Nq, d = q.shape
+    Hk, Nk = k.shape[1], k.shape[2]
+    _require(k.shape[0] == B and k.shape[3] == d and (d == 64 or d == 128), "expected q, k and v of one batch with heads of 64 or 128")
+    _require(min(B, H, Hk, Nq, Nk) > 0 and H % Hk == 0, "expected tokens, and key heads that divide the queries' heads")
+    _require(B * H <= _MOST_ROWS and Nq * (H // Hk) <= _MOST_ROWS and Nk <= _MOST_ROWS, "expected at most 2^30 heads and rows of a head")
+    device, flags, n_docs, given = q.device, 0, 0, [o for o in (q_offsets, k_offsets) if o is not None]
+    if slopes is not None and (slopes.device != device or slopes.dtype != torch.float32 or slopes.shape != (H,) or not slopes.is_contiguous()):
+        raise SvgearError("slopes: expected fp32 [H] on the tensors' device")
+    if given:
+        n_docs = given[0].shape[-1] - 1 if given[0].dim() else -1
+        _require(n_docs >= 1 and (len(given) == 2 or n_docs == 1), "offsets: [B,n+1] of queries and keys; of one of them alone [B,2]")
+    for t, n, what in ((q_offsets, n_docs + 1, "q_offsets"), (k_offsets, n_docs + 1, "k_offsets"), (prefix, max(n_docs, 1), "prefix")):
+        if t is not None and (t.device != device or t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) not in ((n,), (B, n))):
+            raise SvgearError(f"{what}: expected int32 [{n}] or [{B},{n}] on the tensors' device")
+    rows = given + ([prefix] if prefix is not None else [])
+    if rows and any(t.dim() == 1 for t in rows):
+        _require(B == 1 or all(t.dim() == 1 for t in rows), "offsets and prefix: all of them one row for the batch, or one for each entry")
+        flags |= ATTENTION_SHARED_DOCUMENTS
+    _require(causal or prefix is None, "a prefix needs causal=True")
+    cap = 0.0 if cap is None else float(cap)
+    _require(0.0 <= cap < float("inf"), "cap: a number above 0, or None")
+    scale = float(d) ** -0.5 if scale is None else float(scale)
+    _require(abs(scale) < float("inf"), "scale: a finite number")
+    if causal:
+        flags |= ATTENTION_CAUSAL
+    return (B, H, Hk, Nq, Nk, d), (scale, cap, _ptr(slopes), flags, n_docs, _ptr(q_offsets), _ptr(k_offsets), _ptr(prefix))
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: Optional[float] = None, cap: Optional[float] = None,
+              slopes: Optional[torch.Tensor] = None, causal: bool = False, prefix: Optional[torch.Tensor] = None,
+              q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None, want_lse: bool = False,
+              out: Optional[torch.Tensor] = None):
+    """svgear_attention: dense attention of q [B,H,Nq,d] over k, v [B,Hk,Nk,d] (any strides; Hk divides H). cap: scores become
+    cap tanh(score / cap); slopes fp32 [H]: less slopes[h] times the distance; q_offsets, k_offsets int32 [B,n+1] (or [n+1], for all
+    batch entries): documents that see only themselves (k_offsets alone, [B,2]: padded keys); causal: the last query of a document
+    stands at its last key and sees what is not behind it, and the first prefix[b,t] keys (int32 [B,n]) whatever its place. A query that
+    sees no key gives 0, and -inf in lse. Scores are scaled by `scale`, d^-0.5 if none is given. `out` may have any strides. Returns (o,
+    lse [B,H,Nq] fp32 or None). Not a part of torch's graph of gradients: attention_backward is called for them."""
+    dt = _same_place(q, k, v, out)
+    lib = load_library()
+    sizes, mask = _attention_arguments(q, k, v, scale, cap, slopes, causal, prefix, q_offsets, k_offsets)
+    if out is not None and out.shape != q.shape:
+        raise SvgearError("out: expected q's shape")
+    with _on_device(q.device):
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
+        ws, *space = _scratch(lib.svgear_attention_workspace(dt, *sizes, mask[4]), q.device)
+        rc = lib.svgear_attention(q.data_ptr(), _strides_bhn(q, "q"), k.data_ptr(), _strides_bhn(k, "k"), v.data_ptr(), _strides_bhn(v, "v"),
+                                  dt, *sizes, *mask, o.data_ptr(), _strides_bhn(o, "out"), _ptr(lse), *space, _stream_of(q.device))
+    _check(rc, "svgear_attention")
+    return o, lse
+
+
+def attention_backward(dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       scale: Optional[float] = None, cap: Optional[float] = None, slopes: Optional[torch.Tensor] = None,
+                       causal: bool = False, prefix: Optional[torch.Tensor] = None, q_offsets: Optional[torch.Tensor] = None,
+                       k_offsets: Optional[torch.Tensor] = None, want: Sequence[str] = ("dq", "dk", "dv"), out=None):
+    """svgear_attention_backward: the gradients named in `want` ("dq"; "dk" and "dv", both or neither) of attention() for the output's
+    gradient dy, from what it returned with want_lse and the arguments that it had. `out`: a dict of tensors of any strides for
+    them. The slopes get none. Returns a dict."""
+    out = {} if out is None else out
+    dt = _same_place(dy, q, k, v, o, *out.values())
+    lib = load_library()
+    sizes, mask = _attention_arguments(q, k, v, scale, cap, slopes, causal, prefix, q_offsets, k_offsets)
+    _require(dy.shape == q.shape and o.shape == q.shape, "dy and o: expected q's shape")
+    _require(lse is not None and lse.device == q.device and lse.dtype == torch.float32 and lse.shape == q.shape[:3] and lse.is_contiguous(),
+             "lse: expected attention()'s, fp32 [B,H,Nq]")
+    _require(len(want) > 0 and set(want) <= {"dq", "dk", "dv"} and ("dk" in want) == ("dv" in want), "want: dq, dk and dv")
+    _require(set(out) <= set(want), "out: gradients that are wanted")
+    like = {"dq": q, "dk": k, "dv": v}
+    with _on_device(q.device):
+        r = {n: out[n] if n in out else torch.empty(like[n].shape, dtype=q.dtype, device=q.device) for n in want}
+        _require(all(r[n].shape == like[n].shape for n in r), "out: expected the shapes of q, k and v")
+        ends = [x for n in ("dq", "dk", "dv") for x in (_ptr(r.get(n)), _strides_bhn(r[n], n) if n in r else None)]
+        ws, *space = _scratch(lib.svgear_attention_backward_workspace(dt, *sizes, mask[4]), q.device)
+        places = [x for t, n in ((dy, "dy"), (q, "q"), (k, "k"), (v, "v"), (o, "o")) for x in (t.data_ptr(), _strides_bhn(t, n))]
+        rc = lib.svgear_attention_backward(*places, lse.data_ptr(), dt, *sizes, *mask, *ends, *space, _stream_of(q.device))
+    _check(rc, "svgear_attention_backward")
+    return r
 
 
 _SIDE_STREAMS = {}

@@ -1,0 +1,45 @@
+// Shared declarations of dense attention with masks and its backward pass (internal).
+#pragma once
+#include "common.h"
+
+namespace svgear {
+
+// Queries of the H / Hk heads that share a key head are one run of rows: row r of key head hk is token r / G of head
+// hk G + r % G, G = H / Hk. Rows of a document see the keys [0, hi) of it, hi growing with the token (see Rows below).
+struct DenseArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* dy;
+  void* o;  // dq in the backward pass
+  void* dk;
+  void* dv;
+  float* lse;           // forward: out or null
+  const float* lse_in;  // backward
+  float* delta;         // [B,H,Nq]: sum over d of dy o
+  Strides qst, kst, vst, yst, ost, dkst, dvst;
+  const int32_t* q_offsets;  // [B or 1, n_docs + 1], or null: one document of all rows
+  const int32_t* k_offsets;
+  const int32_t* prefix;  // [B or 1, n_docs] or null
+  const float* slopes;    // [H] or null
+  int n_docs;
+  bool docs_shared, causal;
+  float scale, cap;
+  int B, H, Hk, G, Nq, Nk;
+  int slots, splits;  // tiles a key head has at most, parts that the other side's rows are cut into
+  float* part;        // where splits > 1: [splits][B Hk rows][d] (dk, then dv in the backward pass)
+  float2* part_ml;    // forward: maximum and sum of each
+};
+
+constexpr int kDenseWaves = 4;
+constexpr int kDenseRows = 32 * kDenseWaves;  // rows (queries, or keys for their gradients) of a workgroup
+
+// Tiles of `per` rows that `rows` rows in n_docs documents (0: not cut) take at most: a document starts a tile, and so do the
+// rows before the first and behind the last document.
+static inline int64_t dense_slots(int64_t rows, int n_docs, int per) { return n_docs ? rows / per + n_docs + 2 : ceil_div(rows, per); }
+
+int launch_dense_bf16(const DenseArgs& a, int d, int what, hipStream_t s);
+int launch_dense_f32(const DenseArgs& a, int d, int what, hipStream_t s);
+enum { kDenseForward = 0, kDenseDq = 1, kDenseDkv = 2 };
+
+}  // namespace svgear

@@ -1,0 +1,233 @@
+"""Dense attention with masks and its gradients against plain 64-bit forms."""
+import pytest
+import torch
+
+import paper_2603_08982_amd as sv
+from dense_helpers import attention64, attention_backward64, close
+
+pytestmark = pytest.mark.gpu
+
+BF, F = torch.bfloat16, torch.float32
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def make(seed, dtype, B, H, Hk, Nq, Nk, d, spread=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    t = lambda h, n: (torch.randn(B, n, h, d, generator=g, device="cuda") * spread).to(dtype).transpose(1, 2)
+    return t(H, Nq), t(Hk, Nk), t(Hk, Nk), t(H, Nq)
+
+
+def slopes_of(H):
+    return 2.0 ** (-8.0 * torch.arange(1, H + 1, device="cuda") / H)
+
+
+def check(q, k, v, dy, what, **kw):
+    o, lse = sv.attention(q, k, v, want_lse=True, **kw)
+    want, e, want_lse, el = attention64(q, k, v, **kw)
+    close(lse, want_lse, el, ("lse", what))
+    close(o, want, e, ("o", what))
+    alone, none = sv.attention(q, k, v, **kw)
+    assert none is None and torch.equal(alone, o)
+    got = sv.attention_backward(dy, q, k, v, o, lse, **kw)
+    ref = attention_backward64(dy, q, k, v, o, lse, **kw)
+    for n in ("dq", "dk", "dv"):
+        close(got[n], *ref[n], (n, what))
+    return o, lse, got
+
+
+LENGTHS = [(1, 1), (1, 2), (2, 1), (1, 77), (1, 1000), (5, 63), (31, 64), (32, 65), (33, 129), (127, 127), (128, 300), (129, 31), (200, 33),
+           (257, 512), (700, 77), (1030, 1030)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("Nq,Nk", LENGTHS)
+def test_lengths(Nq, Nk, dtype, d):
+    q, k, v, dy = make(Nq + Nk, dtype, 2, 4, 2, Nq, Nk, d)
+    check(q, k, v, dy, "plain")
+    check(q, k, v, dy, "causal", causal=True)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("H,Hk", [(1, 1), (3, 3), (5, 1), (6, 2), (40, 8), (16, 1)])
+@pytest.mark.parametrize("Nq,Nk", [(1, 333), (7, 200), (130, 130)])
+def test_shared_heads(Nq, Nk, H, Hk, dtype):
+    q, k, v, dy = make(H, dtype, 1, H, Hk, Nq, Nk, 64)
+    check(q, k, v, dy, "shared", causal=True, slopes=slopes_of(H))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("kw", [{"cap": 5.0}, {"cap": 50.0, "causal": True}, {"slopes": True}, {"slopes": True, "causal": True},
+                                {"slopes": True, "cap": 3.0}, {"prefix": 100, "causal": True}, {"scale": 0.3}, {"scale": -0.05, "cap": 2.0}],
+                         ids=str)
+def test_scores(kw, dtype, d):
+    q, k, v, dy = make(11, dtype, 2, 4, 4, 301, 345, d, spread=2.0)
+    kw = dict(kw)
+    if "slopes" in kw:
+        kw["slopes"] = slopes_of(4)
+    if "prefix" in kw:
+        kw["prefix"] = i32([kw["prefix"], 345])[:, None].contiguous()
+    check(q, k, v, dy, str(list(kw)), **kw)
+
+
+DOCS = {
+    "one behind the other": ([0, 100, 101, 300, 420], None),
+    "padding behind": ([0, 128, 256, 400], None),
+    "rows in front and behind": ([17, 30, 300], None),
+    "empty ones": ([0, 0, 50, 50, 50, 419, 419], None),
+    "queries without keys": ([0, 64, 200, 420], [0, 0, 333, 333]),
+    "keys without queries": ([0, 0, 130, 130, 400], [5, 100, 200, 300, 333]),
+    "more queries than keys": ([0, 200, 420], [0, 3, 40]),
+    "single tokens": (list(range(0, 60)), None),
+    "many": (list(range(0, 421, 3)), None),
+}
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F, 64)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("name", DOCS)
+def test_documents(name, causal, dtype, d):
+    """Rows outside the documents hold NaN, and reach nothing."""
+    qe, ke = DOCS[name]
+    Nq, Nk = 420, 420 if ke is None else 340
+    q, k, v, dy = make(len(name), dtype, 2, 4, 2, Nq, Nk, d)
+    ke = qe if ke is None else ke
+    for t, e in ((q, qe), (dy, qe), (k, ke), (v, ke)):
+        t[:, :, :e[0]] = float("nan")
+        t[:, :, e[-1]:] = float("nan")
+    prefix = {"prefix": i32([t % 7 for t in range(len(qe) - 1)])} if causal else {}
+    o, lse, got = check(q, k, v, dy, name, causal=causal, q_offsets=i32(qe), k_offsets=i32(ke), **prefix)
+    for t, e in ((o, qe), (got["dq"], qe), (got["dk"], ke), (got["dv"], ke)):
+        assert (t[:, :, :e[0]] == 0).all() and (t[:, :, e[-1]:] == 0).all()
+    assert (lse[:, :, qe[-1]:] == -torch.inf).all()
+    both = i32([qe, qe]), i32([ke, ke])  # one row for each batch entry
+    again, _ = sv.attention(q, k, v, causal=causal, q_offsets=both[0], k_offsets=both[1],
+                            **({"prefix": prefix["prefix"][None].repeat(2, 1)} if causal else {}))
+    assert torch.equal(again, o)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_padded_keys(dtype):
+    q, k, v, dy = make(21, dtype, 3, 4, 4, 333, 200, 128)
+    ends = [200, 77, 0]
+    for b, n in enumerate(ends):
+        k[b, :, n:], v[b, :, n:] = float("inf"), float("nan")
+    o, lse, got = check(q, k, v, dy, "padded", k_offsets=i32([[0, n] for n in ends]))
+    assert (o[2] == 0).all() and (lse[2] == -torch.inf).all() and (got["dq"][2] == 0).all()
+
+
+def test_padded_past_of_single_tokens():
+    """Serving: one new token each over pasts of different lengths, also of one key."""
+    q, k, v, dy = make(22, BF, 4, 10, 2, 1, 3001, 128)
+    ends = [3001, 1, 64, 1500]
+    for b, n in enumerate(ends):
+        k[b, :, n:], v[b, :, n:] = float("nan"), float("inf")
+    check(q, k, v, dy, "single", causal=True, slopes=slopes_of(10), k_offsets=i32([[0, n] for n in ends]))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_any_strides(dtype):
+    B, H, Hk, N, d = 2, 6, 3, 150, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    fused = torch.randn(B, N, H + 2 * Hk, d, generator=g, device="cuda").to(dtype)
+    q, k, v = (t.transpose(1, 2) for t in fused.split([H, Hk, Hk], 2))
+    dy = torch.randn(H, N, B, d, generator=g, device="cuda").to(dtype).permute(2, 0, 1, 3)
+    o, lse, got = check(q, k, v, dy, "fused", causal=True)
+    rows = torch.full((B, N + 1, H, d), 3.0, device="cuda", dtype=dtype)
+    out, _ = sv.attention(q, k, v, causal=True, out=rows[:, :N].transpose(1, 2))
+    assert torch.equal(out, o) and (rows[:, N] == 3).all()
+    grad = torch.full((B, N, H + 2 * Hk, d), 3.0, device="cuda", dtype=dtype)
+    gq, gk, gv = (t.transpose(1, 2) for t in grad.split([H, Hk, Hk], 2))
+    r = sv.attention_backward(dy, q, k, v, out, lse, causal=True, out={"dq": gq, "dk": gk, "dv": gv})
+    for n in got:
+        assert torch.equal(r[n], got[n]), n
+    dense = [t.contiguous() for t in (q, k, v)]
+    assert torch.equal(sv.attention(*dense, causal=True)[0], o)
+
+
+def test_parts_of_the_gradients():
+    q, k, v, dy = make(23, BF, 1, 4, 2, 200, 300, 64)
+    o, lse = sv.attention(q, k, v, want_lse=True)
+    whole = sv.attention_backward(dy, q, k, v, o, lse)
+    assert torch.equal(sv.attention_backward(dy, q, k, v, o, lse, want=["dq"])["dq"], whole["dq"])
+    part = sv.attention_backward(dy, q, k, v, o, lse, want=["dv", "dk"])
+    assert list(part) == ["dv", "dk"] and torch.equal(part["dk"], whole["dk"]) and torch.equal(part["dv"], whole["dv"])
+
+
+def test_large_scores():
+    """Scores of some hundreds, of either sign."""
+    for dtype in (BF, F):
+        q, k, v, dy = make(24, dtype, 1, 2, 2, 100, 150, 64, spread=6.0)
+        check(q, k, v, dy, "large")
+
+
+def test_far_rows():
+    """Offsets past 2^31 elements."""
+    n = (1 << 31) // 128 + 300
+    big = torch.empty(1, 1, n, 128, dtype=BF, device="cuda")
+    k = big[:, :, n - 200:]
+    k.copy_(torch.randn(1, 1, 200, 128, device="cuda"))
+    q = torch.randn(1, 1, 3, 128, device="cuda").to(BF)
+    a, _ = sv.attention(q, big, big, k_offsets=i32([n - 200, n]))
+    b, _ = sv.attention(q, k.clone(), k.clone())
+    assert torch.allclose(a.float(), b.float(), atol=2 ** -6)
+    del big, k
+    torch.cuda.empty_cache()
+
+
+def test_same_bits_again():
+    q, k, v, dy = make(25, BF, 1, 8, 2, 500, 4000, 128)
+    r = [sv.attention(q, k, v, want_lse=True) for _ in range(3)]
+    assert all(torch.equal(r[0][0], x[0]) and torch.equal(r[0][1], x[1]) for x in r)
+    g = [sv.attention_backward(dy, q, k, v, *r[0]) for _ in range(3)]
+    assert all(torch.equal(g[0][n], x[n]) for x in g for n in x)
+
+
+def test_gradient_against_differences():
+    q, k, v, dy = make(26, F, 1, 4, 2, 9, 13, 64)
+    kw = {"cap": 4.0, "slopes": slopes_of(4), "causal": True, "prefix": i32([3])}
+    o, lse = sv.attention(q, k, v, want_lse=True, **kw)
+    got = sv.attention_backward(dy, q, k, v, o, lse, **kw)
+    torch.manual_seed(3)
+    for n, t in (("dq", q), ("dk", k), ("dv", v)):
+        u = torch.randn_like(t).double()
+        step = 2.0 ** -12
+        f = lambda sign: attention64(*[a.double() + sign * step * u if a is t else a.double() for a in (q, k, v)], **kw)[0]
+        want = ((f(1) - f(-1)) * dy.double()).sum() / (2 * step)
+        have = (got[n].double() * u).sum()
+        # third derivatives are some tens at most along u, times the step squared over 6; fp32 on top
+        assert abs(have - want) <= (100 * step ** 2 + 2e-5) * dy.abs().sum().double(), (n, have, want)
+
+
+def test_captured_and_on_two_streams():
+    q, k, v, dy = make(27, BF, 1, 8, 4, 300, 1500, 128)
+    kw = {"causal": True, "q_offsets": i32([0, 100, 300]), "k_offsets": i32([0, 700, 1500])}
+
+    def both():
+        o, lse = sv.attention(q, k, v, want_lse=True, **kw)
+        return [o, lse, *sv.attention_backward(dy, q, k, v, o, lse, **kw).values()]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = both()
+    for i in range(3):
+        q.copy_(torch.randn_like(q))
+        graph.replay()
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.current_stream())
+            other = both()
+        eager = both()
+        torch.cuda.synchronize()
+        for a, b, c in zip(r, eager, other):
+            assert torch.equal(a, b) and torch.equal(a, c), i
