@@ -38,8 +38,10 @@ constexpr int kDenseRows = 32 * kDenseWaves;  // rows (queries, or keys for thei
 // rows before the first and behind the last document.
 static inline int64_t dense_slots(int64_t rows, int n_docs, int per) { return n_docs ? rows / per + n_docs + 2 : ceil_div(rows, per); }
 
-int launch_dense_bf16(const DenseArgs& a, int d, int what, hipStream_t s);
-int launch_dense_f32(const DenseArgs& a, int d, int what, hipStream_t s);
 enum { kDenseForward = 0, kDenseDq = 1, kDenseDkv = 2 };
+int launch_dense_bf16(const DenseArgs& a, int d, hipStream_t s);
+int launch_dense_f32(const DenseArgs& a, int d, hipStream_t s);
+int launch_dense_backward_bf16(const DenseArgs& a, int d, int what, hipStream_t s);
+int launch_dense_backward_f32(const DenseArgs& a, int d, int what, hipStream_t s);
 
 }  // namespace svgear

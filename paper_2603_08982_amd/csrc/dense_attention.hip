@@ -185,7 +185,8 @@ bool space_ok(const void* ws, size_t ws_bytes, size_t need) {
   return need == 0 || (ws && reinterpret_cast<uintptr_t>(ws) % 256 == 0 && ws_bytes >= need);
 }
 int launch(const DenseArgs& a, const Sizes& z, int what, hipStream_t s) {
-  return z.dt == SVGEAR_F32 ? launch_dense_f32(a, z.d, what, s) : launch_dense_bf16(a, z.d, what, s);
+  if (what == kDenseForward) return z.dt == SVGEAR_F32 ? launch_dense_f32(a, z.d, s) : launch_dense_bf16(a, z.d, s);
+  return z.dt == SVGEAR_F32 ? launch_dense_backward_f32(a, z.d, what, s) : launch_dense_backward_bf16(a, z.d, what, s);
 }
 
 template <typename T, int D>

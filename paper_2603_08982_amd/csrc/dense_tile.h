@@ -53,10 +53,10 @@ __device__ __forceinline__ int row_of(int r, int lh) { return 8 * (r >> 2) + 4 *
 // ---- tiles in LDS and the products with them
 // The 16-byte chunks of row r are permuted by XOR with swz(r), so that 16 rows of one chunk (the plain reads) and 4 rows of
 // four chunks (the transposed reads) both lie in different banks.
-template <typename T, int D>
+template <typename T, int D, int BLOCKS = sizeof(T) == 2 ? 2 : 1>
 struct Tile {
   static constexpr bool kHalf = sizeof(T) == 2;
-  static constexpr int kBlocks = kHalf ? 2 : 1;  // of 32 rows
+  static constexpr int kBlocks = BLOCKS;  // of 32 rows
   static constexpr int kRows = 32 * kBlocks;
   static constexpr int kRowBytes = D * (int)sizeof(T);
   static constexpr int kBytes = kRows * kRowBytes;
@@ -113,6 +113,21 @@ struct Tile {
         x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, c.v[s].w, x, 0, 0, 0);
       }
     }
+  }
+
+  // the same with the columns in LDS, each lane's operands where it put them (see park)
+  static constexpr int kParked = 32 * kRowBytes;  // bytes of a wave
+  static __device__ __forceinline__ void park(unsigned char* to, const Column& c, int lane) {
+#pragma unroll
+    for (int s = 0; s < kParked / 1024; ++s) *reinterpret_cast<std::conditional_t<kHalf, bf16x8, float4>*>(to + s * 1024 + lane * 16) = c.v[s];
+  }
+  __device__ __forceinline__ void rows_times(const unsigned char* tile, int kb, const unsigned char* parked, f32x16& x, int lane) const {
+    static_assert(kHalf, "bf16 columns alone are parked");
+    const unsigned char* t = tile + kb * 32 * kRowBytes;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const uint4*>(t + (row_off ^ (s << 5)))),
+                                                  as_bf16x8(*reinterpret_cast<const uint4*>(parked + s * 1024 + lane * 16)), x, 0, 0, 0);
   }
 
   // acc^T += block kb of a tile, transposed, times X (bf16: rounded to it)
@@ -179,9 +194,8 @@ __device__ __forceinline__ void store_four(bf16_t* p, float4 v) {
 
 // Rows of a tensor as 16-byte chunks of lanes: row `at` of tile rows from `first` on, those behind `last` as `last`.
 // (32-bit offsets within a tile: the entry points hold strides to what that takes.)
-template <typename T, int D, typename RowOffset>
+template <typename Z, typename T, typename RowOffset>
 __device__ __forceinline__ void copy_tile(const T* base, uint32_t lds, int wave, int lane, RowOffset offset) {
-  using Z = Tile<T, D>;
 #pragma unroll
   for (int i = 0; i < Z::kCopies; ++i) {
     const int inst = i * kDenseWaves + wave, row = inst * Z::kRowsPerCopy + lane / Z::kChunks;
@@ -268,42 +282,42 @@ __device__ __forceinline__ bool dense_index(const DenseArgs& a, int& bh, int& sl
   return true;
 }
 
-// tanh: for bf16 from the hardware's exponential and reciprocal, off by some 2^-23 of 1, which moves a score of cap 50 by
-// 1e-5 beside the 2^-9 that the rounding of its weight is off by.
+// tanh from the hardware's exponential and reciprocal. For bf16 1 - 2 / (e^2x + 1), off by some 2^-23 of 1, which moves a score of
+// cap 50 by 1e-5 beside the 2^-9 that its weight's rounding is off by. For fp32 (1 - e) / (1 + e) with e = e^-2|x|, and below 0.3,
+// where 1 - e would lose digits, the series, whose next term is 3e-9 of the result there.
 template <typename T>
 __device__ __forceinline__ float tanh_of(float x) {
-  if constexpr (sizeof(T) == 2) return 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f);
-  else return tanhf(x);
+  if constexpr (sizeof(T) == 2) {
+    return 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f);
+  } else {
+    const float a = fabsf(x), e = __builtin_amdgcn_exp2f(a * (-2.f * kLog2e)), z = x * x;
+    const float far = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x);
+    float p = __builtin_fmaf(z, 0.0035921280f, -0.0088632356f);
+    p = __builtin_fmaf(z, p, 0.0218694885f);
+    p = __builtin_fmaf(z, p, -0.0539682540f);
+    p = __builtin_fmaf(z, p, 0.1333333333f);
+    p = __builtin_fmaf(z, p, -0.3333333333f);
+    return a < 0.3f ? __builtin_fmaf(x * z, p, x) : far;
+  }
 }
 
-// Products to exponents of 2. GENERAL: with a cap, or a bias by distance.
-template <typename T, bool GENERAL>
+// Products to exponents of 2, of a query at `dist` from the key. The cap's derivative is 1 - tanh^2.
+template <typename T, bool CAP, bool SLOPES>
 struct Scores {
-  float c, to_cap, cap2;
-  __device__ __forceinline__ Scores(const DenseArgs& a) : c(a.scale * kLog2e) {
-    if (GENERAL) {
-      to_cap = a.cap > 0.f ? a.scale / a.cap : 0.f;
-      cap2 = a.cap * kLog2e;
-    }
+  float c, cap2;
+  __device__ __forceinline__ Scores(const DenseArgs& a) : c(CAP ? a.scale / a.cap : a.scale * kLog2e), cap2(a.cap * kLog2e) {}
+  // tanh (or the product itself)
+  __device__ __forceinline__ float inner(float s) const { return CAP ? tanh_of<T>(s * c) : s; }
+  // exponent less `less`
+  __device__ __forceinline__ float outer(float in, float dist, float slope, float less) const {
+    if (SLOPES) less = __builtin_fmaf(slope, fabsf(dist), less);
+    return __builtin_fmaf(in, CAP ? cap2 : c, -less);
   }
-  // dist: query's position less the key's. `keeps`: 1 - tanh^2.
-  __device__ __forceinline__ float exponent(float s, float dist, float slope, float& keeps) const {
-    if (!GENERAL) return s * c;
-    float x;
-    keeps = 1.f;
-    if (cap2 > 0.f) {
-      const float th = tanh_of<T>(s * to_cap);
-      x = cap2 * th;
-      keeps = __builtin_fmaf(-th, th, 1.f);
-    } else {
-      x = s * c;
-    }
-    return __builtin_fmaf(-slope, fabsf(dist), x);
-  }
+  __device__ __forceinline__ float keeps(float in) const { return __builtin_fmaf(-in, in, 1.f); }
 };
 
 // ---- forward: 128 queries a workgroup
-template <typename T, int D, bool GENERAL>
+template <typename T, int D, bool CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, 2)
 dense_forward_kernel(DenseArgs a) {
   using Z = Tile<T, D>;
@@ -331,19 +345,19 @@ dense_forward_kernel(DenseArgs a) {
 
   typename Z::Column q;
   q.load(static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
-  const float slope = GENERAL && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
   SVGEAR_WAIT_VMCNT(0);  // (the copies below are not seen by the compiler, which would wait for them inside the loop)
 
   const Z z(lane);
-  const Scores<T, GENERAL> scores(a);
+  const Scores<T, CAP, SLOPES> scores(a);
   const uint32_t lds = lds_address(smem);
   const T* kp = static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
   const T* vp = static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
   auto issue = [&](int t) __attribute__((always_inline)) {
     const int last = hi_wg - 1 - t * BN;  // (keys that no row here sees are not read)
-    copy_tile<T, D>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
+    copy_tile<Z>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
                     [&](int r) { return (int64_t)min(r, last) * a.kst.n; });
-    copy_tile<T, D>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
+    copy_tile<Z>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
                     [&](int r) { return (int64_t)min(r, last) * a.vst.n; });
   };
 
@@ -368,8 +382,7 @@ dense_forward_kernel(DenseArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = t * BN + 32 * kb + row_of(r, lh);
-        float keeps;
-        x[kb][r] = scores.exponent(x[kb][r], (float)(pos - j), slope, keeps);
+        x[kb][r] = scores.outer(scores.inner(x[kb][r]), (float)(pos - j), slope, 0.f);
       }
     }
     if ((t + 1) * BN > hi_all) {
@@ -421,8 +434,8 @@ dense_forward_kernel(DenseArgs a) {
 }
 
 // ---- the queries' gradients: 128 queries a workgroup, a pass over the keys
-template <typename T, int D, bool GENERAL>
-__global__ void __launch_bounds__(64 * kDenseWaves, 1)
+template <typename T, int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(64 * kDenseWaves, sizeof(T) == 4 && D == 128 ? 1 : 2)
 dense_dq_kernel(DenseArgs a) {
   using Z = Tile<T, D>;
   constexpr int DB = D / 32, BN = Z::kRows;
@@ -451,19 +464,19 @@ dense_dq_kernel(DenseArgs a) {
   dy.load(static_cast<const T*>(a.dy) + b * a.yst.b + head * a.yst.h + token * a.yst.n, lh);
   const int64_t stat = ((int64_t)b * a.H + head) * a.Nq + token;
   const float lse2 = a.lse_in[stat] * kLog2e, delta = a.delta[stat];
-  const float slope = GENERAL && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+  const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
   SVGEAR_WAIT_VMCNT(0);
 
   const Z z(lane);
-  const Scores<T, GENERAL> scores(a);
+  const Scores<T, CAP, SLOPES> scores(a);
   const uint32_t lds = lds_address(smem);
   const T* kp = static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
   const T* vp = static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
   auto issue = [&](int t) __attribute__((always_inline)) {
     const int last = hi_wg - 1 - t * BN;
-    copy_tile<T, D>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
+    copy_tile<Z>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
                     [&](int r) { return (int64_t)min(r, last) * a.kst.n; });
-    copy_tile<T, D>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
+    copy_tile<Z>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
                     [&](int r) { return (int64_t)min(r, last) * a.vst.n; });
   };
 
@@ -489,10 +502,9 @@ dense_dq_kernel(DenseArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = t * BN + 32 * kb + row_of(r, lh);
-        float keeps = 1.f;
-        const float e = scores.exponent(x[r], (float)(pos - j), slope, keeps);
-        float ds = __builtin_amdgcn_exp2f(e - lse2) * (dp[r] - delta);
-        if (GENERAL) ds *= keeps;
+        const float in = scores.inner(x[r]);
+        float ds = __builtin_amdgcn_exp2f(scores.outer(in, (float)(pos - j), slope, lse2)) * (dp[r] - delta);
+        if (CAP) ds *= scores.keeps(in);
         x[r] = masked && j >= hi ? 0.f : ds;
       }
       z.transposed_times(kt, kb, x, acc, lane);
@@ -511,13 +523,16 @@ dense_dq_kernel(DenseArgs a) {
 }
 
 // ---- the keys' and values' gradients: 128 keys a workgroup, a pass over the queries of all heads that share them
-template <typename T, int D, bool GENERAL>
-__global__ void __launch_bounds__(64 * kDenseWaves, 1)
+template <typename T, int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(64 * kDenseWaves, sizeof(T) == 4 && D == 128 ? 1 : 2)
 dense_dkv_kernel(DenseArgs a) {
-  using Z = Tile<T, D>;
+  // Two waves a SIMD, one's exponentials under the other's products, leave 256 registers: at d = 128 in bf16 the accumulators
+  // take 128 and the keys 32, and the values wait in LDS, under tiles of 32 rows.
+  constexpr bool kPark = sizeof(T) == 2 && D == 128;
+  using Z = Tile<T, D, kPark ? 1 : sizeof(T) == 2 ? 2 : 1>;
   constexpr int DB = D / 32, BN = Z::kRows;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of Q, two of dy
-  __shared__ __attribute__((aligned(256))) float stats[2][2][64];              // log-sum-exp and delta of a tile's rows
+  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes + (kPark ? kDenseWaves * Z::kParked : 0)];  // two of Q, two of dy
+  __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, position
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
@@ -538,12 +553,14 @@ dense_dkv_kernel(DenseArgs a) {
   const int t_lo = first_tile + (int)((int64_t)tiles * split / a.splits), t_hi = first_tile + (int)((int64_t)tiles * (split + 1) / a.splits);
 
   typename Z::Column k, v;
+  unsigned char* parked = smem + 4 * Z::kBytes + (kPark ? wave * Z::kParked : 0);
   k.load(static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + key_c * a.kst.n, lh);
   v.load(static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + key_c * a.vst.n, lh);
+  if constexpr (kPark) Z::park(parked, v, lane);
   SVGEAR_WAIT_VMCNT(0);
 
   const Z z(lane);
-  const Scores<T, GENERAL> scores(a);
+  const Scores<T, CAP, SLOPES> scores(a);
   const uint32_t lds = lds_address(smem), lds_stats = lds_address(stats);
   const T* qp = static_cast<const T*>(a.q) + b * a.qst.b + hk * a.G * a.qst.h + doc.q0 * a.qst.n;
   const T* yp = static_cast<const T*>(a.dy) + b * a.yst.b + hk * a.G * a.yst.h + doc.q0 * a.yst.n;
@@ -553,13 +570,13 @@ dense_dkv_kernel(DenseArgs a) {
       const int row = min(t * BN + r, end - 1), token = a.G == 1 ? row : row / a.G;
       return (row - token * a.G) * st.h + token * st.n;
     };
-    copy_tile<T, D>(qp, lds + (t & 1) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.qst); });
-    copy_tile<T, D>(yp, lds + (2 + (t & 1)) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.yst); });
-    if (wave < 2) {
-      const int row = min(t * BN + lane, end - 1), token = a.G == 1 ? row : row / a.G;
-      const float* from_stat = (wave == 0 ? a.lse_in : a.delta) + stat0 + (int64_t)(row - token * a.G) * a.Nq + token;
-      async_copy_4B(from_stat, (uint32_t)uniform((int)(lds_stats + ((t & 1) * 2 + wave) * 256)));
-    }
+    copy_tile<Z>(qp, lds + (t & 1) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.qst); });
+    copy_tile<Z>(yp, lds + (2 + (t & 1)) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.yst); });
+    const int row = min(t * BN + lane, end - 1), token = a.G == 1 ? row : row / a.G;
+    const uint32_t to = (uint32_t)uniform((int)(lds_stats + ((t & 1) * 4 + wave) * 256));
+    if (wave < 2) async_copy_4B((wave == 0 ? a.lse_in : a.delta) + stat0 + (int64_t)(row - token * a.G) * a.Nq + token, to);
+    if (SLOPES && wave == 2) async_copy_4B(a.slopes + hk * a.G + row - token * a.G, to);
+    if (SLOPES && wave == 3) stats[t & 1][3][lane] = (float)doc.position(token);
   };
 
   f32x16 dk[DB], dv[DB];
@@ -580,27 +597,26 @@ dense_dkv_kernel(DenseArgs a) {
       clear(x);
       clear(dp);
       z.rows_times(qt, kb, k, x);
-      z.rows_times(yt, kb, v, dp);
+      if constexpr (kPark) z.rows_times(yt, kb, parked, dp, lane);
+      else z.rows_times(yt, kb, v, dp);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 ls = *reinterpret_cast<const float4*>(&stats[t & 1][0][32 * kb + 8 * g + 4 * lh]);
-        const float4 de = *reinterpret_cast<const float4*>(&stats[t & 1][1][32 * kb + 8 * g + 4 * lh]);
+        auto of_rows = [&](int what) { return *reinterpret_cast<const float4*>(&stats[t & 1][what][32 * kb + 8 * g + 4 * lh]); };
+        const float4 ls = of_rows(0), de = of_rows(1);
         const float lse[4] = {ls.x, ls.y, ls.z, ls.w}, delta[4] = {de.x, de.y, de.z, de.w};
+        float slope[4] = {0.f, 0.f, 0.f, 0.f}, dist[4] = {0.f, 0.f, 0.f, 0.f};
+        if (SLOPES) {
+          const float4 sl = of_rows(2), po = of_rows(3);
+          slope[0] = sl.x * kLog2e, slope[1] = sl.y * kLog2e, slope[2] = sl.z * kLog2e, slope[3] = sl.w * kLog2e;
+          dist[0] = po.x - (float)j, dist[1] = po.y - (float)j, dist[2] = po.z - (float)j, dist[3] = po.w - (float)j;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * g + i, row = t * BN + 32 * kb + row_of(r, lh);
-          float keeps = 1.f, slope = 0.f, dist = 0.f;
-          if (GENERAL) {
-            if (a.slopes) {
-              const int rc = min(row, end - 1), token = rc / a.G;
-              slope = a.slopes[hk * a.G + rc - token * a.G] * kLog2e;
-              dist = (float)(doc.position(token) - j);
-            }
-          }
-          const float e = scores.exponent(x[r], dist, slope, keeps);
-          float p = __builtin_amdgcn_exp2f(__builtin_fmaf(-lse[i], kLog2e, e));
+          const float in = scores.inner(x[r]);
+          float p = __builtin_amdgcn_exp2f(scores.outer(in, dist[i], slope[i], lse[i] * kLog2e));
           float ds = p * (dp[r] - delta[i]);
-          if (GENERAL) ds *= keeps;
+          if (CAP) ds *= scores.keeps(in);
           if (masked && (row < from || row >= end)) p = ds = 0.f;
           x[r] = p;
           dp[r] = ds;
@@ -625,22 +641,25 @@ dense_dkv_kernel(DenseArgs a) {
   Z::each_four(dv, lh, [&](int d, float4 u) { store_four(ov + d, u); });
 }
 
-template <typename T, int D, bool GENERAL>
-int launch_dense_mode(const DenseArgs& a, int what, hipStream_t s) {
+template <typename T, int D, bool CAP, bool SLOPES, int WHAT>
+int launch_dense_mode(const DenseArgs& a, hipStream_t s) {
   const int64_t groups = ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8;
   const dim3 grid = long_grid(groups, a.splits);
-  if (what == kDenseForward) dense_forward_kernel<T, D, GENERAL><<<grid, 64 * kDenseWaves, 0, s>>>(a);
-  else if (what == kDenseDq) dense_dq_kernel<T, D, GENERAL><<<grid, 64 * kDenseWaves, 0, s>>>(a);
-  else dense_dkv_kernel<T, D, GENERAL><<<grid, 64 * kDenseWaves, 0, s>>>(a);
+  if constexpr (WHAT == kDenseForward) dense_forward_kernel<T, D, CAP, SLOPES><<<grid, 64 * kDenseWaves, 0, s>>>(a);
+  else if constexpr (WHAT == kDenseDq) dense_dq_kernel<T, D, CAP, SLOPES><<<grid, 64 * kDenseWaves, 0, s>>>(a);
+  else dense_dkv_kernel<T, D, CAP, SLOPES><<<grid, 64 * kDenseWaves, 0, s>>>(a);
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }
 
-template <typename T>
-int launch_dense(const DenseArgs& a, int d, int what, hipStream_t s) {
-  const bool general = a.cap > 0.f || a.slopes;
-  if (d == 64) return general ? launch_dense_mode<T, 64, true>(a, what, s) : launch_dense_mode<T, 64, false>(a, what, s);
-  return general ? launch_dense_mode<T, 128, true>(a, what, s) : launch_dense_mode<T, 128, false>(a, what, s);
+template <typename T, int D, int WHAT>
+int launch_dense_width(const DenseArgs& a, hipStream_t s) {
+  if (a.cap > 0.f) return a.slopes ? launch_dense_mode<T, D, true, true, WHAT>(a, s) : launch_dense_mode<T, D, true, false, WHAT>(a, s);
+  return a.slopes ? launch_dense_mode<T, D, false, true, WHAT>(a, s) : launch_dense_mode<T, D, false, false, WHAT>(a, s);
+}
+template <typename T, int WHAT>
+int launch_dense(const DenseArgs& a, int d, hipStream_t s) {
+  return d == 64 ? launch_dense_width<T, 64, WHAT>(a, s) : launch_dense_width<T, 128, WHAT>(a, s);
 }
 
 }  // namespace
