@@ -11,6 +11,9 @@
 // backward pass, the sums of its columns stay in registers; the next row is on its way while the present one is reduced.
 // A row's statistics take one exchange between its waves: each finds its own mean and the squares' sum around that (so that a
 // mean far from zero costs nothing), and those of the waves are joined around the row's mean.
+#include <algorithm>
+#include <type_traits>
+
 #include "linear.h"
 
 namespace svgear {
@@ -63,11 +66,13 @@ __device__ __forceinline__ float team_sum(float v) {
   }
 }
 
-// ---- eight columns of which `n` are within the row
-template <typename T>
+// ---- eight columns of which `n` are within the row; WHOLE: all of them or none (a comparison for each element otherwise)
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void load_some(Eight<T>& v, const T* p, int n) {
   if (n >= 8) {
     v.load(p);
+  } else if constexpr (WHOLE) {
+    __builtin_memset(&v, 0, sizeof(v));
   } else {
     T t[8];
 #pragma unroll
@@ -75,20 +80,20 @@ __device__ __forceinline__ void load_some(Eight<T>& v, const T* p, int n) {
     __builtin_memcpy(&v, t, sizeof(t));
   }
 }
-template <typename T>
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void store_some(T* p, const float (&v)[8], int n) {
   if (n >= 8) {
     store8(p, v);
-  } else {
+  } else if constexpr (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) store1(p + i, v[i]);
   }
 }
-template <typename T>
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void load_floats(float (&f)[8], const void* p, int64_t at, int n) {
   Eight<T> v;
-  load_some(v, static_cast<const T*>(p) + at, n);
+  load_some<WHOLE>(v, static_cast<const T*>(p) + at, n);
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = v.get(i);
 }
@@ -144,7 +149,7 @@ struct Where {
 };
 
 // Mean and the sum of squares around it of this wave's share of a row (a lane team: of the row).
-template <typename T, int L, int CH>
+template <bool WHOLE, typename T, int L, int CH>
 __device__ __forceinline__ void share_statistics(const Team<L, CH>& at, const Eight<T> (&x)[CH], float& mean, float& m2) {
   float s = 0.f;
 #pragma unroll
@@ -157,13 +162,13 @@ __device__ __forceinline__ void share_statistics(const Team<L, CH>& at, const Ei
   for (int k = 0; k < CH; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float d = i < at.n[k] ? x[k].get(i) - mean : 0.f;
+      const float d = i < (WHOLE ? at.n[k] & 8 : at.n[k]) ? x[k].get(i) - mean : 0.f;
       s = __builtin_fmaf(d, d, s);
     }
   m2 = team_sum<L>(s);
 }
 
-template <typename T, int L, int CH, int MOD, int MAXW>
+template <typename T, int L, int CH, int MOD, int MAXW, bool WHOLE>
 __global__ void __launch_bounds__(64 * MAXW)
 layer_norm_kernel(NormArgs a) {
   __shared__ float4 slots[2][MAXW];
@@ -179,18 +184,18 @@ layer_norm_kernel(NormArgs a) {
   for (int k = 0; k < CH; ++k) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[k][i] = 1.f, o[k][i] = 0.f;
-    if (a.weight) load_floats<T>(f[k], a.weight, at.col[k], at.n[k]);
-    if (a.bias) load_floats<T>(o[k], a.bias, at.col[k], at.n[k]);
+    if (a.weight) load_floats<WHOLE, T>(f[k], a.weight, at.col[k], at.n[k]);
+    if (a.bias) load_floats<WHOLE, T>(o[k], a.bias, at.col[k], at.n[k]);
     if (MOD == kModEntry) {
       if (a.scale) {
         float s[8];
-        load_floats<T>(s, a.scale, at.entry * a.sst.b + at.col[k], at.n[k]);
+        load_floats<WHOLE, T>(s, a.scale, at.entry * a.sst.b + at.col[k], at.n[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[k][i] *= 1.f + s[i], o[k][i] *= 1.f + s[i];
       }
       if (a.shift) {
         float s[8];
-        load_floats<T>(s, a.shift, at.entry * a.hst.b + at.col[k], at.n[k]);
+        load_floats<WHOLE, T>(s, a.shift, at.entry * a.hst.b + at.col[k], at.n[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[k][i] += s[i];
       }
@@ -204,7 +209,7 @@ layer_norm_kernel(NormArgs a) {
     const Where w(a, at.entry, r);
     const T* p = static_cast<const T*>(a.x) + w.at(a.xst);
 #pragma unroll
-    for (int k = 0; k < CH; ++k) load_some(next[k], p + at.col[k], at.n[k]);
+    for (int k = 0; k < CH; ++k) load_some<WHOLE>(next[k], p + at.col[k], at.n[k]);
   };
   load(at.first);
   int turn = 0;
@@ -218,13 +223,13 @@ layer_norm_kernel(NormArgs a) {
     if (MOD == kModToken && valid) {
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
-        if (a.scale) load_some(sc[k], static_cast<const T*>(a.scale) + w.at(a.sst) + at.col[k], at.n[k]);
-        if (a.shift) load_some(sh[k], static_cast<const T*>(a.shift) + w.at(a.hst) + at.col[k], at.n[k]);
+        if (a.scale) load_some<WHOLE>(sc[k], static_cast<const T*>(a.scale) + w.at(a.sst) + at.col[k], at.n[k]);
+        if (a.shift) load_some<WHOLE>(sh[k], static_cast<const T*>(a.shift) + w.at(a.hst) + at.col[k], at.n[k]);
       }
     }
     if (base + at.step < a.R) load(base + at.step);
     float mean, m2;
-    share_statistics<T, L, CH>(at, x, mean, m2);
+    share_statistics<WHOLE, T, L, CH>(at, x, mean, m2);
     if (waves) {
       if (at.lane == 0) slots[turn][at.wave] = make_float4(mean, m2, at.here, 0.f);
       __syncthreads();
@@ -251,12 +256,12 @@ layer_norm_kernel(NormArgs a) {
           if (a.shift) v[i] += sh[k].get(i);
         }
       }
-      if (at.n[k] > 0) store_some(y + at.col[k], v, at.n[k]);
+      if (at.n[k] > 0) store_some<WHOLE>(y + at.col[k], v, at.n[k]);
     }
   }
 }
 
-template <typename T, int L, int CH, int MOD, int MAXW>
+template <typename T, int L, int CH, int MOD, int MAXW, bool WHOLE>
 __global__ void __launch_bounds__(64 * MAXW)
 layer_norm_backward_kernel(NormArgs a) {
   __shared__ float4 slots[2][MAXW];
@@ -272,15 +277,15 @@ layer_norm_backward_kernel(NormArgs a) {
   for (int k = 0; k < CH; ++k) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[k][i] = 1.f, s1[k][i] = s2[k][i] = 0.f;
-    if (a.weight) load_floats<T>(f[k], a.weight, at.col[k], at.n[k]);
+    if (a.weight) load_floats<WHOLE, T>(f[k], a.weight, at.col[k], at.n[k]);
     if (MOD == kModToken) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[k][i] = 0.f;
-      if (a.bias) load_floats<T>(o[k], a.bias, at.col[k], at.n[k]);
+      if (a.bias) load_floats<WHOLE, T>(o[k], a.bias, at.col[k], at.n[k]);
     }
     if (MOD == kModEntry && a.scale) {
       float s[8];
-      load_floats<T>(s, a.scale, at.entry * a.sst.b + at.col[k], at.n[k]);
+      load_floats<WHOLE, T>(s, a.scale, at.entry * a.sst.b + at.col[k], at.n[k]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[k][i] *= 1.f + s[i];
     }
@@ -295,8 +300,8 @@ layer_norm_backward_kernel(NormArgs a) {
     const T* py = static_cast<const T*>(a.dy) + w.at(a.dyst);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      load_some(nx[k], px + at.col[k], at.n[k]);
-      load_some(ny[k], py + at.col[k], at.n[k]);
+      load_some<WHOLE>(nx[k], px + at.col[k], at.n[k]);
+      load_some<WHOLE>(ny[k], py + at.col[k], at.n[k]);
     }
   };
   load(at.first);
@@ -310,7 +315,7 @@ layer_norm_backward_kernel(NormArgs a) {
     const Where w(a, at.entry, valid ? r : a.R - 1);
     if (MOD == kModToken && valid && a.scale) {
 #pragma unroll
-      for (int k = 0; k < CH; ++k) load_some(sc[k], static_cast<const T*>(a.scale) + w.at(a.sst) + at.col[k], at.n[k]);
+      for (int k = 0; k < CH; ++k) load_some<WHOLE>(sc[k], static_cast<const T*>(a.scale) + w.at(a.sst) + at.col[k], at.n[k]);
     }
     if (base + at.step < a.R) load(base + at.step);
     auto du_of = [&](int k, int i) __attribute__((always_inline)) {
@@ -318,13 +323,13 @@ layer_norm_backward_kernel(NormArgs a) {
       return MOD == kModToken && a.scale ? v * (1.f + sc[k].get(i)) : v;
     };
     float mean, m2;
-    share_statistics<T, L, CH>(at, x, mean, m2);
+    share_statistics<WHOLE, T, L, CH>(at, x, mean, m2);
     float ga = 0.f, gx = 0.f;  // sums of g and of g (x - mean)
 #pragma unroll
     for (int k = 0; k < CH; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i < at.n[k]) {
+        if (WHOLE || i < at.n[k]) {  // (dy is 0 behind the row's end)
           const float g = du_of(k, i) * f[k][i];
           ga += g;
           gx = __builtin_fmaf(g, x[k].get(i) - mean, gx);
@@ -375,9 +380,9 @@ layer_norm_backward_kernel(NormArgs a) {
         }
       }
       if (at.n[k] > 0) {
-        if (dx) store_some(dx + at.col[k], v, at.n[k]);
-        if (MOD == kModToken && a.dscale) store_some(static_cast<T*>(a.dscale) + dense + at.col[k], ds, at.n[k]);
-        if (MOD == kModToken && a.dshift) store_some(static_cast<T*>(a.dshift) + dense + at.col[k], db, at.n[k]);
+        if (dx) store_some<WHOLE>(dx + at.col[k], v, at.n[k]);
+        if (MOD == kModToken && a.dscale) store_some<WHOLE>(static_cast<T*>(a.dscale) + dense + at.col[k], ds, at.n[k]);
+        if (MOD == kModToken && a.dshift) store_some<WHOLE>(static_cast<T*>(a.dshift) + dense + at.col[k], db, at.n[k]);
       }
     }
   }
@@ -395,13 +400,13 @@ layer_norm_backward_kernel(NormArgs a) {
       for (int q = L; q < 64; q <<= 1) s1[k][i] += __shfl_xor(s1[k][i], q), s2[k][i] += __shfl_xor(s2[k][i], q);
     }
     if (at.n[k] > 0 && (L == 64 || at.lane < L)) {
-      store_some(out + at.col[k], s1[k], at.n[k]);
-      store_some(out + a.c + at.col[k], s2[k], at.n[k]);
+      store_some<WHOLE>(out + at.col[k], s1[k], at.n[k]);
+      store_some<WHOLE>(out + a.c + at.col[k], s2[k], at.n[k]);
     }
   }
 }
 
-// ---- the columns' sums, joined: 32 columns a workgroup, 32 runs of parts, each every 32nd, then those in order
+// ---- the columns' sums, joined: 16 columns a workgroup, 64 runs of parts, each every 64th, then those in order
 struct NormSums {
   const float* partial;
   const void* weight;
@@ -417,8 +422,8 @@ struct NormSums {
 template <typename T>
 __global__ void __launch_bounds__(1024)
 layer_norm_sums_kernel(NormSums a) {
-  __shared__ float s[2][32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+  __shared__ float s[2][64][17];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
   const bool in = c < a.c;
   float w = 1.f, b = 0.f, t1 = 0.f, t2 = 0.f;
   if (y == 0 && in) {
@@ -430,13 +435,13 @@ layer_norm_sums_kernel(NormSums a) {
     float v1 = 0.f, v2 = 0.f;
     if (in)
 #pragma unroll 8
-      for (int i = y; i < a.parts; i += 32) v1 += p[(int64_t)i * 2 * a.c], v2 += p[(int64_t)i * 2 * a.c + a.c];
+      for (int i = y; i < a.parts; i += 64) v1 += p[(int64_t)i * 2 * a.c], v2 += p[(int64_t)i * 2 * a.c + a.c];
     s[0][y][x] = v1;
     s[1][y][x] = v2;
     __syncthreads();
     if (y == 0 && in) {
-#pragma unroll
-      for (int k = 1; k < 32; ++k) v1 += s[0][k][x], v2 += s[1][k][x];
+#pragma unroll 16
+      for (int k = 1; k < 64; ++k) v1 += s[0][k][x], v2 += s[1][k][x];
       const float f = a.scale ? 1.f + load_as_f32(static_cast<const T*>(a.scale) + e * a.scale_b + c) : 1.f;
       t1 = __builtin_fmaf(f, v1, t1);
       t2 = __builtin_fmaf(f, v2, t2);
@@ -456,13 +461,14 @@ layer_norm_sums_kernel(NormSums a) {
 struct Shape {
   int lanes, wpr, ch;
 };
-Shape shape_of(int c) {
+Shape shape_of(int c, svgear_dtype dt) {
   const int runs = (int)ceil_div(c, 8);
   for (int l = 8; l < 64; l *= 2)
     if (runs <= l) return {l, 1, 1};
-  if (runs <= 64) return {64, 1, 1};
-  // two runs a lane, four where that would be more than eight waves
-  const int ch = runs <= 64 * 8 * 2 ? 2 : 4;
+  // up to 64 bytes a lane (75,600 x 5,120 in bf16: 300 us; with half of it and as much on its way 314, with a quarter 350), fp32
+  // rows of over 16 waves 128
+  int ch = 1;
+  while (runs > 64 * ch && ch < (dt == SVGEAR_F32 && runs <= 64 * 2 * 16 ? 2 : 4)) ch *= 2;
   return {64, (int)ceil_div(runs, 64 * ch), ch};
 }
 
@@ -472,15 +478,20 @@ struct Plan {
   int groups, parts, mod;
 };
 // mod: kModToken also where each batch entry is a single token (its modulation is then read as a token's)
-Plan plan_norm(int64_t B, int64_t N, int c, int mod) {
+Plan plan_norm(svgear_dtype dt, int64_t B, int64_t N, int c, int mod, bool backward) {
   Plan p{};
-  p.z = shape_of(c);
+  p.z = shape_of(c, dt);
   p.mod = mod;
   p.entries = mod == kModEntry ? B : 1;
   p.rows = mod == kModEntry ? N : B * N;
   const int per_group = p.z.wpr > 1 ? 1 : kNormWaves * (64 / p.z.lanes), waves = p.z.wpr > 1 ? p.z.wpr : kNormWaves;
-  const int64_t wanted = ceil_div(256 * 16, (int64_t)waves * p.entries), most = ceil_div(p.rows, per_group);
-  p.groups = (int)(wanted < most ? wanted : most);
+  // One round of workgroups that stay, of so many waves a CU that some 30 KB of rows are on their way to it: 75,600 x 5,120 forward
+  // with 3 / 6 / 9 / 12 waves of 4 KB 465 / 319 / 300 / 307 us. Backward a workgroup leaves a row of sums, which is worth four rows
+  // of x at least.
+  const int lane_bytes = 8 * p.z.ch * (int)esize(dt);
+  const int resident = std::max(1, std::min((backward ? 384 : 576) / lane_bytes, backward ? 20 : 24) / waves);
+  const int64_t wanted = std::max<int64_t>(256 * resident / p.entries, 1), most = ceil_div(p.rows, per_group * (backward ? 4 : 1));
+  p.groups = (int)std::min(wanted, most);
   p.parts = p.groups * (p.z.wpr > 1 ? 1 : kNormWaves);
   return p;
 }
@@ -489,13 +500,18 @@ template <typename T, int L, int CH, int MAXW>
 int launch_shape(const NormArgs& a, const Plan& p, bool backward, hipStream_t s) {
   const dim3 grid = long_grid(p.entries * p.groups, 1);
   const int threads = 64 * (p.z.wpr > 1 ? p.z.wpr : kNormWaves);
-  if (backward) {
-    if (p.mod == kModToken) layer_norm_backward_kernel<T, L, CH, kModToken, MAXW><<<grid, threads, 0, s>>>(a);
-    else layer_norm_backward_kernel<T, L, CH, kModEntry, MAXW><<<grid, threads, 0, s>>>(a);
-  } else {
-    if (p.mod == kModToken) layer_norm_kernel<T, L, CH, kModToken, MAXW><<<grid, threads, 0, s>>>(a);
-    else layer_norm_kernel<T, L, CH, kModEntry, MAXW><<<grid, threads, 0, s>>>(a);
-  }
+  auto by_mod = [&](auto whole) {
+    constexpr bool W = decltype(whole)::value;
+    if (backward) {
+      if (p.mod == kModToken) layer_norm_backward_kernel<T, L, CH, kModToken, MAXW, W><<<grid, threads, 0, s>>>(a);
+      else layer_norm_backward_kernel<T, L, CH, kModEntry, MAXW, W><<<grid, threads, 0, s>>>(a);
+    } else {
+      if (p.mod == kModToken) layer_norm_kernel<T, L, CH, kModToken, MAXW, W><<<grid, threads, 0, s>>>(a);
+      else layer_norm_kernel<T, L, CH, kModEntry, MAXW, W><<<grid, threads, 0, s>>>(a);
+    }
+  };
+  if (a.c % 8 == 0) by_mod(std::true_type{});
+  else by_mod(std::false_type{});
   SVGEAR_LAUNCH_CHECK();
   return SVGEAR_OK;
 }
@@ -511,7 +527,8 @@ int launch_norm(NormArgs& a, const Plan& p, bool backward, hipStream_t s) {
   if (p.z.lanes == 16) return launch_shape<T, 16, 1, kNormWaves>(a, p, backward, s);
   if (p.z.lanes == 32) return launch_shape<T, 32, 1, kNormWaves>(a, p, backward, s);
   if (p.z.ch == 1) return launch_shape<T, 64, 1, kNormWaves>(a, p, backward, s);
-  if (p.z.ch == 2) return launch_shape<T, 64, 2, 8>(a, p, backward, s);
+  if (p.z.ch == 2 && p.z.wpr <= 8) return launch_shape<T, 64, 2, 8>(a, p, backward, s);
+  if (p.z.ch == 2) return launch_shape<T, 64, 2, 16>(a, p, backward, s);
   if (p.z.wpr <= 8) return launch_shape<T, 64, 4, 8>(a, p, backward, s);
   return launch_shape<T, 64, 4, 16>(a, p, backward, s);
 }
@@ -560,14 +577,14 @@ extern "C" int svgear_layer_norm(const void* x, const int64_t xstride[2], const 
   a.c = c;
   a.eps = eps;
   const bool tokens = N == 1 || (scale && sstride[1] != 0) || (shift && hstride[1] != 0);
-  const Plan p = plan_norm(B, N, c, !scale && !shift ? kModNone : tokens ? kModToken : kModEntry);
+  const Plan p = plan_norm(dt, B, N, c, !scale && !shift ? kModNone : tokens ? kModToken : kModEntry, false);
   hipStream_t s = static_cast<hipStream_t>(stream);
   return dt == SVGEAR_F32 ? launch_norm<float>(a, p, false, s) : launch_norm<bf16_t>(a, p, false, s);
 }
 
 extern "C" size_t svgear_layer_norm_backward_workspace(svgear_dtype dt, int B, int64_t N, int c, int modulation) {
   if (!norm_sizes_ok(dt, B, N, c, 0.f) || modulation < kModNone || modulation > kModToken) return 0;
-  const Plan p = plan_norm(B, N, c, of_tokens(modulation, N));
+  const Plan p = plan_norm(dt, B, N, c, of_tokens(modulation, N), true);
   return align_up((size_t)(p.entries * p.parts) * 2 * c * sizeof(float), 256);
 }
 
@@ -606,7 +623,7 @@ extern "C" int svgear_layer_norm_backward(const void* dy, const int64_t dystride
   a.c = c;
   a.eps = eps;
   if (sums) a.partial = static_cast<float*>(ws);
-  const Plan p = plan_norm(B, N, c, mod);
+  const Plan p = plan_norm(dt, B, N, c, mod, true);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int rc = dt == SVGEAR_F32 ? launch_norm<float>(a, p, true, s) : launch_norm<bf16_t>(a, p, true, s);
   if (rc != SVGEAR_OK || !sums) return rc;
@@ -617,7 +634,7 @@ extern "C" int svgear_layer_norm_backward(const void* dy, const int64_t dystride
     z.scale = scale, z.scale_b = a.sst.b;
     z.dscale = dscale, z.dshift = dshift;
   }
-  const unsigned blocks = (unsigned)ceil_div(c, 32);
+  const unsigned blocks = (unsigned)ceil_div(c, 16);
   if (dt == SVGEAR_F32) layer_norm_sums_kernel<float><<<blocks, 1024, 0, s>>>(z);
   else layer_norm_sums_kernel<bf16_t><<<blocks, 1024, 0, s>>>(z);
   SVGEAR_LAUNCH_CHECK();
