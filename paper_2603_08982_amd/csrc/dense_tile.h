@@ -243,6 +243,7 @@ __device__ __forceinline__ Place place_of(const int32_t* offsets, int n_docs, in
 struct Document {
   int q0, nq, k0, nk, prefix;
   bool causal;
+  __device__ __forceinline__ explicit Document(const DenseArgs& a) : causal(a.causal) {}
   __device__ __forceinline__ Document(const DenseArgs& a, int b, int doc) {
     const int64_t row = a.docs_shared ? 0 : b;
     q0 = 0, nq = a.Nq, k0 = 0, nk = a.Nk, prefix = 0;
