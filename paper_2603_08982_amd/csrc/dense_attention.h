@@ -26,8 +26,7 @@ struct DenseArgs {
   bool docs_shared, causal;
   float scale, cap;
   int B, H, Hk, G, Nq, Nk;
-  int slots, splits;  // tiles (bf16 forward: runs of `run` tiles) a key head has at most, parts that the other side's rows are cut into
-  int run;
+  int slots, splits;  // tiles a key head has at most, parts that the other side's rows are cut into
   float* part;        // where splits > 1: [splits][B Hk rows][d] (dk, then dv in the backward pass)
   float2* part_ml;    // forward: maximum and sum of each
 };

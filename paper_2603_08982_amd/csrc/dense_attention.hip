@@ -12,9 +12,6 @@ namespace {
 
 constexpr int64_t kMaxDenseRows = (int64_t)1 << 30;
 constexpr int kMaxDocs = 1 << 20;
-#ifndef RUN
-#define RUN 1
-#endif
 constexpr int kThreads = 256;
 
 // Where a row of `part` goes: row r of key head (b, hk) is token r / G of head hk G + r % G.
@@ -255,12 +252,6 @@ extern "C" int svgear_attention(const void* q, const int64_t qstride[3], const v
   a.lse = lse;
   a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, kDenseRows);
   a.splits = parts_over_keys(z);
-  if (dt == SVGEAR_BF16 && a.splits == 1) {
-    a.run = RUN;
-    a.slots = (int)ceil_div(a.slots, a.run);
-  } else {
-    a.run = 1;
-  }
   if (a.splits > 1) {
     Workspace w(ws, ws_bytes);
     a.part = w.take<float>((size_t)a.splits * q_rows(z) * d);

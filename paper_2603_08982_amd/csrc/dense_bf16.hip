@@ -1,12 +1,9 @@
 // Dense attention with masks in bf16: the kernel of dense_tile.h with its phases laid over each other.
 //
 // What bounds it: the matrix cores and the vector unit alike. A step of a wave (64 keys, 32 queries, d = 128) is 32 products of 32
-// cycles, and 32 exponentials a lane at a quarter of the rate with their scaling, maximum, sum and conversion, some 900 cycles.
+// cycles, and 32 exponentials a lane at a quarter of the rate with their scaling, maximum, sum and conversion, some 950 cycles.
 // So a wave issues the exponentials of a tile between the products of the next tile's scores, and the next tile's maximum between
-// the products with the values; two workgroups share a CU and fill what is left. A workgroup goes on to further tiles of
-// queries of its head without a pause: the next queries are loaded when the last scores of the present ones are done, and the
-// keys and values of the next step are on their way whatever tile it is of, since with few keys the start of a tile (lookups, first
-// copies) takes as long as its steps.
+// the products with the values; two workgroups share a CU and fill what is left.
 #include "dense_tile.h"
 
 namespace svgear {
@@ -16,14 +13,26 @@ namespace {
 template <int D>
 constexpr float kHeadroom = D == 64 ? 0.f : 8.f;
 
-// A tile of queries: its rows, its document, and its steps (tiles of keys) in this part of them.
-struct QueryTile {
-  Place at;
-  int i;            // of the workgroup's run
-  int t0, steps;    // first tile of keys, and how many
-  int seen;         // keys of the document that its rows see
-  int q0, nq, k0, nk, prefix;
-};
+// A value that is found again where it is used: the compiler otherwise keeps what follows from it in registers through the loop.
+__device__ __forceinline__ int again(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// A row of results: the lanes l and l + 32 hold alternate fours of its columns; they exchange halves and store 16 bytes each.
+template <int DB>
+__device__ __forceinline__ void store_whole(bf16_t* o, const f32x16 (&acc)[DB], float f, int lh, bool live) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      const f32x16& x = acc[db];
+      const uint32_t a0 = pack2_bf16(x[4 * g] * f, x[4 * g + 1] * f), a1 = pack2_bf16(x[4 * g + 2] * f, x[4 * g + 3] * f);
+      const uint32_t b0 = pack2_bf16(x[4 * g + 4] * f, x[4 * g + 5] * f), b1 = pack2_bf16(x[4 * g + 6] * f, x[4 * g + 7] * f);
+      const auto u = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), v = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+      if (live) *reinterpret_cast<uint4*>(o + 32 * db + 8 * g + 8 * lh) = make_uint4(u[0], v[0], u[1], v[1]);
+    }
+}
 
 template <int D, bool CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, 2)
@@ -31,102 +40,64 @@ dense_forward_bf16_kernel(DenseArgs a) {
   using Z = Tile<bf16_t, D>;
   constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes, AHEAD = 4;
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
-  int bh, run;
-  if (!dense_index(a, bh, run)) return;
-  if (a.causal) run = a.slots - 1 - run;  // the longest first
+  int bh, slot;
+  if (!dense_index(a, bh, slot)) return;
+  if (a.causal) slot = a.slots - 1 - slot;  // the longest first
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const int32_t* qo = a.q_offsets ? a.q_offsets + (a.docs_shared ? 0 : (int64_t)b * (a.n_docs + 1)) : nullptr;
-  const int split = blockIdx.y;
-  const int64_t part_rows = (int64_t)a.B * a.Hk * a.Nq * a.G;
+  const Place at = place_of(qo, a.n_docs, a.Nq, a.G, kDenseRows, slot, lane);
+  if (at.first >= at.end) return;
+  const Document doc(a, b, at.doc);
 
-  auto document = [&](const QueryTile& c) {
-    Document d(a);
-    d.q0 = c.q0, d.nq = c.nq, d.k0 = c.k0, d.nk = c.nk, d.prefix = c.prefix;
-    return d;
-  };
-  // a row's output: what it has summed, or nothing
-  auto store_row = [&](int row, const f32x16 (&acc)[DB], float m, float l) __attribute__((always_inline)) {
-    if (a.splits > 1) {
-      const int64_t out = split * part_rows + (int64_t)bh * a.Nq * a.G + row;
-      if (lh == 0) a.part_ml[out] = make_float2(m, l);
-      Z::each_four(acc, lh, [&](int d, float4 v) {
-        __builtin_amdgcn_sched_barrier(0);  // (one after the other: together they take registers that the loop then misses)
-        store_four(a.part + out * D + d, v);
-      });
-      return;
-    }
-    const int token = row / a.G, head = hk * a.G + (row - token * a.G);
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-    bf16_t* o = static_cast<bf16_t*>(a.o) + b * a.ost.b + head * a.ost.h + token * a.ost.n;
-    Z::each_four(acc, lh, [&](int d, float4 v) {
-      __builtin_amdgcn_sched_barrier(0);
-      store_four(o + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-    });
-    if (a.lse && lh == 0) a.lse[((int64_t)b * a.H + head) * a.Nq + token] = (m + log2f(l)) * kLn2;
-  };
-  // The first tile from the run's i-th on that has steps; those that see no key (or none of this part) are written here. False: none.
-  auto seek = [&](QueryTile& c) {
-    for (; c.i < a.run; ++c.i) {
-      if (c.at.first + kDenseRows < c.at.end) {  // the next tile of the same document
-        c.at.first += kDenseRows;
-      } else {
-        const Place p = place_of(qo, a.n_docs, a.Nq, a.G, kDenseRows, run * a.run + c.i, lane);
-        if (p.first >= p.end || p.first < c.at.end) continue;  // an empty slot
-        c.at = p;
-        const Document d(a, b, p.doc);
-        c.q0 = d.q0, c.nq = d.nq, c.k0 = d.k0, c.nk = d.nk, c.prefix = d.prefix;
-      }
-      const int end = min(c.at.first + kDenseRows, c.at.end);
-      c.seen = document(c).seen((end - 1) / a.G - c.q0);
-      const int tiles = (c.seen + BN - 1) / BN;
-      c.t0 = (int)((int64_t)tiles * split / a.splits);
-      c.steps = (int)((int64_t)tiles * (split + 1) / a.splits) - c.t0;
-      if (c.steps > 0) return true;
-      f32x16 none[DB];
+  const int wave_row = at.first + 32 * wave, row = min(wave_row + li, at.end - 1);
+  const int token = row / a.G, head = hk * a.G + (row - token * a.G);
+  const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
+  // keys that every row of this wave sees, and that some row of the workgroup sees
+  const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0));
+  const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0));
+  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
+  const int t_lo = uniform((int)((int64_t)tiles * split / a.splits)), t_hi = uniform((int)((int64_t)tiles * (split + 1) / a.splits));
+
+  typename Z::Column q;
+  q.load(static_cast<const bf16_t*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
+  if (a.scale < 0.f) {  // (the maximum is that of the unscaled scores)
 #pragma unroll
-      for (int db = 0; db < DB; ++db) clear(none[db]);
-      const int row = c.at.first + 32 * wave + li;
-      if (row < end) store_row(row, none, -INFINITY, 0.f);
+    for (int s = 0; s < KS; ++s) {
+      union { bf16x8 v; uint4 u; } c;
+      c.v = q.v[s];
+      c.u.x ^= 0x80008000u, c.u.y ^= 0x80008000u, c.u.z ^= 0x80008000u, c.u.w ^= 0x80008000u;
+      q.v[s] = c.v;
     }
-    return false;
-  };
+  }
+  const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
 
   const Z z(lane);
   const uint32_t lds = lds_address(smem);
-  const bf16_t* kb = static_cast<const bf16_t*>(a.k) + b * a.kst.b + hk * a.kst.h;
-  const bf16_t* vb = static_cast<const bf16_t*>(a.v) + b * a.vst.b + hk * a.vst.h;
-  auto issue = [&](const QueryTile& c, int t, const bf16_t* base, int64_t st, int buffer) __attribute__((always_inline)) {
-    const int key = (c.t0 + t) * BN, last = c.seen - 1 - key;  // (keys that no row here sees are not read)
-    copy_tile<Z>(base + ((int64_t)c.k0 + key) * st, lds + buffer * Z::kBytes, wave, lane, [&](int r) { return min(r, last) * st; });
-  };
-  auto row_of_lane = [&](const QueryTile& c) { return min(c.at.first + 32 * wave + li, c.at.end - 1); };
-
-  typename Z::Column q;
-  auto load_queries = [&](const QueryTile& c) __attribute__((always_inline)) {
-    const int row = row_of_lane(c), token = row / a.G, head = hk * a.G + (row - token * a.G);
-    q.load(static_cast<const bf16_t*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
-    if (a.scale < 0.f) {  // (the maximum is that of the unscaled scores)
+  const bf16_t* kp = static_cast<const bf16_t*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
+  const bf16_t* vp = static_cast<const bf16_t*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
+  // Rows of a whole tile lie at one offset of the lane from addresses that the wave shares; in the last tile, rows behind the last key
+  // that a query here sees are not read.
+  const int copy_row = wave * Z::kRowsPerCopy + lane / Z::kChunks, copy_chunk = ((lane % Z::kChunks) ^ Z::swz(copy_row)) * 16;
+  constexpr int kStep = kDenseWaves * Z::kRowsPerCopy;
+  static_assert(kStep % 16 == 0, "all copies of a lane have one chunk");
+  const uint32_t k_lane = (uint32_t)copy_row * (uint32_t)a.kst.n * 2u + copy_chunk, v_lane = (uint32_t)copy_row * (uint32_t)a.vst.n * 2u + copy_chunk;
+  auto issue = [&](int t, const bf16_t* base, int64_t st, uint32_t at_lane, int buffer) __attribute__((always_inline)) {
+    const bf16_t* rows = static_cast<const bf16_t*>(uniform_ptr(base + (int64_t)t * BN * st));
+    const uint32_t to = (uint32_t)uniform((int)(lds + buffer * Z::kBytes + wave * 1024));
+    const int last = hi_wg - 1 - t * BN;
+    if (last >= BN - 1) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        union { bf16x8 v; uint4 u; } c2;
-        c2.v = q.v[s];
-        c2.u.x ^= 0x80008000u, c2.u.y ^= 0x80008000u, c2.u.z ^= 0x80008000u, c2.u.w ^= 0x80008000u;
-        q.v[s] = c2.v;
-      }
+      for (int i = 0; i < Z::kCopies; ++i) async_copy_16B(rows + (int64_t)(i * kStep) * st, at_lane, to + i * kDenseWaves * 1024);
+    } else {
+      const int mine = again(copy_row);
+#pragma unroll
+      for (int i = 0; i < Z::kCopies; ++i)
+        async_copy_16B(rows, (uint32_t)min(i * kStep + mine, last) * (uint32_t)st * 2u + copy_chunk, to + i * kDenseWaves * 1024);
     }
   };
-  // what this lane's query sees, and what all of the wave's do
-  int pos = 0, hi = 0, hi_all = 0;
-  float slope = 0.f;
-  auto look_at_row = [&](const QueryTile& c) __attribute__((always_inline)) {
-    const Document d = document(c);
-    const int row = row_of_lane(c), token = row / a.G;
-    pos = d.position(token - c.q0);
-    hi = d.seen(token - c.q0);
-    hi_all = d.seen(min(c.at.first + 32 * wave, c.at.end - 1) / a.G - c.q0);
-    if (SLOPES) slope = a.slopes[hk * a.G + (row - token * a.G)] * kLog2e;
-  };
+  auto issue_k = [&](int t) __attribute__((always_inline)) { issue(t, kp, a.kst.n, k_lane, (t - t_lo) & 1); };
+  auto issue_v = [&](int t) __attribute__((always_inline)) { issue(t, vp, a.vst.n, v_lane, 2 + ((t - t_lo) & 1)); };
 
   Scores<bf16_t, CAP, SLOPES> scores_of(a);
   scores_of.c = fabsf(scores_of.c);
@@ -209,15 +180,14 @@ dense_forward_bf16_kernel(DenseArgs a) {
       m = m_new;
     }
   };
-  // O^T += V^T P^T with the V tile that v_off points into, and between those products, with MORE, the maximum of the next scores sn
-  int v_off = 2 * Z::kBytes + z.tr_off;
-  auto values = [&](const f32x16 (&sn)[2], auto more_tag) __attribute__((always_inline)) {
+  // O^T += V^T P^T with the V tile in `buffer`, and between those products, with MORE, the maximum of the next scores sn
+  auto values = [&](int buffer, const f32x16 (&sn)[2], auto more_tag) __attribute__((always_inline)) {
     constexpr bool MORE = decltype(more_tag)::value && !CAP && !SLOPES;
     constexpr int N = 4 * DB;
     bf16x8 vf[N];
     auto rd = [&](int i) {
-      const unsigned char* at = smem + (i / DB) * 16 * ROWB;
-      const int off = v_off ^ ((i % DB) << 6);
+      const unsigned char* at = smem + (2 + buffer) * Z::kBytes + (i / DB) * 16 * ROWB;
+      const int off = z.tr_off ^ ((i % DB) << 6);
       union { struct { v4i16 a, b; } s; bf16x8 v; } u;
       u.s.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(at + off));
       u.s.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(at + 8 * ROWB + (off ^ 32)));
@@ -242,90 +212,69 @@ dense_forward_bf16_kernel(DenseArgs a) {
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
   };
 
-  // Step t of a tile takes the weights of its scores and its values, and finds the scores of step t + 1; K(t + 2) and V(t + 1) are
-  // copied meanwhile, over K(t) and V(t - 1), which step t - 1 was the last to read. In the last step both K buffers and one of V's are
-  // free for the first steps of the next tile, whose queries are loaded.
-  QueryTile now;
-  now.at = Place{0, 0, -1};
-  now.i = 0;
-  now.q0 = now.nq = now.k0 = now.nk = now.prefix = 0;
-  bool more = seek(now);
-  auto start = [&](const QueryTile& c, int v_buffer) __attribute__((always_inline)) {
-    issue(c, 0, kb, a.kst.n, 0);
-    issue(c, 0, vb, a.vst.n, v_buffer);
-    if (c.steps > 1) issue(c, 1, kb, a.kst.n, 1);
-    load_queries(c);
-  };
-  int v_buffer = 2;  // that the present step's values are in
-  if (more) {
-    start(now, v_buffer);
-    look_at_row(now);
-  }
-  while (more) {
+  // Step t takes the weights of its scores and its values, and finds the scores of step t + 1; K(t + 2) and V(t + 1) are copied
+  // meanwhile, over K(t) and V(t - 1), which step t - 1 was the last to read.
+  if (t_lo < t_hi) {
+    issue_k(t_lo);
+    issue_v(t_lo);
     SVGEAR_WAIT_VMCNT(0);
     __syncthreads();
+    if (t_lo + 1 < t_hi) issue_k(t_lo + 1);
     scores(0, sA, sB, std::false_type{});
-    {
-      float mx = -INFINITY;
+    float mx = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) max_pair(sA, mx, e);
-      settle(now.t0, sA, mx, std::false_type{});
-    }
-    __syncthreads();  // everyone is done with the first K tile before it is copied over
+    for (int e = 0; e < 16; ++e) max_pair(sA, mx, e);
+    settle(t_lo, sA, mx, std::false_type{});
+    SVGEAR_WAIT_VMCNT(0);
+    __syncthreads();
     auto step = [&](int t, int parity, f32x16 (&s_now)[2], f32x16 (&s_next)[2], auto whole_tag) __attribute__((always_inline)) {
-      if (t + 2 < now.steps) issue(now, t + 2, kb, a.kst.n, parity);
-      issue(now, t + 1, vb, a.vst.n, v_buffer ^ 1);
+      if (t + 2 < t_hi) issue(t + 2, kp, a.kst.n, k_lane, parity);
+      issue(t + 1, vp, a.vst.n, v_lane, 2 + (parity ^ 1));
       scores(parity ^ 1, s_next, s_now, std::true_type{});
-      const float mx = values(s_next, std::true_type{});
-      settle(now.t0 + t + 1, s_next, mx, whole_tag);
-      v_buffer ^= 1;
-      v_off ^= Z::kBytes;
+      const float next = values(parity, s_next, std::true_type{});
+      settle(t + 1, s_next, next, whole_tag);
       SVGEAR_WAIT_VMCNT(0);
       __syncthreads();
     };
-    int t = 0;
-    const int whole = min(now.steps, hi_all / BN - now.t0);  // steps without a mask for this wave
+    int t = t_lo;
+    const int whole = min(t_hi, hi_all / BN);  // up to here without a mask for this wave
     for (; t + 2 < whole; t += 2) {
       step(t, 0, sA, sB, std::true_type{});
       step(t + 1, 1, sB, sA, std::true_type{});
     }
-    for (; t + 2 < now.steps; t += 2) {
+    for (; t + 2 < t_hi; t += 2) {
       step(t, 0, sA, sB, std::false_type{});
       step(t + 1, 1, sB, sA, std::false_type{});
     }
-    if (t + 1 < now.steps) {
-      step(t, 0, sA, sB, std::false_type{});
-#pragma unroll
-      for (int k = 0; k < 2; ++k) sA[k] = sB[k];
-    }
-    // the last step
-    QueryTile next = now;
-    ++next.i;
-    more = seek(next);
-    if (more) start(next, v_buffer ^ 1);
-    {
+    auto last = [&](int parity, const f32x16 (&s)[2]) __attribute__((always_inline)) {
       const float neg_m = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) weigh(sA, e, neg_m);
+      for (int e = 0; e < 16; ++e) weigh(s, e, neg_m);
+      __builtin_amdgcn_sched_barrier(0);
+      values(parity, s, std::false_type{});
+    };
+    if (t + 1 < t_hi) {
+      step(t, 0, sA, sB, std::false_type{});
+      last(1, sB);
+    } else {
+      last(0, sA);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    values(sB, std::false_type{});
-    __builtin_amdgcn_sched_barrier(0);
-    float l = (ls[0] + ls[1]) + (ls[2] + ls[3]);
-    l += swap32(l);
-    const int row = now.at.first + 32 * wave + li;
-    if (row < now.at.end) store_row(row, acc, m, l);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int db = 0; db < DB; ++db) clear(acc[db]);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) ls[u] = 0.f;
-    m = -INFINITY;
-    v_buffer ^= 1;
-    v_off ^= Z::kBytes;
-    now = next;
-    if (more) look_at_row(now);
   }
+
+  float l = (ls[0] + ls[1]) + (ls[2] + ls[3]);
+  l += swap32(l);
+  const int out_row = again(row), out_token = out_row / a.G, out_head = hk * a.G + (out_row - out_token * a.G);
+  const bool live = wave_row + again(li) < at.end;
+  if (a.splits > 1) {
+    if (!live) return;
+    const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + out_row;
+    if (lh == 0) a.part_ml[out] = make_float2(m, l);
+    Z::each_four(acc, lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  store_whole(static_cast<bf16_t*>(a.o) + b * a.ost.b + out_head * a.ost.h + out_token * a.ost.n, acc, inv, lh, live);
+  if (live && a.lse && lh == 0) a.lse[((int64_t)b * a.H + out_head) * a.Nq + out_token] = (m + log2f(l)) * kLn2;
 }
 
 template <int D, bool CAP, bool SLOPES>
