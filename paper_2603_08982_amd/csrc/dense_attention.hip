@@ -100,11 +100,13 @@ dense_delta_kernel(const T* dy, Strides yst, const T* o, Strides ost, int H, int
 }
 
 // ---- how many parts the rows of the other side are cut into: so many that some 512 workgroups (two a CU) have work, but two
-// tiles a part at least. `own`: rows a key head has on the workgroups' side, `other`: on the other.
+// tiles a part at least. `own`: rows a key head has on the workgroups' side, `other`: on the other. Where a head's rows are one
+// tile (single tokens), the parts cost little and are finer, four tiles each, so that pasts of different lengths even out.
 int parts_of(int64_t heads, int64_t own, int64_t other, int n_docs, svgear_dtype dt) {
   const int64_t tiles = heads * ceil_div(own, kDenseRows), each = ceil_div(other, n_docs > 1 ? n_docs : 1);
   const int64_t most = ceil_div(each, 2 * (dt == SVGEAR_F32 ? 32 : 64));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, most), 64));
+  const int64_t wanted = own <= kDenseRows ? std::min<int64_t>(1024 / tiles, most / 2) : 512 / tiles;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(std::max<int64_t>(wanted, 512 / tiles), most), 64));
 }
 
 struct Sizes {

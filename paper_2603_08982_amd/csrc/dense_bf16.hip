@@ -38,7 +38,8 @@ template <int D, bool CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, 2)
 dense_forward_bf16_kernel(DenseArgs a) {
   using Z = Tile<bf16_t, D>;
-  constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes, AHEAD = 4;
+  constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes;
+  constexpr int AHEAD = CAP && !SLOPES ? 3 : 4;  // operands read before the product that takes them; as many as registers are left
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
@@ -52,7 +53,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
 
   const int wave_row = at.first + 32 * wave, row = min(wave_row + li, at.end - 1);
   const int token = row / a.G, head = hk * a.G + (row - token * a.G);
-  const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
+  const int pos = doc.position(token - doc.q0) - 4 * lh, hi = doc.seen(token - doc.q0) - 4 * lh;  // (less what a lane's first key is)
   // keys that every row of this wave sees, and that some row of the workgroup sees
   const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0));
   const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0));
@@ -90,17 +91,37 @@ dense_forward_bf16_kernel(DenseArgs a) {
 #pragma unroll
       for (int i = 0; i < Z::kCopies; ++i) async_copy_16B(rows + (int64_t)(i * kStep) * st, at_lane, to + i * kDenseWaves * 1024);
     } else {
-      const int mine = again(copy_row);
+      const int l = again(lane), mine = wave * Z::kRowsPerCopy + l / Z::kChunks, chunk = ((l % Z::kChunks) ^ Z::swz(mine)) * 16;
 #pragma unroll
       for (int i = 0; i < Z::kCopies; ++i)
-        async_copy_16B(rows, (uint32_t)min(i * kStep + mine, last) * (uint32_t)st * 2u + copy_chunk, to + i * kDenseWaves * 1024);
+        async_copy_16B(rows, (uint32_t)min(i * kStep + mine, last) * (uint32_t)st * 2u + chunk, to + i * kDenseWaves * 1024);
     }
   };
   auto issue_k = [&](int t) __attribute__((always_inline)) { issue(t, kp, a.kst.n, k_lane, (t - t_lo) & 1); };
   auto issue_v = [&](int t) __attribute__((always_inline)) { issue(t, vp, a.vst.n, v_lane, 2 + ((t - t_lo) & 1)); };
 
   Scores<bf16_t, CAP, SLOPES> scores_of(a);
-  scores_of.c = fabsf(scores_of.c);
+  scores_of.c = uniform(fabsf(scores_of.c));
+  scores_of.cap2 = uniform(scores_of.cap2);
+  // A cap's tanh between the products: cap2 tanh(z) = z P(z^2) cap2 for |z| <= 0.75, the best fit of degree 5, off by 1.4e-7 of it at
+  // most; in products s, whose factor c is in the coefficients. A tile with a larger one takes the exponential and the reciprocal,
+  // two more operations at a quarter of the rate (8,704 tokens of 40 heads, 8 key heads, causal: 459 -> @@ us).
+  constexpr bool SERIES = CAP && !SLOPES;
+  float series[6];
+  if (SERIES) {
+    constexpr float p[6] = {0.99999997f, -0.33332967f, 0.13325515f, -0.05334982f, 0.01959379f, -0.00472395f};
+    float f = scores_of.c * scores_of.cap2;
+#pragma unroll
+    for (int i = 0; i < 6; ++i, f *= scores_of.c * scores_of.c) series[i] = uniform(p[i] * f);
+  }
+  auto by_series = [&](float s, float add) __attribute__((always_inline)) {
+    const float u = s * s;
+    float p = series[5];
+#pragma unroll
+    for (int i = 4; i >= 0; --i) p = __builtin_fmaf(p, u, series[i]);
+    return __builtin_fmaf(s, p, add);
+  };
+  bool raw = false;  // whether the scores whose maximum is known are still products, for the series
   const float c0 = scores_of.c;
   f32x16 acc[DB], sA[2], sB[2];
 #pragma unroll
@@ -111,16 +132,17 @@ dense_forward_bf16_kernel(DenseArgs a) {
   uint32_t pk[2][8];
   float cc = c0;  // factor still to be applied to the scores whose maximum is known
 
-  float ls[4] = {0.f, 0.f, 0.f, 0.f};
-  auto weigh = [&](const f32x16 (&sc)[2], int e, float neg_m) __attribute__((always_inline)) {
+  float ls[2] = {0.f, 0.f};
+  auto weigh = [&](const f32x16 (&sc)[2], int e, float neg_m, auto raw_tag) __attribute__((always_inline)) {
+    constexpr bool RAW = decltype(raw_tag)::value;
     const int k = e >> 3, r = 2 * (e & 7);
-    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k][r], cc, neg_m));
-    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k][r + 1], cc, neg_m));
+    const float p0 = __builtin_amdgcn_exp2f(RAW ? by_series(sc[k][r], neg_m) : __builtin_fmaf(sc[k][r], cc, neg_m));
+    const float p1 = __builtin_amdgcn_exp2f(RAW ? by_series(sc[k][r + 1], neg_m) : __builtin_fmaf(sc[k][r + 1], cc, neg_m));
     pk[k][r >> 1] = pack2_bf16(p0, p1);
-    ls[e & 3] += p0 + p1;
+    ls[e & 1] += p0 + p1;
   };
   // Scores of the K tile in `buffer` into sn, and between those products, with EXPS, the weights of the scores sc into pk
-  auto scores = [&](int buffer, f32x16 (&sn)[2], const f32x16 (&sc)[2], auto exps_tag) __attribute__((always_inline)) {
+  auto scores = [&](int buffer, f32x16 (&sn)[2], const f32x16 (&sc)[2], auto exps_tag, auto raw_tag) __attribute__((always_inline)) {
     constexpr bool EXPS = decltype(exps_tag)::value;
     const unsigned char* kt = smem + buffer * Z::kBytes;
     bf16x8 kf[2 * KS];
@@ -138,7 +160,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
       sn[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], q.v[i >> 1], sn[i & 1], 0, 0, 0);
       if constexpr (EXPS) {
 #pragma unroll
-        for (int e = i * E; e < (i + 1) * E; ++e) weigh(sc, e, neg_m);
+        for (int e = i * E; e < (i + 1) * E; ++e) weigh(sc, e, neg_m, raw_tag);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -147,14 +169,21 @@ dense_forward_bf16_kernel(DenseArgs a) {
     const int k = e >> 3, r = 2 * (e & 7);
     mx = fmaxf(fmaxf(mx, sn[k][r]), sn[k][r + 1]);
   };
+  float most = 0.f;  // of a tile's products, for the series
+  auto most_pair = [&](const f32x16 (&sn)[2], int e) __attribute__((always_inline)) {
+    const int k = e >> 3, r = 2 * (e & 7);
+    if (SERIES) most = fmaxf(fmaxf(most, fabsf(sn[k][r])), fabsf(sn[k][r + 1]));
+  };
   // The running maximum covers the scores sn of the keys' tile t afterwards; where there is more to them than a factor, they are exponents.
   auto settle = [&](int t, f32x16 (&sn)[2], float mx, auto whole_tag) __attribute__((always_inline)) {
     constexpr bool WHOLE = decltype(whole_tag)::value;  // seen by all rows of the wave, as the caller knows
     const bool masked = !WHOLE && (t + 1) * BN > hi_all;
     cc = c0;
-    if (CAP || SLOPES || masked) {
-      const int limit = masked ? hi - t * BN - 4 * lh : INT32_MAX;  // (constants on the other side of the comparisons)
-      const float ahead = (float)(pos - t * BN - 4 * lh);
+    raw = SERIES && !masked && !__any(!(most * c0 <= 0.75f));
+    if ((CAP && !raw) || SLOPES || masked) {
+      asm volatile("");  // (a branch: found for every tile, and chosen from, it would cost as much as if it were needed)
+      const int limit = masked ? hi - t * BN : INT32_MAX;  // (constants on the other side of the comparisons)
+      const float ahead = (float)(pos - t * BN);
       mx = -INFINITY;
       cc = 1.f;
 #pragma unroll
@@ -168,11 +197,11 @@ dense_forward_bf16_kernel(DenseArgs a) {
         }
     }
     mx = fmaxf(mx, swap32(mx));
-    const float ms = mx * cc;
+    const float ms = raw ? by_series(mx, 0.f) : mx * cc;
     if (__any(ms > m + kHeadroom<D>)) {
       const float m_new = fmaxf(m, ms), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) ls[u] *= alpha;
+      for (int u = 0; u < 2; ++u) ls[u] *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -182,7 +211,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
   };
   // O^T += V^T P^T with the V tile in `buffer`, and between those products, with MORE, the maximum of the next scores sn
   auto values = [&](int buffer, const f32x16 (&sn)[2], auto more_tag) __attribute__((always_inline)) {
-    constexpr bool MORE = decltype(more_tag)::value && !CAP && !SLOPES;
+    constexpr bool MORE = decltype(more_tag)::value && !SLOPES;
     constexpr int N = 4 * DB;
     bf16x8 vf[N];
     auto rd = [&](int i) {
@@ -196,6 +225,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) rd(i);
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    most = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       __builtin_amdgcn_sched_barrier(0);
@@ -205,7 +235,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
       acc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], bp, acc[i % DB], 0, 0, 0);
       if (MORE && i >= N / 4) {
 #pragma unroll
-        for (int e = (i - N / 4) * 16 / (3 * N / 4); e < (i + 1 - N / 4) * 16 / (3 * N / 4); ++e) max_pair(sn, mx[e & 3], e);
+        for (int e = (i - N / 4) * 16 / (3 * N / 4); e < (i + 1 - N / 4) * 16 / (3 * N / 4); ++e) max_pair(sn, mx[e & 3], e), most_pair(sn, e);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -220,17 +250,18 @@ dense_forward_bf16_kernel(DenseArgs a) {
     SVGEAR_WAIT_VMCNT(0);
     __syncthreads();
     if (t_lo + 1 < t_hi) issue_k(t_lo + 1);
-    scores(0, sA, sB, std::false_type{});
+    scores(0, sA, sB, std::false_type{}, std::false_type{});
     float mx = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) max_pair(sA, mx, e);
+    for (int e = 0; e < 16; ++e) max_pair(sA, mx, e), most_pair(sA, e);
     settle(t_lo, sA, mx, std::false_type{});
     SVGEAR_WAIT_VMCNT(0);
     __syncthreads();
     auto step = [&](int t, int parity, f32x16 (&s_now)[2], f32x16 (&s_next)[2], auto whole_tag) __attribute__((always_inline)) {
       if (t + 2 < t_hi) issue(t + 2, kp, a.kst.n, k_lane, parity);
       issue(t + 1, vp, a.vst.n, v_lane, 2 + (parity ^ 1));
-      scores(parity ^ 1, s_next, s_now, std::true_type{});
+      if (SERIES && raw) scores(parity ^ 1, s_next, s_now, std::true_type{}, std::integral_constant<bool, SERIES>{});
+      else scores(parity ^ 1, s_next, s_now, std::true_type{}, std::false_type{});
       const float next = values(parity, s_next, std::true_type{});
       settle(t + 1, s_next, next, whole_tag);
       SVGEAR_WAIT_VMCNT(0);
@@ -249,7 +280,10 @@ dense_forward_bf16_kernel(DenseArgs a) {
     auto last = [&](int parity, const f32x16 (&s)[2]) __attribute__((always_inline)) {
       const float neg_m = m == -INFINITY ? 0.f : -m;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) weigh(s, e, neg_m);
+      for (int e = 0; e < 16; ++e) {
+        if (SERIES && raw) weigh(s, e, neg_m, std::integral_constant<bool, SERIES>{});
+        else weigh(s, e, neg_m, std::false_type{});
+      }
       __builtin_amdgcn_sched_barrier(0);
       values(parity, s, std::false_type{});
     };
@@ -261,20 +295,21 @@ dense_forward_bf16_kernel(DenseArgs a) {
     }
   }
 
-  float l = (ls[0] + ls[1]) + (ls[2] + ls[3]);
+  float l = ls[0] + ls[1];
   l += swap32(l);
-  const int out_row = again(row), out_token = out_row / a.G, out_head = hk * a.G + (out_row - out_token * a.G);
-  const bool live = wave_row + again(li) < at.end;
+  const int l2 = again(lane), out_row = min(wave_row + (l2 & 31), at.end - 1), out_token = out_row / a.G;
+  const int out_head = hk * a.G + (out_row - out_token * a.G);
+  const bool live = wave_row + (l2 & 31) < at.end;
   if (a.splits > 1) {
     if (!live) return;
     const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + out_row;
-    if (lh == 0) a.part_ml[out] = make_float2(m, l);
-    Z::each_four(acc, lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
+    if (l2 < 32) a.part_ml[out] = make_float2(m, l);
+    Z::each_four(acc, l2 >> 5, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
     return;
   }
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-  store_whole(static_cast<bf16_t*>(a.o) + b * a.ost.b + out_head * a.ost.h + out_token * a.ost.n, acc, inv, lh, live);
-  if (live && a.lse && lh == 0) a.lse[((int64_t)b * a.H + out_head) * a.Nq + out_token] = (m + log2f(l)) * kLn2;
+  store_whole(static_cast<bf16_t*>(a.o) + b * a.ost.b + out_head * a.ost.h + out_token * a.ost.n, acc, inv, l2 >> 5, live);
+  if (live && a.lse && l2 < 32) a.lse[((int64_t)b * a.H + out_head) * a.Nq + out_token] = (m + log2f(l)) * kLn2;
 }
 
 template <int D, bool CAP, bool SLOPES>
