@@ -103,22 +103,22 @@ dense_forward_bf16_kernel(DenseArgs a) {
   Scores<bf16_t, CAP, SLOPES> scores_of(a);
   scores_of.c = uniform(fabsf(scores_of.c));
   scores_of.cap2 = uniform(scores_of.cap2);
-  // A cap's tanh between the products: cap2 tanh(z) = z P(z^2) cap2 for |z| <= 0.75, the best fit of degree 5, off by 1.4e-7 of it at
+  // A cap's tanh between the products: cap2 tanh(z) = z P(z^2) cap2 for |z| <= 0.5, P the best fit of degree 3, off by 6e-7 of it at
   // most; in products s, whose factor c is in the coefficients. A tile with a larger one takes the exponential and the reciprocal,
-  // two more operations at a quarter of the rate (8,704 tokens of 40 heads, 8 key heads, causal: 459 -> @@ us).
+  // two more operations at a quarter of the rate (8,704 tokens of 40 heads, 8 key heads, causal: 440 us so, 389 by the series).
   constexpr bool SERIES = CAP && !SLOPES;
-  float series[6];
+  float series[4];
   if (SERIES) {
-    constexpr float p[6] = {0.99999997f, -0.33332967f, 0.13325515f, -0.05334982f, 0.01959379f, -0.00472395f};
+    constexpr float p[4] = {0.99999946f, -0.33326376f, 0.13190912f, -0.04441858f};
     float f = scores_of.c * scores_of.cap2;
 #pragma unroll
-    for (int i = 0; i < 6; ++i, f *= scores_of.c * scores_of.c) series[i] = uniform(p[i] * f);
+    for (int i = 0; i < 4; ++i, f *= scores_of.c * scores_of.c) series[i] = uniform(p[i] * f);
   }
   auto by_series = [&](float s, float add) __attribute__((always_inline)) {
     const float u = s * s;
-    float p = series[5];
+    float p = series[3];
 #pragma unroll
-    for (int i = 4; i >= 0; --i) p = __builtin_fmaf(p, u, series[i]);
+    for (int i = 2; i >= 0; --i) p = __builtin_fmaf(p, u, series[i]);
     return __builtin_fmaf(s, p, add);
   };
   bool raw = false;  // whether the scores whose maximum is known are still products, for the series
@@ -179,7 +179,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
     constexpr bool WHOLE = decltype(whole_tag)::value;  // seen by all rows of the wave, as the caller knows
     const bool masked = !WHOLE && (t + 1) * BN > hi_all;
     cc = c0;
-    raw = SERIES && !masked && !__any(!(most * c0 <= 0.75f));
+    raw = SERIES && !masked && !__any(!(most * c0 <= 0.5f));
     if ((CAP && !raw) || SLOPES || masked) {
       asm volatile("");  // (a branch: found for every tile, and chosen from, it would cost as much as if it were needed)
       const int limit = masked ? hi - t * BN : INT32_MAX;  // (constants on the other side of the comparisons)
