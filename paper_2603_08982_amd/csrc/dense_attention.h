@@ -32,7 +32,7 @@ struct DenseArgs {
 };
 
 constexpr int kDenseWaves = 4;
-constexpr int kDenseRows = 32 * kDenseWaves;  // rows (queries, or keys for their gradients) of a workgroup
+constexpr int kDenseRows = 32 * kDenseWaves;  // rows (queries, or keys for their gradients) of a workgroup in bf16
 
 // Tiles of `per` rows that `rows` rows in n_docs documents (0: not cut) take at most: a document starts a tile, and so do the
 // rows before the first and behind the last document.

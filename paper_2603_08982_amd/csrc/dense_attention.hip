@@ -102,11 +102,11 @@ dense_delta_kernel(const T* dy, Strides yst, const T* o, Strides ost, int H, int
 // ---- how many parts the rows of the other side are cut into: so many that some 512 workgroups (two a CU) have work, but two
 // tiles a part at least. `own`: rows a key head has on the workgroups' side, `other`: on the other. Where a head's rows are one
 // tile (single tokens), the parts cost little and are finer, four tiles each, so that pasts of different lengths even out.
+int rows_of_tile(svgear_dtype dt) { return dt == SVGEAR_F32 ? 32 : kDenseRows; }
 int parts_of(int64_t heads, int64_t own, int64_t other, int n_docs, svgear_dtype dt) {
-  const int64_t tiles = heads * ceil_div(own, kDenseRows), each = ceil_div(other, n_docs > 1 ? n_docs : 1);
-  const int64_t most = ceil_div(each, 2 * (dt == SVGEAR_F32 ? 32 : 64));
-  const int64_t wanted = own <= kDenseRows ? std::min<int64_t>(1024 / tiles, most / 2) : 512 / tiles;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(std::max<int64_t>(wanted, 512 / tiles), most), 64));
+  const int64_t tiles = heads * ceil_div(own, rows_of_tile(dt)), each = ceil_div(other, n_docs > 1 ? n_docs : 1), most = ceil_div(each, 128);
+  const int64_t wanted = own <= kDenseRows ? std::max<int64_t>(512 / tiles, std::min<int64_t>(1024 / tiles, most / 2)) : 512 / tiles;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(wanted, most), 64));
 }
 
 struct Sizes {
@@ -122,7 +122,7 @@ bool sizes_ok(const Sizes& z) {
     return false;
   const int64_t heads = (int64_t)z.B * z.Hk;
   if ((int64_t)z.B * z.H > kMaxDenseRows || (z.H / z.Hk) * z.Nq > kMaxDenseRows) return false;
-  const int64_t q = dense_slots((z.H / z.Hk) * z.Nq, z.n_docs, kDenseRows), k = dense_slots(z.Nk, z.n_docs, kDenseRows);
+  const int64_t q = dense_slots((z.H / z.Hk) * z.Nq, z.n_docs, rows_of_tile(z.dt)), k = dense_slots(z.Nk, z.n_docs, rows_of_tile(z.dt));
   return heads * std::max(q, k) <= kMaxDenseRows && (__int128)z.B * z.H * z.Nq <= ((__int128)1 << 40) &&
          (__int128)heads * z.Nk <= ((__int128)1 << 40);
 }
@@ -252,7 +252,7 @@ extern "C" int svgear_attention(const void* q, const int64_t qstride[3], const v
   a.o = o;
   a.ost = strides_of(ostride, z, H, Nq);
   a.lse = lse;
-  a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, kDenseRows);
+  a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
   a.splits = parts_over_keys(z);
   if (a.splits > 1) {
     Workspace w(ws, ws_bytes);
@@ -310,7 +310,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
   if (dq) {
     a.o = dq;
     a.ost = strides_of(dqstride, z, H, Nq);
-    a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, kDenseRows);
+    a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
     a.splits = parts_over_keys(z);
     done = launch(a, z, kDenseDq, s);
     if (done != SVGEAR_OK) return done;
@@ -324,7 +324,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
   a.dk = dk, a.dv = dv;
   a.dkst = strides_of(dkstride, z, Hk, Nk);
   a.dvst = strides_of(dvstride, z, Hk, Nk);
-  a.slots = (int)dense_slots(Nk, k_offsets ? n_docs : 0, kDenseRows);
+  a.slots = (int)dense_slots(Nk, k_offsets ? n_docs : 0, rows_of_tile(dt));
   a.splits = parts_over_queries(z);
   done = launch(a, z, kDenseDkv, s);
   if (done != SVGEAR_OK || a.splits == 1) return done;

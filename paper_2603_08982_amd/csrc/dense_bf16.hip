@@ -1,4 +1,4 @@
-// Dense attention with masks in bf16: the kernel of dense_tile.h with its phases laid over each other.
+// Dense attention with masks in bf16.
 //
 // What bounds it: the matrix cores and the vector unit alike. A step of a wave (64 keys, 32 queries, d = 128) is 32 products of 32
 // cycles, and 32 exponentials a lane at a quarter of the rate with their scaling, maximum, sum and conversion, some 950 cycles.
@@ -46,10 +46,9 @@ dense_forward_bf16_kernel(DenseArgs a) {
   if (a.causal) slot = a.slots - 1 - slot;  // the longest first
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const int32_t* qo = a.q_offsets ? a.q_offsets + (a.docs_shared ? 0 : (int64_t)b * (a.n_docs + 1)) : nullptr;
-  const Place at = place_of(qo, a.n_docs, a.Nq, a.G, kDenseRows, slot, lane);
+  const Found at = find_tile<true>(a, b, kDenseRows, slot, lane);
   if (at.first >= at.end) return;
-  const Document doc(a, b, at.doc);
+  const Document& doc = at.doc;
 
   const int wave_row = at.first + 32 * wave, row = min(wave_row + li, at.end - 1);
   const int token = row / a.G, head = hk * a.G + (row - token * a.G);
@@ -312,20 +311,16 @@ dense_forward_bf16_kernel(DenseArgs a) {
   if (live && a.lse && l2 < 32) a.lse[((int64_t)b * a.H + out_head) * a.Nq + out_token] = (m + log2f(l)) * kLn2;
 }
 
-template <int D, bool CAP, bool SLOPES>
-int launch_bf16_mode(const DenseArgs& a, hipStream_t s) {
-  const int64_t groups = ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8;
-  dense_forward_bf16_kernel<D, CAP, SLOPES><<<long_grid(groups, a.splits), 64 * kDenseWaves, 0, s>>>(a);
-  SVGEAR_LAUNCH_CHECK();
-  return SVGEAR_OK;
-}
 template <int D>
-int launch_bf16_width(const DenseArgs& a, hipStream_t s) {
-  if (a.cap > 0.f) return a.slopes ? launch_bf16_mode<D, true, true>(a, s) : launch_bf16_mode<D, true, false>(a, s);
-  return a.slopes ? launch_bf16_mode<D, false, true>(a, s) : launch_bf16_mode<D, false, false>(a, s);
+int launch(const DenseArgs& a, hipStream_t s) {
+  return by_scores(a, [&](auto cap, auto slopes) -> int {
+    dense_forward_bf16_kernel<D, decltype(cap)::value, decltype(slopes)::value><<<dense_grid(a), 64 * kDenseWaves, 0, s>>>(a);
+    SVGEAR_LAUNCH_CHECK();
+    return SVGEAR_OK;
+  });
 }
 
 }  // namespace
 
-int launch_dense_bf16(const DenseArgs& a, int d, hipStream_t s) { return d == 64 ? launch_bf16_width<64>(a, s) : launch_bf16_width<128>(a, s); }
+int launch_dense_bf16(const DenseArgs& a, int d, hipStream_t s) { return d == 64 ? launch<64>(a, s) : launch<128>(a, s); }
 }  // namespace svgear

@@ -4,8 +4,8 @@
 //   backward: p_ij = e^(s_ij - lse_i), ds_ij = p_ij (dy_i v_j - dy_i o_i) (1 - tanh^2),
 //   dq_i = scale sum_j ds_ij k_j, dk_j = scale sum_i ds_ij q_i, dv_j = sum_i p_ij dy_i
 //
-// A wave owns 32 rows (queries; keys for dk and dv) as columns of the matrix products, in registers, and the workgroup's four
-// waves share tiles of the other side's rows, which go from global memory straight into LDS, the next under the present one:
+// A wave owns 32 rows (queries; keys for dk and dv) as columns of the matrix products, in registers, and reads tiles of the other
+// side's rows, which go from global memory straight into LDS, the next under the present one:
 //   X^T = tile columns^T  (32 x 32: a register holds tile rows 8 (r / 4) + 4 (lane / 32) + r % 4 of column lane % 32)
 //   acc^T += tile^T X     (those registers are operands as they stand; bf16 reads the tile transposed with ds_read_b64_tr_b16)
 // No atomics: dq is made by a pass over the keys, dk and dv by one over the queries, which finds the scores again (7 products
@@ -214,64 +214,10 @@ __device__ __forceinline__ void copy_tile(const T* base, uint32_t lds, int wave,
 // ---- documents and masks
 __device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-// The tile that slot t of batch entry b stands for: rows [first, end) of document doc (-1: rows of no document).
-struct Place {
-  int first, end, doc;
-};
-// Document c's tiles begin at slot floor(start_c rows / per) + c, which leaves room for what precedes it and needs no list; rows
-// before the first and behind the last document count as documents. Lanes look at 64 documents at once. Offsets out of range
-// are taken as the nearest in range.
-__device__ __forceinline__ Place place_of(const int32_t* offsets, int n_docs, int N, int G, int per, int t, int lane) {
-  if (!offsets) return {t * per, N * G, 0};
-  const int all = n_docs + 2;
-  int c = -1;
-  for (int c0 = 0; c0 < all; c0 += 64) {
-    const int i = c0 + lane;
-    bool before = false;
-    if (i < all) {
-      const int start = i == 0 ? 0 : clamp_to(offsets[i - 1], 0, N);
-      before = (int64_t)start * G / per + i <= t;
-    }
-    const unsigned long long votes = __ballot(before);
-    c += __popcll(votes);
-    if (votes != ~0ull) break;
-  }
-  c = max(c, 0);
-  const int start = c == 0 ? 0 : clamp_to(offsets[c - 1], 0, N), end = c == all - 1 ? N : clamp_to(offsets[c], 0, N);
-  Place p;
-  const int64_t first = (int64_t)start * G + (t - ((int64_t)start * G / per + c)) * per;
-  p.first = uniform((int)(first < 0 ? 0 : first < INT32_MAX ? first : INT32_MAX));
-  p.end = uniform(end * G);
-  p.doc = uniform(c >= 1 && c <= n_docs ? c - 1 : -1);
-  return p;
-}
-
 // A document: its first query and key, how many of each, and what each query sees.
 struct Document {
   int q0, nq, k0, nk, prefix;
   bool causal;
-  __device__ __forceinline__ explicit Document(const DenseArgs& a) : causal(a.causal) {}
-  __device__ __forceinline__ Document(const DenseArgs& a, int b, int doc) {
-    const int64_t row = a.docs_shared ? 0 : b;
-    q0 = 0, nq = a.Nq, k0 = 0, nk = a.Nk, prefix = 0;
-    causal = a.causal;
-    if (doc < 0) {
-      nq = nk = 0;
-      return;
-    }
-    if (a.q_offsets) {
-      const int32_t* o = a.q_offsets + row * (a.n_docs + 1) + doc;
-      q0 = clamp_to(o[0], 0, a.Nq);
-      nq = clamp_to(o[1], q0, a.Nq) - q0;
-    }
-    if (a.k_offsets) {
-      const int32_t* o = a.k_offsets + row * (a.n_docs + 1) + doc;
-      k0 = clamp_to(o[0], 0, a.Nk);
-      nk = clamp_to(o[1], k0, a.Nk) - k0;
-    }
-    if (a.prefix) prefix = clamp_to(a.prefix[row * a.n_docs + doc], 0, nk);
-    q0 = uniform(q0), nq = uniform(nq), k0 = uniform(k0), nk = uniform(nk), prefix = uniform(prefix);
-  }
   // where the document's query i stands among its keys: the last query at the last key
   __device__ __forceinline__ int position(int i) const { return i + nk - nq; }
   // query i sees the keys [0, seen(i)), which grows with i
@@ -280,13 +226,74 @@ struct Document {
   __device__ __forceinline__ int first_seer(int j) const { return causal && j >= prefix ? max(j - (nk - nq), 0) : 0; }
 };
 
-// Workgroup to (key head of the batch, slot): consecutive logical indexes, which share keys or queries, on one XCD.
+// The tile that slot t of a head of batch entry b stands for: rows [first, end) of a document, of which the tile has the first `per`
+// (QUERIES: rows of queries; otherwise keys). Rows of no document are those of one that has nothing.
+// Document c's tiles begin at slot floor(start_c rows / per) + c, which leaves room for what precedes it and needs no list; the rows
+// before the first and behind the last document count as documents. A lane looks at a document each, and all that is to be known of
+// it comes with one round of loads (three, one after the other, took 2 us of every workgroup). Offsets out of range are taken as the
+// nearest in range.
+struct Found {
+  int first, end;
+  Document doc;
+};
+template <bool QUERIES>
+__device__ __forceinline__ Found find_tile(const DenseArgs& a, int b, int per, int t, int lane) {
+  const int64_t row = a.docs_shared ? 0 : b, pitch = a.n_docs + 1;
+  const int32_t* own = QUERIES ? a.q_offsets : a.k_offsets;
+  const int32_t* other = QUERIES ? a.k_offsets : a.q_offsets;
+  const int n_own = QUERIES ? a.Nq : a.Nk, n_other = QUERIES ? a.Nk : a.Nq, G = QUERIES ? a.G : 1;
+  if (own) own += row * pitch;
+  if (other) other += row * pitch;
+  const int all = own ? a.n_docs + 2 : 1;  // (without offsets the one document alone)
+  int c = 0, start = 0, end = 0, lo = 0, hi = 0, prefix = 0;
+  for (int c0 = 0; c0 < all; c0 += 64) {
+    const int i = c0 + lane, d = own ? i - 1 : i;  // its number among the documents
+    const bool real = d >= 0 && d < a.n_docs;
+    const int v_start = own && i > 0 && i < all ? clamp_to(own[i - 1], 0, n_own) : 0;
+    const int v_end = own && i < all - 1 ? clamp_to(own[i], 0, n_own) : n_own;
+    const int v_lo = real && other ? clamp_to(other[d], 0, n_other) : 0;
+    const int v_hi = !real ? 0 : other ? clamp_to(other[d + 1], 0, n_other) : n_other;
+    const int v_prefix = real && a.prefix ? a.prefix[row * a.n_docs + d] : 0;
+    const unsigned long long votes = __ballot(i < all && (int64_t)v_start * G / per + i <= t);
+    const int found = __popcll(votes);
+    if (found == 0) break;
+    c = c0 + found - 1;
+    start = __builtin_amdgcn_readlane(v_start, found - 1);
+    end = __builtin_amdgcn_readlane(v_end, found - 1);
+    lo = __builtin_amdgcn_readlane(v_lo, found - 1);
+    hi = max(__builtin_amdgcn_readlane(v_hi, found - 1), lo);
+    prefix = __builtin_amdgcn_readlane(v_prefix, found - 1);
+    if (found < 64) break;
+  }
+  const bool real = !own || (c >= 1 && c <= a.n_docs);
+  const int n = real ? max(end - start, 0) : 0;
+  Found f;
+  const int64_t first = (int64_t)start * G + (t - ((int64_t)start * G / per + c)) * per;
+  f.first = first < 0 ? 0 : first < INT32_MAX ? (int)first : INT32_MAX;
+  f.end = end * G;
+  f.doc.q0 = QUERIES ? start : lo, f.doc.nq = QUERIES ? n : hi - lo;
+  f.doc.k0 = QUERIES ? lo : start, f.doc.nk = QUERIES ? hi - lo : n;
+  f.doc.prefix = clamp_to(prefix, 0, f.doc.nk);
+  f.doc.causal = a.causal;
+  return f;
+}
+
+// Workgroup to (key head of the batch, slot). Workgroups go to the 8 XCDs in turn: each takes whole heads, whose keys and values (or
+// queries) its L2 then holds once, and the heads that are left over when each has as many are dealt out by the slot, so that tiles
+// of different lengths (documents, the triangle of a causal mask) fall on all of them alike.
 __device__ __forceinline__ bool dense_index(const DenseArgs& a, int& bh, int& slot) {
-  const unsigned total = (unsigned)(a.B * a.Hk) * (unsigned)a.slots, per = (total + 7) / 8, wg = long_grid_index();
-  const unsigned logical = (wg & 7) * per + (wg >> 3);
-  if ((wg >> 3) >= per || logical >= total) return false;
-  bh = (int)(logical / (unsigned)a.slots);
-  slot = (int)(logical - (unsigned)bh * (unsigned)a.slots);
+  const unsigned heads = (unsigned)(a.B * a.Hk), slots = (unsigned)a.slots, whole = heads / 8, rest = heads % 8;
+  const unsigned wg = long_grid_index(), xcd = wg & 7, i = wg >> 3;
+  if (i < whole * slots) {
+    const unsigned h = i / slots;
+    bh = (int)(h * 8 + xcd);
+    slot = (int)(i - h * slots);
+    return true;
+  }
+  const unsigned r = (i - whole * slots) * 8 + xcd;
+  if (rest == 0 || r >= rest * slots) return false;
+  slot = (int)(r / rest);
+  bh = (int)(whole * 8 + (r - (unsigned)slot * rest));
   return true;
 }
 
@@ -324,351 +331,14 @@ struct Scores {
   __device__ __forceinline__ float keeps(float in) const { return __builtin_fmaf(-in, in, 1.f); }
 };
 
-// ---- forward: 128 queries a workgroup
-template <typename T, int D, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(64 * kDenseWaves, 2)
-dense_forward_kernel(DenseArgs a) {
-  using Z = Tile<T, D>;
-  constexpr int DB = D / 32, BN = Z::kRows;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
-  if (a.causal) slot = a.slots - 1 - slot;  // the longest first
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const int32_t* qo = a.q_offsets ? a.q_offsets + (a.docs_shared ? 0 : (int64_t)b * (a.n_docs + 1)) : nullptr;
-  const Place at = place_of(qo, a.n_docs, a.Nq, a.G, kDenseRows, slot, lane);
-  if (at.first >= at.end) return;
-  const Document doc(a, b, at.doc);
-
-  const int wave_row = at.first + 32 * wave, row = wave_row + li, row_c = min(row, at.end - 1);
-  const bool active = wave_row < at.end;
-  const int token = row_c / a.G, head = hk * a.G + (row_c - token * a.G);
-  const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
-  // keys that every row of this wave sees, that some row of it sees, and of the workgroup
-  const int hi_all = doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0), hi_any = doc.seen(min(wave_row + 31, at.end - 1) / a.G - doc.q0);
-  const int hi_wg = doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0);
-  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
-  const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
-
-  typename Z::Column q;
-  q.load(static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
-  const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
-  SVGEAR_WAIT_VMCNT(0);  // (the copies below are not seen by the compiler, which would wait for them inside the loop)
-
-  const Z z(lane);
-  const Scores<T, CAP, SLOPES> scores(a);
-  const uint32_t lds = lds_address(smem);
-  const T* kp = static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
-  const T* vp = static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const int last = hi_wg - 1 - t * BN;  // (keys that no row here sees are not read)
-    copy_tile<Z>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
-                    [&](int r) { return (int64_t)min(r, last) * a.kst.n; });
-    copy_tile<Z>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
-                    [&](int r) { return (int64_t)min(r, last) * a.vst.n; });
-  };
-
-  f32x16 acc[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) clear(acc[db]);
-  float m = -INFINITY, l = 0.f;
-  if (t_lo < t_hi) issue(t_lo);
-  for (int t = t_lo; t < t_hi; ++t) {
-    SVGEAR_WAIT_VMCNT(0);
-    __syncthreads();
-    if (t + 1 < t_hi) issue(t + 1);
-    if (!active || t * BN >= hi_any) continue;
-    const unsigned char* kt = smem + (t & 1) * Z::kBytes;
-    const unsigned char* vt = smem + (2 + (t & 1)) * Z::kBytes;
-    f32x16 x[Z::kBlocks];
-    float mx = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < Z::kBlocks; ++kb) {
-      clear(x[kb]);
-      z.rows_times(kt, kb, q, x[kb]);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = t * BN + 32 * kb + row_of(r, lh);
-        x[kb][r] = scores.outer(scores.inner(x[kb][r]), (float)(pos - j), slope, 0.f);
-      }
-    }
-    if ((t + 1) * BN > hi_all) {
-#pragma unroll
-      for (int kb = 0; kb < Z::kBlocks; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (t * BN + 32 * kb + row_of(r, lh) >= hi) x[kb][r] = -INFINITY;
-    }
-#pragma unroll
-    for (int kb = 0; kb < Z::kBlocks; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[kb][r]);
-    mx = fmaxf(mx, swap32(mx));
-    if (__any(mx > m)) {
-      const float m_new = fmaxf(m, mx), alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
-      m = m_new;
-    }
-    const float m_use = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int kb = 0; kb < Z::kBlocks; ++kb) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[kb][r] = __builtin_amdgcn_exp2f(x[kb][r] - m_use);
-        l += x[kb][r];
-      }
-      z.transposed_times(vt, kb, x[kb], acc, lane);
-    }
-  }
-
-  if (!active) return;
-  l += swap32(l);
-  if (row >= at.end) return;
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + row;
-    if (lh == 0) a.part_ml[out] = make_float2(m, l);
-    Z::each_four(acc, lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
-    return;
-  }
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-  T* o = static_cast<T*>(a.o) + b * a.ost.b + head * a.ost.h + token * a.ost.n;
-  Z::each_four(acc, lh, [&](int d, float4 v) { store_four(o + d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv)); });
-  if (a.lse && lh == 0) a.lse[((int64_t)b * a.H + head) * a.Nq + token] = (m + log2f(l)) * kLn2;
+// f(cap, slopes) as types, for what a call has
+template <typename F>
+int by_scores(const DenseArgs& a, F f) {
+  if (a.cap > 0.f) return a.slopes ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+  return a.slopes ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
-
-// ---- the queries' gradients: 128 queries a workgroup, a pass over the keys
-template <typename T, int D, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(64 * kDenseWaves, sizeof(T) == 4 && D == 128 ? 1 : 2)
-dense_dq_kernel(DenseArgs a) {
-  using Z = Tile<T, D>;
-  constexpr int DB = D / 32, BN = Z::kRows;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
-  if (a.causal) slot = a.slots - 1 - slot;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const int32_t* qo = a.q_offsets ? a.q_offsets + (a.docs_shared ? 0 : (int64_t)b * (a.n_docs + 1)) : nullptr;
-  const Place at = place_of(qo, a.n_docs, a.Nq, a.G, kDenseRows, slot, lane);
-  if (at.first >= at.end) return;
-  const Document doc(a, b, at.doc);
-
-  const int wave_row = at.first + 32 * wave, row = wave_row + li, row_c = min(row, at.end - 1);
-  const bool active = wave_row < at.end;
-  const int token = row_c / a.G, head = hk * a.G + (row_c - token * a.G);
-  const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
-  const int hi_all = doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0), hi_any = doc.seen(min(wave_row + 31, at.end - 1) / a.G - doc.q0);
-  const int hi_wg = doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0);
-  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
-  const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
-
-  typename Z::Column q, dy;
-  q.load(static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
-  dy.load(static_cast<const T*>(a.dy) + b * a.yst.b + head * a.yst.h + token * a.yst.n, lh);
-  const int64_t stat = ((int64_t)b * a.H + head) * a.Nq + token;
-  const float lse2 = a.lse_in[stat] * kLog2e, delta = a.delta[stat];
-  const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
-  SVGEAR_WAIT_VMCNT(0);
-
-  const Z z(lane);
-  const Scores<T, CAP, SLOPES> scores(a);
-  const uint32_t lds = lds_address(smem);
-  const T* kp = static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
-  const T* vp = static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const int last = hi_wg - 1 - t * BN;
-    copy_tile<Z>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
-                    [&](int r) { return (int64_t)min(r, last) * a.kst.n; });
-    copy_tile<Z>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
-                    [&](int r) { return (int64_t)min(r, last) * a.vst.n; });
-  };
-
-  f32x16 acc[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) clear(acc[db]);
-  if (t_lo < t_hi) issue(t_lo);
-  for (int t = t_lo; t < t_hi; ++t) {
-    SVGEAR_WAIT_VMCNT(0);
-    __syncthreads();
-    if (t + 1 < t_hi) issue(t + 1);
-    if (!active || t * BN >= hi_any) continue;
-    const unsigned char* kt = smem + (t & 1) * Z::kBytes;
-    const unsigned char* vt = smem + (2 + (t & 1)) * Z::kBytes;
-    const bool masked = (t + 1) * BN > hi_all;
-#pragma unroll
-    for (int kb = 0; kb < Z::kBlocks; ++kb) {
-      f32x16 x, dp;
-      clear(x);
-      clear(dp);
-      z.rows_times(kt, kb, q, x);
-      z.rows_times(vt, kb, dy, dp);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = t * BN + 32 * kb + row_of(r, lh);
-        const float in = scores.inner(x[r]);
-        float ds = __builtin_amdgcn_exp2f(scores.outer(in, (float)(pos - j), slope, lse2)) * (dp[r] - delta);
-        if (CAP) ds *= scores.keeps(in);
-        x[r] = masked && j >= hi ? 0.f : ds;
-      }
-      z.transposed_times(kt, kb, x, acc, lane);
-    }
-  }
-
-  if (!active || row >= at.end) return;
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + row;
-    Z::each_four(acc, lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
-    return;
-  }
-  T* o = static_cast<T*>(a.o) + b * a.ost.b + head * a.ost.h + token * a.ost.n;
-  const float f = a.scale;
-  Z::each_four(acc, lh, [&](int d, float4 v) { store_four(o + d, make_float4(v.x * f, v.y * f, v.z * f, v.w * f)); });
-}
-
-// ---- the keys' and values' gradients: 128 keys a workgroup, a pass over the queries of all heads that share them
-template <typename T, int D, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(64 * kDenseWaves, sizeof(T) == 4 && D == 128 ? 1 : 2)
-dense_dkv_kernel(DenseArgs a) {
-  // Two waves a SIMD, one's exponentials under the other's products, leave 256 registers: at d = 128 in bf16 the accumulators
-  // take 128 and the keys 32, and the values wait in LDS, under tiles of 32 rows.
-  constexpr bool kPark = sizeof(T) == 2 && D == 128;
-  using Z = Tile<T, D, kPark ? 1 : sizeof(T) == 2 ? 2 : 1>;
-  constexpr int DB = D / 32, BN = Z::kRows;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes + (kPark ? kDenseWaves * Z::kParked : 0)];  // two of Q, two of dy
-  __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, position
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const int32_t* ko = a.k_offsets ? a.k_offsets + (a.docs_shared ? 0 : (int64_t)b * (a.n_docs + 1)) : nullptr;
-  const Place at = place_of(ko, a.n_docs, a.Nk, 1, kDenseRows, slot, lane);
-  if (at.first >= at.end) return;
-  const Document doc(a, b, at.doc);
-
-  const int wave_key = at.first + 32 * wave, key = wave_key + li, key_c = min(key, at.end - 1);
-  const bool active = wave_key < at.end;
-  // rows of the document [from, end) see key j of it; rows from `from_all` on see all keys of this wave, from from_any on one of them
-  const int j = key_c - doc.k0, from = doc.first_seer(j) * a.G, end = doc.nq * a.G;
-  const int from_all = doc.first_seer(min(wave_key + 31, at.end - 1) - doc.k0) * a.G;
-  const int from_any = doc.first_seer(min(wave_key, at.end - 1) - doc.k0) * a.G;
-  const int first_tile = doc.first_seer(at.first - doc.k0) * a.G / BN, tiles_end = (end + BN - 1) / BN;
-  const int tiles = max(tiles_end - first_tile, 0), split = blockIdx.y;
-  const int t_lo = first_tile + (int)((int64_t)tiles * split / a.splits), t_hi = first_tile + (int)((int64_t)tiles * (split + 1) / a.splits);
-
-  typename Z::Column k, v;
-  unsigned char* parked = smem + 4 * Z::kBytes + (kPark ? wave * Z::kParked : 0);
-  k.load(static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + key_c * a.kst.n, lh);
-  v.load(static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + key_c * a.vst.n, lh);
-  if constexpr (kPark) Z::park(parked, v, lane);
-  SVGEAR_WAIT_VMCNT(0);
-
-  const Z z(lane);
-  const Scores<T, CAP, SLOPES> scores(a);
-  const uint32_t lds = lds_address(smem), lds_stats = lds_address(stats);
-  const T* qp = static_cast<const T*>(a.q) + b * a.qst.b + hk * a.G * a.qst.h + doc.q0 * a.qst.n;
-  const T* yp = static_cast<const T*>(a.dy) + b * a.yst.b + hk * a.G * a.yst.h + doc.q0 * a.yst.n;
-  const int64_t stat0 = ((int64_t)b * a.H + hk * a.G) * a.Nq + doc.q0;
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    auto offset = [&](int r, const Strides& st) {
-      const int row = min(t * BN + r, end - 1), token = a.G == 1 ? row : row / a.G;
-      return (row - token * a.G) * st.h + token * st.n;
-    };
-    copy_tile<Z>(qp, lds + (t & 1) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.qst); });
-    copy_tile<Z>(yp, lds + (2 + (t & 1)) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.yst); });
-    const int row = min(t * BN + lane, end - 1), token = a.G == 1 ? row : row / a.G;
-    const uint32_t to = (uint32_t)uniform((int)(lds_stats + ((t & 1) * 4 + wave) * 256));
-    if (wave < 2) async_copy_4B((wave == 0 ? a.lse_in : a.delta) + stat0 + (int64_t)(row - token * a.G) * a.Nq + token, to);
-    if (SLOPES && wave == 2) async_copy_4B(a.slopes + hk * a.G + row - token * a.G, to);
-    if (SLOPES && wave == 3) stats[t & 1][3][lane] = (float)doc.position(token);
-  };
-
-  f32x16 dk[DB], dv[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) clear(dk[db]), clear(dv[db]);
-  if (t_lo < t_hi) issue(t_lo);
-  for (int t = t_lo; t < t_hi; ++t) {
-    SVGEAR_WAIT_VMCNT(0);
-    __syncthreads();
-    if (t + 1 < t_hi) issue(t + 1);
-    if (!active || (t + 1) * BN <= from_any) continue;
-    const unsigned char* qt = smem + (t & 1) * Z::kBytes;
-    const unsigned char* yt = smem + (2 + (t & 1)) * Z::kBytes;
-    const bool masked = t * BN < from_all || (t + 1) * BN > end;
-#pragma unroll
-    for (int kb = 0; kb < Z::kBlocks; ++kb) {
-      f32x16 x, dp;
-      clear(x);
-      clear(dp);
-      z.rows_times(qt, kb, k, x);
-      if constexpr (kPark) z.rows_times(yt, kb, parked, dp, lane);
-      else z.rows_times(yt, kb, v, dp);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        auto of_rows = [&](int what) { return *reinterpret_cast<const float4*>(&stats[t & 1][what][32 * kb + 8 * g + 4 * lh]); };
-        const float4 ls = of_rows(0), de = of_rows(1);
-        const float lse[4] = {ls.x, ls.y, ls.z, ls.w}, delta[4] = {de.x, de.y, de.z, de.w};
-        float slope[4] = {0.f, 0.f, 0.f, 0.f}, dist[4] = {0.f, 0.f, 0.f, 0.f};
-        if (SLOPES) {
-          const float4 sl = of_rows(2), po = of_rows(3);
-          slope[0] = sl.x * kLog2e, slope[1] = sl.y * kLog2e, slope[2] = sl.z * kLog2e, slope[3] = sl.w * kLog2e;
-          dist[0] = po.x - (float)j, dist[1] = po.y - (float)j, dist[2] = po.z - (float)j, dist[3] = po.w - (float)j;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * g + i, row = t * BN + 32 * kb + row_of(r, lh);
-          const float in = scores.inner(x[r]);
-          float p = __builtin_amdgcn_exp2f(scores.outer(in, dist[i], slope[i], lse[i] * kLog2e));
-          float ds = p * (dp[r] - delta[i]);
-          if (CAP) ds *= scores.keeps(in);
-          if (masked && (row < from || row >= end)) p = ds = 0.f;
-          x[r] = p;
-          dp[r] = ds;
-        }
-      }
-      z.transposed_times(yt, kb, x, dv, lane);
-      z.transposed_times(qt, kb, dp, dk, lane);
-    }
-  }
-
-  if (!active || key >= at.end) return;
-  const float f = a.scale;
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.B * a.Hk * a.Nk, out = split * rows + (int64_t)bh * a.Nk + key;
-    Z::each_four(dk, lh, [&](int d, float4 u) { store_four(a.part + out * D + d, make_float4(u.x * f, u.y * f, u.z * f, u.w * f)); });
-    Z::each_four(dv, lh, [&](int d, float4 u) { store_four(a.part + (a.splits * rows + out) * D + d, u); });
-    return;
-  }
-  T* ok = static_cast<T*>(a.dk) + b * a.dkst.b + hk * a.dkst.h + key * a.dkst.n;
-  T* ov = static_cast<T*>(a.dv) + b * a.dvst.b + hk * a.dvst.h + key * a.dvst.n;
-  Z::each_four(dk, lh, [&](int d, float4 u) { store_four(ok + d, make_float4(u.x * f, u.y * f, u.z * f, u.w * f)); });
-  Z::each_four(dv, lh, [&](int d, float4 u) { store_four(ov + d, u); });
-}
-
-template <typename T, int D, bool CAP, bool SLOPES, int WHAT>
-int launch_dense_mode(const DenseArgs& a, hipStream_t s) {
-  const int64_t groups = ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8;
-  const dim3 grid = long_grid(groups, a.splits);
-  if constexpr (WHAT == kDenseForward) dense_forward_kernel<T, D, CAP, SLOPES><<<grid, 64 * kDenseWaves, 0, s>>>(a);
-  else if constexpr (WHAT == kDenseDq) dense_dq_kernel<T, D, CAP, SLOPES><<<grid, 64 * kDenseWaves, 0, s>>>(a);
-  else dense_dkv_kernel<T, D, CAP, SLOPES><<<grid, 64 * kDenseWaves, 0, s>>>(a);
-  SVGEAR_LAUNCH_CHECK();
-  return SVGEAR_OK;
-}
-
-template <typename T, int D, int WHAT>
-int launch_dense_width(const DenseArgs& a, hipStream_t s) {
-  if (a.cap > 0.f) return a.slopes ? launch_dense_mode<T, D, true, true, WHAT>(a, s) : launch_dense_mode<T, D, true, false, WHAT>(a, s);
-  return a.slopes ? launch_dense_mode<T, D, false, true, WHAT>(a, s) : launch_dense_mode<T, D, false, false, WHAT>(a, s);
-}
-template <typename T, int WHAT>
-int launch_dense(const DenseArgs& a, int d, hipStream_t s) {
-  return d == 64 ? launch_dense_width<T, 64, WHAT>(a, s) : launch_dense_width<T, 128, WHAT>(a, s);
-}
+// Workgroups of a launch: those of dense_index, and the parts along y.
+inline dim3 dense_grid(const DenseArgs& a) { return long_grid(ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8, a.splits); }
 
 }  // namespace
 }  // namespace svgear
