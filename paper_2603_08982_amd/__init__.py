@@ -17,6 +17,8 @@ from .binding import (  # noqa: F401
     unpermute,
     attention_layer,
     attention_block,
+    cross_attention_block,
+    cross_attention_block_backward,
     linear,
     linear_backward,
     rotary,

@@ -991,3 +991,72 @@ def attention_block(x: torch.Tensor, w_qkv: torch.Tensor, w_out: torch.Tensor, i
         _, r = attention_layer(q, k, v, init_q, init_k, iters, budget_cost, n_tail, out=o.transpose(1, 2), **layer)
         y, _ = linear(o.view(B, N, H * d), w_out, b_out, gate=gate, residual=residual)
         return y, r
+
+
+def cross_attention_block(x: torch.Tensor, context: torch.Tensor, w_q: torch.Tensor, w_kv: torch.Tensor, w_out: torch.Tensor, heads: int,
+                          lengths: Optional[torch.Tensor] = None, norm_weight: Optional[torch.Tensor] = None,
+                          norm_bias: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                          shift: Optional[torch.Tensor] = None, eps: float = 1e-6, b_q: Optional[torch.Tensor] = None,
+                          b_kv: Optional[torch.Tensor] = None, b_out: Optional[torch.Tensor] = None,
+                          gate: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, saved: bool = False):
+    """The attention of a video transformer's tokens to the text of their prompt, from the block's input to its output: layer_norm()
+    of x, linear() into queries and of the context into keys and values, attention() over the context's first `lengths[b]` tokens,
+    and linear() back with gate and residual.
+
+    x [B,N,c], context [B,M,c_text], lengths int32 [B] or None; w_q [H*d,c] for H = `heads`, w_kv [2*Hk*d,c_text] (rows: keys of all
+    heads, values), w_out [c_out,H*d], their biases; norm_weight, norm_bias, scale, shift, eps as in layer_norm(), gate and residual
+    as in linear(). Returns (y [B,N,c_out], what cross_attention_block_backward() needs if `saved`, else None)."""
+    _require(x.dim() == 3 and context.dim() == 3 and context.shape[0] == x.shape[0], "x: expected [B,N,c], context [B,M,c_text]")
+    B, N, _ = x.shape
+    M = context.shape[1]
+    _require(heads > 0 and w_q.dim() == 2 and w_kv.dim() == 2 and w_q.shape[0] % heads == 0, "w_q: expected [heads*d,c]")
+    d = w_q.shape[0] // heads
+    _require(w_kv.shape[0] % (2 * d) == 0 and w_out.dim() == 2 and w_out.shape[1] == heads * d,
+             "w_kv: expected [2*Hk*d,c_text], w_out: [c_out,heads*d]")
+    Hk = w_kv.shape[0] // (2 * d)
+    _require(lengths is None or (lengths.dtype == torch.int32 and tuple(lengths.shape) == (B,)), "lengths: expected int32 [B]")
+    _need_gpu(x, context, lengths)
+    with _on_device(x.device):
+        k_offsets = None if lengths is None else torch.stack([torch.zeros_like(lengths), lengths], 1)
+        h = layer_norm(x, norm_weight, norm_bias, scale=scale, shift=shift, eps=eps)
+        q = linear(h, w_q, b_q)[0].view(B, N, heads, d).transpose(1, 2)
+        k, v = linear(context, w_kv, b_kv)[0].view(B, M, 2, Hk, d).permute(2, 0, 3, 1, 4)
+        o = torch.empty(B, N, heads, d, dtype=x.dtype, device=x.device)
+        _, lse = attention(q, k, v, k_offsets=k_offsets, want_lse=saved, out=o.transpose(1, 2))
+        y, pre = linear(o.view(B, N, heads * d), w_out, b_out, gate=gate, residual=residual, want_pre=saved and gate is not None)
+    kept = None
+    if saved:
+        kept = {"x": x, "context": context, "w_q": w_q, "w_kv": w_kv, "w_out": w_out, "norm_weight": norm_weight, "norm_bias": norm_bias,
+                "scale": scale, "shift": shift, "eps": eps, "gate": gate, "b_q": b_q, "b_kv": b_kv, "b_out": b_out,
+                "k_offsets": k_offsets, "h": h, "q": q, "k": k, "v": v, "o": o, "lse": lse, "pre": pre}
+    return y, kept
+
+
+def cross_attention_block_backward(dy: torch.Tensor, kept: dict):
+    """The gradients of cross_attention_block() for its output's gradient dy, from what it kept: a dict of "x", "context", "w_q", "w_kv",
+    "w_out" and, of the arguments that were given, "b_q", "b_kv", "b_out", "gate", "norm_weight", "norm_bias", "scale", "shift" (which
+    needs a scale). The residual's is dy itself, and "x" is the norm's input's alone: where x is the residual too, the two are added."""
+    f = kept
+    B, N, H, d = f["o"].shape
+    M, Hk = f["context"].shape[1], f["k"].shape[1]
+    given = lambda name, gradient: [gradient] if f[name] is not None else []
+    with _on_device(dy.device):
+        out = linear_backward(dy, f["o"].view(B, N, H * d), f["w_out"], pre=f["pre"], gate=f["gate"],
+                              want=["dx", "dw"] + given("b_out", "dbias") + given("gate", "dgate"))
+        dq = torch.empty(B, N, H, d, dtype=dy.dtype, device=dy.device)
+        dkv = torch.empty(B, M, 2, Hk, d, dtype=dy.dtype, device=dy.device)
+        dk, dv = dkv.permute(2, 0, 3, 1, 4)
+        attention_backward(out["dx"].view(B, N, H, d).transpose(1, 2), f["q"], f["k"], f["v"], f["o"].transpose(1, 2), f["lse"],
+                           k_offsets=f["k_offsets"], out={"dq": dq.transpose(1, 2), "dk": dk, "dv": dv})
+        into = linear_backward(dq.view(B, N, H * d), f["h"], f["w_q"], want=["dx", "dw"] + given("b_q", "dbias"))
+        text = linear_backward(dkv.view(B, M, 2 * Hk * d), f["context"], f["w_kv"], want=["dx", "dw"] + given("b_kv", "dbias"))
+        modulated = given("scale", "dscale") + (given("shift", "dshift") if f["scale"] is not None else [])
+        norm = layer_norm_backward(into["dx"], f["x"], f["norm_weight"], f["norm_bias"], scale=f["scale"], eps=f["eps"],
+                                   want=["dx"] + given("norm_weight", "dweight") + given("norm_bias", "dbias") + modulated)
+    r = {"x": norm["dx"], "context": text["dx"], "w_q": into["dw"], "w_kv": text["dw"], "w_out": out["dw"]}
+    for name, source, gradient in (("b_q", into, "dbias"), ("b_kv", text, "dbias"), ("b_out", out, "dbias"), ("gate", out, "dgate"),
+                                   ("norm_weight", norm, "dweight"), ("norm_bias", norm, "dbias"), ("scale", norm, "dscale"),
+                                   ("shift", norm, "dshift")):
+        if gradient in source and f[name] is not None:
+            r[name] = source[gradient]
+    return r

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxDenseRows = (int64_t)1 << 30;
 constexpr int kMaxDocs = 1 << 20;
+constexpr int64_t kMaxKeyStride = 1 << 24;
 constexpr int kThreads = 256;
 
 // Where a row of `part` goes: row r of key head (b, hk) is token r / G of head hk G + r % G.
@@ -169,6 +170,8 @@ int fill(DenseArgs& a, const Sizes& z, const void* q, const int64_t qst[3], cons
       (prefix && !(flags & SVGEAR_ATTENTION_CAUSAL)) || reinterpret_cast<uintptr_t>(slopes) % 4 ||
       reinterpret_cast<uintptr_t>(q_offsets) % 4 || reinterpret_cast<uintptr_t>(k_offsets) % 4 || reinterpret_cast<uintptr_t>(prefix) % 4)
     return SVGEAR_ERR_INVALID;
+  // (a tile's keys are addressed by 32-bit byte offsets)
+  if (z.Nk > 1 && (kst[2] > kMaxKeyStride || vst[2] > kMaxKeyStride)) return SVGEAR_ERR_INVALID;
   const bool some = q_offsets || k_offsets, both = q_offsets && k_offsets;
   if ((z.n_docs > 0) != some || (!both && z.n_docs > 1)) return SVGEAR_ERR_INVALID;
   a.q = q, a.k = k, a.v = v;
