@@ -502,8 +502,9 @@ int svgear_layer_norm_backward(const void* dy, const int64_t dystride[2], const 
  * [k_offsets[t], k_offsets[t+1]); a query sees keys of its own document alone. With n queries and m keys in it, query i (from 0)
  * stands at key position p_i = i + m - n: the last query at the last key, new tokens behind a past. With
  * SVGEAR_ATTENTION_CAUSAL it sees the keys j <= p_i and those before the document's prefix; otherwise all. A query that sees no
- * key (of no document, of one without keys, before the first key) has o = 0 and lse = -inf. K and V rows of no document,
- * and keys behind the last that a tile of 128 queries sees, are not read.
+ * key (of no document, of one without keys, before the first key) has o = 0 and lse = -inf. K and V rows of no document
+ * are not read, and what is masked may be infinite or NaN: it reaches no query that does not see it (nor, in the backward pass,
+ * a key from queries that do not see that). Tiles of queries that such keys lie beside are found again by a slow path.
  *   q [B,H,Nq,d], k, v [B,Hk,Nk,d] dt, element strides qstride.. = {stride_b, stride_h, stride_n}, d contiguous
  *   slopes    [H] fp32 or NULL
  *   q_offsets, k_offsets  [B,n_docs+1] int32, ascending from 0 on within the rows (what is not is taken as the nearest
@@ -518,7 +519,7 @@ int svgear_layer_norm_backward(const void* dy, const int64_t dystride[2], const 
  * 2^24; that of a dimension of one element does not matter), those of o such that no two rows meet; no output at the address of
  * another tensor of the call. Nq H / Hk, Nk, B H <= 2^30; n_docs <= 2^20. Where the tiles of queries (128 rows in bf16, 32 in fp32)
  * are fewer than 256 (single tokens in bf16: 512), the keys are cut into parts, up to 64, whose results lie in the workspace:
- * parts * B*H*Nq * (4 d + 8) bytes. Where it is 0, ws may be NULL.
+ * parts * B*H*Nq * (4 d + 8) bytes, and for more than one query 16 bytes for a tile and part. Where it is 0, ws may be NULL.
  */
 #define SVGEAR_ATTENTION_CAUSAL 1u
 #define SVGEAR_ATTENTION_SHARED_DOCUMENTS 2u
@@ -537,7 +538,7 @@ int svgear_attention(const void* q, const int64_t qstride[3], const void* k, con
  * summed over the query heads that share a key head. dq may be NULL, or dk and dv both. Rows that see nothing, or are seen by
  * nothing, get zeros. No gradient of the slopes. bf16: p and ds are rounded to bf16 for the products, whose sums are fp32. All
  * sums are made in one fixed order, without atomics. Arguments as above; dy, o [B,H,Nq,d], strided; dq, dk, dv as q, k, v, strided.
- * The workspace holds dy_i.o_i and partial sums.
+ * The workspace holds dy_i.o_i, partial sums, and 16 bytes for a tile and part.
  */
 size_t svgear_attention_backward_workspace(svgear_dtype dt, int B, int H, int Hk, int64_t Nq, int64_t Nk, int d, int n_docs);
 int svgear_attention_backward(const void* dy, const int64_t dystride[3], const void* q, const int64_t qstride[3], const void* k,

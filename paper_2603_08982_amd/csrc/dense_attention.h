@@ -29,6 +29,7 @@ struct DenseArgs {
   int slots, splits;  // tiles a key head has at most, parts that the other side's rows are cut into
   float* part;        // where splits > 1: [splits][B Hk rows][d] (dk, then dv in the backward pass)
   float2* part_ml;    // forward: maximum and sum of each
+  int32_t* marks;     // with a causal mask: [splits][B Hk][slots][4], see dense_again.hip
 };
 
 constexpr int kDenseWaves = 4;
@@ -43,5 +44,7 @@ int launch_dense_bf16(const DenseArgs& a, int d, hipStream_t s);
 int launch_dense_f32(const DenseArgs& a, int d, hipStream_t s);
 int launch_dense_backward_bf16(const DenseArgs& a, int d, int what, hipStream_t s);
 int launch_dense_backward_f32(const DenseArgs& a, int d, int what, hipStream_t s);
+// The rows that a causal launch of `what` has marked, once their parts are joined.
+int launch_dense_again(const DenseArgs& a, svgear_dtype dt, int d, int what, hipStream_t s);
 
 }  // namespace svgear

@@ -127,6 +127,10 @@ bool sizes_ok(const Sizes& z) {
   return heads * std::max(q, k) <= kMaxDenseRows && (__int128)z.B * z.H * z.Nq <= ((__int128)1 << 40) &&
          (__int128)heads * z.Nk <= ((__int128)1 << 40);
 }
+// Marks of a launch (whether or not it is a causal one): a wave of each tile and part.
+size_t mark_bytes(const Sizes& z, int64_t heads, int64_t rows, int splits) {
+  return z.Nq > 1 ? align_up((size_t)heads * dense_slots(rows, z.n_docs, rows_of_tile(z.dt)) * splits * kDenseWaves * sizeof(int32_t), 256) : 0;
+}
 size_t part_bytes(int splits, int64_t rows, int d, int tensors) {
   return splits > 1 ? align_up((size_t)splits * rows * d * sizeof(float) * tensors, 256) : 0;
 }
@@ -181,7 +185,7 @@ int fill(DenseArgs& a, const Sizes& z, const void* q, const int64_t qst[3], cons
   a.q_offsets = q_offsets, a.k_offsets = k_offsets, a.prefix = prefix, a.slopes = slopes;
   a.n_docs = std::max(z.n_docs, 1);
   a.docs_shared = flags & SVGEAR_ATTENTION_SHARED_DOCUMENTS;
-  a.causal = flags & SVGEAR_ATTENTION_CAUSAL;
+  a.causal = (flags & SVGEAR_ATTENTION_CAUSAL) && z.Nq > 1;  // (a single query stands at the last key)
   a.scale = scale, a.cap = cap;
   a.B = z.B, a.H = z.H, a.Hk = z.Hk, a.G = z.H / z.Hk, a.Nq = (int)z.Nq, a.Nk = (int)z.Nk;
   return SVGEAR_OK;
@@ -233,7 +237,8 @@ extern "C" size_t svgear_attention_workspace(svgear_dtype dt, int B, int H, int 
   const Sizes z{dt, B, H, Hk, Nq, Nk, d, n_docs};
   if (!sizes_ok(z)) return 0;
   const int splits = parts_over_keys(z);
-  return part_bytes(splits, q_rows(z), d, 1) + (splits > 1 ? align_up((size_t)splits * q_rows(z) * sizeof(float2), 256) : 0);
+  return mark_bytes(z, (int64_t)B * Hk, Nq * (H / Hk), splits) + part_bytes(splits, q_rows(z), d, 1) +
+         (splits > 1 ? align_up((size_t)splits * q_rows(z) * sizeof(float2), 256) : 0);
 }
 
 extern "C" int svgear_attention(const void* q, const int64_t qstride[3], const void* k, const int64_t kstride[3], const void* v,
@@ -257,21 +262,24 @@ extern "C" int svgear_attention(const void* q, const int64_t qstride[3], const v
   a.lse = lse;
   a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
   a.splits = parts_over_keys(z);
+  Workspace w(ws, ws_bytes);
+  if (a.causal) a.marks = w.take<int32_t>(mark_bytes(z, (int64_t)B * Hk, Nq * a.G, a.splits) / sizeof(int32_t));
   if (a.splits > 1) {
-    Workspace w(ws, ws_bytes);
     a.part = w.take<float>((size_t)a.splits * q_rows(z) * d);
     a.part_ml = w.take<float2>((size_t)a.splits * q_rows(z));
   }
-  const int done = launch(a, z, kDenseForward, s);
-  if (done != SVGEAR_OK || a.splits == 1) return done;
-  return by_kind(z, [&](auto t, auto dim) { return merge<decltype(t), decltype(dim)::value>(a, q_rows(z), s); });
+  int done = launch(a, z, kDenseForward, s);
+  if (done == SVGEAR_OK && a.splits > 1)
+    done = by_kind(z, [&](auto t, auto dim) { return merge<decltype(t), decltype(dim)::value>(a, q_rows(z), s); });
+  return done == SVGEAR_OK && a.causal ? launch_dense_again(a, dt, d, kDenseForward, s) : done;
 }
 
 extern "C" size_t svgear_attention_backward_workspace(svgear_dtype dt, int B, int H, int Hk, int64_t Nq, int64_t Nk, int d, int n_docs) {
   const Sizes z{dt, B, H, Hk, Nq, Nk, d, n_docs};
   if (!sizes_ok(z)) return 0;
   return align_up((size_t)q_rows(z) * sizeof(float), 256) +
-         std::max(part_bytes(parts_over_keys(z), q_rows(z), d, 1), part_bytes(parts_over_queries(z), k_rows(z), d, 2));
+         std::max(mark_bytes(z, (int64_t)B * Hk, Nq * (H / Hk), parts_over_keys(z)) + part_bytes(parts_over_keys(z), q_rows(z), d, 1),
+                  mark_bytes(z, (int64_t)B * Hk, Nk, parts_over_queries(z)) + part_bytes(parts_over_queries(z), k_rows(z), d, 2));
 }
 
 extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[3], const void* q, const int64_t qstride[3],
@@ -306,7 +314,13 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
   a.yst = strides_of(dystride, z, H, Nq);
   a.lse_in = lse;
   a.delta = w.take<float>((size_t)q_rows(z));
-  a.part = reinterpret_cast<float*>(w.base + w.used);
+  // marks and parts of either launch, one after the other in the same room
+  auto room = [&](int64_t rows) {
+    char* p = w.base + w.used;
+    const size_t marks = a.causal ? mark_bytes(z, (int64_t)B * Hk, rows, a.splits) : 0;
+    a.marks = a.causal ? reinterpret_cast<int32_t*>(p) : nullptr;
+    a.part = reinterpret_cast<float*>(p + marks);
+  };
   const Strides ost = strides_of(ostride, z, H, Nq);
   int done = by_kind(z, [&](auto t, auto dim) { return find_delta<decltype(t), decltype(dim)::value>(a, o, ost, s); });
   if (done != SVGEAR_OK) return done;
@@ -315,6 +329,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
     a.ost = strides_of(dqstride, z, H, Nq);
     a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
     a.splits = parts_over_keys(z);
+    room(Nq * a.G);
     done = launch(a, z, kDenseDq, s);
     if (done != SVGEAR_OK) return done;
     if (a.splits > 1) {
@@ -322,6 +337,8 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
       done = by_kind(z, [&](auto t, auto dim) { return sum<decltype(t), decltype(dim)::value>(a, q_rows(z), scale, out, nullptr, s); });
       if (done != SVGEAR_OK) return done;
     }
+    if (a.causal) done = launch_dense_again(a, dt, d, kDenseDq, s);
+    if (done != SVGEAR_OK) return done;
   }
   if (!dk) return SVGEAR_OK;
   a.dk = dk, a.dv = dv;
@@ -329,8 +346,11 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
   a.dvst = strides_of(dvstride, z, Hk, Nk);
   a.slots = (int)dense_slots(Nk, k_offsets ? n_docs : 0, rows_of_tile(dt));
   a.splits = parts_over_queries(z);
+  room(Nk);
   done = launch(a, z, kDenseDkv, s);
-  if (done != SVGEAR_OK || a.splits == 1) return done;
-  const Out out_k{dk, a.dkst, a.Nk, 1, Hk}, out_v{dv, a.dvst, a.Nk, 1, Hk};
-  return by_kind(z, [&](auto t, auto dim) { return sum<decltype(t), decltype(dim)::value>(a, k_rows(z), 1.f, out_k, &out_v, s); });
+  if (done == SVGEAR_OK && a.splits > 1) {
+    const Out out_k{dk, a.dkst, a.Nk, 1, Hk}, out_v{dv, a.dvst, a.Nk, 1, Hk};
+    done = by_kind(z, [&](auto t, auto dim) { return sum<decltype(t), decltype(dim)::value>(a, k_rows(z), 1.f, out_k, &out_v, s); });
+  }
+  return done == SVGEAR_OK && a.causal ? launch_dense_again(a, dt, d, kDenseDkv, s) : done;
 }

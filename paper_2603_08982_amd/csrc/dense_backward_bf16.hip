@@ -14,10 +14,9 @@ dense_dq_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  if (a.causal) slot = a.slots - 1 - slot;
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const Found at = find_tile<true>(a, b, kDenseRows, slot, lane);
+  const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
@@ -82,7 +81,12 @@ dense_dq_kernel(DenseArgs a) {
     }
   }
 
-  if (!active || row >= at.end) return;
+  if (!active) return;
+  if (a.marks) {
+    const bool spoiled = Z::unbounded(acc);
+    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
+  }
+  if (row >= at.end) return;
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + row;
     Z::each_four(acc, lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
@@ -199,7 +203,12 @@ dense_dkv_kernel(DenseArgs a) {
     }
   }
 
-  if (!active || key >= at.end) return;
+  if (!active) return;
+  if (a.marks) {
+    const bool spoiled = Z::unbounded(dk) || Z::unbounded(dv);
+    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
+  }
+  if (key >= at.end) return;
   const float f = a.scale;
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.B * a.Hk * a.Nk, out = split * rows + (int64_t)bh * a.Nk + key;

@@ -14,10 +14,9 @@ dense_dq_f32_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[kDenseWaves * S::kWave];  // of a wave: a tile of K, one of V
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  if (a.causal) slot = a.slots - 1 - slot;
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const Found at = find_tile<true>(a, b, S::kRows, slot, lane);
+  const Found at = find_tile<true>(a, b, S::kRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
@@ -81,6 +80,10 @@ dense_dq_f32_kernel(DenseArgs a) {
     if (more) issue(kp, a.kst.n, t + kDenseWaves, lds);
   }
 
+  if (a.marks) {
+    const bool spoiled = Z::unbounded(acc);
+    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
+  }
   const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, part0 = split * rows + (int64_t)bh * a.Nq * a.G + at.first;
   meet<D>(smem, acc, wave, lane, [](int, int) { return 1.f; }, [&](int r, int d, float4 v) {
     if (at.first + r >= at.end) return;
@@ -205,6 +208,10 @@ dense_dkv_f32_kernel(DenseArgs a) {
     if (more) issue(qp, a.qst, t + kDenseWaves, lds);
   }
 
+  if (a.marks) {
+    const bool spoiled = Z::unbounded(dk) || Z::unbounded(dv);
+    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
+  }
   const int64_t rows = (int64_t)a.B * a.Hk * a.Nk, part0 = split * rows + (int64_t)bh * a.Nk + at.first;
   auto put = [&](void* to, const Strides& st, int64_t part, float f) {
     return [=, &a](int r, int d, float4 u) {

@@ -43,10 +43,9 @@ dense_forward_bf16_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  if (a.causal) slot = a.slots - 1 - slot;  // the longest first
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const Found at = find_tile<true>(a, b, kDenseRows, slot, lane);
+  const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
@@ -294,6 +293,10 @@ dense_forward_bf16_kernel(DenseArgs a) {
     }
   }
 
+  if (a.marks) {
+    const bool spoiled = Z::unbounded(acc);
+    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
+  }
   float l = ls[0] + ls[1];
   l += swap32(l);
   const int l2 = again(lane), out_row = min(wave_row + (l2 & 31), at.end - 1), out_token = out_row / a.G;

@@ -14,10 +14,9 @@ dense_forward_f32_kernel(DenseArgs a) {
   __shared__ float ml[kDenseWaves][2][32];                                              // of a wave: maximum, sum of each row
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  if (a.causal) slot = a.slots - 1 - slot;  // the longest first
   const int b = bh / a.Hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const Found at = find_tile<true>(a, b, S::kRows, slot, lane);
+  const Found at = find_tile<true>(a, b, S::kRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
@@ -99,6 +98,10 @@ dense_forward_f32_kernel(DenseArgs a) {
     if (more) issue(vp, a.vst.n, t + kDenseWaves, lds + Z::kBytes);
   }
 
+  if (a.marks) {
+    const bool spoiled = Z::unbounded(acc);
+    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
+  }
   l += swap32(l);
   if (lh == 0) ml[wave][0][li] = m, ml[wave][1][li] = l;
   const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, part0 = split * rows + (int64_t)bh * a.Nq * a.G + at.first;

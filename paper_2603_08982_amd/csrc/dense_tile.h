@@ -175,6 +175,16 @@ struct Tile {
     }
   }
 
+  // Whether a wave's accumulators hold an infinity or a NaN: nothing else keeps 0 times itself from 0.
+  static __device__ __forceinline__ bool unbounded(const f32x16 (&acc)[DB]) {
+    float zero = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) zero = __builtin_fmaf(acc[db][r], 0.f, zero);
+    return __any(!(zero == 0.f));
+  }
+
   // f(first of four columns, their values) for what the lane's accumulators hold of its row
   template <typename F>
   static __device__ __forceinline__ void each_four(const f32x16 (&acc)[DB], int lh, F f) {
@@ -330,6 +340,11 @@ struct Scores {
   }
   __device__ __forceinline__ float keeps(float in) const { return __builtin_fmaf(-in, in, 1.f); }
 };
+
+// The mark of a wave of a workgroup (bh, slot) and its part: whether what it found is unbounded.
+__device__ __forceinline__ int32_t* mark_of(const DenseArgs& a, int part, int bh, int slot, int wave) {
+  return a.marks + (((int64_t)part * (a.B * a.Hk) + bh) * a.slots + slot) * kDenseWaves + wave;
+}
 
 // f(cap, slopes) as types, for what a call has
 template <typename F>

@@ -186,11 +186,16 @@ static void attention(void) {
     expect("attention: no room for the parts", call_att(a), -2);
   }
   expect("attention_workspace: invalid", (long long)svgear_attention_workspace(BF, 2, 4, 3, 100, 50, 64, 0), 0);
-  expect("attention_workspace: none for many queries", (long long)svgear_attention_workspace(BF, 1, 40, 40, 75600, 512, 128, 1), 0);
+  expect("attention_workspace: none for a query and few keys", (long long)svgear_attention_workspace(BF, 2, 4, 2, 1, 60, 64, 0), 0);
+  {
+    const size_t w = svgear_attention_workspace(BF, 1, 40, 40, 75600, 512, 128, 1);
+    expect("attention_workspace: no parts for many queries", w >= (size_t)40 * 591 * 16 && w <= (size_t)40 * 600 * 16, 1);
+  }
   {
     const size_t w = svgear_attention_workspace(BF, 8, 40, 8, 1, 32760, 128, 1);
     expect("attention_workspace: parts of single tokens", w >= (size_t)2 * 320 * 520 && w <= (size_t)64 * 320 * 520 + 512, 1);
-    expect("attention_workspace: sizes at their limits", svgear_attention_workspace(SVGEAR_F32, 1, 1, 1, (int64_t)1 << 30, (int64_t)1 << 30, 128, 0), 0);
+    expect("attention_workspace: sizes at their limits", svgear_attention_workspace(SVGEAR_F32, 1, 1, 1, (int64_t)1 << 30, (int64_t)1 << 30, 128, 0),
+           (long long)1 << 29);
   }
 }
 

@@ -181,6 +181,68 @@ def test_far_rows():
     torch.cuda.empty_cache()
 
 
+# (what a masked place holds, which tensors hold it)
+UNBOUNDED = [(float("nan"), 64), (float("inf"), 1)]
+SHAPES = [(1, 4, 4, 300, 300), (2, 4, 2, 150, 150), (1, 6, 2, 70, 1900), (1, 2, 1, 40, 5000), (1, 3, 1, 260, 100)]
+
+
+@pytest.mark.parametrize("value,width", UNBOUNDED)
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F, 128), (F, 64)])
+@pytest.mark.parametrize("kw", [{}, {"prefix": 20}, {"cap": 10.0, "slopes": True}])
+@pytest.mark.parametrize("B,H,Hk,Nq,Nk", SHAPES)
+def test_unbounded_values_behind_a_causal_mask(B, H, Hk, Nq, Nk, kw, dtype, d, value, width):
+    """A key, or value, that is infinite or NaN reaches the queries that see it alone; a query the keys that it sees."""
+    q, k, v, dy = make(28, dtype, B, H, Hk, Nq, Nk, d)
+    kw = dict(kw, causal=True)
+    if kw.get("slopes"):
+        kw["slopes"] = slopes_of(H)
+    if "prefix" in kw:
+        kw["prefix"] = i32([[kw["prefix"]]] * B)
+    what = (B, H, Hk, Nq, Nk, kw, dtype, d, value)
+    # keys: two of the last ones that not all queries see; queries before the first of them do not see either
+    i = min(Nq - 1, Nk - 1) * 2 // 3
+    j = Nk - 1 - i
+    j = max(j, 20) if "prefix" in kw else j
+    ok = max(j + Nq - Nk, 0)  # queries [0, ok) see neither
+    assert 0 < ok < Nq
+    K, V = k.clone(), v.clone()
+    K[:, :, j + min(2, i), :width] = value
+    V[:, :, j, :width] = value
+    V[:, :, -1, width // 2] = -value
+    o, lse = sv.attention(q, K, V, want_lse=True, **kw)
+    want, e, want_lse, el = attention64(q, k, v, **kw)
+    close(lse[:, :, :ok], want_lse[:, :, :ok], el[:, :, :ok], ("lse", what))
+    close(o[:, :, :ok], want[:, :, :ok], e[:, :, :ok], ("o", what))
+    assert not o[:, :, ok:, :width].isfinite().any(), what
+    # the other columns of those that see the value alone are as they would be
+    if width < d and i > 2:
+        close(o[:, :, ok:ok + 2, width + 1:], want[:, :, ok:ok + 2, width + 1:], e[:, :, ok:ok + 2, width + 1:], ("o, other columns", what))
+    got = sv.attention_backward(dy, q, K, V, o, lse, **kw)
+    ref = attention_backward64(dy[:, :, :ok], q[:, :, :ok], k[:, :, :j], v[:, :, :j], o[:, :, :ok], lse[:, :, :ok], **kw)["dq"]
+    close(got["dq"][:, :, :ok], ref[0], ref[1], ("dq", what))
+    assert not got["dq"][:, :, -1, :width].isfinite().all(), what
+
+    # queries: one of the first ones that not all keys are seen by
+    Q, Y = q.clone(), dy.clone()
+    o, lse = sv.attention(q, k, v, want_lse=True, **kw)
+    Q[:, :, ok - 1, :width] = value
+    Y[:, :, max(ok - 3, 0), :width] = value
+    got = sv.attention_backward(Y, Q, k, v, o, lse, **kw)
+    ref = attention_backward64(dy, q, k, v, o, lse, **kw)
+    for n in ("dk", "dv"):  # keys from j on are seen by queries from ok on
+        close(got[n][:, :, j:], ref[n][0][:, :, j:], ref[n][1][:, :, j:], (n, what))
+    assert not got["dv"][:, :, j - 3, :width].isfinite().any(), what
+
+
+def test_unbounded_everywhere():
+    """Where all is lost nothing takes long, and all is a NaN."""
+    q, k, v, dy = make(29, BF, 1, 4, 2, 3000, 3000, 128)
+    o, lse = sv.attention(q * float("nan"), k, v, want_lse=True, causal=True)
+    assert o.isnan().all() and lse.isnan().all()
+    got = sv.attention_backward(dy, q * float("nan"), k * float("nan"), v, o, lse, causal=True)
+    assert got["dq"].isnan().all() and got["dk"].isnan().all() and got["dv"].isnan().all()
+
+
 def test_same_bits_again():
     q, k, v, dy = make(25, BF, 1, 8, 2, 500, 4000, 128)
     r = [sv.attention(q, k, v, want_lse=True) for _ in range(3)]
