@@ -27,7 +27,7 @@ dense_dq_kernel(DenseArgs a) {
   const int hi_all = doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0), hi_any = doc.seen(min(wave_row + 31, at.end - 1) / a.G - doc.q0);
   const int hi_wg = doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0);
   const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
-  const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column q, dy;
   q.load(static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
@@ -125,7 +125,7 @@ dense_dkv_kernel(DenseArgs a) {
   const int from_any = doc.first_seer(min(wave_key, at.end - 1) - doc.k0) * a.G;
   const int first_tile = doc.first_seer(at.first - doc.k0) * a.G / BN, tiles_end = (end + BN - 1) / BN;
   const int tiles = max(tiles_end - first_tile, 0), split = blockIdx.y;
-  const int t_lo = first_tile + (int)((int64_t)tiles * split / a.splits), t_hi = first_tile + (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int t_lo = first_tile + part_begin(tiles, split, a.splits), t_hi = first_tile + part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column k, v;
   unsigned char* parked = smem + 4 * Z::kBytes + (kPark ? wave * Z::kParked : 0);

@@ -24,7 +24,7 @@ dense_dq_f32_kernel(DenseArgs a) {
   const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
   const int hi_all = doc.seen(at.first / a.G - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.G - doc.q0);
   const int split = blockIdx.y, tiles = (hi_any + BN - 1) / BN;
-  const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column q, dy;
   q.load(static_cast<const float*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
@@ -118,7 +118,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
   const int from_all = doc.first_seer(min(at.first + S::kRows, at.end) - 1 - doc.k0) * a.G;
   const int first_tile = doc.first_seer(at.first - doc.k0) * a.G / BN;
   const int tiles = max((end + BN - 1) / BN - first_tile, 0), split = blockIdx.y;
-  const int t_lo = first_tile + (int)((int64_t)tiles * split / a.splits), t_hi = first_tile + (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int t_lo = first_tile + part_begin(tiles, split, a.splits), t_hi = first_tile + part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column k, v;
   k.load(static_cast<const float*>(a.k) + b * a.kst.b + hk * a.kst.h + key * a.kst.n, lh);

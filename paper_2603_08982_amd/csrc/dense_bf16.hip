@@ -56,19 +56,8 @@ dense_forward_bf16_kernel(DenseArgs a) {
   const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0));
   const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0));
   const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
-  const int t_lo = uniform((int)((int64_t)tiles * split / a.splits)), t_hi = uniform((int)((int64_t)tiles * (split + 1) / a.splits));
+  const int t_lo = uniform(part_begin(tiles, split, a.splits)), t_hi = uniform(part_begin(tiles, split + 1, a.splits));
 
-  typename Z::Column q;
-  q.load(static_cast<const bf16_t*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
-  if (a.scale < 0.f) {  // (the maximum is that of the unscaled scores)
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      union { bf16x8 v; uint4 u; } c;
-      c.v = q.v[s];
-      c.u.x ^= 0x80008000u, c.u.y ^= 0x80008000u, c.u.z ^= 0x80008000u, c.u.w ^= 0x80008000u;
-      q.v[s] = c.v;
-    }
-  }
   const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
 
   const Z z(lane);
@@ -97,6 +86,23 @@ dense_forward_bf16_kernel(DenseArgs a) {
   };
   auto issue_k = [&](int t) __attribute__((always_inline)) { issue(t, kp, a.kst.n, k_lane, (t - t_lo) & 1); };
   auto issue_v = [&](int t) __attribute__((always_inline)) { issue(t, vp, a.vst.n, v_lane, 2 + ((t - t_lo) & 1)); };
+
+  // the first tiles are on their way while the queries are fetched
+  if (t_lo < t_hi) {
+    issue_k(t_lo);
+    issue_v(t_lo);
+  }
+  typename Z::Column q;
+  q.load(static_cast<const bf16_t*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
+  if (a.scale < 0.f) {  // (the maximum is that of the unscaled scores)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      union { bf16x8 v; uint4 u; } c;
+      c.v = q.v[s];
+      c.u.x ^= 0x80008000u, c.u.y ^= 0x80008000u, c.u.z ^= 0x80008000u, c.u.w ^= 0x80008000u;
+      q.v[s] = c.v;
+    }
+  }
 
   Scores<bf16_t, CAP, SLOPES> scores_of(a);
   scores_of.c = uniform(fabsf(scores_of.c));
@@ -243,8 +249,6 @@ dense_forward_bf16_kernel(DenseArgs a) {
   // Step t takes the weights of its scores and its values, and finds the scores of step t + 1; K(t + 2) and V(t + 1) are copied
   // meanwhile, over K(t) and V(t - 1), which step t - 1 was the last to read.
   if (t_lo < t_hi) {
-    issue_k(t_lo);
-    issue_v(t_lo);
     SVGEAR_WAIT_VMCNT(0);
     __syncthreads();
     if (t_lo + 1 < t_hi) issue_k(t_lo + 1);

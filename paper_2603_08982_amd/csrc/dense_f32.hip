@@ -25,7 +25,7 @@ dense_forward_f32_kernel(DenseArgs a) {
   // keys that every row sees, and that some row sees
   const int hi_all = doc.seen(at.first / a.G - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.G - doc.q0);
   const int split = blockIdx.y, tiles = (hi_any + BN - 1) / BN;
-  const int t_lo = (int)((int64_t)tiles * split / a.splits), t_hi = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column q;
   q.load(static_cast<const float*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);

@@ -288,6 +288,9 @@ __device__ __forceinline__ Found find_tile(const DenseArgs& a, int b, int per, i
   return f;
 }
 
+// Where part `split` of `splits` begins among so many tiles: 2^25 and a few at most, and 64 parts.
+__device__ __forceinline__ int part_begin(int tiles, int split, int splits) { return (int)((unsigned)tiles * (unsigned)split / (unsigned)splits); }
+
 // Workgroup to (key head of the batch, slot). Workgroups go to the 8 XCDs in turn: each takes whole heads, whose keys and values (or
 // queries) its L2 then holds once, and the heads that are left over when each has as many are dealt out by the slot, so that tiles
 // of different lengths (documents, the triangle of a causal mask) fall on all of them alike.
