@@ -131,7 +131,7 @@ __device__ __forceinline__ void again_dkv(const T* k, const T* v, const T* q, in
   acc.set(0.f);
   for (int r = r_lo; r < r_hi; ++r) {
     if (r % 64 == 63 && __all(acc.lost())) break;
-    const int token = r / a.G, h = r - token * a.G;
+    const int token = r / a.by_g, h = r - token * a.G;
     const T* qr = q + h * qh + token * qn;
     const T* yr = dy + h * yh + token * yn;
     const int64_t stat = (int64_t)h * a.Nq + token;
@@ -154,7 +154,7 @@ dense_again_kernel(DenseArgs a) {
   constexpr bool SOLO = sizeof(T) == 4;
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), b = bh / a.by_hk, hk = bh - b * a.Hk;
   if (SOLO && wave > 0) return;
   const int tile = a.causal && WHAT != kDenseDkv ? a.slots - 1 - slot : slot;
   const Found at = find_tile<WHAT != kDenseDkv>(a, b, SOLO ? 32 : kDenseRows, tile, lane);
@@ -190,8 +190,8 @@ dense_again_kernel(DenseArgs a) {
                                         a.delta + stat0, slopes, r_lo, end, from, ahead, a,
                                         static_cast<T*>(a.dv) + b * a.dvst.b + hk * a.dvst.h + own * a.dvst.n, live);
   } else {
-    const int token = own / a.G, head = hk * a.G + (own - token * a.G);
-    const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0), hi_any = doc.seen((min(first + 32, at.end) - 1) / a.G - doc.q0);
+    const int token = own / a.by_g, head = hk * a.G + (own - token * a.G);
+    const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0), hi_any = doc.seen((min(first + 32, at.end) - 1) / a.by_g - doc.q0);
     const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
     const int64_t stat = ((int64_t)b * a.H + head) * a.Nq + token;
     const T* q = static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n;
@@ -199,7 +199,7 @@ dense_again_kernel(DenseArgs a) {
     kp += doc.k0 * a.kst.n;
     vp += doc.k0 * a.vst.n;
     // keys that the wave has read for nothing: a workgroup's tiles end at, or up to 64 keys behind, the last that its last row sees
-    const int lo = doc.seen(first / a.G - doc.q0), past = doc.seen((min(at.first + (SOLO ? 32 : kDenseRows), at.end) - 1) / a.G - doc.q0) + 64;
+    const int lo = doc.seen(first / a.by_g - doc.q0), past = doc.seen((min(at.first + (SOLO ? 32 : kDenseRows), at.end) - 1) / a.by_g - doc.q0) + 64;
     if (!unbounded_rows<D>(WHAT == kDenseDq ? kp : vp, WHAT == kDenseDq ? a.kst.n : a.vst.n, lo, min(past, doc.nk), lane)) return;
     if constexpr (WHAT == kDenseForward) {
       again_forward<T, D, CAP, SLOPES>(q, kp, a.kst.n, vp, a.vst.n, hi_any, hi, pos, slope, a, o, a.lse ? a.lse + stat : nullptr, live);

@@ -4,6 +4,20 @@
 
 namespace svgear {
 
+// Division of 0 <= n < 2^31 by a number that a launch has once: n / d = (2 n mul / 2^32) / 2^shift with mul = 2^(31 + shift) / d rounded
+// up, 2^shift >= d, exact, since what the rounding adds, n / 2^(31 + shift) at most, is below 1 / d of the quotient. (A workgroup divides
+// eight times before it knows its first address; the instructions of a division are some twenty, one waiting for the other.)
+struct Divider {
+  uint32_t mul = 1u << 31;
+  int shift = 0;
+  Divider() = default;
+  explicit Divider(int d) {
+    while (((int64_t)1 << shift) < d) ++shift;
+    mul = (uint32_t)((((uint64_t)1 << (31 + shift)) + d - 1) / d);
+  }
+  friend __device__ __forceinline__ int operator/(int n, const Divider& d) { return (int)(__umulhi(2u * (unsigned)n, d.mul) >> d.shift); }
+};
+
 // Queries of the H / Hk heads that share a key head are one run of rows: row r of key head hk is token r / G of head
 // hk G + r % G, G = H / Hk. Rows of a document see the keys [0, hi) of it, hi growing with the token (see Rows below).
 struct DenseArgs {
@@ -26,6 +40,7 @@ struct DenseArgs {
   bool docs_shared, causal;
   float scale, cap;
   int B, H, Hk, G, Nq, Nk;
+  Divider by_hk, by_g, by_slots;
   int slots, splits;  // tiles a key head has at most, parts that the other side's rows are cut into
   float* part;        // where splits > 1: [splits][B Hk rows][d] (dk, then dv in the backward pass)
   float2* part_ml;    // forward: maximum and sum of each

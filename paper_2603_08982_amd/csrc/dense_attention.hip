@@ -188,6 +188,7 @@ int fill(DenseArgs& a, const Sizes& z, const void* q, const int64_t qst[3], cons
   a.causal = (flags & SVGEAR_ATTENTION_CAUSAL) && z.Nq > 1;  // (a single query stands at the last key)
   a.scale = scale, a.cap = cap;
   a.B = z.B, a.H = z.H, a.Hk = z.Hk, a.G = z.H / z.Hk, a.Nq = (int)z.Nq, a.Nk = (int)z.Nk;
+  a.by_hk = Divider(a.Hk), a.by_g = Divider(a.G);
   return SVGEAR_OK;
 }
 bool space_ok(const void* ws, size_t ws_bytes, size_t need) {
@@ -261,6 +262,7 @@ extern "C" int svgear_attention(const void* q, const int64_t qstride[3], const v
   a.ost = strides_of(ostride, z, H, Nq);
   a.lse = lse;
   a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
+  a.by_slots = Divider(a.slots);
   a.splits = parts_over_keys(z);
   Workspace w(ws, ws_bytes);
   if (a.causal) a.marks = w.take<int32_t>(mark_bytes(z, (int64_t)B * Hk, Nq * a.G, a.splits) / sizeof(int32_t));
@@ -328,6 +330,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
     a.o = dq;
     a.ost = strides_of(dqstride, z, H, Nq);
     a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
+    a.by_slots = Divider(a.slots);
     a.splits = parts_over_keys(z);
     room(Nq * a.G);
     done = launch(a, z, kDenseDq, s);
@@ -345,6 +348,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
   a.dkst = strides_of(dkstride, z, Hk, Nk);
   a.dvst = strides_of(dvstride, z, Hk, Nk);
   a.slots = (int)dense_slots(Nk, k_offsets ? n_docs : 0, rows_of_tile(dt));
+  a.by_slots = Divider(a.slots);
   a.splits = parts_over_queries(z);
   room(Nk);
   done = launch(a, z, kDenseDkv, s);

@@ -14,7 +14,7 @@ dense_dq_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
@@ -22,10 +22,10 @@ dense_dq_kernel(DenseArgs a) {
 
   const int wave_row = at.first + 32 * wave, row = wave_row + li, row_c = min(row, at.end - 1);
   const bool active = wave_row < at.end;
-  const int token = row_c / a.G, head = hk * a.G + (row_c - token * a.G);
+  const int token = row_c / a.by_g, head = hk * a.G + (row_c - token * a.G);
   const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
-  const int hi_all = doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0), hi_any = doc.seen(min(wave_row + 31, at.end - 1) / a.G - doc.q0);
-  const int hi_wg = doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0);
+  const int hi_all = doc.seen(min(wave_row, at.end - 1) / a.by_g - doc.q0), hi_any = doc.seen(min(wave_row + 31, at.end - 1) / a.by_g - doc.q0);
+  const int hi_wg = doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.by_g - doc.q0);
   const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
   const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
@@ -111,7 +111,7 @@ dense_dkv_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, position
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<false>(a, b, kDenseRows, slot, lane);
   if (at.first >= at.end) return;
@@ -142,12 +142,12 @@ dense_dkv_kernel(DenseArgs a) {
   const int64_t stat0 = ((int64_t)b * a.H + hk * a.G) * a.Nq + doc.q0;
   auto issue = [&](int t) __attribute__((always_inline)) {
     auto offset = [&](int r, const Strides& st) {
-      const int row = min(t * BN + r, end - 1), token = a.G == 1 ? row : row / a.G;
+      const int row = min(t * BN + r, end - 1), token = row / a.by_g;
       return (row - token * a.G) * st.h + token * st.n;
     };
     copy_tile<Z>(qp, lds + (t & 1) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.qst); });
     copy_tile<Z>(yp, lds + (2 + (t & 1)) * Z::kBytes, wave, lane, [&](int r) { return offset(r, a.yst); });
-    const int row = min(t * BN + lane, end - 1), token = a.G == 1 ? row : row / a.G;
+    const int row = min(t * BN + lane, end - 1), token = row / a.by_g;
     const uint32_t to = (uint32_t)uniform((int)(lds_stats + ((t & 1) * 4 + wave) * 256));
     if (wave < 2) async_copy_4B((wave == 0 ? a.lse_in : a.delta) + stat0 + (int64_t)(row - token * a.G) * a.Nq + token, to);
     if (SLOPES && wave == 2) async_copy_4B(a.slopes + hk * a.G + row - token * a.G, to);

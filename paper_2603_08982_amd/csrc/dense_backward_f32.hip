@@ -14,15 +14,15 @@ dense_dq_f32_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[kDenseWaves * S::kWave];  // of a wave: a tile of K, one of V
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, S::kRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
-  const int row = min(at.first + li, at.end - 1), token = row / a.G, head = hk * a.G + (row - token * a.G);
+  const int row = min(at.first + li, at.end - 1), token = row / a.by_g, head = hk * a.G + (row - token * a.G);
   const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
-  const int hi_all = doc.seen(at.first / a.G - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.G - doc.q0);
+  const int hi_all = doc.seen(at.first / a.by_g - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.by_g - doc.q0);
   const int split = blockIdx.y, tiles = (hi_any + BN - 1) / BN;
   const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
@@ -91,7 +91,7 @@ dense_dq_f32_kernel(DenseArgs a) {
       store_four(a.part + (part0 + r) * D + d, v);
       return;
     }
-    const int tok = (at.first + r) / a.G, hd = hk * a.G + (at.first + r - tok * a.G);
+    const int tok = (at.first + r) / a.by_g, hd = hk * a.G + (at.first + r - tok * a.G);
     store_four(static_cast<float*>(a.o) + b * a.ost.b + hd * a.ost.h + tok * a.ost.n + d, times(v, a.scale));
   });
 }
@@ -107,7 +107,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) float stats_s[kDenseWaves][4][64];           // of its rows: log-sum-exp, delta, slope, position
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<false>(a, b, S::kRows, slot, lane);
   if (at.first >= at.end) return;
@@ -136,13 +136,13 @@ dense_dkv_f32_kernel(DenseArgs a) {
   const int64_t stat0 = ((int64_t)b * a.H + hk * a.G) * a.Nq + doc.q0;
   auto issue = [&](const float* base, const Strides& st, int t, uint32_t to) __attribute__((always_inline)) {
     copy_solo<D>(base, to, lane, [&](int r) {
-      const int row = min(t * BN + r, end - 1), token = a.G == 1 ? row : row / a.G;
+      const int row = min(t * BN + r, end - 1), token = row / a.by_g;
       return (row - token * a.G) * st.h + token * st.n;
     });
   };
   constexpr int kStats = 2 + SLOPES;
   auto issue_stats = [&](int t) __attribute__((always_inline)) {
-    const int row = min(t * BN + li, end - 1), token = a.G == 1 ? row : row / a.G;
+    const int row = min(t * BN + li, end - 1), token = row / a.by_g;
     const int64_t stat = stat0 + (int64_t)(row - token * a.G) * a.Nq + token;
     async_copy_4B(a.lse_in + stat, (uint32_t)uniform((int)lds_stats));
     async_copy_4B(a.delta + stat, (uint32_t)uniform((int)(lds_stats + 256)));

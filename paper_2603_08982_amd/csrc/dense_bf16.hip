@@ -43,18 +43,18 @@ dense_forward_bf16_kernel(DenseArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
   const int wave_row = at.first + 32 * wave, row = min(wave_row + li, at.end - 1);
-  const int token = row / a.G, head = hk * a.G + (row - token * a.G);
+  const int token = row / a.by_g, head = hk * a.G + (row - token * a.G);
   const int pos = doc.position(token - doc.q0) - 4 * lh, hi = doc.seen(token - doc.q0) - 4 * lh;  // (less what a lane's first key is)
   // keys that every row of this wave sees, and that some row of the workgroup sees
-  const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.G - doc.q0));
-  const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.G - doc.q0));
+  const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.by_g - doc.q0));
+  const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.by_g - doc.q0));
   const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
   const int t_lo = uniform(part_begin(tiles, split, a.splits)), t_hi = uniform(part_begin(tiles, split + 1, a.splits));
 
@@ -303,7 +303,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
   }
   float l = ls[0] + ls[1];
   l += swap32(l);
-  const int l2 = again(lane), out_row = min(wave_row + (l2 & 31), at.end - 1), out_token = out_row / a.G;
+  const int l2 = again(lane), out_row = min(wave_row + (l2 & 31), at.end - 1), out_token = out_row / a.by_g;
   const int out_head = hk * a.G + (out_row - out_token * a.G);
   const bool live = wave_row + (l2 & 31) < at.end;
   if (a.splits > 1) {

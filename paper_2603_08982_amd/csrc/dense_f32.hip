@@ -14,16 +14,16 @@ dense_forward_f32_kernel(DenseArgs a) {
   __shared__ float ml[kDenseWaves][2][32];                                              // of a wave: maximum, sum of each row
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.Hk, hk = bh - b * a.Hk;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, S::kRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
   if (at.first >= at.end) return;
   const Document& doc = at.doc;
 
-  const int row = min(at.first + li, at.end - 1), token = row / a.G, head = hk * a.G + (row - token * a.G);
+  const int row = min(at.first + li, at.end - 1), token = row / a.by_g, head = hk * a.G + (row - token * a.G);
   const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
   // keys that every row sees, and that some row sees
-  const int hi_all = doc.seen(at.first / a.G - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.G - doc.q0);
+  const int hi_all = doc.seen(at.first / a.by_g - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.by_g - doc.q0);
   const int split = blockIdx.y, tiles = (hi_any + BN - 1) / BN;
   const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
@@ -122,7 +122,7 @@ dense_forward_f32_kernel(DenseArgs a) {
       if (d == 0) a.part_ml[part0 + r] = make_float2(top(r), sum);
       return;
     }
-    const int tok = (at.first + r) / a.G, hd = hk * a.G + (at.first + r - tok * a.G);
+    const int tok = (at.first + r) / a.by_g, hd = hk * a.G + (at.first + r - tok * a.G);
     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
     store_four(static_cast<float*>(a.o) + b * a.ost.b + hd * a.ost.h + tok * a.ost.n + d, times(v, inv));
     if (a.lse && d == 0) a.lse[((int64_t)b * a.H + hd) * a.Nq + tok] = (top(r) + log2f(sum)) * kLn2;

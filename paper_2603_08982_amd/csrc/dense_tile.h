@@ -289,7 +289,9 @@ __device__ __forceinline__ Found find_tile(const DenseArgs& a, int b, int per, i
 }
 
 // Where part `split` of `splits` begins among so many tiles: 2^25 and a few at most, and 64 parts.
-__device__ __forceinline__ int part_begin(int tiles, int split, int splits) { return (int)((unsigned)tiles * (unsigned)split / (unsigned)splits); }
+__device__ __forceinline__ int part_begin(int tiles, int split, int splits) {
+  return splits == 1 ? split * tiles : (int)((unsigned)tiles * (unsigned)split / (unsigned)splits);
+}
 
 // Workgroup to (key head of the batch, slot). Workgroups go to the 8 XCDs in turn: each takes whole heads, whose keys and values (or
 // queries) its L2 then holds once, and the heads that are left over when each has as many are dealt out by the slot, so that tiles
@@ -298,7 +300,7 @@ __device__ __forceinline__ bool dense_index(const DenseArgs& a, int& bh, int& sl
   const unsigned heads = (unsigned)(a.B * a.Hk), slots = (unsigned)a.slots, whole = heads / 8, rest = heads % 8;
   const unsigned wg = long_grid_index(), xcd = wg & 7, i = wg >> 3;
   if (i < whole * slots) {
-    const unsigned h = i / slots;
+    const unsigned h = (unsigned)((int)i / a.by_slots);
     bh = (int)(h * 8 + xcd);
     slot = (int)(i - h * slots);
     return true;
