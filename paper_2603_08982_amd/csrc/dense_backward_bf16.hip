@@ -1,101 +1,15 @@
-// The gradients of dense attention with masks in bf16: the workgroup's four waves own 128 rows and share the other side's tiles.
+// The gradients of dense attention with masks in bf16: a workgroup owns 128 rows, 64 each of its two waves, which share the other side's
+// tiles.
+//
+// A wave has a SIMD to itself, with 512 registers, and an operand that it reads from a tile goes into two products (with 32 rows a wave,
+// two waves a SIMD, the reads of LDS took as long as the products). What it computes from one pair of sums it issues between the products of the
+// next, and the operands are read AHEAD pairs of products before their own.
 #include "dense_tile.h"
 
 namespace svgear {
 namespace {
 
-// ---- the queries' gradients: 128 queries a workgroup, a pass over the keys
-template <int D, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(64 * kDenseWaves, 2)
-dense_dq_kernel(DenseArgs a) {
-  using T = bf16_t;
-  using Z = Tile<T, D>;
-  constexpr int DB = D / 32, BN = Z::kRows;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
-  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
-  const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
-  if (at.first >= at.end) return;
-  const Document& doc = at.doc;
-
-  const int wave_row = at.first + 32 * wave, row = wave_row + li, row_c = min(row, at.end - 1);
-  const bool active = wave_row < at.end;
-  const int token = row_c / a.by_g, head = hk * a.G + (row_c - token * a.G);
-  const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
-  const int hi_all = doc.seen(min(wave_row, at.end - 1) / a.by_g - doc.q0), hi_any = doc.seen(min(wave_row + 31, at.end - 1) / a.by_g - doc.q0);
-  const int hi_wg = doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.by_g - doc.q0);
-  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
-  const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
-
-  typename Z::Column q, dy;
-  q.load(static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
-  dy.load(static_cast<const T*>(a.dy) + b * a.yst.b + head * a.yst.h + token * a.yst.n, lh);
-  const int64_t stat = ((int64_t)b * a.H + head) * a.Nq + token;
-  const float lse2 = a.lse_in[stat] * kLog2e, delta = a.delta[stat];
-  const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;
-  SVGEAR_WAIT_VMCNT(0);
-
-  const Z z(lane);
-  const Scores<T, CAP, SLOPES> scores(a);
-  const uint32_t lds = lds_address(smem);
-  const T* kp = static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
-  const T* vp = static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const int last = hi_wg - 1 - t * BN;
-    copy_tile<Z>(kp + (int64_t)t * BN * a.kst.n, lds + (t & 1) * Z::kBytes, wave, lane,
-                    [&](int r) { return (int64_t)min(r, last) * a.kst.n; });
-    copy_tile<Z>(vp + (int64_t)t * BN * a.vst.n, lds + (2 + (t & 1)) * Z::kBytes, wave, lane,
-                    [&](int r) { return (int64_t)min(r, last) * a.vst.n; });
-  };
-
-  f32x16 acc[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) clear(acc[db]);
-  if (t_lo < t_hi) issue(t_lo);
-  for (int t = t_lo; t < t_hi; ++t) {
-    SVGEAR_WAIT_VMCNT(0);
-    __syncthreads();
-    if (t + 1 < t_hi) issue(t + 1);
-    if (!active || t * BN >= hi_any) continue;
-    const unsigned char* kt = smem + (t & 1) * Z::kBytes;
-    const unsigned char* vt = smem + (2 + (t & 1)) * Z::kBytes;
-    const bool masked = (t + 1) * BN > hi_all;
-#pragma unroll
-    for (int kb = 0; kb < Z::kBlocks; ++kb) {
-      f32x16 x, dp;
-      clear(x);
-      clear(dp);
-      z.rows_times(kt, kb, q, x);
-      z.rows_times(vt, kb, dy, dp);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = t * BN + 32 * kb + row_of(r, lh);
-        const float in = scores.inner(x[r]);
-        float ds = __builtin_amdgcn_exp2f(scores.outer(in, (float)(pos - j), slope, lse2)) * (dp[r] - delta);
-        if (CAP) ds *= scores.keeps(in);
-        x[r] = masked && j >= hi ? 0.f : ds;
-      }
-      z.transposed_times(kt, kb, x, acc, lane);
-    }
-  }
-
-  if (!active) return;
-  if (a.marks) {
-    const bool spoiled = Z::unbounded(acc);
-    if (lane == 0) *mark_of(a, split, bh, slot, wave) = spoiled;
-  }
-  if (row >= at.end) return;
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + row;
-    Z::each_four(acc, lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
-    return;
-  }
-  T* o = static_cast<T*>(a.o) + b * a.ost.b + head * a.ost.h + token * a.ost.n;
-  const float f = a.scale;
-  Z::each_four(acc, lh, [&](int d, float4 v) { store_four(o + d, make_float4(v.x * f, v.y * f, v.z * f, v.w * f)); });
-}
+constexpr int kWaves = 2;  // of a workgroup
 
 // f(0), f(1), .. f(N - 1) with constants (a loop of this length over so much is not unrolled)
 template <int N, typename F>
@@ -106,13 +20,6 @@ __device__ __forceinline__ void each(F f) {
   }
 }
 
-// ---- the keys' and values' gradients: 128 keys a workgroup, a pass over the queries of all heads that share them
-// A wave has 64 keys and a SIMD to itself: 512 registers, of which the accumulators take 256 at d = 128 and the keys 64, and the values
-// wait in LDS. An operand read from a tile goes into two products (with 32 keys a wave, two waves a SIMD, the reads of LDS took longer
-// than the products). A step of 32 queries is 4 x 16 products of 32 cycles; the exponentials lie between the products of dy and v, the
-// differences from delta between those of p and dy, and the operands are read AHEAD pairs of products before their own.
-constexpr int kDkvWaves = 2;
-
 // Products whose sums are kept in vector registers (x) and in accumulation registers (acc): the compiler, which is free to choose, moves
 // half of the accumulators between the two kinds in every step. It does not know of these instructions' latency: a sum that is read by
 // another kind of instruction is read behind `settled` (11 cycles of 4 at least after the last product; here 20), and the two
@@ -121,21 +28,219 @@ __device__ __forceinline__ void product(f32x16& x, const bf16x8& a, const bf16x8
   if (first) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x) : "v"(a), "v"(b));
   else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x) : "v"(a), "v"(b));
 }
+// The same with the columns in accumulation registers (`keep`).
+__device__ __forceinline__ void product_kept(f32x16& x, const bf16x8& a, const bf16x8& b, bool first) {
+  if (first) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x) : "v"(a), "a"(b));
+  else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x) : "v"(a), "a"(b));
+}
+__device__ __forceinline__ void keep(bf16x8& b) { asm volatile("" : "+a"(b)); }
 __device__ __forceinline__ void settled(f32x16 (&x)[2]) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(x[0]), "+v"(x[1])); }
 __device__ __forceinline__ void accumulate(f32x16& acc, const bf16x8& a, const bf16x8& b) {
   asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void settled_acc(f32x16& acc) { asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc)); }
 
+// ---- the queries' gradients: a pass over the keys
+// A tile of 64 keys is 6 x 16 products of 32 cycles at d = 128: of its first and second 32 keys, those of k and q, of v and dy, and of
+// ds and k. The exponentials lie between those of v and dy, ds = p (dp - delta) between what follows.
 template <int D, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(64 * kDkvWaves, 1)
+__global__ void __launch_bounds__(64 * kWaves, 1)
+dense_dq_kernel(DenseArgs a) {
+  using T = bf16_t;
+  using Z = Tile<T, D>;
+  constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes, AHEAD = 3;
+  static_assert(kWaves * 64 == kDenseRows && 2 * DB == KS, "the tiles of the other kernels; as many pairs of products each");
+  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
+  int bh, slot;
+  if (!dense_index(a, bh, slot)) return;
+  const int b = bh / a.by_hk, hk = bh - b * a.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
+  const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
+  if (at.first >= at.end) return;
+  const Document& doc = at.doc;
+
+  const int wave_row = at.first + 64 * wave;
+  const bool active = wave_row < at.end;
+  const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.by_g - doc.q0));
+  const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.by_g - doc.q0));
+  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
+  const int t_lo = uniform(part_begin(tiles, split, a.splits)), t_hi = uniform(part_begin(tiles, split + 1, a.splits));
+
+  const Z z(lane);
+  const Scores<T, CAP, SLOPES> scores(a);
+  const uint32_t lds = lds_address(smem);
+  const T* kp = static_cast<const T*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
+  const T* vp = static_cast<const T*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
+  // Rows of a whole tile lie at one offset of the lane from addresses that the wave shares; in the last tile, rows behind the last key
+  // that a query here sees are not read.
+  constexpr int kCopies = BN / Z::kRowsPerCopy / kWaves, kStep = kWaves * Z::kRowsPerCopy;
+  const int copy_row = wave * Z::kRowsPerCopy + lane / Z::kChunks;
+  auto issue_rows = [&](int t, const T* base, int64_t st, int buffer) __attribute__((always_inline)) {
+    const T* rows = static_cast<const T*>(uniform_ptr(base + (int64_t)t * BN * st));
+    const uint32_t to = (uint32_t)uniform((int)(lds + buffer * Z::kBytes + wave * 1024));
+    const int last = hi_wg - 1 - t * BN;
+    if (last >= BN - 1) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i)
+        async_copy_16B(rows + (int64_t)(i * kStep) * st, (uint32_t)copy_row * (uint32_t)st * 2u + ((lane % Z::kChunks) ^ Z::swz(i * kStep + copy_row)) * 16,
+                       to + i * kWaves * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i)
+        async_copy_16B(rows, (uint32_t)min(i * kStep + copy_row, last) * (uint32_t)st * 2u + ((lane % Z::kChunks) ^ Z::swz(i * kStep + copy_row)) * 16,
+                       to + i * kWaves * 1024);
+    }
+  };
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    issue_rows(t, kp, a.kst.n, t & 1);
+    issue_rows(t, vp, a.vst.n, 2 + (t & 1));
+  };
+  if (t_lo < t_hi) issue(t_lo);
+
+  typename Z::Column q[2], dy[2];
+  int pos[2], hi[2];
+  float lse2[2], delta[2], slope[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = min(wave_row + 32 * c + li, at.end - 1), token = row / a.by_g, head = hk * a.G + (row - token * a.G);
+    pos[c] = doc.position(token - doc.q0), hi[c] = doc.seen(token - doc.q0);
+    q[c].load(static_cast<const T*>(a.q) + b * a.qst.b + head * a.qst.h + token * a.qst.n, lh);
+    dy[c].load(static_cast<const T*>(a.dy) + b * a.yst.b + head * a.yst.h + token * a.yst.n, lh);
+    const int64_t stat = ((int64_t)b * a.H + head) * a.Nq + token;
+    lse2[c] = a.lse_in[stat] * kLog2e, delta[c] = a.delta[stat];
+    slope[c] = SLOPES ? a.slopes[head] * kLog2e : 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) keep(q[c].v[s]), keep(dy[c].v[s]);
+  }
+
+  f32x16 acc[2][DB];
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) clear(acc[c][db]);
+
+  for (int t = t_lo; t < t_hi; ++t) {
+    SVGEAR_WAIT_VMCNT(0);
+    __syncthreads();
+    if (t + 1 < t_hi) issue(t + 1);
+    const bool masked = (t + 1) * BN > hi_all;
+    const unsigned char* kt = smem + (t & 1) * Z::kBytes;
+    const unsigned char* vt = smem + (2 + (t & 1)) * Z::kBytes;
+    constexpr int N = 6 * KS;
+    bf16x8 op[N];
+    // pairs of products: KS each of k q and v dy of the first 32 keys, of the second, and of ds k of both
+    auto rd = [&](int i) __attribute__((always_inline)) {
+      const int phase = i / KS, s = i % KS;
+      if (phase < 4) {
+        op[i] = as_bf16x8(*reinterpret_cast<const uint4*>((phase & 1 ? vt : kt) + (phase >> 1) * 32 * ROWB + (z.row_off ^ (s << 5))));
+      } else {
+        const unsigned char* from16 = kt + (phase - 4) * 32 * ROWB + (s / DB) * 16 * ROWB;
+        const int off = z.tr_off ^ ((s % DB) << 6);
+        union { struct { v4i16 a, b; } s; bf16x8 v; } x;
+        x.s.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(from16 + off));
+        x.s.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(from16 + 8 * ROWB + (off ^ 32)));
+        op[i] = x.v;
+      }
+    };
+    f32x16 x[2][2], dp[2][2];  // of a block, of a column
+    uint32_t dsk[2][2][8];
+    auto weights = [&](int blk, int e) __attribute__((always_inline)) {  // of registers 2 e, 2 e + 1
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int r = 2 * e; r < 2 * e + 2; ++r) {
+          const float in = scores.inner(x[blk][c][r]);
+          const float dist = SLOPES ? (float)(pos[c] - (t * BN + 32 * blk + row_of(r, lh))) : 0.f;
+          const float p = __builtin_amdgcn_exp2f(scores.outer(in, dist, slope[c], lse2[c]));
+          x[blk][c][r] = CAP ? p * scores.keeps(in) : p;
+        }
+    };
+    auto differences = [&](int blk, int e) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        dsk[blk][c][e] = pack2_bf16(x[blk][c][2 * e] * (dp[blk][c][2 * e] - delta[c]), x[blk][c][2 * e + 1] * (dp[blk][c][2 * e + 1] - delta[c]));
+    };
+    // What keys that a row does not see have is taken out where there are such (a branch that no accumulator's value goes through: in one
+    // that it did, the compiler would move it).
+    auto hide = [&](int blk) __attribute__((always_inline)) {
+      if (!masked) return;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int limit = hi[c] - (t * BN + 32 * blk + 4 * lh);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (row_of(2 * e, 0) >= limit) dsk[blk][c][e] &= 0xffff0000u;
+          if (row_of(2 * e + 1, 0) >= limit) dsk[blk][c][e] &= 0xffffu;
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) rd(i);
+    each<N>([&](auto group) __attribute__((always_inline)) {
+      constexpr int i = decltype(group)::value, phase = i / KS, s = i % KS, E = 8 / KS;
+      __builtin_amdgcn_sched_barrier(0);
+      if (i == 4 * KS) hide(0);
+      if (i == 5 * KS) hide(1);
+      if (i + AHEAD < N) rd(i + AHEAD);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (phase < 4) {
+          if (phase & 1) product_kept(dp[phase >> 1][c], op[i], dy[c].v[s], s == 0);
+          else product_kept(x[phase >> 1][c], op[i], q[c].v[s], s == 0);
+        } else {
+          const uint32_t(&w)[8] = dsk[phase == 5][c];
+          constexpr int q4 = (s / DB) * 4;
+          accumulate(acc[c][s % DB], op[i], as_bf16x8(make_uint4(w[q4], w[q4 + 1], w[q4 + 2], w[q4 + 3])));
+        }
+      }
+      // sums of the phase before, behind its last products and this group's
+      if (s == 0 && (phase == 1 || phase == 3)) settled(x[phase >> 1]);
+      if (s == 0 && (phase == 2 || phase == 4)) settled(dp[phase / 2 - 1]);
+#pragma unroll
+      for (int e = s * E; e < (s + 1) * E; ++e) {
+        if (phase == 1 || phase == 3) weights(phase >> 1, e);
+        if (phase == 2 || phase == 4) differences(phase / 2 - 1, e);
+      }
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) settled_acc(acc[c][db]);
+  if (!active) return;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    if (a.marks) {
+      const bool spoiled = Z::unbounded(acc[c]);
+      if (lane == 0) *mark_of(a, split, bh, slot, 2 * wave + c) = spoiled;
+    }
+    const int row = wave_row + 32 * c + li, token = row / a.by_g, head = hk * a.G + (row - token * a.G);
+    if (row >= at.end) continue;
+    if (a.splits > 1) {
+      const int64_t rows = (int64_t)a.B * a.Hk * a.Nq * a.G, out = split * rows + (int64_t)bh * a.Nq * a.G + row;
+      Z::each_four(acc[c], lh, [&](int d, float4 v) { store_four(a.part + out * D + d, v); });
+      continue;
+    }
+    T* o = static_cast<T*>(a.o) + b * a.ost.b + head * a.ost.h + token * a.ost.n;
+    const float f = a.scale;
+    Z::each_four(acc[c], lh, [&](int d, float4 v) { store_four(o + d, make_float4(v.x * f, v.y * f, v.z * f, v.w * f)); });
+  }
+}
+
+// ---- the keys' and values' gradients: 128 keys a workgroup, a pass over the queries of all heads that share them
+// Of a wave's registers the accumulators take 256 at d = 128 and the keys 64, and the values wait in LDS. A step of 32 queries is 4 x 16
+// products of 32 cycles; the exponentials lie between the products of dy and v, ds = p (dp - delta) between those of p and dy.
+template <int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(64 * kWaves, 1)
 dense_dkv_kernel(DenseArgs a) {
   constexpr bool kPark = D == 128;
   using T = bf16_t;
   using Z = Tile<T, D, kPark ? 1 : 2>;
   constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes, AHEAD = 3;
-  static_assert(kDkvWaves * 64 == kDenseRows, "the tiles of the other kernels");
-  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes + (kPark ? 2 * kDkvWaves * Z::kParked : 0)];  // two of Q, two of dy
+  static_assert(kWaves * 64 == kDenseRows, "the tiles of the other kernels");
+  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes + (kPark ? 2 * kWaves * Z::kParked : 0)];  // two of Q, two of dy
   __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, position
   int bh, slot;
   if (!dense_index(a, bh, slot)) return;
@@ -165,7 +270,7 @@ dense_dkv_kernel(DenseArgs a) {
   const int64_t stat0 = ((int64_t)b * a.H + hk * a.G) * a.Nq + doc.q0;
   // Rows of a whole tile lie at one offset of the lane from addresses that the wave shares, where a key head has one query head and
   // the strides leave the offsets within 32 bits.
-  constexpr int kCopies = BN / Z::kRowsPerCopy / kDkvWaves, kStep = kDkvWaves * Z::kRowsPerCopy;
+  constexpr int kCopies = BN / Z::kRowsPerCopy / kWaves, kStep = kWaves * Z::kRowsPerCopy;
   const int copy_row = wave * Z::kRowsPerCopy + lane / Z::kChunks;
   const bool even = a.G == 1 && a.qst.n <= (1 << 24) && a.yst.n <= (1 << 24);
   auto issue_rows = [&](int t, const T* base, const Strides& st, int buffer) __attribute__((always_inline)) {
@@ -175,12 +280,12 @@ dense_dkv_kernel(DenseArgs a) {
 #pragma unroll
       for (int i = 0; i < kCopies; ++i)
         async_copy_16B(rows + (int64_t)(i * kStep) * st.n, (uint32_t)copy_row * (uint32_t)st.n * 2u + ((lane % Z::kChunks) ^ Z::swz(i * kStep + copy_row)) * 16,
-                       to + i * kDkvWaves * 1024);
+                       to + i * kWaves * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < kCopies; ++i) {
         const int r = i * kStep + copy_row, row = min(t * BN + r, end - 1), token = row / a.by_g;
-        async_copy_16B(base + (row - token * a.G) * st.h + token * st.n + ((lane % Z::kChunks) ^ Z::swz(r)) * 8, to + i * kDkvWaves * 1024);
+        async_copy_16B(base + (row - token * a.G) * st.h + token * st.n + ((lane % Z::kChunks) ^ Z::swz(r)) * 8, to + i * kWaves * 1024);
       }
     }
   };
@@ -361,8 +466,8 @@ template <int D>
 int launch(const DenseArgs& a, int what, hipStream_t s) {
   return by_scores(a, [&](auto cap, auto slopes) -> int {
     constexpr bool C = decltype(cap)::value, S = decltype(slopes)::value;
-    if (what == kDenseDq) dense_dq_kernel<D, C, S><<<dense_grid(a), 64 * kDenseWaves, 0, s>>>(a);
-    else dense_dkv_kernel<D, C, S><<<dense_grid(a), 64 * kDkvWaves, 0, s>>>(a);
+    if (what == kDenseDq) dense_dq_kernel<D, C, S><<<dense_grid(a), 64 * kWaves, 0, s>>>(a);
+    else dense_dkv_kernel<D, C, S><<<dense_grid(a), 64 * kWaves, 0, s>>>(a);
     SVGEAR_LAUNCH_CHECK();
     return SVGEAR_OK;
   });
