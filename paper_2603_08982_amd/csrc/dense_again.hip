@@ -152,8 +152,8 @@ template <typename T, int D, bool CAP, bool SLOPES, int WHAT>
 __global__ void __launch_bounds__(64 * kDenseWaves)
 dense_again_kernel(DenseArgs a) {
   constexpr bool SOLO = sizeof(T) == 4;
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split) || split > 0) return;
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), b = bh / a.by_hk, hk = bh - b * a.Hk;
   if (SOLO && wave > 0) return;
   const int tile = a.causal && WHAT != kDenseDkv ? a.slots - 1 - slot : slot;
@@ -212,9 +212,8 @@ dense_again_kernel(DenseArgs a) {
 
 template <typename T, int D, int WHAT>
 int launch(const DenseArgs& a, hipStream_t s) {
-  const dim3 all = dense_grid(a), grid(all.x, 1, all.z);
   return by_scores(a, [&](auto cap, auto slopes) -> int {
-    dense_again_kernel<T, D, decltype(cap)::value, decltype(slopes)::value, WHAT><<<grid, 64 * kDenseWaves, 0, s>>>(a);
+    dense_again_kernel<T, D, decltype(cap)::value, decltype(slopes)::value, WHAT><<<dense_grid(a), 64 * kDenseWaves, 0, s>>>(a);
     SVGEAR_LAUNCH_CHECK();
     return SVGEAR_OK;
   });

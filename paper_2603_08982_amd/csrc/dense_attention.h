@@ -40,7 +40,7 @@ struct DenseArgs {
   bool docs_shared, causal;
   float scale, cap;
   int B, H, Hk, G, Nq, Nk;
-  Divider by_hk, by_g, by_slots;
+  Divider by_hk, by_g, by_slots, by_splits;
   int slots, splits;  // tiles a key head has at most, parts that the other side's rows are cut into
   float* part;        // where splits > 1: [splits][B Hk rows][d] (dk, then dv in the backward pass)
   float2* part_ml;    // forward: maximum and sum of each

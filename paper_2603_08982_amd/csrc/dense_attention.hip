@@ -264,6 +264,7 @@ extern "C" int svgear_attention(const void* q, const int64_t qstride[3], const v
   a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
   a.by_slots = Divider(a.slots);
   a.splits = parts_over_keys(z);
+  a.by_splits = Divider(a.splits);
   Workspace w(ws, ws_bytes);
   if (a.causal) a.marks = w.take<int32_t>(mark_bytes(z, (int64_t)B * Hk, Nq * a.G, a.splits) / sizeof(int32_t));
   if (a.splits > 1) {
@@ -332,6 +333,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
     a.slots = (int)dense_slots(Nq * a.G, q_offsets ? n_docs : 0, rows_of_tile(dt));
     a.by_slots = Divider(a.slots);
     a.splits = parts_over_keys(z);
+    a.by_splits = Divider(a.splits);
     room(Nq * a.G);
     done = launch(a, z, kDenseDq, s);
     if (done != SVGEAR_OK) return done;
@@ -350,6 +352,7 @@ extern "C" int svgear_attention_backward(const void* dy, const int64_t dystride[
   a.slots = (int)dense_slots(Nk, k_offsets ? n_docs : 0, rows_of_tile(dt));
   a.by_slots = Divider(a.slots);
   a.splits = parts_over_queries(z);
+  a.by_splits = Divider(a.splits);
   room(Nk);
   done = launch(a, z, kDenseDkv, s);
   if (done == SVGEAR_OK && a.splits > 1) {

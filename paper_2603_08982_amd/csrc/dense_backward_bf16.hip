@@ -51,8 +51,8 @@ dense_dq_kernel(DenseArgs a) {
   constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes, AHEAD = 3;
   static_assert(kWaves * 64 == kDenseRows && 2 * DB == KS, "the tiles of the other kernels; as many pairs of products each");
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
@@ -63,7 +63,7 @@ dense_dq_kernel(DenseArgs a) {
   const bool active = wave_row < at.end;
   const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.by_g - doc.q0));
   const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.by_g - doc.q0));
-  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
+  const int tiles = (hi_wg + BN - 1) / BN;
   const int t_lo = uniform(part_begin(tiles, split, a.splits)), t_hi = uniform(part_begin(tiles, split + 1, a.splits));
 
   const Z z(lane);
@@ -242,8 +242,8 @@ dense_dkv_kernel(DenseArgs a) {
   static_assert(kWaves * 64 == kDenseRows, "the tiles of the other kernels");
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes + (kPark ? 2 * kWaves * Z::kParked : 0)];  // two of Q, two of dy
   __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, position
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<false>(a, b, kDenseRows, slot, lane);
@@ -259,7 +259,7 @@ dense_dkv_kernel(DenseArgs a) {
   for (int kb = 0; kb < 2; ++kb) from[kb] = doc.first_seer(min(wave_key + 32 * kb + li, at.end - 1) - doc.k0) * a.G;
   const int from_all = uniform(doc.first_seer(min(wave_key + 63, at.end - 1) - doc.k0) * a.G);
   const int first_tile = doc.first_seer(at.first - doc.k0) * a.G / BN, tiles_end = (end + BN - 1) / BN;
-  const int tiles = max(tiles_end - first_tile, 0), split = blockIdx.y;
+  const int tiles = max(tiles_end - first_tile, 0);
   const int t_lo = uniform(first_tile + part_begin(tiles, split, a.splits)), t_hi = uniform(first_tile + part_begin(tiles, split + 1, a.splits));
 
   const Z z(lane);

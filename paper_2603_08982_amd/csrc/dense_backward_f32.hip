@@ -12,8 +12,8 @@ dense_dq_f32_kernel(DenseArgs a) {
   using S = Solo<D>;
   constexpr int DB = D / 32, BN = S::kRows;
   __shared__ __attribute__((aligned(256))) unsigned char smem[kDenseWaves * S::kWave];  // of a wave: a tile of K, one of V
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, S::kRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
@@ -23,7 +23,7 @@ dense_dq_f32_kernel(DenseArgs a) {
   const int row = min(at.first + li, at.end - 1), token = row / a.by_g, head = hk * a.G + (row - token * a.G);
   const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
   const int hi_all = doc.seen(at.first / a.by_g - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.by_g - doc.q0);
-  const int split = blockIdx.y, tiles = (hi_any + BN - 1) / BN;
+  const int tiles = (hi_any + BN - 1) / BN;
   const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column q, dy;
@@ -105,8 +105,8 @@ dense_dkv_f32_kernel(DenseArgs a) {
   constexpr int DB = D / 32, BN = S::kRows;
   __shared__ __attribute__((aligned(256))) unsigned char smem[kDenseWaves * S::kWave];  // of a wave: a tile of Q, one of dy
   __shared__ __attribute__((aligned(256))) float stats_s[kDenseWaves][4][64];           // of its rows: log-sum-exp, delta, slope, position
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<false>(a, b, S::kRows, slot, lane);
@@ -117,7 +117,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
   const int key = min(at.first + li, at.end - 1), j = key - doc.k0, from = doc.first_seer(j) * a.G, end = doc.nq * a.G;
   const int from_all = doc.first_seer(min(at.first + S::kRows, at.end) - 1 - doc.k0) * a.G;
   const int first_tile = doc.first_seer(at.first - doc.k0) * a.G / BN;
-  const int tiles = max((end + BN - 1) / BN - first_tile, 0), split = blockIdx.y;
+  const int tiles = max((end + BN - 1) / BN - first_tile, 0);
   const int t_lo = first_tile + part_begin(tiles, split, a.splits), t_hi = first_tile + part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column k, v;

@@ -41,8 +41,8 @@ dense_forward_bf16_kernel(DenseArgs a) {
   constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes;
   constexpr int AHEAD = CAP && !SLOPES ? 3 : 4;  // operands read before the product that takes them; as many as registers are left
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes];  // two of K, two of V
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, kDenseRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
@@ -55,7 +55,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
   // keys that every row of this wave sees, and that some row of the workgroup sees
   const int hi_all = uniform(doc.seen(min(wave_row, at.end - 1) / a.by_g - doc.q0));
   const int hi_wg = uniform(doc.seen((min(at.first + kDenseRows, at.end) - 1) / a.by_g - doc.q0));
-  const int split = blockIdx.y, tiles = (hi_wg + BN - 1) / BN;
+  const int tiles = (hi_wg + BN - 1) / BN;
   const int t_lo = uniform(part_begin(tiles, split, a.splits)), t_hi = uniform(part_begin(tiles, split + 1, a.splits));
 
   const float slope = SLOPES ? a.slopes[head] * kLog2e : 0.f;

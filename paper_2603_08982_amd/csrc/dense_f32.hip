@@ -12,8 +12,8 @@ dense_forward_f32_kernel(DenseArgs a) {
   constexpr int DB = D / 32, BN = S::kRows;
   __shared__ __attribute__((aligned(256))) unsigned char smem[kDenseWaves * S::kWave];  // of a wave: a tile of K, one of V
   __shared__ float ml[kDenseWaves][2][32];                                              // of a wave: maximum, sum of each row
-  int bh, slot;
-  if (!dense_index(a, bh, slot)) return;
+  int bh, slot, split;
+  if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5, wave = uniform(tid >> 6);
   const Found at = find_tile<true>(a, b, S::kRows, a.causal ? a.slots - 1 - slot : slot, lane);  // causal: the longest first
@@ -24,7 +24,7 @@ dense_forward_f32_kernel(DenseArgs a) {
   const int pos = doc.position(token - doc.q0), hi = doc.seen(token - doc.q0);
   // keys that every row sees, and that some row sees
   const int hi_all = doc.seen(at.first / a.by_g - doc.q0), hi_any = doc.seen((min(at.first + S::kRows, at.end) - 1) / a.by_g - doc.q0);
-  const int split = blockIdx.y, tiles = (hi_any + BN - 1) / BN;
+  const int tiles = (hi_any + BN - 1) / BN;
   const int t_lo = part_begin(tiles, split, a.splits), t_hi = part_begin(tiles, split + 1, a.splits);
 
   typename Z::Column q;

@@ -296,9 +296,10 @@ __device__ __forceinline__ int part_begin(int tiles, int split, int splits) {
 // Workgroup to (key head of the batch, slot). Workgroups go to the 8 XCDs in turn: each takes whole heads, whose keys and values (or
 // queries) its L2 then holds once, and the heads that are left over when each has as many are dealt out by the slot, so that tiles
 // of different lengths (documents, the triangle of a causal mask) fall on all of them alike.
-__device__ __forceinline__ bool dense_index(const DenseArgs& a, int& bh, int& slot) {
+__device__ __forceinline__ bool dense_index(const DenseArgs& a, int& bh, int& slot, int& split) {
   const unsigned heads = (unsigned)(a.B * a.Hk), slots = (unsigned)a.slots, whole = heads / 8, rest = heads % 8;
-  const unsigned wg = long_grid_index(), xcd = wg & 7, i = wg >> 3;
+  const unsigned wg = long_grid_index(), xcd = wg & 7, all = wg >> 3, i = (unsigned)((int)all / a.by_splits);
+  split = (int)(all - i * (unsigned)a.splits);
   if (i < whole * slots) {
     const unsigned h = (unsigned)((int)i / a.by_slots);
     bh = (int)(h * 8 + xcd);
@@ -357,8 +358,8 @@ int by_scores(const DenseArgs& a, F f) {
   if (a.cap > 0.f) return a.slopes ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
   return a.slopes ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
-// Workgroups of a launch: those of dense_index, and the parts along y.
-inline dim3 dense_grid(const DenseArgs& a) { return long_grid(ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8, a.splits); }
+// Workgroups of a launch: those of dense_index.
+inline dim3 dense_grid(const DenseArgs& a) { return long_grid(ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8 * a.splits, 1); }
 
 }  // namespace
 }  // namespace svgear
