@@ -134,15 +134,24 @@ dense_dkv_f32_kernel(DenseArgs a) {
   const float* qp = static_cast<const float*>(a.q) + b * a.qst.b + hk * a.G * a.qst.h + doc.q0 * a.qst.n;
   const float* yp = static_cast<const float*>(a.dy) + b * a.yst.b + hk * a.G * a.yst.h + doc.q0 * a.yst.n;
   const int64_t stat0 = ((int64_t)b * a.H + hk * a.G) * a.Nq + doc.q0;
+  // (the heads of a key head divide the rows of a copy, and the strides leave a lane's offset within 32 bits)
+  constexpr int64_t kNear = 1 << 24;
+  const bool even = Z::kRowsPerCopy % a.G == 0 && a.qst.n <= kNear && a.yst.n <= kNear && (a.G == 1 || (a.qst.h <= kNear && a.yst.h <= kNear));
   auto issue = [&](const float* base, const Strides& st, int t, uint32_t to) __attribute__((always_inline)) {
-    copy_solo<D>(base, to, lane, [&](int r) {
+    if (even && (t + 1) * BN <= end) {
+      const int l = again(lane), r = l / Z::kChunks, token = r / a.by_g;
+      copy_solo<D>(base + (t * BN) / a.by_g * st.n, Z::kRowsPerCopy / a.by_g * st.n,
+                   ((uint32_t)(r - token * a.G) * (uint32_t)st.h + (uint32_t)token * (uint32_t)st.n) * 4u, to, l);
+      return;
+    }
+    copy_solo<D>(base, to, again(lane), [&](int r) {
       const int row = min(t * BN + r, end - 1), token = row / a.by_g;
       return (row - token * a.G) * st.h + token * st.n;
     });
   };
   constexpr int kStats = 2 + SLOPES;
   auto issue_stats = [&](int t) __attribute__((always_inline)) {
-    const int row = min(t * BN + li, end - 1), token = row / a.by_g;
+    const int row = min(t * BN + (again(lane) & 31), end - 1), token = row / a.by_g;
     const int64_t stat = stat0 + (int64_t)(row - token * a.G) * a.Nq + token;
     async_copy_4B(a.lse_in + stat, (uint32_t)uniform((int)lds_stats));
     async_copy_4B(a.delta + stat, (uint32_t)uniform((int)(lds_stats + 256)));

@@ -13,12 +13,6 @@ namespace {
 template <int D>
 constexpr float kHeadroom = D == 64 ? 0.f : 8.f;
 
-// A value that is found again where it is used: the compiler otherwise keeps what follows from it in registers through the loop.
-__device__ __forceinline__ int again(int v) {
-  asm volatile("" : "+v"(v));
-  return v;
-}
-
 // A row of results: the lanes l and l + 32 hold alternate fours of its columns; they exchange halves and store 16 bytes each.
 template <int DB>
 __device__ __forceinline__ void store_whole(bf16_t* o, const f32x16 (&acc)[DB], float f, int lh, bool live) {

@@ -34,6 +34,20 @@ __device__ __forceinline__ void copy_solo(const float* base, uint32_t lds, int l
   }
 }
 
+// The same where all 32 rows are there and a lane's row of copy i is i * step elements from that of the first: one offset a lane,
+// `at_lane` bytes, from addresses that the wave shares.
+template <int D>
+__device__ __forceinline__ void copy_solo(const float* base, int64_t step, uint32_t at_lane, uint32_t lds, int lane) {
+  using Z = Tile<float, D>;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < Solo<D>::kCopies; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int chunk = (lane % Z::kChunks) ^ Z::swz(i * Z::kRowsPerCopy + lane / Z::kChunks);
+    async_copy_16B(uniform_ptr(base + i * step), at_lane + chunk * 16, (uint32_t)uniform((int)(lds + i * 1024)));
+  }
+}
+
 // The waves' sums of 32 rows, added in their order by all threads: out(row, first of four columns, their sum), each wave's times
 // weight(wave, row).
 template <int D, typename Weight, typename Put>

@@ -221,6 +221,12 @@ __device__ __forceinline__ void copy_tile(const T* base, uint32_t lds, int wave,
   }
 }
 
+// A value that is found again where it is used: the compiler otherwise keeps what follows from it in registers through the loop.
+__device__ __forceinline__ int again(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // ---- documents and masks
 __device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
