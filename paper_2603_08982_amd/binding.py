@@ -463,13 +463,13 @@ def _gate_strides(gate, lead, d_out: int, what: str = "gate", width: str = "d_ou
     """Strides of a gate (or another vector for each token) of tokens (lead + (d_out,)) or of batch entries (without the tokens' axis), and whether it is the first."""
     if gate is None:
         return _NO_ROWS, False
-    per_token = gate.dim() == len(lead) + 1
-    _require(tuple(gate.shape) == (*lead, d_out) or tuple(gate.shape) == (*lead[:-1], d_out),
-             f"{what}: expected [B,N,{width}] or [B,{width}] ([N,{width}] or [{width}] for one batch entry)")
-    _require(d_out == 1 or gate.stride(-1) == 1, f"{what}: expected contiguous {width}")
-    if per_token:
-        return _I64x2(gate.stride(0) if len(lead) == 2 else 0, gate.stride(-2)), True
-    return _I64x2(gate.stride(0) if len(lead) == 2 else 0, 0), False
+    shape, st, batches = gate.shape, gate.stride(), len(lead) == 2
+    per_token = len(shape) == len(lead) + 1
+    if shape != (*(lead if per_token else lead[:-1]), d_out):
+        raise SvgearError(f"{what}: expected [B,N,{width}] or [B,{width}] ([N,{width}] or [{width}] for one batch entry)")
+    if d_out != 1 and st[-1] != 1:
+        raise SvgearError(f"{what}: expected contiguous {width}")
+    return _I64x2(st[0] if batches else 0, st[-2] if per_token else 0), per_token
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
@@ -700,18 +700,21 @@ def _norm_arguments(x, weight, bias, scale, shift, eps: float):
     """The checked arguments that layer_norm and its backward pass share: (B, N, c, x's strides, strides of scale, of shift, whether
     either is one of tokens)."""
     B, N, c, xst = _as_bnd(x, "x")
-    _require(0 < B * N <= _MOST_ROWS and 0 < c <= 1 << 15, f"{B} x {N} tokens of {c}: expected 1 to 2^30 tokens of 1 to 2^15 each")
+    if not (0 < B * N <= _MOST_ROWS and 0 < c <= 1 << 15):
+        raise SvgearError(f"{B} x {N} tokens of {c}: expected 1 to 2^30 tokens of 1 to 2^15 each")
     for w in (weight, bias):
         if w is not None and (w.shape != (c,) or not w.is_contiguous()):
             raise SvgearError("weight, bias: expected [c]")
-    _require(0.0 <= eps < float("inf"), "eps: expected a number from 0 on")
-    places, of_tokens = [], []
-    for m, what in ((scale, "scale"), (shift, "shift")):
-        st, per_token = _gate_strides(m, x.shape[:-1], c, what, "c")
-        places.append(st)
-        of_tokens.append(per_token and m is not None)
-    _require(scale is None or shift is None or of_tokens[0] == of_tokens[1], "scale and shift: both of batch entries or both of tokens")
-    return B, N, c, xst, places[0], places[1], any(of_tokens)
+    if not 0.0 <= eps < float("inf"):
+        raise SvgearError("eps: expected a number from 0 on")
+    if scale is None and shift is None:
+        return B, N, c, xst, _NO_ROWS, _NO_ROWS, False
+    lead = x.shape[:-1]
+    sst, of_tokens = _gate_strides(scale, lead, c, "scale", "c")
+    hst, shift_of_tokens = _gate_strides(shift, lead, c, "shift", "c")
+    if scale is not None and shift is not None and of_tokens != shift_of_tokens:
+        raise SvgearError("scale and shift: both of batch entries or both of tokens")
+    return B, N, c, xst, sst, hst, of_tokens or shift_of_tokens
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -726,7 +729,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     if out is not None and out.shape != x.shape:
         raise SvgearError("out: expected x's shape")
     with _on_device(x.device):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        y = out if out is not None else torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
         rc = lib.svgear_layer_norm(x.data_ptr(), xst, _ptr(weight), _ptr(bias), _ptr(scale), sst, _ptr(shift), hst, dt, B, N, c,
                                    float(eps), y.data_ptr(), _as_bnd(y, "out")[3], _stream_of(x.device))
     _check(rc, "svgear_layer_norm")
@@ -746,8 +749,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     _require(scale is not None or not {"dscale", "dshift"} & set(want), "dscale and dshift need the scale")
     modulation = 0 if scale is None else 2 if per_token else 1
     with _on_device(x.device):
-        new = lambda *shape: torch.empty(*shape, dtype=x.dtype, device=x.device)
-        r = {n: new(*x.shape) if n == "dx" else new(c) if n in ("dweight", "dbias") else new(*scale.shape) for n in want}
+        r = {n: x.new_empty(x.shape if n == "dx" else c if n in ("dweight", "dbias") else scale.shape) for n in want}
         dx = r.get("dx")
         sums = {"dweight", "dbias"} & set(want) or (modulation == 1 and {"dscale", "dshift"} & set(want))
         ws, *space = _scratch(lib.svgear_layer_norm_backward_workspace(dt, B, N, c, modulation) if sums else 0, x.device)
@@ -813,7 +815,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: Optional
     if out is not None and out.shape != q.shape:
         raise SvgearError("out: expected q's shape")
     with _on_device(q.device):
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        o = q.new_empty(q.shape) if out is None else out
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if want_lse else None
         ws, *space = _scratch(lib.svgear_attention_workspace(dt, *sizes, mask[4]), q.device)
         rc = lib.svgear_attention(q.data_ptr(), _strides_bhn(q, "q"), k.data_ptr(), _strides_bhn(k, "k"), v.data_ptr(), _strides_bhn(v, "v"),
@@ -840,7 +842,7 @@ def attention_backward(dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     _require(set(out) <= set(want), "out: gradients that are wanted")
     like = {"dq": q, "dk": k, "dv": v}
     with _on_device(q.device):
-        r = {n: out[n] if n in out else torch.empty(like[n].shape, dtype=q.dtype, device=q.device) for n in want}
+        r = {n: out[n] if n in out else q.new_empty(like[n].shape) for n in want}
         _require(all(r[n].shape == like[n].shape for n in r), "out: expected the shapes of q, k and v")
         ends = [x for n in ("dq", "dk", "dv") for x in (_ptr(r.get(n)), _strides_bhn(r[n], n) if n in r else None)]
         ws, *space = _scratch(lib.svgear_attention_backward_workspace(dt, *sizes, mask[4]), q.device)
