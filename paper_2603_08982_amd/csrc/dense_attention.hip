@@ -38,16 +38,29 @@ dense_merge_kernel(const float* part, const float2* ml, int splits, int64_t rows
   if (row >= rows) return;
   const int d = 8 * (int)(u % (D / 8));
   float M = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) M = fmaxf(M, ml[s * rows + row].x);
-  for (int s = 0; s < splits; ++s) {
-    const float2 p = ml[s * rows + row];
-    if (p.x == -INFINITY && p.y == 0.f) continue;  // no key there
-    const float w = __builtin_amdgcn_exp2f(p.x - M);
-    float v[8];
-    load8(part + (s * rows + row) * D + d, v);
-    l = __builtin_fmaf(w, p.y, l);
+  // (eight parts' loads at a time: one after the other, 50 parts of 320 rows took 22 us)
+  constexpr int U = 8;
+  for (int s = 0; s < splits; s += U) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(w, v[i], acc[i]);
+    for (int u = 0; u < U; ++u) M = fmaxf(M, ml[min(s + u, splits - 1) * rows + row].x);
+  }
+  for (int s = 0; s < splits; s += U) {
+    float2 p[U];
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(s + u, splits - 1) * rows + row;
+      p[u] = ml[at];
+      load8(part + at * D + d, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= splits || (p[u].x == -INFINITY && p[u].y == 0.f)) continue;  // no key there
+      const float w = __builtin_amdgcn_exp2f(p[u].x - M);
+      l = __builtin_fmaf(w, p[u].y, l);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(w, v[u][i], acc[i]);
+    }
   }
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
 #pragma unroll
