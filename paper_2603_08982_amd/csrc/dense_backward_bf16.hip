@@ -38,6 +38,8 @@ __device__ __forceinline__ void settled(f32x16 (&x)[2]) { asm volatile("s_nop 15
 __device__ __forceinline__ void accumulate(f32x16& acc, const bf16x8& a, const bf16x8& b) {
   asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
 }
+// Behind the last products of a loop, and in it: what the compiler moves as it leaves the loop comes before any other statement.
+__device__ __forceinline__ void settled_all() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
 __device__ __forceinline__ void settled_acc(f32x16& acc) { asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc)); }
 
 // ---- the queries' gradients: a pass over the keys
@@ -203,6 +205,7 @@ dense_dq_kernel(DenseArgs a) {
       }
     });
     __builtin_amdgcn_sched_barrier(0);
+    if (t + 1 == t_hi) settled_all();
   }
 
 #pragma unroll
@@ -433,6 +436,7 @@ dense_dkv_kernel(DenseArgs a) {
     const bool masked = t * BN < from_all || (t + 1) * BN > end;
 #pragma unroll
     for (int rb = 0; rb < Z::kBlocks; ++rb) rows_of_tile(t, rb, masked);
+    if (t + 1 == t_hi) settled_all();
   }
 
 #pragma unroll

@@ -61,11 +61,11 @@ dense_dq_f32_kernel(DenseArgs a) {
     clear(dp);
     SVGEAR_WAIT_VMCNT(S::kCopies);  // V has landed, which was issued first
     asm volatile("" ::: "memory");
-    z.rows_times(vt, 0, dy, dp);
+    z.rows_times(vt, dy, dp);
     SVGEAR_WAIT_VMCNT(0);
     asm volatile("" ::: "memory");
     if (more) issue(vp, a.vst.n, t + kDenseWaves, lds + Z::kBytes);
-    z.rows_times(kt, 0, q, x);
+    z.rows_times(kt, q, x);
     const bool masked = (t + 1) * BN > hi_all;
     const int base = t * BN + 4 * lh, limit = hi - base;
     const float ahead = (float)(pos - base);
@@ -76,7 +76,7 @@ dense_dq_f32_kernel(DenseArgs a) {
       if (CAP) ds *= scores.keeps(in);
       x[r] = masked && row_of(r, 0) >= limit ? 0.f : ds;
     }
-    z.transposed_times(kt, 0, x, acc, lane);
+    z.transposed_times(kt, x, acc, lane);
     if (more) issue(kp, a.kst.n, t + kDenseWaves, lds);
   }
 
@@ -177,10 +177,10 @@ dense_dkv_f32_kernel(DenseArgs a) {
     clear(dp);
     SVGEAR_WAIT_VMCNT(S::kCopies + kStats);  // dy has landed, which was issued first
     asm volatile("" ::: "memory");
-    z.rows_times(yt, 0, v, dp);
+    z.rows_times(yt, v, dp);
     SVGEAR_WAIT_VMCNT(0);
     asm volatile("" ::: "memory");
-    z.rows_times(qt, 0, k, x);
+    z.rows_times(qt, k, x);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -207,13 +207,13 @@ dense_dkv_f32_kernel(DenseArgs a) {
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    z.transposed_times(yt, 0, x, dv, lane);
+    z.transposed_times(yt, x, dv, lane);
     __builtin_amdgcn_sched_barrier(0);
     if (more) {
       issue(yp, a.yst, t + kDenseWaves, lds + Z::kBytes);
       issue_stats(t + kDenseWaves);
     }
-    z.transposed_times(qt, 0, dp, dk, lane);
+    z.transposed_times(qt, dp, dk, lane);
     if (more) issue(qp, a.qst, t + kDenseWaves, lds);
   }
 

@@ -59,7 +59,7 @@ dense_forward_f32_kernel(DenseArgs a) {
     const bool more = t + kDenseWaves < t_hi;
     f32x16 x;
     clear(x);
-    z.rows_times(kt, 0, q, x);
+    z.rows_times(kt, q, x);
     if (more) issue(kp, a.kst.n, t + kDenseWaves, lds);
     float mx = -INFINITY;
     const int base = t * BN + 4 * lh, limit = hi - base;
@@ -94,7 +94,7 @@ dense_forward_f32_kernel(DenseArgs a) {
     if (more) SVGEAR_WAIT_VMCNT(S::kCopies);  // V has landed; the next K may be on its way
     else SVGEAR_WAIT_VMCNT(0);
     asm volatile("" ::: "memory");
-    z.transposed_times(vt, 0, x, acc, lane);
+    z.transposed_times(vt, x, acc, lane);
     if (more) issue(vp, a.vst.n, t + kDenseWaves, lds + Z::kBytes);
   }
 

@@ -4,7 +4,7 @@
 //   backward: p_ij = e^(s_ij - lse_i), ds_ij = p_ij (dy_i v_j - dy_i o_i) (1 - tanh^2),
 //   dq_i = scale sum_j ds_ij k_j, dk_j = scale sum_i ds_ij q_i, dv_j = sum_i p_ij dy_i
 //
-// A wave owns 32 rows (queries; keys for dk and dv) as columns of the matrix products, in registers, and reads tiles of the other
+// A wave owns 32 rows (queries; keys for dk and dv; 64 in bf16's backward pass) as columns of the matrix products, in registers, and reads tiles of the other
 // side's rows, which go from global memory straight into LDS, the next under the present one:
 //   X^T = tile columns^T  (32 x 32: a register holds tile rows 8 (r / 4) + 4 (lane / 32) + r % 4 of column lane % 32)
 //   acc^T += tile^T X     (those registers are operands as they stand; bf16 reads the tile transposed with ds_read_b64_tr_b16)
@@ -103,74 +103,44 @@ struct Tile {
     }
   }
 
-  // X^T of block kb of a tile
-  __device__ __forceinline__ void rows_times(const unsigned char* tile, int kb, const Column& c, f32x16& x) const {
-    const unsigned char* t = tile + kb * 32 * kRowBytes;
-    if constexpr (kHalf) {
+  // X^T of a tile (fp32; the kernels in bf16 have their products among what else they do)
+  __device__ __forceinline__ void rows_times(const unsigned char* tile, const Column& c, f32x16& x) const {
+    static_assert(!kHalf, "fp32");
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s)
-        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const uint4*>(t + (row_off ^ (s << 5)))), c.v[s], x, 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int s = 0; s < D / 8; ++s) {
-        const float4 a = *reinterpret_cast<const float4*>(t + (row_off ^ (s << 4)));
-        x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, c.v[s].x, x, 0, 0, 0);
-        x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, c.v[s].y, x, 0, 0, 0);
-        x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, c.v[s].z, x, 0, 0, 0);
-        x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, c.v[s].w, x, 0, 0, 0);
-      }
+    for (int s = 0; s < D / 8; ++s) {
+      const float4 a = *reinterpret_cast<const float4*>(tile + (row_off ^ (s << 4)));
+      x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, c.v[s].x, x, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, c.v[s].y, x, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, c.v[s].z, x, 0, 0, 0);
+      x = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, c.v[s].w, x, 0, 0, 0);
     }
   }
 
-  // the same with the columns in LDS, each lane's operands where it put them (see park)
+  // columns that wait in LDS, each lane's operands where it put them
   static constexpr int kParked = 32 * kRowBytes;  // bytes of a wave
   static __device__ __forceinline__ void park(unsigned char* to, const Column& c, int lane) {
 #pragma unroll
     for (int s = 0; s < kParked / 1024; ++s) *reinterpret_cast<std::conditional_t<kHalf, bf16x8, float4>*>(to + s * 1024 + lane * 16) = c.v[s];
   }
-  __device__ __forceinline__ void rows_times(const unsigned char* tile, int kb, const unsigned char* parked, f32x16& x, int lane) const {
-    static_assert(kHalf, "bf16 columns alone are parked");
-    const unsigned char* t = tile + kb * 32 * kRowBytes;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s)
-      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const uint4*>(t + (row_off ^ (s << 5)))),
-                                                  as_bf16x8(*reinterpret_cast<const uint4*>(parked + s * 1024 + lane * 16)), x, 0, 0, 0);
-  }
 
-  // acc^T += block kb of a tile, transposed, times X (bf16: rounded to it)
-  __device__ __forceinline__ void transposed_times(const unsigned char* tile, int kb, const f32x16& x, f32x16 (&acc)[DB], int lane) const {
-    const unsigned char* t = tile + kb * 32 * kRowBytes;
-    if constexpr (kHalf) {
+  // acc^T += a tile, transposed, times X (fp32). Columns DB i .. of row i of the accumulators, so that a lane reads what it needs of a
+  // tile row at once.
+  __device__ __forceinline__ void transposed_times(const unsigned char* tile, const f32x16& x, f32x16 (&acc)[DB], int lane) const {
+    static_assert(!kHalf, "fp32");
+    const int li = lane & 31, lh = lane >> 5;
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const bf16x8 b = as_bf16x8(make_uint4(pack2_bf16(x[8 * ks], x[8 * ks + 1]), pack2_bf16(x[8 * ks + 2], x[8 * ks + 3]),
-                                              pack2_bf16(x[8 * ks + 4], x[8 * ks + 5]), pack2_bf16(x[8 * ks + 6], x[8 * ks + 7])));
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const int off = tr_off ^ (db << 6);
-          union { struct { v4i16 a, b; } s; bf16x8 v; } u;
-          u.s.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(t + ks * 16 * kRowBytes + off));
-          u.s.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)(t + (ks * 16 + 8) * kRowBytes + (off ^ 32)));
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u.v, b, acc[db], 0, 0, 0);
-        }
-      }
-    } else {
-      // columns DB i .. of row i of the accumulators, so that a lane reads what it needs of a tile row at once
-      const int li = lane & 31, lh = lane >> 5;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = row_of(r, lh);
-        if constexpr (DB == 4) {
-          const float4 a = *reinterpret_cast<const float4*>(t + row * kRowBytes + ((li ^ swz(row)) << 4));
-          acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, x[r], acc[0], 0, 0, 0);
-          acc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, x[r], acc[1], 0, 0, 0);
-          acc[2] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, x[r], acc[2], 0, 0, 0);
-          acc[3] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, x[r], acc[3], 0, 0, 0);
-        } else {
-          const float2 a = *reinterpret_cast<const float2*>(t + row * kRowBytes + (((li >> 1) ^ swz(row)) << 4) + (li & 1) * 8);
-          acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, x[r], acc[0], 0, 0, 0);
-          acc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, x[r], acc[1], 0, 0, 0);
-        }
+    for (int r = 0; r < 16; ++r) {
+      const int row = row_of(r, lh);
+      if constexpr (DB == 4) {
+        const float4 a = *reinterpret_cast<const float4*>(tile + row * kRowBytes + ((li ^ swz(row)) << 4));
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, x[r], acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, x[r], acc[1], 0, 0, 0);
+        acc[2] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, x[r], acc[2], 0, 0, 0);
+        acc[3] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, x[r], acc[3], 0, 0, 0);
+      } else {
+        const float2 a = *reinterpret_cast<const float2*>(tile + row * kRowBytes + (((li >> 1) ^ swz(row)) << 4) + (li & 1) * 8);
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, x[r], acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, x[r], acc[1], 0, 0, 0);
       }
     }
   }
@@ -207,18 +177,6 @@ struct Tile {
 __device__ __forceinline__ void store_four(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void store_four(bf16_t* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(v.x, v.y), pack2_bf16(v.z, v.w));
-}
-
-// Rows of a tensor as 16-byte chunks of lanes: row `at` of tile rows from `first` on, those behind `last` as `last`.
-// (32-bit offsets within a tile: the entry points hold strides to what that takes.)
-template <typename Z, typename T, typename RowOffset>
-__device__ __forceinline__ void copy_tile(const T* base, uint32_t lds, int wave, int lane, RowOffset offset) {
-#pragma unroll
-  for (int i = 0; i < Z::kCopies; ++i) {
-    const int inst = i * kDenseWaves + wave, row = inst * Z::kRowsPerCopy + lane / Z::kChunks;
-    const int chunk = (lane % Z::kChunks) ^ Z::swz(row);
-    async_copy_16B(base + offset(row) + chunk * (16 / (int)sizeof(T)), (uint32_t)uniform((int)(lds + inst * 1024)));
-  }
 }
 
 // A value that is found again where it is used: the compiler otherwise keeps what follows from it in registers through the loop.
