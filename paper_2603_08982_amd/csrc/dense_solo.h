@@ -4,7 +4,8 @@
 // What bounds it: the fp32 matrix cores, 64 cycles for a product of two rows of the contraction, so that copies, softmax and LDS
 // reads hide behind the products of the wave itself and of the other wave of its SIMD (d = 64). Waves that share nothing need no
 // barrier in the loop, and a workgroup of 32 rows is small enough that short documents and the triangle of a causal mask leave no CU
-// behind (2 x 6 heads of 1,237 tokens in three documents: 58 us with 128 rows to a workgroup and shared tiles).
+// behind (2 x 6 heads of 1,237 tokens in three documents 49 us; with 128 rows to a workgroup and shared tiles 61). There the matrix cores
+// are busy 30 % of the cycles: 464 workgroups, the longest of which share a SIMD; with twice the parts it takes longer.
 #pragma once
 #include "dense_tile.h"
 
