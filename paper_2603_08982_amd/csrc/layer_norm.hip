@@ -487,7 +487,7 @@ Plan plan_norm(svgear_dtype dt, int64_t B, int64_t N, int c, int mod, bool backw
   const int per_group = p.z.wpr > 1 ? 1 : kNormWaves * (64 / p.z.lanes), waves = p.z.wpr > 1 ? p.z.wpr : kNormWaves;
   // One round of workgroups that stay, of so many waves a CU that some 30 KB of rows are on their way to it: 75,600 x 5,120 forward
   // with 3 / 6 / 9 / 12 waves of 4 KB 465 / 319 / 300 / 307 us. Backward a workgroup leaves a row of sums, which is worth three rows
-  // of x at least (2 x 777 x 1,541 in fp32, with 4 / 3 / 2 of them 21.4 / 20.2 / 21.9 us).
+  // of x at least (2 x 777 rows of 1,541 in fp32, with 4 / 3 / 2 of them 21.4 / 20.2 / 21.9 us).
   const int lane_bytes = 8 * p.z.ch * (int)esize(dt);
   const int resident = std::max(1, std::min((backward ? 384 : 576) / lane_bytes, backward ? 20 : 24) / waves);
   const int64_t wanted = std::max<int64_t>(256 * resident / p.entries, 1), most = ceil_div(p.rows, per_group * (backward ? 3 : 1));
