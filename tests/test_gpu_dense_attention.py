@@ -181,6 +181,33 @@ def test_far_rows():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("layout", ["tokens", "heads", "far heads", "far tokens"])
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F, 64), (F, 128)])
+@pytest.mark.parametrize("H,Hk", [(2, 2), (4, 2), (8, 2), (8, 1)])
+def test_heads_and_layouts_of_whole_tiles(H, Hk, dtype, d, layout):
+    """Rows of whole tiles are copied at one offset a lane where heads and strides allow it, and one by one elsewhere."""
+    Nq, Nk = 100, 70
+
+    def tensor(h, n):
+        if layout == "tokens":
+            return torch.randn(1, n, h, d, device="cuda", dtype=dtype).transpose(1, 2)
+        x = torch.randn(1, h, n, d, device="cuda", dtype=dtype)
+        if layout == "heads":
+            return x
+        far = (1 << 24) + 16
+        st = (far * h, far, d) if layout == "far heads" else (0, d, far)
+        big = torch.empty(far * ((h if layout == "far heads" else n) - 1) + n * h * d, device="cuda", dtype=dtype)
+        return big.as_strided((1, h, n, d), (*st, 1)).copy_(x)
+
+    torch.manual_seed(31)
+    q, dy = tensor(H, Nq), tensor(H, Nq)
+    near = layout != "far tokens"
+    k, v = (tensor(Hk, Nk) if near else torch.randn(1, Hk, Nk, d, device="cuda", dtype=dtype) for _ in range(2))
+    check(q, k, v, dy, (H, Hk, dtype, d, layout))
+    del q, k, v, dy
+    torch.cuda.empty_cache()
+
+
 # (what a masked place holds, which tensors hold it)
 UNBOUNDED = [(float("nan"), 64), (float("inf"), 1)]
 SHAPES = [(1, 4, 4, 300, 300), (2, 4, 2, 150, 150), (1, 6, 2, 70, 1900), (1, 2, 1, 40, 5000), (1, 3, 1, 260, 100)]
