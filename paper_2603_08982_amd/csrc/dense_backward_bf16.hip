@@ -6,7 +6,7 @@
 // next, and the operands are read AHEAD pairs of products before their own (2: as fast; 4: registers spill).
 // 9,450 packed tokens of 16 heads: dq 740 us (with 32 rows a wave 760 to 810), dk and dv 1,005 (1,210 to 1,270), the matrix cores busy 47 %
 // of the cycles at 1.9 GHz. Of dk's and dv's time the copies are 80 us, the exponentials 55, the differences 50, the operands' reads 80.
-// A cap's tanh makes the vector unit the bound: 4,000 causal tokens of 40 heads, 8 key heads, 1,270 us (with two waves a SIMD 1,100).
+// A cap's tanh makes the vector unit the bound: 4,000 causal tokens of 40 heads, 8 key heads, 1,180 us (with two waves a SIMD 1,100).
 #include "dense_tile.h"
 
 namespace svgear {
@@ -274,30 +274,43 @@ dense_dkv_kernel(DenseArgs a) {
   const T* qp = static_cast<const T*>(a.q) + b * a.qst.b + hk * a.G * a.qst.h + doc.q0 * a.qst.n;
   const T* yp = static_cast<const T*>(a.dy) + b * a.yst.b + hk * a.G * a.yst.h + doc.q0 * a.yst.n;
   const int64_t stat0 = ((int64_t)b * a.H + hk * a.G) * a.Nq + doc.q0;
-  // Rows of a whole tile lie at one offset of the lane from addresses that the wave shares, where a key head has one query head and
-  // the strides leave the offsets within 32 bits.
+  // Where the strides leave a tile's offsets within 32 bits, rows lie at an offset of the lane from an address that the wave shares: at the
+  // same one in every whole tile, if a key head has one query head.
   constexpr int kCopies = BN / Z::kRowsPerCopy / kWaves, kStep = kWaves * Z::kRowsPerCopy;
   const int copy_row = wave * Z::kRowsPerCopy + lane / Z::kChunks;
-  const bool even = a.G == 1 && a.qst.n <= (1 << 24) && a.yst.n <= (1 << 24);
-  auto issue_rows = [&](int t, const T* base, const Strides& st, int buffer) __attribute__((always_inline)) {
-    const uint32_t to = (uint32_t)uniform((int)(lds + buffer * Z::kBytes + wave * 1024));
-    if (even && (t + 1) * BN <= end) {
-      const T* rows = static_cast<const T*>(uniform_ptr(base + (int64_t)t * BN * st.n));
+  auto is_near = [&](const Strides& st) { return st.n < (1 << 24) && (a.G == 1 || (st.h < (1 << 24) && a.G * st.h <= (1 << 29))); };
+  const bool near = is_near(a.qst) && is_near(a.yst);
+  auto issue_rows = [&](int t) __attribute__((always_inline)) {
+    const uint32_t q_to = (uint32_t)uniform((int)(lds + (t & 1) * Z::kBytes + wave * 1024)), y_to = q_to + 2 * Z::kBytes;
+    auto chunk = [&](int i) { return ((lane % Z::kChunks) ^ Z::swz(i * kStep + copy_row)) * 16; };
+    if (near && a.G == 1 && (t + 1) * BN <= end) {
+      const T* q = static_cast<const T*>(uniform_ptr(qp + (int64_t)t * BN * a.qst.n));
+      const T* y = static_cast<const T*>(uniform_ptr(yp + (int64_t)t * BN * a.yst.n));
 #pragma unroll
       for (int i = 0; i < kCopies; ++i)
-        async_copy_16B(rows + (int64_t)(i * kStep) * st.n, (uint32_t)copy_row * (uint32_t)st.n * 2u + ((lane % Z::kChunks) ^ Z::swz(i * kStep + copy_row)) * 16,
-                       to + i * kWaves * 1024);
-    } else {
+        async_copy_16B(q + (int64_t)(i * kStep) * a.qst.n, (uint32_t)copy_row * (uint32_t)a.qst.n * 2u + chunk(i), q_to + i * kWaves * 1024);
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        const int r = i * kStep + copy_row, row = min(t * BN + r, end - 1), token = row / a.by_g;
-        async_copy_16B(base + (row - token * a.G) * st.h + token * st.n + ((lane % Z::kChunks) ^ Z::swz(r)) * 8, to + i * kWaves * 1024);
+      for (int i = 0; i < kCopies; ++i)
+        async_copy_16B(y + (int64_t)(i * kStep) * a.yst.n, (uint32_t)copy_row * (uint32_t)a.yst.n * 2u + chunk(i), y_to + i * kWaves * 1024);
+      return;
+    }
+    const int token0 = uniform(t * BN / a.by_g);
+    const T* q = static_cast<const T*>(uniform_ptr(qp + token0 * a.qst.n));
+    const T* y = static_cast<const T*>(uniform_ptr(yp + token0 * a.yst.n));
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int row = min(t * BN + i * kStep + copy_row, end - 1), token = row / a.by_g, h = row - token * a.G, ahead = token - token0;
+      if (near) {
+        async_copy_16B(q, (__umul24(h, (uint32_t)a.qst.h) + __umul24(ahead, (uint32_t)a.qst.n)) * 2u + chunk(i), q_to + i * kWaves * 1024);
+        async_copy_16B(y, (__umul24(h, (uint32_t)a.yst.h) + __umul24(ahead, (uint32_t)a.yst.n)) * 2u + chunk(i), y_to + i * kWaves * 1024);
+      } else {
+        async_copy_16B(q + h * a.qst.h + ahead * a.qst.n + chunk(i) / 2, q_to + i * kWaves * 1024);
+        async_copy_16B(y + h * a.yst.h + ahead * a.yst.n + chunk(i) / 2, y_to + i * kWaves * 1024);
       }
     }
   };
   auto issue = [&](int t) __attribute__((always_inline)) {
-    issue_rows(t, qp, a.qst, t & 1);
-    issue_rows(t, yp, a.yst, 2 + (t & 1));
+    issue_rows(t);
     const int row = min(t * BN + lane, end - 1), token = row / a.by_g;
     const uint32_t to = (uint32_t)uniform((int)(lds_stats + ((t & 1) * 4 + wave) * 256));
     async_copy_4B((wave == 0 ? a.lse_in : a.delta) + stat0 + (int64_t)(row - token * a.G) * a.Nq + token, to);
