@@ -11,7 +11,7 @@ namespace {
 // each row of the other side for those alone that see it, up to where every sum is a NaN. Without a mark they read that and end. (Checks
 // of the tiles themselves, in the loops that copy them, cost registers that are not there.) The two halves of a wave have half of a
 // row's columns each. Without a mark a launch costs its length: 8,704 tokens of 40 heads with a prefix 397 -> 404 us, the gradients of
-// 8 heads of 1,531 tokens in fp32 121 -> 129 (two launches).
+// 8 heads of 1,531 tokens in fp32 121 -> 129 (two launches). A marked wave takes some 2 us a key.
 __device__ __forceinline__ float4 load_four(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ float4 load_four(const bf16_t* p) {
   const uint2 w = *reinterpret_cast<const uint2*>(p);
@@ -54,7 +54,7 @@ struct Half {
 template <int D, typename T>
 __device__ __forceinline__ float dot_halves(const T* a, const T* b) {
   float s = 0.f;
-#pragma unroll 2
+#pragma unroll 8
   for (int d = 0; d < D / 2; d += 4) {
     const float4 u = load_four(a + d), v = load_four(b + d);
     s = __builtin_fmaf(u.x, v.x, s), s = __builtin_fmaf(u.y, v.y, s), s = __builtin_fmaf(u.z, v.z, s), s = __builtin_fmaf(u.w, v.w, s);
