@@ -181,6 +181,13 @@ def test_far_rows():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (F, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("name", DOCS)
+def test_documents_at_the_other_widths(name, causal, dtype, d):
+    test_documents(name, causal, dtype, d)
+
+
 @pytest.mark.parametrize("layout", ["tokens", "heads", "far heads", "far tokens"])
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F, 64), (F, 128)])
 @pytest.mark.parametrize("H,Hk", [(2, 2), (4, 2), (8, 2), (8, 1)])
