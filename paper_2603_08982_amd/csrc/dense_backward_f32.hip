@@ -123,6 +123,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
   typename Z::Column k, v;
   k.load(static_cast<const float*>(a.k) + b * a.kst.b + hk * a.kst.h + key * a.kst.n, lh);
   v.load(static_cast<const float*>(a.v) + b * a.vst.b + hk * a.vst.h + key * a.vst.n, lh);
+  if (D == 128) k.keep(), v.keep();
   SVGEAR_WAIT_VMCNT(0);
 
   const Z z(lane);
