@@ -247,7 +247,7 @@ dense_dkv_kernel(DenseArgs a) {
   constexpr int DB = D / 32, KS = D / 16, BN = Z::kRows, ROWB = Z::kRowBytes, AHEAD = 3;
   static_assert(kWaves * 64 == kDenseRows, "the tiles of the other kernels");
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * Z::kBytes + (kPark ? 2 * kWaves * Z::kParked : 0)];  // two of Q, two of dy
-  __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, position
+  __shared__ __attribute__((aligned(256))) float stats[2][4][64];  // of a tile's rows: log-sum-exp, delta, slope, distance from the workgroup's first key
   int bh, slot, split;
   if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
@@ -259,7 +259,7 @@ dense_dkv_kernel(DenseArgs a) {
   const int wave_key = at.first + 64 * wave;
   const bool active = wave_key < at.end;
   // rows of the document [from, end) see key j of it; rows from `from_all` on see all keys of this wave
-  const int j0 = wave_key + li - doc.k0, end = doc.nq * a.G;
+  const int end = doc.nq * a.G;
   int from[2];
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) from[kb] = doc.first_seer(min(wave_key + 32 * kb + li, at.end - 1) - doc.k0) * a.G;
@@ -315,7 +315,8 @@ dense_dkv_kernel(DenseArgs a) {
     const uint32_t to = (uint32_t)uniform((int)(lds_stats + ((t & 1) * 4 + wave) * 256));
     async_copy_4B((wave == 0 ? a.lse_in : a.delta) + stat0 + (int64_t)(row - token * a.G) * a.Nq + token, to);
     if (SLOPES && wave == 0) async_copy_4B(a.slopes + hk * a.G + row - token * a.G, to + 512);
-    if (SLOPES && wave == 1) stats[t & 1][3][lane] = (float)doc.position(token);
+    // (less a key's place among the workgroup's afterwards: as numbers of fp32, positions past 2^24 would lose what they differ by)
+    if (SLOPES && wave == 1) stats[t & 1][3][lane] = (float)(doc.position(token) - (at.first - doc.k0));
   };
   if (t_lo < t_hi) issue(t_lo);
 
@@ -389,7 +390,7 @@ dense_dkv_kernel(DenseArgs a) {
           const int r = 2 * e + i;
           const float in = scores.inner(x[kb][r]);
           const float slope = SLOPES ? (w ? (i ? sl.w : sl.z) : (i ? sl.y : sl.x)) * kLog2e : 0.f;
-          const float dist = SLOPES ? (w ? (i ? po.w : po.z) : (i ? po.y : po.x)) - (float)(j0 + 32 * kb) : 0.f;
+          const float dist = SLOPES ? (w ? (i ? po.w : po.z) : (i ? po.y : po.x)) - (float)(64 * wave + 32 * kb + li) : 0.f;
           p[i] = __builtin_amdgcn_exp2f(scores.outer(in, dist, slope, lse[i]));
           x[kb][r] = CAP ? p[i] * scores.keeps(in) : p[i];
         }

@@ -104,7 +104,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
   using S = Solo<D>;
   constexpr int DB = D / 32, BN = S::kRows;
   __shared__ __attribute__((aligned(256))) unsigned char smem[kDenseWaves * S::kWave];  // of a wave: a tile of Q, one of dy
-  __shared__ __attribute__((aligned(256))) float stats_s[kDenseWaves][4][64];           // of its rows: log-sum-exp, delta, slope, position
+  __shared__ __attribute__((aligned(256))) float stats_s[kDenseWaves][4][64];           // of its rows: log-sum-exp, delta, slope, distance from the first key
   int bh, slot, split;
   if (!dense_index(a, bh, slot, split)) return;
   const int b = bh / a.by_hk, hk = bh - b * a.Hk;
@@ -158,7 +158,8 @@ dense_dkv_f32_kernel(DenseArgs a) {
     async_copy_4B(a.delta + stat, (uint32_t)uniform((int)(lds_stats + 256)));
     if (SLOPES) {
       async_copy_4B(a.slopes + hk * a.G + row - token * a.G, (uint32_t)uniform((int)(lds_stats + 512)));
-      stats[3][lane] = (float)doc.position(token);
+      // (positions past 2^24 would lose as numbers of fp32 what they differ by)
+      stats[3][lane] = (float)(doc.position(token) - (at.first - doc.k0));
     }
   };
 
@@ -193,7 +194,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
       if (SLOPES) {
         const float4 sl = of_rows(2), po = of_rows(3);
         slope[0] = sl.x * kLog2e, slope[1] = sl.y * kLog2e, slope[2] = sl.z * kLog2e, slope[3] = sl.w * kLog2e;
-        dist[0] = po.x - (float)j, dist[1] = po.y - (float)j, dist[2] = po.z - (float)j, dist[3] = po.w - (float)j;
+        dist[0] = po.x - (float)li, dist[1] = po.y - (float)li, dist[2] = po.z - (float)li, dist[3] = po.w - (float)li;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
