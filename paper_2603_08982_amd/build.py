@@ -10,7 +10,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libsvgear.so")
 SOURCES = ["api.hip", "permute.hip", "kmeans.hip", "kmeans_small.hip", "probe.hip", "route.hip", "attention.hip", "attention_bf16.hip",
            "attention_f32.hip", "rotary.hip", "linear.hip", "linear_bf16.hip", "linear_f32.hip", "linear_rows.hip", "layer_norm.hip",
-           "dense_attention.hip", "dense_again.hip", "dense_bf16.hip", "dense_f32.hip", "dense_backward_bf16.hip", "dense_backward_f32.hip"]
+           "dense_attention.hip", "dense_again.hip", "dense_bf16.hip", "dense_f32.hip", "dense_backward_bf16.hip",
+           "dense_backward_far_cap.hip", "dense_backward_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -74,10 +74,10 @@ __device__ __forceinline__ bool unbounded_rows(const T* rows, int64_t rn, int lo
 }
 
 // A query's output over its keys [0, hi); j_hi: the most that one of the wave has.
-template <typename T, int D, bool CAP, bool SLOPES>
+template <typename T, int D, int CAP, bool SLOPES>
 __device__ __forceinline__ void again_forward(const T* q, const T* k, int64_t kn, const T* v, int64_t vn, int j_hi, int hi, int pos,
                                               float slope, const DenseArgs& a, T* o, float* lse, bool live) {
-  const Scores<T, CAP, SLOPES> scores(a);
+  const Scores<float, CAP, SLOPES> scores(a);  // (fp32's, which is right for all caps)
   const int at = (threadIdx.x & 32) ? D / 2 : 0;
   Half<D> acc;
   acc.set(0.f);
@@ -100,10 +100,10 @@ __device__ __forceinline__ void again_forward(const T* q, const T* k, int64_t kn
 }
 
 // A query's gradient.
-template <typename T, int D, bool CAP, bool SLOPES>
+template <typename T, int D, int CAP, bool SLOPES>
 __device__ __forceinline__ void again_dq(const T* q, const T* dy, const T* k, int64_t kn, const T* v, int64_t vn, int j_hi, int hi,
                                          int pos, float slope, float lse2, float delta, const DenseArgs& a, T* o, bool live) {
-  const Scores<T, CAP, SLOPES> scores(a);
+  const Scores<float, CAP, SLOPES> scores(a);  // (fp32's, which is right for all caps)
   const int at = (threadIdx.x & 32) ? D / 2 : 0;
   Half<D> acc;
   acc.set(0.f);
@@ -121,11 +121,11 @@ __device__ __forceinline__ void again_dq(const T* q, const T* dy, const T* k, in
 }
 
 // A key's gradient (DK), or a value's, over the rows [r_lo, r_hi) from `from` on: token r / G of head r % G.
-template <typename T, int D, bool CAP, bool SLOPES, bool DK>
+template <typename T, int D, int CAP, bool SLOPES, bool DK>
 __device__ __forceinline__ void again_dkv(const T* k, const T* v, const T* q, int64_t qh, int64_t qn, const T* dy, int64_t yh, int64_t yn,
                                           const float* lse, const float* delta, const float* slopes, int r_lo, int r_hi, int from, int ahead,
                                           const DenseArgs& a, T* o, bool live) {
-  const Scores<T, CAP, SLOPES> scores(a);
+  const Scores<float, CAP, SLOPES> scores(a);  // (fp32's, which is right for all caps)
   const int at = (threadIdx.x & 32) ? D / 2 : 0;
   Half<D> acc;
   acc.set(0.f);
@@ -148,7 +148,7 @@ __device__ __forceinline__ void again_dkv(const T* k, const T* v, const T* q, in
 
 // The rows of the workgroups' waves that have left a mark in a part of theirs. WHAT as of the kernel that left it, on the same grid.
 // SOLO: a workgroup's waves share 32 rows (fp32).
-template <typename T, int D, bool CAP, bool SLOPES, int WHAT>
+template <typename T, int D, int CAP, bool SLOPES, int WHAT>
 __global__ void __launch_bounds__(64 * kDenseWaves)
 dense_again_kernel(DenseArgs a) {
   constexpr bool SOLO = sizeof(T) == 4;

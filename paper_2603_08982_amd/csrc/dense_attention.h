@@ -58,6 +58,7 @@ enum { kDenseForward = 0, kDenseDq = 1, kDenseDkv = 2 };
 int launch_dense_bf16(const DenseArgs& a, int d, hipStream_t s);
 int launch_dense_f32(const DenseArgs& a, int d, hipStream_t s);
 int launch_dense_backward_bf16(const DenseArgs& a, int d, int what, hipStream_t s);
+int launch_dense_backward_far_cap(const DenseArgs& a, int d, int what, hipStream_t s);  // (bf16, with caps over kFarCap)
 int launch_dense_backward_f32(const DenseArgs& a, int d, int what, hipStream_t s);
 // The rows that a causal launch of `what` has marked, once their parts are joined.
 int launch_dense_again(const DenseArgs& a, svgear_dtype dt, int d, int what, hipStream_t s);

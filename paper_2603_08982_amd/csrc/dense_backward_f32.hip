@@ -5,7 +5,7 @@ namespace svgear {
 namespace {
 
 // ---- the queries' gradients: 32 queries a workgroup, a pass over the keys
-template <int D, bool CAP, bool SLOPES>
+template <int D, int CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, D == 64 ? 2 : 1)
 dense_dq_f32_kernel(DenseArgs a) {
   using Z = Tile<float, D>;
@@ -97,7 +97,7 @@ dense_dq_f32_kernel(DenseArgs a) {
 }
 
 // ---- the keys' and values' gradients: 32 keys a workgroup, a pass over the queries of all heads that share them
-template <int D, bool CAP, bool SLOPES>
+template <int D, int CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, D == 64 ? 2 : 1)
 dense_dkv_f32_kernel(DenseArgs a) {
   using Z = Tile<float, D>;
@@ -240,7 +240,8 @@ dense_dkv_f32_kernel(DenseArgs a) {
 template <int D>
 int launch(const DenseArgs& a, int what, hipStream_t s) {
   return by_scores(a, [&](auto cap, auto slopes) -> int {
-    constexpr bool C = decltype(cap)::value, S = decltype(slopes)::value;
+    constexpr int C = decltype(cap)::value;
+    constexpr bool S = decltype(slopes)::value;
     if (what == kDenseDq) dense_dq_f32_kernel<D, C, S><<<dense_grid(a), 64 * kDenseWaves, 0, s>>>(a);
     else dense_dkv_f32_kernel<D, C, S><<<dense_grid(a), 64 * kDenseWaves, 0, s>>>(a);
     SVGEAR_LAUNCH_CHECK();

@@ -31,7 +31,7 @@ __device__ __forceinline__ void store_whole(bf16_t* o, const f32x16 (&acc)[DB], 
     }
 }
 
-template <int D, bool CAP, bool SLOPES>
+template <int D, int CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, 2)
 dense_forward_bf16_kernel(DenseArgs a) {
   using Z = Tile<bf16_t, D>;
@@ -317,7 +317,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
 
 template <int D>
 int launch(const DenseArgs& a, hipStream_t s) {
-  return by_scores(a, [&](auto cap, auto slopes) -> int {
+  return by_scores<true>(a, [&](auto cap, auto slopes) -> int {
     dense_forward_bf16_kernel<D, decltype(cap)::value, decltype(slopes)::value><<<dense_grid(a), 64 * kDenseWaves, 0, s>>>(a);
     SVGEAR_LAUNCH_CHECK();
     return SVGEAR_OK;

@@ -4,7 +4,7 @@
 namespace svgear {
 namespace {
 
-template <int D, bool CAP, bool SLOPES>
+template <int D, int CAP, bool SLOPES>
 __global__ void __launch_bounds__(64 * kDenseWaves, D == 64 ? 2 : 1)
 dense_forward_f32_kernel(DenseArgs a) {
   using Z = Tile<float, D>;

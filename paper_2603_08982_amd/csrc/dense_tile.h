@@ -283,12 +283,12 @@ __device__ __forceinline__ bool dense_index(const DenseArgs& a, int& bh, int& sl
   return true;
 }
 
-// tanh from the hardware's exponential and reciprocal. For bf16 1 - 2 / (e^2x + 1), off by some 2^-23 of 1, which moves a score of
-// cap 50 by 1e-5 beside the 2^-9 that its weight's rounding is off by. For fp32 (1 - e) / (1 + e) with e = e^-2|x|, and below 0.3,
-// where 1 - e would lose digits, the series, whose next term is 3e-9 of the result there.
-template <typename T>
+// tanh from the hardware's exponential and reciprocal. NEAR: 1 - 2 / (e^2x + 1), off by up to 2.7e-7 of 1 (half steps of the sum and
+// of its exponential, a step of each), however small x is. Otherwise (1 - e) / (1 + e) with e = e^-2|x|, and below 0.3, where 1 - e would lose
+// digits, the series, whose next term is 3e-9 of the result there: off by some 10 half steps of the result.
+template <bool NEAR>
 __device__ __forceinline__ float tanh_of(float x) {
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (NEAR) {
     return 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f);
   } else {
     const float a = fabsf(x), e = __builtin_amdgcn_exp2f(a * (-2.f * kLog2e)), z = x * x;
@@ -302,13 +302,20 @@ __device__ __forceinline__ float tanh_of(float x) {
   }
 }
 
+// What a call's cap is. With a cap a score is off by what its tanh is off by, times the cap: in bf16 the short form is good for caps up to
+// 256, which it moves by 7e-5 at most, beside the 2^-9 that a weight's rounding is off by. (At 1e6 that would be 0.3.) The long form
+// is some ten operations more a pair: gradients of 4,000 causal tokens of 40 heads, 8 key heads of 128, 1,180 us with a cap of 50 or 256, 1,535 with
+// one of 1,000; the forward pass, whose whole tiles take a series with both, 204 and 207.
+enum { kCapNone = 0, kCapNear = 1, kCapFar = 2 };
+constexpr float kFarCap = 256.f;
+
 // Products to exponents of 2, of a query at `dist` from the key. The cap's derivative is 1 - tanh^2.
-template <typename T, bool CAP, bool SLOPES>
+template <typename T, int CAP, bool SLOPES>
 struct Scores {
   float c, cap2;
   __device__ __forceinline__ Scores(const DenseArgs& a) : c(CAP ? a.scale / a.cap : a.scale * kLog2e), cap2(a.cap * kLog2e) {}
   // tanh (or the product itself)
-  __device__ __forceinline__ float inner(float s) const { return CAP ? tanh_of<T>(s * c) : s; }
+  __device__ __forceinline__ float inner(float s) const { return CAP ? tanh_of<sizeof(T) == 2 && CAP == kCapNear>(s * c) : s; }
   // exponent less `less`
   __device__ __forceinline__ float outer(float in, float dist, float slope, float less) const {
     if (SLOPES) less = __builtin_fmaf(slope, fabsf(dist), less);
@@ -322,11 +329,13 @@ __device__ __forceinline__ int32_t* mark_of(const DenseArgs& a, int part, int bh
   return a.marks + (((int64_t)part * (a.B * a.Hk) + bh) * a.slots + slot) * kDenseWaves + wave;
 }
 
-// f(cap, slopes) as types, for what a call has
-template <typename F>
+// f(cap, slopes) as types, for what a call has; FAR: caps over kFarCap by themselves
+template <bool FAR = false, typename F>
 int by_scores(const DenseArgs& a, F f) {
-  if (a.cap > 0.f) return a.slopes ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
-  return a.slopes ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
+  auto with = [&](auto cap) -> int { return a.slopes ? f(cap, std::true_type{}) : f(cap, std::false_type{}); };
+  if constexpr (FAR)
+    if (a.cap > kFarCap) return with(std::integral_constant<int, kCapFar>{});
+  return a.cap > 0.f ? with(std::integral_constant<int, kCapNear>{}) : with(std::integral_constant<int, kCapNone>{});
 }
 // Workgroups of a launch: those of dense_index.
 inline dim3 dense_grid(const DenseArgs& a) { return long_grid(ceil_div((int64_t)a.B * a.Hk * a.slots, 8) * 8 * a.splits, 1); }

@@ -40,3 +40,54 @@ def test_distances_over_many_parts(Nq, Nk, dtype, d):
     q, k, v, dy = make(42, dtype, 1, 6, 3, Nq, Nk, d)
     for kw in ({}, {"causal": True, "cap": 20.0}):
         check(q, k, v, dy, (Nq, Nk, kw), slopes=slopes_of(6), **kw)
+
+
+def relative_scores(monkeypatch):
+    """scores64 with a bound that is relative to the score, for any cap. In half steps (U32): the series for small scores is the best fit of its
+    degree to 10 (bf16) or below 1 (fp32), its coefficients' factors 4, its sums 4; the exponential and reciprocal some 10, see
+    the factors below; the cap's product and the sum 2."""
+    import dense_helpers
+
+    plain = dense_helpers.scores64
+
+    def scores(q, k, scale, cap, slopes, **mask):
+        s, e, keeps, seen = plain(q, k, scale, None, slopes, **mask)
+        if cap:
+            full, _, keeps, _ = plain(q, k, scale, cap, slopes, **mask)
+            raw = plain(q, k, scale, cap, None, **mask)[0]
+            # what the product is off by counts by the slope, which is 1 at most
+            e = e + torch.where(seen, 24 * dense_helpers.U32 * raw.abs(), 0.0)
+            if q.dtype == BF and cap <= 256:
+                e = e + torch.where(seen, 16 * dense_helpers.U32 * cap, 0.0)
+            s = full
+        return s, e, keeps, seen
+
+    monkeypatch.setattr(dense_helpers, "scores64", scores)
+
+
+# (cap, scale or none: with one of 8 scores are of the size of a cap of some hundreds)
+CAPS = [(256.0, None), (256.0, 8.0), (257.0, 8.0), (1000.0, 8.0), (1e3, None), (3e4, None), (1e6, None), (1e6, -0.125), (1e9, None)]
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64), (F, 128)])
+@pytest.mark.parametrize("kw", [{}, {"causal": True}, {"slopes": True}, {"slopes": True, "causal": True}], ids=str)
+@pytest.mark.parametrize("cap,scale", CAPS)
+def test_large_caps(monkeypatch, cap, scale, kw, dtype, d):
+    """Far from its cap a score is what it was, whatever the cap; 203 keys are no whole tiles."""
+    relative_scores(monkeypatch)
+    q, k, v, dy = make(43, dtype, 1, 4, 2, 140, 203, d, spread=2.0)
+    kw = dict(kw, slopes=slopes_of(4)) if "slopes" in kw else kw
+    check(q, k, v, dy, (cap, scale, kw), cap=cap, scale=scale, **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_a_cap_out_of_reach_is_none(dtype):
+    """Scores of some units under a cap of 2^40 are those without one, to their last digits, in both passes."""
+    q, k, v, dy = make(44, dtype, 2, 4, 4, 130, 333, 64)
+    plain, far = check(q, k, v, dy, "without"), sv.attention(q, k, v, want_lse=True, cap=2.0 ** 40)
+    # bf16: weights and results of both are rounded once, 4 times 2^-8; fp32: 24 half steps of scores up to 8
+    tol = 2.0 ** -6 if dtype == BF else 24 * 2.0 ** -24 * 8
+    assert (far[0].double() - plain[0].double()).norm() <= tol * plain[0].double().norm()
+    got = sv.attention_backward(dy, q, k, v, *far, cap=2.0 ** 40)
+    for n in got:
+        assert (got[n].double() - plain[2][n].double()).norm() <= 2 * tol * plain[2][n].double().norm(), n

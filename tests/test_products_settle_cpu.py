@@ -60,3 +60,18 @@ def test_no_result_is_read_early(tmp_path):
         lines = body.split("\n")
         assert sum("v_mfma" in line for line in lines) >= 48, name
         assert not early(lines), (name, early(lines)[:3])
+
+
+def test_no_result_is_read_early_with_far_caps(tmp_path):
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("needs the compiler")
+    out = tmp_path / "listing.s"
+    flags = [f for f in build.FLAGS if f != "-fPIC"]
+    subprocess.run([build.HIPCC, *flags, "-S", "--cuda-device-only", os.path.join(build.CSRC, "dense_backward_far_cap.hip"), "-o", str(out)],
+                   check=True, capture_output=True)
+    kernels = re.findall(r"^(_ZN\S*dense_d(?:q|kv)_kernel\S*):.*?\n(.*?)^\s*\.section", out.read_text(), re.M | re.S)
+    assert len(kernels) == 8
+    for name, body in kernels:
+        lines = body.split("\n")
+        assert sum("v_mfma" in line for line in lines) >= 48, name
+        assert not early(lines), (name, early(lines)[:3])
