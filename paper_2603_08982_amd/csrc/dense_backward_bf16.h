@@ -300,13 +300,16 @@ dense_dkv_kernel(DenseArgs a) {
     const T* y = static_cast<const T*>(uniform_ptr(yp + token0 * a.yst.n));
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
+      // rows behind the document's last one: q's are that row's once more, whose products are masked, those of dy are 0
+      const bool there = t * BN + i * kStep + copy_row < end;
       const int row = min(t * BN + i * kStep + copy_row, end - 1), token = row / a.by_g, h = row - token * a.G, ahead = token - token0;
+      if (!there) clear_16B(y_to + i * kWaves * 1024 + lane * 16);
       if (near) {
         async_copy_16B(q, (__umul24(h, (uint32_t)a.qst.h) + __umul24(ahead, (uint32_t)a.qst.n)) * 2u + chunk(i), q_to + i * kWaves * 1024);
-        async_copy_16B(y, (__umul24(h, (uint32_t)a.yst.h) + __umul24(ahead, (uint32_t)a.yst.n)) * 2u + chunk(i), y_to + i * kWaves * 1024);
+        if (there) async_copy_16B(y, (__umul24(h, (uint32_t)a.yst.h) + __umul24(ahead, (uint32_t)a.yst.n)) * 2u + chunk(i), y_to + i * kWaves * 1024);
       } else {
         async_copy_16B(q + h * a.qst.h + ahead * a.qst.n + chunk(i) / 2, q_to + i * kWaves * 1024);
-        async_copy_16B(y + h * a.yst.h + ahead * a.yst.n + chunk(i) / 2, y_to + i * kWaves * 1024);
+        if (there) async_copy_16B(y + h * a.yst.h + ahead * a.yst.n + chunk(i) / 2, y_to + i * kWaves * 1024);
       }
     }
   };

@@ -179,6 +179,7 @@ dense_dkv_f32_kernel(DenseArgs a) {
     clear(dp);
     SVGEAR_WAIT_VMCNT(S::kCopies + kStats);  // dy has landed, which was issued first
     asm volatile("" ::: "memory");
+    if ((t + 1) * BN > end) clear_solo<D>(lds + Z::kBytes, end - t * BN, again(lane));
     z.rows_times(yt, v, dp);
     SVGEAR_WAIT_VMCNT(0);
     asm volatile("" ::: "memory");

@@ -62,12 +62,12 @@ dense_forward_bf16_kernel(DenseArgs a) {
   const bf16_t* kp = static_cast<const bf16_t*>(a.k) + b * a.kst.b + hk * a.kst.h + doc.k0 * a.kst.n;
   const bf16_t* vp = static_cast<const bf16_t*>(a.v) + b * a.vst.b + hk * a.vst.h + doc.k0 * a.vst.n;
   // Rows of a whole tile lie at one offset of the lane from addresses that the wave shares; in the last tile, rows behind the last key
-  // that a query here sees are not read.
+  // that a query here sees are not read: K's are that key's once more, whose scores are masked, V's are 0.
   const int copy_row = wave * Z::kRowsPerCopy + lane / Z::kChunks, copy_chunk = ((lane % Z::kChunks) ^ Z::swz(copy_row)) * 16;
   constexpr int kStep = kDenseWaves * Z::kRowsPerCopy;
   static_assert(kStep % 16 == 0, "all copies of a lane have one chunk");
   const uint32_t k_lane = (uint32_t)copy_row * (uint32_t)a.kst.n * 2u + copy_chunk, v_lane = (uint32_t)copy_row * (uint32_t)a.vst.n * 2u + copy_chunk;
-  auto issue = [&](int t, const bf16_t* base, int64_t st, uint32_t at_lane, int buffer) __attribute__((always_inline)) {
+  auto issue = [&](int t, const bf16_t* base, int64_t st, uint32_t at_lane, int buffer, bool values) __attribute__((always_inline)) {
     const bf16_t* rows = static_cast<const bf16_t*>(uniform_ptr(base + (int64_t)t * BN * st));
     const uint32_t to = (uint32_t)uniform((int)(lds + buffer * Z::kBytes + wave * 1024));
     const int last = hi_wg - 1 - t * BN;
@@ -77,12 +77,14 @@ dense_forward_bf16_kernel(DenseArgs a) {
     } else {
       const int l = again(lane), mine = wave * Z::kRowsPerCopy + l / Z::kChunks, chunk = ((l % Z::kChunks) ^ Z::swz(mine)) * 16;
 #pragma unroll
-      for (int i = 0; i < Z::kCopies; ++i)
-        async_copy_16B(rows, (uint32_t)min(i * kStep + mine, last) * (uint32_t)st * 2u + chunk, to + i * kDenseWaves * 1024);
+      for (int i = 0; i < Z::kCopies; ++i) {
+        if (values && i * kStep + mine > last) clear_16B(to + i * kDenseWaves * 1024 + l * 16);
+        else async_copy_16B(rows, (uint32_t)min(i * kStep + mine, last) * (uint32_t)st * 2u + chunk, to + i * kDenseWaves * 1024);
+      }
     }
   };
-  auto issue_k = [&](int t) __attribute__((always_inline)) { issue(t, kp, a.kst.n, k_lane, (t - t_lo) & 1); };
-  auto issue_v = [&](int t) __attribute__((always_inline)) { issue(t, vp, a.vst.n, v_lane, 2 + ((t - t_lo) & 1)); };
+  auto issue_k = [&](int t) __attribute__((always_inline)) { issue(t, kp, a.kst.n, k_lane, (t - t_lo) & 1, false); };
+  auto issue_v = [&](int t) __attribute__((always_inline)) { issue(t, vp, a.vst.n, v_lane, 2 + ((t - t_lo) & 1), true); };
 
   // the first tiles are on their way while the queries are fetched
   if (t_lo < t_hi) {
@@ -257,8 +259,8 @@ dense_forward_bf16_kernel(DenseArgs a) {
     SVGEAR_WAIT_VMCNT(0);
     __syncthreads();
     auto step = [&](int t, int parity, f32x16 (&s_now)[2], f32x16 (&s_next)[2], auto whole_tag) __attribute__((always_inline)) {
-      if (t + 2 < t_hi) issue(t + 2, kp, a.kst.n, k_lane, parity);
-      issue(t + 1, vp, a.vst.n, v_lane, 2 + (parity ^ 1));
+      if (t + 2 < t_hi) issue(t + 2, kp, a.kst.n, k_lane, parity, false);
+      issue(t + 1, vp, a.vst.n, v_lane, 2 + (parity ^ 1), true);
       if (SERIES && raw) scores(parity ^ 1, s_next, s_now, std::true_type{}, std::integral_constant<bool, SERIES>{});
       else scores(parity ^ 1, s_next, s_now, std::true_type{}, std::false_type{});
       const float next = values(parity, s_next, std::true_type{});

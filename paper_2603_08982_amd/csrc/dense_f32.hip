@@ -94,6 +94,7 @@ dense_forward_f32_kernel(DenseArgs a) {
     if (more) SVGEAR_WAIT_VMCNT(S::kCopies);  // V has landed; the next K may be on its way
     else SVGEAR_WAIT_VMCNT(0);
     asm volatile("" ::: "memory");
+    if ((t + 1) * BN > hi_any) clear_solo<D>(lds + Z::kBytes, hi_any - t * BN, again(lane));
     z.transposed_times(vt, x, acc, lane);
     if (more) issue(vp, a.vst.n, t + kDenseWaves, lds + Z::kBytes);
   }

@@ -49,6 +49,13 @@ __device__ __forceinline__ void copy_solo(const float* base, int64_t step, uint3
   }
 }
 
+// Rows [from, 32) of a wave's tile, whose copies have landed, are 0.
+template <int D>
+__device__ __forceinline__ void clear_solo(uint32_t lds, int from, int lane) {
+  constexpr int C = Tile<float, D>::kChunks;
+  for (int e = from * C + lane; e < Solo<D>::kRows * C; e += 64) clear_16B(lds + e * 16);
+}
+
 // The waves' sums of 32 rows, added in their order by all threads: out(row, first of four columns, their sum), each wave's times
 // weight(wave, row).
 template <int D, typename Weight, typename Put>

@@ -49,6 +49,14 @@ __device__ __forceinline__ const void* uniform_ptr(const void* p) {
   return reinterpret_cast<const void*>(((uint64_t)hi << 32) | lo);
 }
 
+// 16 bytes of zeros in LDS: rows behind the last one of a tile that is multiplied by weights of 0, which an infinity there would not survive
+__device__ __forceinline__ void clear_16B(uint32_t lds) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  uint32_t zero;
+  asm volatile("v_mov_b32 %0, 0" : "=v"(zero));  // (the compiler would keep four registers of them through the loop)
+  *(__attribute__((address_space(3))) u32x4*)(uintptr_t)lds = u32x4{zero, zero, zero, zero};
+}
+
 __device__ __forceinline__ void clear(f32x16& v) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) v[r] = 0.f;

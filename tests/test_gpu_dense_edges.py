@@ -91,3 +91,46 @@ def test_a_cap_out_of_reach_is_none(dtype):
     got = sv.attention_backward(dy, q, k, v, *far, cap=2.0 ** 40)
     for n in got:
         assert (got[n].double() - plain[2][n].double()).norm() <= 2 * tol * plain[2][n].double().norm(), n
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64), (F, 128)])
+@pytest.mark.parametrize("kw", [{}, {"causal": True}, {"slopes": True, "cap": 300.0}, {"docs": True}], ids=str)
+@pytest.mark.parametrize("Nq,Nk", [(64, 64), (70, 70), (33, 97), (1, 1), (5, 2003), (700, 65), (130, 191), (1, 999)])
+def test_an_infinity_in_the_last_row(Nq, Nk, kw, dtype, d):
+    """What the last key's value has, and in the gradients the last query's dy, comes out as the formula says, whether or not the rows are
+    whole tiles: an infinity in a column is one of the rows that see it, and touches no other column."""
+    q, k, v, dy = make(45, dtype, 2, 4, 2, Nq, Nk, d, spread=0.5)
+    kw = dict(kw)
+    if "slopes" in kw:  # (so flat that no weight vanishes)
+        kw["slopes"] = torch.full((4,), 1e-3, device="cuda")
+    if kw.pop("docs", False):  # a document in front, a document of the rest, one row of padding
+        if Nq < 4:
+            return
+        kw.update(q_offsets=torch.tensor([0, 2, Nq - 1], dtype=torch.int32, device="cuda"),
+                  k_offsets=torch.tensor([0, 3, Nk - 1], dtype=torch.int32, device="cuda"))
+    last_q, last_k = (int(kw[n][-1]) if n in kw else e for n, e in (("q_offsets", Nq), ("k_offsets", Nk)))
+    what = (Nq, Nk, list(kw), dtype, d)
+    plain = [t.clone() for t in (v, dy)]
+    v[:, :, last_k - 1, 3], v[:, :, last_k - 1, d - 1] = float("inf"), -float("inf")
+    o, lse = sv.attention(q, k, v, want_lse=True, **kw)
+    want, e, want_lse, el = attention64(q, k, plain[0], **kw)
+    close(lse, want_lse, el, ("lse", what))
+    mid = torch.arange(d, device="cuda")
+    mid = mid[(mid != 3) & (mid != d - 1)]
+    close(o[..., mid], want[..., mid], e[..., mid], ("o", what))
+    first = 2 if "q_offsets" in kw else 0
+    sees = torch.arange(Nq, device="cuda") >= (last_q - 1 if kw.get("causal") else first)
+    sees &= torch.arange(Nq, device="cuda") < last_q
+    assert (o[:, :, sees, 3] == torch.inf).all() and (o[:, :, sees, d - 1] == -torch.inf).all(), what
+    close(o[:, :, ~sees], want[:, :, ~sees], e[:, :, ~sees], ("o of others", what))
+
+    o, lse = sv.attention(q, k, plain[0], want_lse=True, **kw)
+    dy[:, :, last_q - 1, 3] = float("inf")
+    got = sv.attention_backward(dy, q, k, plain[0], o, lse, **kw)["dv"]
+    want, e = attention_backward64(plain[1], q, k, plain[0], o, lse, **kw)["dv"]
+    others = torch.arange(d, device="cuda") != 3
+    close(got[..., others], want[..., others], e[..., others], ("dv", what))
+    seen = torch.arange(Nk, device="cuda") >= (3 if "k_offsets" in kw else 0)
+    seen &= torch.arange(Nk, device="cuda") < last_k
+    assert (got[:, :, seen, 3] == torch.inf).all(), what
+    close(got[:, :, ~seen], want[:, :, ~seen], e[:, :, ~seen], ("dv of others", what))
