@@ -300,18 +300,24 @@ dense_dkv_kernel(DenseArgs a) {
     const T* y = static_cast<const T*>(uniform_ptr(yp + token0 * a.yst.n));
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-      // rows behind the document's last one: q's are that row's once more, whose products are masked, those of dy are 0
-      const bool there = t * BN + i * kStep + copy_row < end;
       const int row = min(t * BN + i * kStep + copy_row, end - 1), token = row / a.by_g, h = row - token * a.G, ahead = token - token0;
-      if (!there) clear_16B(y_to + i * kWaves * 1024 + lane * 16);
       if (near) {
         async_copy_16B(q, (__umul24(h, (uint32_t)a.qst.h) + __umul24(ahead, (uint32_t)a.qst.n)) * 2u + chunk(i), q_to + i * kWaves * 1024);
-        if (there) async_copy_16B(y, (__umul24(h, (uint32_t)a.yst.h) + __umul24(ahead, (uint32_t)a.yst.n)) * 2u + chunk(i), y_to + i * kWaves * 1024);
+        async_copy_16B(y, (__umul24(h, (uint32_t)a.yst.h) + __umul24(ahead, (uint32_t)a.yst.n)) * 2u + chunk(i), y_to + i * kWaves * 1024);
       } else {
         async_copy_16B(q + h * a.qst.h + ahead * a.qst.n + chunk(i) / 2, q_to + i * kWaves * 1024);
-        if (there) async_copy_16B(y + h * a.yst.h + ahead * a.yst.n + chunk(i) / 2, y_to + i * kWaves * 1024);
+        async_copy_16B(y + h * a.yst.h + ahead * a.yst.n + chunk(i) / 2, y_to + i * kWaves * 1024);
       }
     }
+  };
+  // Rows behind the document's last one: q's are that row's once more, whose products are masked, those of dy are cleared by the wave that
+  // has copied them (as they are copied, lane by lane, it cost 4 % where heads share keys).
+  auto clear_rows = [&](int t) __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");  // (behind the wait for the copies)
+    const uint32_t to = (uint32_t)uniform((int)(lds + (2 + (t & 1)) * Z::kBytes + wave * 1024));
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i)
+      if (t * BN + i * kStep + copy_row >= end) clear_16B(to + i * kWaves * 1024 + lane * 16);
   };
   auto issue = [&](int t) __attribute__((always_inline)) {
     issue_rows(t);
@@ -452,6 +458,7 @@ dense_dkv_kernel(DenseArgs a) {
 
   for (int t = t_lo; t < t_hi; ++t) {
     SVGEAR_WAIT_VMCNT(0);
+    if ((t + 1) * BN > end) clear_rows(t);
     __syncthreads();
     if (t + 1 < t_hi) issue(t + 1);
     const bool masked = t * BN < from_all || (t + 1) * BN > end;
