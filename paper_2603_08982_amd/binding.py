@@ -737,19 +737,23 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
-                        scale: Optional[torch.Tensor] = None, eps: float = 1e-6, want: Sequence[str] = ("dx",)):
+                        scale: Optional[torch.Tensor] = None, eps: float = 1e-6, want: Sequence[str] = ("dx",),
+                        shift: Optional[torch.Tensor] = None):
     """svgear_layer_norm_backward: the gradients named in `want` ("dx", "dweight", "dbias", "dscale", "dshift") of layer_norm() for
-    the output's gradient dy. bias is needed for dscale; dscale and dshift have scale's shape and need it. Returns a dict."""
-    dt = _same_place(dy, x, weight, bias, scale)
+    the output's gradient dy. bias is needed for dscale; dscale has scale's shape, and dshift too, or where there was no scale that of
+    `shift`, which is given for it. Returns a dict."""
+    dt = _same_place(dy, x, weight, bias, scale, shift)
     lib = load_library()
     _require(dy.shape == x.shape, "dy: expected x's shape")
-    B, N, c, xst, sst, _, per_token = _norm_arguments(x, weight, bias, scale, None, eps)
+    B, N, c, xst, sst, _, per_token = _norm_arguments(x, weight, bias, scale, shift, eps)
     yst = _as_bnd(dy, "dy")[3]
     _require(len(want) > 0 and set(want) <= {"dx", "dweight", "dbias", "dscale", "dshift"}, "want: dx, dweight, dbias, dscale, dshift")
-    _require(scale is not None or not {"dscale", "dshift"} & set(want), "dscale and dshift need the scale")
-    modulation = 0 if scale is None else 2 if per_token else 1
+    mod = scale if scale is not None else shift
+    _require(scale is not None or "dscale" not in want, "dscale needs the scale")
+    _require(mod is not None or "dshift" not in want, "dshift needs the scale, or the shift")
+    modulation = 0 if mod is None else 2 if per_token else 1
     with _on_device(x.device):
-        r = {n: x.new_empty(x.shape if n == "dx" else c if n in ("dweight", "dbias") else scale.shape) for n in want}
+        r = {n: x.new_empty(x.shape if n == "dx" else c if n in ("dweight", "dbias") else mod.shape) for n in want}
         dx = r.get("dx")
         sums = {"dweight", "dbias"} & set(want) or (modulation == 1 and {"dscale", "dshift"} & set(want))
         ws, *space = _scratch(lib.svgear_layer_norm_backward_workspace(dt, B, N, c, modulation) if sums else 0, x.device)
@@ -1036,8 +1040,8 @@ def cross_attention_block(x: torch.Tensor, context: torch.Tensor, w_q: torch.Ten
 
 def cross_attention_block_backward(dy: torch.Tensor, kept: dict):
     """The gradients of cross_attention_block() for its output's gradient dy, from what it kept: a dict of "x", "context", "w_q", "w_kv",
-    "w_out" and, of the arguments that were given, "b_q", "b_kv", "b_out", "gate", "norm_weight", "norm_bias", "scale", "shift" (which
-    needs a scale). The residual's is dy itself, and "x" is the norm's input's alone: where x is the residual too, the two are added."""
+    "w_out" and, of the arguments that were given, "b_q", "b_kv", "b_out", "gate", "norm_weight", "norm_bias", "scale", "shift". The
+    residual's is dy itself, and "x" is the norm's input's alone: where x is the residual too, the two are added."""
     f = kept
     B, N, H, d = f["o"].shape
     M, Hk = f["context"].shape[1], f["k"].shape[1]
@@ -1052,9 +1056,9 @@ def cross_attention_block_backward(dy: torch.Tensor, kept: dict):
                            k_offsets=f["k_offsets"], out={"dq": dq.transpose(1, 2), "dk": dk, "dv": dv})
         into = linear_backward(dq.view(B, N, H * d), f["h"], f["w_q"], want=["dx", "dw"] + given("b_q", "dbias"))
         text = linear_backward(dkv.view(B, M, 2 * Hk * d), f["context"], f["w_kv"], want=["dx", "dw"] + given("b_kv", "dbias"))
-        modulated = given("scale", "dscale") + (given("shift", "dshift") if f["scale"] is not None else [])
-        norm = layer_norm_backward(into["dx"], f["x"], f["norm_weight"], f["norm_bias"], scale=f["scale"], eps=f["eps"],
-                                   want=["dx"] + given("norm_weight", "dweight") + given("norm_bias", "dbias") + modulated)
+        norm = layer_norm_backward(into["dx"], f["x"], f["norm_weight"], f["norm_bias"], scale=f["scale"], eps=f["eps"], shift=f["shift"],
+                                   want=["dx"] + given("norm_weight", "dweight") + given("norm_bias", "dbias") + given("scale", "dscale")
+                                   + given("shift", "dshift"))
     r = {"x": norm["dx"], "context": text["dx"], "w_q": into["dw"], "w_kv": text["dw"], "w_out": out["dw"]}
     for name, source, gradient in (("b_q", into, "dbias"), ("b_kv", text, "dbias"), ("b_out", out, "dbias"), ("gate", out, "dgate"),
                                    ("norm_weight", norm, "dweight"), ("norm_bias", norm, "dbias"), ("scale", norm, "dscale"),

@@ -183,3 +183,15 @@ def test_layer_norm_refuses(no_library, what):
 def test_attention_refuses(no_library, what):
     with pytest.raises(sv.SvgearError):
         BAD_ATTENTION[what]()
+
+
+def test_the_shift_of_a_gradient(no_library):
+    """dshift takes its shape from the scale or, without one, from the shift; dscale needs the scale."""
+    for kw in ({"shift": t(2, 16)}, {"shift": t(*X)}, {"scale": t(2, 16), "shift": t(2, 16)}):
+        with pytest.raises(Reached):
+            sv.layer_norm_backward(t(*X), t(*X), want=["dshift", "dx"], **kw)
+    for kw in ({"shift": t(3, 16)}, {"shift": t(2, 16, dtype=F)}, {"scale": t(*X), "shift": t(2, 16)}, {"shift": t(2, 32)[:, ::2]}):
+        with pytest.raises(sv.SvgearError):
+            sv.layer_norm_backward(t(*X), t(*X), want=["dshift"], **kw)
+    with pytest.raises(sv.SvgearError, match="dscale"):
+        sv.layer_norm_backward(t(*X), t(*X), want=["dscale"], shift=t(2, 16))

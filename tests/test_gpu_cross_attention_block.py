@@ -110,3 +110,19 @@ def test_refuses(change):
         kw[n] = torch.zeros(*v, dtype=torch.bfloat16, device="cuda") if isinstance(v, tuple) else v.cuda() if isinstance(v, torch.Tensor) else v
     with pytest.raises(sv.SvgearError):
         sv.cross_attention_block(**kw)
+
+
+@pytest.mark.parametrize("without", [["scale"], ["shift"], ["scale", "norm_weight", "norm_bias", "gate"], ["b_q", "b_kv", "b_out"]], ids=str)
+def test_gradients_of_what_is_given(without):
+    """Every argument that is given has its gradient, a shift without a scale too."""
+    a, lengths, dy = make(torch.float32, 5)
+    full = dict(a)
+    for n in without:
+        del a[n]
+        full[n] = torch.ones_like(full[n]) if n in ("norm_weight", "gate") else torch.zeros_like(full[n])
+    y, grads = run(a, lengths, dy)
+    want, leaves = plain64(full, lengths)
+    want.backward(dy.double())
+    assert set(grads) == set(a) - {"residual"}
+    for n, g in grads.items():
+        assert g.shape == a[n].shape and (g.double() - leaves[n].grad).norm() < TOL[torch.float32] * leaves[n].grad.norm(), n

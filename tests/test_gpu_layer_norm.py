@@ -169,3 +169,19 @@ def test_captured():
         assert torch.equal(y, eager)
         for n in names:
             assert torch.equal(r[n], grads[n]), (k, n)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("mod", ["batch", "token"])
+@pytest.mark.parametrize("B,N,c", [(2, 19, 200), (3, 1, 65), (1, 777, 1003)])
+def test_gradient_of_a_shift_alone(B, N, c, mod, dtype):
+    """Without a scale (1 + scale) is 1, and dshift has the shift's shape."""
+    x, w, b, s, h, dy = make(12, dtype, B, N, c, True, mod)
+    ref = norm_backward64(dy, x, w, b, torch.zeros_like(s), EPS)
+    for names in (["dshift"], ["dx", "dweight", "dbias", "dshift"]):
+        got = sv.layer_norm_backward(dy, x, w, b, shift=h, want=names)
+        assert got["dshift"].shape == h.shape
+        for n in names:
+            close(got[n], *ref[n], (n, B, N, c, mod))
+    both, one = (sv.layer_norm_backward(dy, x, w, b, scale=s, want=["dx", "dscale", "dshift"], **kw) for kw in ({"shift": h}, {}))
+    assert all(torch.equal(both[n], one[n]) for n in one)
