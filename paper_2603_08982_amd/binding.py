@@ -1015,9 +1015,9 @@ def cross_attention_block(x: torch.Tensor, context: torch.Tensor, w_q: torch.Ten
     _require(x.dim() == 3 and context.dim() == 3 and context.shape[0] == x.shape[0], "x: expected [B,N,c], context [B,M,c_text]")
     B, N, _ = x.shape
     M = context.shape[1]
-    _require(heads > 0 and w_q.dim() == 2 and w_kv.dim() == 2 and w_q.shape[0] % heads == 0, "w_q: expected [heads*d,c]")
+    _require(heads > 0 and w_q.dim() == 2 and w_kv.dim() == 2 and w_q.shape[0] > 0 and w_q.shape[0] % heads == 0, "w_q: expected [heads*d,c]")
     d = w_q.shape[0] // heads
-    _require(w_kv.shape[0] % (2 * d) == 0 and w_out.dim() == 2 and w_out.shape[1] == heads * d,
+    _require(w_kv.shape[0] > 0 and w_kv.shape[0] % (2 * d) == 0 and w_out.dim() == 2 and w_out.shape[1] == heads * d,
              "w_kv: expected [2*Hk*d,c_text], w_out: [c_out,heads*d]")
     Hk = w_kv.shape[0] // (2 * d)
     _require(lengths is None or (lengths.dtype == torch.int32 and tuple(lengths.shape) == (B,)), "lengths: expected int32 [B]")

@@ -195,3 +195,23 @@ def test_the_shift_of_a_gradient(no_library):
             sv.layer_norm_backward(t(*X), t(*X), want=["dshift"], **kw)
     with pytest.raises(sv.SvgearError, match="dscale"):
         sv.layer_norm_backward(t(*X), t(*X), want=["dscale"], shift=t(2, 16))
+
+
+BLOCK = {"x": (2, 3, 16), "context": (2, 5, 24), "w_q": (128, 16), "w_kv": (256, 24), "w_out": (16, 128), "heads": 2}
+
+
+def block(**change):
+    a = {n: t(*v) if isinstance(v, tuple) else v for n, v in {**BLOCK, **change}.items()}
+    return sv.cross_attention_block(**a)
+
+
+def test_cross_attention_block_reaches_the_library(no_library):
+    with pytest.raises(Reached):
+        block()
+
+
+@pytest.mark.parametrize("change", [{"w_q": (0, 16)}, {"w_kv": (0, 24)}, {"w_q": (129, 16)}, {"w_kv": (200, 24)}, {"w_out": (16, 64)}, {"heads": 0},
+                                    {"heads": -1}, {"x": (3, 16)}, {"context": (1, 5, 24)}, {"w_q": (128,)}, {"w_out": (128,)}], ids=str)
+def test_cross_attention_block_refuses(no_library, change):
+    with pytest.raises(sv.SvgearError):
+        block(**change)
