@@ -7,6 +7,8 @@
 // TFLOP/s with the matrix cores busy 57 % of the cycles at 1.75 GHz, the power limit's clock. Where there are few tiles of keys, what
 // precedes the first products counts as much as they do: 2 x 37,800 queries over texts of at most 512 735 us, of a workgroup's 29,000 cycles 12,500
 // in the loop. (Rows by way of LDS, 256 bytes of a row at a time, change nothing there; nor do workgroups that take several tiles of queries.)
+#include <cfloat>
+
 #include "dense_tile.h"
 
 namespace svgear {
@@ -108,7 +110,7 @@ dense_forward_bf16_kernel(DenseArgs a) {
   scores_of.cap2 = uniform(scores_of.cap2);
   // A cap's tanh between the products: cap2 tanh(z) = z P(z^2) cap2 for |z| <= 0.5, P the best fit of degree 3, off by 6e-7 of it at
   // most; in products s, whose factor c is in the coefficients. A tile with a larger one takes the exponential and the reciprocal,
-  // two more operations at a quarter of the rate (8,704 tokens of 40 heads, 8 key heads, causal, the kernel: 440 us so, 390 by the series).
+  // two more operations at a quarter of the rate, and so does every tile where a factor is so large that a coefficient would be (8,704 tokens of 40 heads, 8 key heads, causal, the kernel: 440 us so, 390 by the series).
   constexpr bool SERIES = CAP && !SLOPES;
   float series[4];
   if (SERIES) {
@@ -125,7 +127,8 @@ dense_forward_bf16_kernel(DenseArgs a) {
     return __builtin_fmaf(s, p, add);
   };
   bool raw = false;  // whether the scores whose maximum is known are still products, for the series
-  const float c0 = scores_of.c;
+  // (infinite where no tile takes the series: no product times it is 0.5 or less; a series' tile has no other use for it)
+  const float c0 = SERIES && !(fabsf(series[3]) <= FLT_MAX) ? INFINITY : scores_of.c;
   f32x16 acc[DB], sA[2], sB[2];
 #pragma unroll
   for (int db = 0; db < DB; ++db) clear(acc[db]);

@@ -134,3 +134,18 @@ def test_an_infinity_in_the_last_row(Nq, Nk, kw, dtype, d):
     seen &= torch.arange(Nk, device="cuda") < last_k
     assert (got[:, :, seen, 3] == torch.inf).all(), what
     close(got[:, :, ~seen], want[:, :, ~seen], e[:, :, ~seen], ("dv of others", what))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64), (F, 128)])
+@pytest.mark.parametrize("cap", [1e37, 1e30, 1e-3, 1e-9, 1e-20, 1e-37])
+def test_caps_at_the_ends_of_fp32(monkeypatch, cap, dtype, d):
+    """Products are whole numbers, so that none is off by more than a small cap, and those of some tiles are all 0."""
+    relative_scores(monkeypatch)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(46)
+    whole = lambda h, n: torch.randint(-2, 3, (2, h, n, d), generator=g, device="cuda").to(dtype)
+    q, k = whole(4, 150), whole(2, 260)
+    q[:, :, 40:80], k[:, :, 64:128] = 0, 0
+    _, _, v, dy = make(46, dtype, 2, 4, 2, 150, 260, d)
+    for kw in ({}, {"causal": True}, {"slopes": torch.full((4,), 0.01, device="cuda")}):
+        check(q, k, v, dy, (cap, list(kw)), cap=cap, scale=0.125, **kw)
