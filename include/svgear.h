@@ -516,6 +516,7 @@ int svgear_layer_norm_backward(const void* dy, const int64_t dystride[2], const 
  *   o [B,H,Nq,d] dt out, ostride;  lse [B,H,Nq] fp32 out dense, or NULL
  * bf16: products and sums in fp32, the weights e^(s - running maximum) rounded to bf16 for the product with v, o rounded once.
  * fp32: everything in fp32. Results do not depend on the stream, on other calls or on where tensors lie.
+ * scale, scale log2(e), cap log2(e) and scale / cap within the normal numbers of fp32 (scale may be 0).
  * d = 64 or 128; Hk divides H; tensors 16-byte aligned, strides multiples of 16 bytes from 0 to 2^48 (stride_n of k and v: to
  * 2^24; that of a dimension of one element does not matter), those of o such that no two rows meet; no output at the address of
  * another tensor of the call. Nq H / Hk, Nk, B H <= 2^30; n_docs <= 2^20. Where the tiles of queries (128 rows in bf16, 32 in fp32)

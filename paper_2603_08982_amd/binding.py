@@ -795,7 +795,7 @@ def _attention_arguments(q, k, v, scale, cap, slopes, causal, prefix, q_offsets,
         flags |= ATTENTION_SHARED_DOCUMENTS
     _require(causal or prefix is None, "a prefix needs causal=True")
     cap = 0.0 if cap is None else float(cap)
-    _require(0.0 <= cap < float("inf"), "cap: a number above 0, or None")
+    _require(cap == 0.0 or 2.0 ** -126 <= cap < float("inf"), "cap: a number above 0 that fp32 has, or None")
     scale = float(d) ** -0.5 if scale is None else float(scale)
     _require(abs(scale) < float("inf"), "scale: a finite number")
     if causal:

@@ -3,6 +3,7 @@
 #include "dense_attention.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "linear.h"
@@ -177,12 +178,20 @@ Strides strides_of(const int64_t st[3], const Sizes& z, int64_t H, int64_t N) {
   return Strides{z.B > 1 ? st[0] : 0, H > 1 ? st[1] : 0, N > 1 ? st[2] : 0};
 }
 
+// Factors of the scores that fp32 has: those of the exponents, log2(e) scale, or log2(e) cap and scale / cap.
+bool factors_ok(float scale, float cap) {
+  if (!std::isfinite(scale) || !std::isfinite(cap) || cap < 0.f) return false;
+  const float s = std::fabs(scale), log2e = 1.4426950408889634f;
+  if (cap == 0.f) return std::isfinite(s * log2e);
+  return std::isfinite(cap * log2e) && std::isfinite(s * log2e) && std::isfinite(s / cap) && (s == 0.f || s / cap >= FLT_MIN);
+}
+
 // The arguments that both passes share.
 int fill(DenseArgs& a, const Sizes& z, const void* q, const int64_t qst[3], const void* k, const int64_t kst[3], const void* v,
          const int64_t vst[3], float scale, float cap, const float* slopes, unsigned flags, const int32_t* q_offsets,
          const int32_t* k_offsets, const int32_t* prefix) {
   if (!sizes_ok(z) || !tensor_ok(q, qst, z, z.H, z.Nq) || !tensor_ok(k, kst, z, z.Hk, z.Nk) || !tensor_ok(v, vst, z, z.Hk, z.Nk) ||
-      !std::isfinite(scale) || !std::isfinite(cap) || cap < 0.f ||
+      !factors_ok(scale, cap) ||
       (flags & ~(SVGEAR_ATTENTION_CAUSAL | SVGEAR_ATTENTION_SHARED_DOCUMENTS)) ||
       (prefix && !(flags & SVGEAR_ATTENTION_CAUSAL)) || reinterpret_cast<uintptr_t>(slopes) % 4 ||
       reinterpret_cast<uintptr_t>(q_offsets) % 4 || reinterpret_cast<uintptr_t>(k_offsets) % 4 || reinterpret_cast<uintptr_t>(prefix) % 4)

@@ -215,3 +215,26 @@ def test_cross_attention_block_reaches_the_library(no_library):
 def test_cross_attention_block_refuses(no_library, change):
     with pytest.raises(sv.SvgearError):
         block(**change)
+
+
+@pytest.mark.parametrize("kw", [{"cap": 1e-46}, {"cap": 1e-40}, {"cap": float("inf")}, {"cap": float("nan")}, {"cap": -0.5}], ids=str)
+def test_caps_that_fp32_has_not(no_library, kw):
+    with pytest.raises(sv.SvgearError):
+        at(**kw)
+    with pytest.raises(sv.SvgearError):
+        back(**kw)
+
+
+@pytest.mark.parametrize("scale,cap", [(3e38, 0.0), (-3e38, 0.0), (0.125, 3e38), (1e10, 1e-37), (-1e10, 1e-37), (1e-8, 1e37), (1e-45, 1.0), (3e38, 1e38)])
+def test_factors_that_fp32_has_not(scale, cap):
+    """scale log2(e), cap log2(e) and scale / cap have to be numbers of fp32: refused by the library, in front of all that touches a device."""
+    import ctypes
+
+    lib = sv.load_library()
+    stride = lambda *n: (ctypes.c_int64 * 3)(*n)
+    q, k, sizes = stride(25600, 6400, 64), stride(6400, 3200, 64), (1, 2, 4, 2, 100, 50, 64)
+    p = [0x10000 * (i + 1) for i in range(12)]
+    mask = (scale, cap, None, 0, 0, None, None, None)
+    assert lib.svgear_attention(p[0], q, p[1], k, p[2], k, *sizes, *mask, p[3], q, None, p[4], 1 << 40, None) == -1
+    assert lib.svgear_attention_backward(p[0], q, p[1], q, p[2], k, p[3], k, p[4], q, p[5], *sizes, *mask, p[6], q, p[7], k, p[8], k, p[9], 1 << 40,
+                                         None) == -1
