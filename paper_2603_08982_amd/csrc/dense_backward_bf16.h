@@ -279,7 +279,7 @@ dense_dkv_kernel(DenseArgs a) {
   // same one in every whole tile, if a key head has one query head.
   constexpr int kCopies = BN / Z::kRowsPerCopy / kWaves, kStep = kWaves * Z::kRowsPerCopy;
   const int copy_row = wave * Z::kRowsPerCopy + lane / Z::kChunks;
-  auto is_near = [&](const Strides& st) { return st.n < (1 << 24) && (a.G == 1 || (st.h < (1 << 24) && a.G * st.h <= (1 << 29))); };
+  auto is_near = [&](const Strides& st) { return st.n < (1 << 24) && (a.G == 1 || (a.G <= (1 << 24) && st.h < (1 << 24) && a.G * st.h <= (1 << 29))); };
   const bool near = is_near(a.qst) && is_near(a.yst);
   auto issue_rows = [&](int t) __attribute__((always_inline)) {
     const uint32_t q_to = (uint32_t)uniform((int)(lds + (t & 1) * Z::kBytes + wave * 1024)), y_to = q_to + 2 * Z::kBytes;

@@ -149,3 +149,27 @@ def test_caps_at_the_ends_of_fp32(monkeypatch, cap, dtype, d):
     _, _, v, dy = make(46, dtype, 2, 4, 2, 150, 260, d)
     for kw in ({}, {"causal": True}, {"slopes": torch.full((4,), 0.01, device="cuda")}):
         check(q, k, v, dy, (cap, list(kw)), cap=cap, scale=0.125, **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_more_heads_than_24_bits(dtype):
+    """2^24 + 64 heads share a key head; their rows overlap, eight columns apart, and only the last 80 of dy are not 0."""
+    H, n, d = (1 << 24) + 64, 80, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(47)
+
+    def rows():
+        flat = torch.zeros(8 * H + d, dtype=dtype, device="cuda")
+        flat[8 * (H - n) + d - 8:] = torch.randn(8 * n + 8, generator=g, device="cuda").to(dtype)
+        return flat.as_strided((1, H, 1, d), (0, 8, 0, 1))
+
+    q, dy = rows(), rows()
+    k, v = (torch.randn(1, 1, 2, d, generator=g, device="cuda").to(dtype) for _ in range(2))
+    o, lse = sv.attention(q, k, v, want_lse=True)
+    got = sv.attention_backward(dy, q, k, v, o, lse, want=["dk", "dv"])
+    last = [t[:, -n:].contiguous() for t in (dy, q)]
+    ref = attention_backward64(last[0], last[1], k, v, o[:, -n:], lse[:, -n:])
+    for name in got:
+        close(got[name], *ref[name], name)
+    del q, dy, o, lse
+    torch.cuda.empty_cache()
