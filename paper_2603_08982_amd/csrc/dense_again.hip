@@ -62,12 +62,13 @@ __device__ __forceinline__ float dot_halves(const T* a, const T* b) {
   return s + swap32(s);
 }
 
-// Whether one of rows [lo, hi), `rn` apart, is unbounded.
+// Whether one of rows [lo, hi), `rn` apart, is unbounded: D / 4 lanes a row. (Up to 2^30 rows, behind a prefix: no count of their elements.)
 template <int D, typename T>
 __device__ __forceinline__ bool unbounded_rows(const T* rows, int64_t rn, int lo, int hi, int lane) {
+  constexpr int L = D / 4;
   float zero = 0.f;
-  for (int e = lane; e < (hi - lo) * (D / 4); e += 64) {
-    const float4 u = load_four(rows + (lo + e / (D / 4)) * rn + e % (D / 4) * 4);
+  for (int r = lo + lane / L; r < hi; r += 64 / L) {
+    const float4 u = load_four(rows + r * rn + lane % L * 4);
     for (float x : {u.x, u.y, u.z, u.w}) zero = __builtin_fmaf(x, 0.f, zero);
   }
   return __any(!(zero == 0.f));

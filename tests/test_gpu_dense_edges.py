@@ -173,3 +173,21 @@ def test_more_heads_than_24_bits(dtype):
         close(got[name], *ref[name], name)
     del q, dy, o, lse
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F, 128), (F, 64)])
+@pytest.mark.parametrize("row", [0, 1, 777, 2899])
+def test_unbounded_rows_that_keys_behind_a_prefix_do_not_see(row, dtype, d):
+    """3,000 queries over 100 keys, 10 of them a prefix: the first tile of keys reads all queries, and its keys from 10 on see the last 90 at
+    most. A NaN in any query before those reaches the prefix alone. (Where such rows' elements are more than 2^31, the same takes minutes.)"""
+    q, k, v, dy = make(48, dtype, 1, 2, 1, 3000, 100, d)
+    kw = {"causal": True, "prefix": torch.tensor([10], dtype=torch.int32, device="cuda")}
+    o, lse = sv.attention(q, k, v, want_lse=True, **kw)
+    ref = attention_backward64(dy, q, k, v, o, lse, **kw)
+    for spoilt in ("dy", "q"):
+        Q, Y = q.clone(), dy.clone()
+        (Y if spoilt == "dy" else Q)[:, :, row] = float("nan")
+        got = sv.attention_backward(Y, Q, k, v, o, lse, **kw)
+        for name in ("dk", "dv"):
+            close(got[name][:, :, 10:], ref[name][0][:, :, 10:], ref[name][1][:, :, 10:], (name, spoilt))
+            assert got[name][:, :, :10].isnan().all(), (name, spoilt)
