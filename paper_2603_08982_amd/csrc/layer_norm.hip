@@ -22,6 +22,7 @@ namespace {
 constexpr int kMaxNormWidth = 1 << 15;
 constexpr int64_t kMaxNormRows = 1 << 30;
 constexpr int kNormWaves = 4;  // waves of a workgroup whose teams are a wave or less
+constexpr int kEntriesOfOne = 4;  // entries whose sums one workgroup joins: a second launch costs as much
 
 enum { kModNone = SVGEAR_NORM_PLAIN, kModEntry = SVGEAR_NORM_BATCH, kModToken = SVGEAR_NORM_TOKEN };
 
@@ -407,8 +408,12 @@ layer_norm_backward_kernel(NormArgs a) {
 }
 
 // ---- the columns' sums, joined: 16 columns a workgroup, 64 runs of parts, each every 64th, then those in order
+// An entry takes a workgroup some 1.6 us, whatever its parts are, so the entries are dealt out to workgroups too. Each then leaves its
+// sums for dweight and dbias where its first entry's part 0 was, which nobody else reads, and a second launch joins those (16,384 entries of
+// two tokens of 24, the whole call: one workgroup for all entries 26 ms, dealt out 0.2).
 struct NormSums {
-  const float* partial;
+  float* partial;
+  int64_t joined_pitch;  // elements from a part to the next, of the second launch
   const void* weight;
   const void* bias;
   const void* scale;  // of entries
@@ -417,9 +422,9 @@ struct NormSums {
   void* dbias;
   void* dscale;
   void* dshift;
-  int entries, parts, c;
+  int entries, parts, c, dealt;
 };
-template <typename T>
+template <typename T, bool JOINED>  // (a pitch that the compiler does not see made of c: 7.1 us for 5.0 at 2 x 777 rows of 1,541)
 __global__ void __launch_bounds__(1024)
 layer_norm_sums_kernel(NormSums a) {
   __shared__ float s[2][64][17];
@@ -430,12 +435,15 @@ layer_norm_sums_kernel(NormSums a) {
     if (a.weight) w = load_as_f32(static_cast<const T*>(a.weight) + c);
     if (a.bias) b = load_as_f32(static_cast<const T*>(a.bias) + c);
   }
-  for (int e = 0; e < a.entries; ++e) {
+  for (int e = blockIdx.y; e < a.entries; e += a.dealt) {
     const float* p = a.partial + (int64_t)e * a.parts * 2 * a.c + c;
     float v1 = 0.f, v2 = 0.f;
     if (in)
 #pragma unroll 8
-      for (int i = y; i < a.parts; i += 64) v1 += p[(int64_t)i * 2 * a.c], v2 += p[(int64_t)i * 2 * a.c + a.c];
+      for (int i = y; i < a.parts; i += 64) {
+        const int64_t at = JOINED ? i * a.joined_pitch : (int64_t)i * 2 * a.c;
+        v1 += p[at], v2 += p[at + a.c];
+      }
     s[0][y][x] = v1;
     s[1][y][x] = v2;
     __syncthreads();
@@ -450,9 +458,13 @@ layer_norm_sums_kernel(NormSums a) {
     }
     __syncthreads();
   }
-  if (y == 0 && in) {
+  if (y == 0 && in && a.dealt == 1) {
     if (a.dbias) store1(static_cast<T*>(a.dbias) + c, t1);
     if (a.dweight) store1(static_cast<T*>(a.dweight) + c, t2);
+  } else if (y == 0 && in && (a.dbias || a.dweight)) {
+    float* p = a.partial + (int64_t)blockIdx.y * a.parts * 2 * a.c + c;
+    p[0] = t1;
+    p[a.c] = t2;
   }
 }
 
@@ -635,8 +647,19 @@ extern "C" int svgear_layer_norm_backward(const void* dy, const int64_t dystride
     z.dscale = dscale, z.dshift = dshift;
   }
   const unsigned blocks = (unsigned)ceil_div(c, 16);
-  if (dt == SVGEAR_F32) layer_norm_sums_kernel<float><<<blocks, 1024, 0, s>>>(z);
-  else layer_norm_sums_kernel<bf16_t><<<blocks, 1024, 0, s>>>(z);
-  SVGEAR_LAUNCH_CHECK();
-  return SVGEAR_OK;
+  const unsigned dealt = z.entries <= kEntriesOfOne ? 1u : std::min((unsigned)z.entries, std::max(2048u / blocks, 8u));
+  auto launch = [&](unsigned workgroups, auto joined) -> int {
+    z.dealt = (int)workgroups;
+    if (dt == SVGEAR_F32) layer_norm_sums_kernel<float, decltype(joined)::value><<<dim3(blocks, workgroups), 1024, 0, s>>>(z);
+    else layer_norm_sums_kernel<bf16_t, decltype(joined)::value><<<dim3(blocks, workgroups), 1024, 0, s>>>(z);
+    SVGEAR_LAUNCH_CHECK();
+    return SVGEAR_OK;
+  };
+  const int summed = launch(dealt, std::false_type{});
+  if (summed != SVGEAR_OK || dealt == 1 || (!dweight && !dbias)) return summed;
+  z.joined_pitch = (int64_t)z.parts * 2 * c;
+  z.entries = 1, z.parts = (int)dealt;
+  z.weight = z.bias = z.scale = nullptr;
+  z.dscale = z.dshift = nullptr;
+  return launch(1, std::true_type{});
 }

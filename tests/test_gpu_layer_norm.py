@@ -185,3 +185,36 @@ def test_gradient_of_a_shift_alone(B, N, c, mod, dtype):
             close(got[n], *ref[n], (n, B, N, c, mod))
     both, one = (sv.layer_norm_backward(dy, x, w, b, scale=s, want=["dx", "dscale", "dshift"], **kw) for kw in ({"shift": h}, {}))
     assert all(torch.equal(both[n], one[n]) for n in one)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,N,c", [(4, 3, 40), (5, 3, 40), (9, 130, 513), (300, 2, 5120), (2500, 3, 24), (20000, 2, 8)])
+def test_many_entries(B, N, c, dtype):
+    """Sums of a batch entry and of all of them: few entries by one workgroup, many dealt out and joined."""
+    x, w, b, s, h, dy = make(B + c, dtype, B, N, c, True, "batch")
+    names = ["dx", "dweight", "dbias", "dscale", "dshift"]
+    got = sv.layer_norm_backward(dy, x, w, b, scale=s, eps=EPS, want=names)
+    ref = norm_backward64(dy, x, w, b, s, EPS)
+    for n in names:
+        close(got[n], *ref[n], (n, B, N, c))
+    for some in (["dscale", "dshift"], ["dweight"], ["dbias", "dscale"]):
+        part = sv.layer_norm_backward(dy, x, w, b, scale=s, eps=EPS, want=some)
+        assert all(torch.equal(part[n], got[n]) for n in some)
+
+
+def test_entries_by_the_hundred_thousand():
+    """As many batch entries as tokens of one: a second's work for one workgroup after the other, a millisecond's for all."""
+    B, N, c = 600000, 2, 8
+    x, w, b, s, h, dy = make(17, torch.float32, B, N, c, True, "batch")
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    sv.layer_norm_backward(dy, x, w, b, scale=s, want=["dscale"])
+    begin.record()
+    got = sv.layer_norm_backward(dy, x, w, b, scale=s, want=["dscale", "dshift", "dweight"])
+    end.record()
+    torch.cuda.synchronize()
+    assert begin.elapsed_time(end) < 200
+    ref = norm_backward64(dy, x, w, b, s, EPS)
+    for n in ("dscale", "dshift"):
+        close(got[n], *ref[n], n)
+    # (2^11 workgroups of 293 entries each, 32 of them one behind the other: 400 roundings as elsewhere)
+    close(got["dweight"], *ref["dweight"], "dweight")
