@@ -191,3 +191,39 @@ def test_unbounded_rows_that_keys_behind_a_prefix_do_not_see(row, dtype, d):
         for name in ("dk", "dv"):
             close(got[name][:, :, 10:], ref[name][0][:, :, 10:], ref[name][1][:, :, 10:], (name, spoilt))
             assert got[name][:, :, :10].isnan().all(), (name, spoilt)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64)])
+@pytest.mark.parametrize("docs", [62, 63, 64, 65, 127, 1000, 4097])
+def test_many_documents(docs, dtype, d):
+    """Documents of 0 to 3 queries and keys, some rows in front and behind, found among up to 4,099."""
+    g = torch.Generator().manual_seed(docs)
+    ends = lambda most: torch.cat([torch.tensor([3]), torch.randint(0, most + 1, (docs,), generator=g)]).cumsum(0).to(torch.int32)
+    qe, ke = ends(3), ends(2)
+    qe[docs // 2:] += 40  # a longer one
+    ke[docs // 2:] += 70
+    Nq, Nk = int(qe[-1]) + 5, int(ke[-1]) + 2
+    H = 2 if docs > 1000 else 4
+    q, k, v, dy = make(49 + docs, dtype, 1, H, H // 2, Nq, Nk, d)
+    for causal in (False, True):
+        check(q, k, v, dy, (docs, causal), causal=causal, q_offsets=qe.cuda(), k_offsets=ke.cuda())
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_as_many_documents_as_are_taken(dtype):
+    """2^20 documents of one token each: their outputs are their values, and nothing but dv has a gradient. Looked through 64 after
+    64 they would take minutes."""
+    n, d = 1 << 20, 64
+    q, k, v, dy = make(50, dtype, 1, 1, 1, n, n, d)
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    o, lse = sv.attention(q, k, v, want_lse=True, q_offsets=off, k_offsets=off)
+    assert torch.equal(o, v)
+    got = sv.attention_backward(dy, q, k, v, o, lse, q_offsets=off, k_offsets=off)
+    # p = 2^(x - lse log2(e)) for lse = x ln(2): two products and two constants, rounded, of the exponent, whose half step is 2^-24 |s|, and two
+    # half steps of the exponential: it is no exact 1
+    s = (q.double() * k.double()).sum(-1, keepdim=True).abs() * d ** -0.5
+    close(got["dv"], dy.double(), 2.0 ** -24 * (2 + 4 * s) * dy.double().abs(), "dv")
+    # dy v and dy o differ by the order of their sums
+    for name, other in (("dq", k), ("dk", q)):
+        bound = 2 * (d + 2) * 2.0 ** -24 * (dy.double().abs() * v.double().abs()).sum(-1, keepdim=True) * other.double().abs() * d ** -0.5
+        close(got[name], torch.zeros_like(bound), 2 * bound, name)
