@@ -540,8 +540,12 @@ int launch_norm(NormArgs& a, const Plan& p, bool backward, hipStream_t s) {
   if (p.z.lanes == 32) return launch_shape<T, 32, 1, kNormWaves>(a, p, backward, s);
   if (p.z.ch == 1) return launch_shape<T, 64, 1, kNormWaves>(a, p, backward, s);
   if (p.z.ch == 2 && p.z.wpr <= 8) return launch_shape<T, 64, 2, 8>(a, p, backward, s);
-  if (p.z.ch == 2) return launch_shape<T, 64, 2, 16>(a, p, backward, s);
-  if (p.z.wpr <= 8) return launch_shape<T, 64, 4, 8>(a, p, backward, s);
+  // (two runs a lane are one wave in bf16, four are nine waves at least in fp32)
+  if constexpr (sizeof(T) == 4) {
+    if (p.z.ch == 2) return launch_shape<T, 64, 2, 16>(a, p, backward, s);
+  } else {
+    if (p.z.wpr <= 8) return launch_shape<T, 64, 4, 8>(a, p, backward, s);
+  }
   return launch_shape<T, 64, 4, 16>(a, p, backward, s);
 }
 
