@@ -227,3 +227,13 @@ def test_as_many_documents_as_are_taken(dtype):
     for name, other in (("dq", k), ("dk", q)):
         bound = 2 * (d + 2) * 2.0 ** -24 * (dy.double().abs() * v.double().abs()).sum(-1, keepdim=True) * other.double().abs() * d ** -0.5
         close(got[name], torch.zeros_like(bound), 2 * bound, name)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("cap", [None, 20.0, 1e4])
+def test_scale_of_zero(cap, dtype):
+    """All weights are alike, and queries and keys have no gradient."""
+    q, k, v, dy = make(51, dtype, 2, 4, 2, 70, 333, 64)
+    for kw in ({}, {"causal": True}):
+        _, _, got = check(q, k, v, dy, (cap, kw), scale=0.0, cap=cap, **kw)
+        assert not got["dq"].any() and not got["dk"].any()
