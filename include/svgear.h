@@ -504,7 +504,8 @@ int svgear_layer_norm_backward(const void* dy, const int64_t dystride[2], const 
  * SVGEAR_ATTENTION_CAUSAL it sees the keys j <= p_i and those before the document's prefix; otherwise all. A query that sees no
  * key (of no document, of one without keys, before the first key) has o = 0 and lse = -inf. K and V rows of no document
  * are not read, and what is masked may be infinite or NaN: it reaches no query that does not see it (nor, in the backward pass,
- * a key from queries that do not see that). Tiles of queries that such keys lie beside are found again by a slow path,
+ * a key from queries that do not see that); an infinity that a query sees makes its column one, unless its weight is below 2^-126,
+ * which counts as 0. Tiles of queries that such keys lie beside are found again by a slow path,
  * some 2 us a key.
  *   q [B,H,Nq,d], k, v [B,Hk,Nk,d] dt, element strides qstride.. = {stride_b, stride_h, stride_n}, d contiguous
  *   slopes    [H] fp32 or NULL

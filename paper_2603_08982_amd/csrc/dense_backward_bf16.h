@@ -4,9 +4,11 @@
 // A wave has a SIMD to itself, with 512 registers, and an operand that it reads from a tile goes into two products (with 32 rows a wave,
 // two waves a SIMD, the reads of LDS took as long as the products). What it computes from one pair of sums it issues between the products of the
 // next, and the operands are read AHEAD pairs of products before their own (2: as fast; 4: registers spill).
-// 9,450 packed tokens of 16 heads: dq 740 us (with 32 rows a wave 760 to 810), dk and dv 1,005 (1,210 to 1,270), the matrix cores busy 47 %
-// of the cycles at 1.9 GHz. Of dk's and dv's time the copies are 80 us, the exponentials 55, the differences 50, the operands' reads 80.
-// A cap's tanh makes the vector unit the bound: 4,000 causal tokens of 40 heads, 8 key heads, 1,180 us (with two waves a SIMD 1,100).
+// 9,450 packed tokens of 16 heads, warm: delta 14 us, dq 637 (1,100 TFLOP/s), dk and dv 868 (1,080), the matrix cores busy 47 and 45 % of the
+// cycles at 2.1 GHz (the whole call with 32 rows a wave for dk and dv 1,833 us, then 1,646; for dq too 1,626, then 1,534). Of dk's and dv's
+// time the copies are 80 us, the exponentials 55, the differences 50, the operands' reads 80.
+// A cap's tanh makes the vector unit the bound: 4,000 causal tokens of 40 heads, 8 key heads, 1,195 us (with two waves a SIMD 1,100). dk and dv
+// at d = 128 spill registers in their loop there: 8 with a cap, 11 with slopes too, 4 with slopes alone (far caps 0 and 6).
 #pragma once
 #include "dense_tile.h"
 

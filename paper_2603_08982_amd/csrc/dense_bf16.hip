@@ -4,8 +4,8 @@
 // cycles, and 32 exponentials a lane at a quarter of the rate with their scaling, maximum, sum and conversion, some 950 cycles.
 // So a wave issues the exponentials of a tile between the products of the next tile's scores, and the next tile's maximum between
 // the products with the values; two workgroups share a CU and fill what is left. 9,450 packed tokens of 40 heads take 1,075 us, 1,090
-// TFLOP/s with the matrix cores busy 57 % of the cycles at 1.75 GHz, the power limit's clock. Where there are few tiles of keys, what
-// precedes the first products counts as much as they do: 2 x 37,800 queries over texts of at most 512 735 us, of a workgroup's 29,000 cycles 12,500
+// TFLOP/s with the matrix cores busy 58 % of the cycles at 1.7 GHz, the power limit's clock. Where there are few tiles of keys, what
+// precedes the first products counts as much as they do: 2 x 37,800 queries over texts of at most 512 758 us, of a workgroup's 29,000 cycles 12,500
 // in the loop. (Rows by way of LDS, 256 bytes of a row at a time, change nothing there; nor do workgroups that take several tiles of queries.)
 #include <cfloat>
 

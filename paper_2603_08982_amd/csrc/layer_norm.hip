@@ -11,6 +11,10 @@
 // backward pass, the sums of its columns stay in registers; the next row is on its way while the present one is reduced.
 // A row's statistics take one exchange between its waves: each finds its own mean and the squares' sum around that (so that a
 // mean far from zero costs nothing), and those of the waves are joined around the row's mean.
+// Registers hold all that up to 16,384 columns in the forward pass and, with a modulation of entries, up to 8,192 in fp32's and whole chunks of
+// 16,384 in bf16's backward pass. Wider rows spill 96 registers and more, and a token's modulation in the backward pass does from 1,025
+// columns in bf16 and 8,193 in fp32: 9,450 x 5,120 in bf16, gradients with a modulation of entries 79 us, of tokens 487 for a copy's 115; 3,000
+// rows of 16,384 in bf16 forward 37 us, backward 80, of 16,392 columns 128 and 590.
 #include <algorithm>
 #include <type_traits>
 
